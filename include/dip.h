@@ -57,14 +57,19 @@ typedef enum {
 typedef enum {
     DIP_W_F32 = 0,             /* binary32 weights                                                   */
     DIP_W_BF16 = 1,            /* bfloat16 weights                                                   */
-    DIP_W_INT4_G128 = 2        /* 4-bit symmetric codes, one binary16 scale per 128 input indices    */
+    DIP_W_INT4_G128 = 2,       /* 4-bit symmetric codes, one binary16 scale per 128 input indices    */
+    DIP_W_FP8_B128 = 3         /* e4m3 codes, one binary32 scale per block of 128 x 128 (grouped products only) */
 } dip_wtype;
 
 enum {
     DIP_MAX_D = 32768,         /* largest masked dimension (d_model or d_ff)                         */
     DIP_MAX_BATCH = 16,
     DIP_INT4_GROUP = 128,
-    DIP_CACHE_META_INTS = 8    /* length of dip_cache_state.meta                                     */
+    DIP_CACHE_META_INTS = 8,   /* length of dip_cache_state.meta                                     */
+    DIP_FP8_BLOCK = 128,       /* input indices (and outputs) that share a scale in DIP_W_FP8_B128   */
+    DIP_MAX_EXPERTS = 512,
+    DIP_MAX_TOP_K = 16,        /* experts per token                                                  */
+    DIP_MAX_TOKENS = 65536     /* tokens per call of the router and the expert block                 */
 };
 
 typedef struct dip_ctx dip_ctx;   /* opaque; owns scratch workspace on one device */
@@ -569,6 +574,126 @@ dip_status dip_mlp_step_tiered(dip_ctx *ctx, const dip_mlp_weights *w,
 dip_status dip_sparse_gemv_down_noalloc(const dip_mlp_weights *w, const float *h,
                                         const int32_t *kept_idx, int n_kept,
                                         float *y, void *stream);
+
+/* ========================================================================
+ * Mixtures of SwiGLU blocks, and prompts through a dense one.  A mixture layer
+ * has n_experts SwiGLU blocks (Eq. 2 each) and a router that names top_k of
+ * them for every token; a dense layer is the mixture of one.  Here the choice
+ * of weights is the model's own, per token and per block, where DIP's is made
+ * per column; a call takes as many tokens as a prompt has.
+ *
+ * Activations are bfloat16 rows [n][d], sums are binary32.  A router's rows are
+ * grouped by expert: rows offset[e] .. offset[e + 1] - 1 belong to expert e
+ * (offset [n_experts + 1], device int32, not decreasing, offset[0] = 0; an offset below
+ * one in front of it counts as that one, what lies outside [0, n_rows] is cut off).  Rows behind offset[n_experts] are not
+ * read and not written.  offset == NULL: one expert, and all rows are its own.
+ *
+ * Weights are the matrices as checkpoints have them, row-major
+ * [n_experts][d_out][d_in]; d_out and d_in are multiples of 32, at least 32 and at
+ * most DIP_MAX_D.
+ *   DIP_W_BF16      rows are bfloat16.
+ *   DIP_W_FP8_B128  values are e4m3 codes, scales [n_experts][ceil(d_out/128)]
+ *                   [ceil(d_in/128)] binary32; rows are e4m3 codes too, with scales
+ *                   [n_rows][ceil(d_in/128)] (dip_stage_rows).  A product is
+ *                   the sum over the blocks b of 128 input indices of
+ *                   (sum of code * code in b) * (row scale * weight scale of b).
+ * ======================================================================== */
+typedef struct {
+    int32_t wtype;           /* DIP_W_BF16 or DIP_W_FP8_B128 */
+    int32_t n_experts;
+    int32_t d_out;
+    int32_t d_in;
+    const void *values;
+    const float *scales;     /* NULL unless FP8 */
+} dip_grouped_matrix;
+
+/* What a router decides, and the grouping of the rows that follows from it (caller's buffers):
+ *   expert    [n_tokens][top_k]  the token's experts, largest logit first; -1 where no expert is left
+ *   weight    [n_tokens][top_k]  their weights (0 where expert is -1)
+ *   offset    [n_experts + 1]    first row of each expert's group
+ *   row_token [n_tokens * top_k] the token of each row: ascending within a group
+ *   token_row [n_tokens][top_k]  the row of each choice, -1 where expert is -1 */
+typedef struct {
+    int32_t n_tokens;
+    int32_t n_experts;
+    int32_t top_k;
+    int32_t reserved;
+    int32_t *expert;
+    float *weight;
+    int32_t *offset;
+    int32_t *row_token;
+    int32_t *token_row;
+} dip_expert_route;
+
+/* ------------------------------------------------------------------------
+ * dip_route_experts — the top_k experts of every token and the grouping of
+ * their rows.  logits [n_tokens][n_experts] binary32, or bfloat16
+ * (logits_bf16 != 0).  Experts are taken in the order of (logit descending, index
+ * ascending).  weight = exp(logit - max) / sum, the sum over all experts, or
+ * over the chosen ones (renormalize != 0).  A logit of -infinity or NaN closes
+ * that expert to the token: it is not chosen and has no share of the sum; a
+ * token without an open expert (padding) has no row at all.  Where logits of
+ * +infinity stand, they share the sum evenly and the others get 0.
+ * row_token behind offset[n_experts] is left as it was.
+ * 1 <= n_tokens <= DIP_MAX_TOKENS, 1 <= n_experts <= DIP_MAX_EXPERTS,
+ * 1 <= top_k <= min(n_experts, DIP_MAX_TOP_K).
+ * ------------------------------------------------------------------------ */
+dip_status dip_route_experts(dip_ctx *ctx, const void *logits, int logits_bf16, int renormalize,
+                             const dip_expert_route *route, void *stream);
+
+/* ------------------------------------------------------------------------
+ * dip_stage_rows — the rows of a grouped product out of the tokens'
+ * activations x [n_tokens][d] (bfloat16): row r is x[route->row_token[r]], or, with
+ * route == NULL, x[r].  wtype DIP_W_BF16: rows [n][d] bfloat16, a copy.
+ * DIP_W_FP8_B128: rows [n][d] e4m3 codes with scales [n][ceil(d/128)]:
+ * per row and block of 128 columns scale = max(max|x| / 448, 2^-126) and
+ * code = round-to-nearest-even(x / scale), quotients in binary32.  A row with
+ * a value that is not finite has a NaN among its codes and so NaN products.
+ * n_tokens <= DIP_MAX_TOKENS; a route has the same n_tokens.
+ * ------------------------------------------------------------------------ */
+dip_status dip_stage_rows(dip_ctx *ctx, const void *x, int n_tokens, int d, const dip_expert_route *route,
+                          int wtype, void *rows, float *scales, void *stream);
+
+/* ------------------------------------------------------------------------
+ * dip_grouped_product — y[r] = W[e(r)] rows[r] for the rows of every group.
+ *   rows [n_rows][d_in] (row_scales: FP8);  y [n_rows][d_out] bfloat16, or
+ *   binary32 (y_f32 != 0).  1 <= n_rows <= DIP_MAX_TOKENS * DIP_MAX_TOP_K.
+ * dip_grouped_gate_up — h[r] = silu(Wg[e(r)] rows[r]) * (Wu[e(r)] rows[r]) in
+ * one pass over rows and weights: the first half of Eq. 2 for every group.  h [n_rows][d_out]
+ * is bfloat16, or (FP8) e4m3 codes with h_scales, as dip_stage_rows makes them of the binary32 h.
+ * ------------------------------------------------------------------------ */
+dip_status dip_grouped_product(dip_ctx *ctx, const dip_grouped_matrix *w, const void *rows, const float *row_scales,
+                               int n_rows, const int32_t *offset, void *y, int y_f32, void *stream);
+dip_status dip_grouped_gate_up(dip_ctx *ctx, const dip_grouped_matrix *gate, const dip_grouped_matrix *up,
+                               const void *rows, const float *row_scales, int n_rows, const int32_t *offset,
+                               void *h, float *h_scales, void *stream);
+
+/* ------------------------------------------------------------------------
+ * dip_combine_rows — y[t] = sum over j of weight[t][j] * rows[token_row[t][j]]
+ * in the order of j, binary32 sums, bfloat16 rows and y; a choice that is -1 adds
+ * nothing, a token without any gets 0.  d as above.
+ * ------------------------------------------------------------------------ */
+dip_status dip_combine_rows(dip_ctx *ctx, const void *rows, const dip_expert_route *route, int d, void *y, void *stream);
+
+/* Buffers of dip_expert_mlp for n = n_tokens * top_k rows (n_tokens without a route); the caller's. */
+typedef struct {
+    void *rows;          /* [n][d_model]: bfloat16, or e4m3.  NULL for BF16 without a route    */
+    float *row_scales;   /* [n][ceil(d_model/128)], FP8 only                                   */
+    void *h;             /* [n][d_ff]: bfloat16, or e4m3                                       */
+    float *h_scales;     /* [n][ceil(d_ff/128)], FP8 only                                      */
+    void *out;           /* [n][d_model] bfloat16.  NULL without a route                       */
+} dip_expert_work;
+
+/* ------------------------------------------------------------------------
+ * dip_expert_mlp — a mixture of SwiGLU blocks for any number of tokens:
+ * dip_stage_rows, dip_grouped_gate_up, dip_grouped_product, dip_combine_rows.
+ * route == NULL: the dense block (n_experts 1), x straight to y.
+ *   x [n_tokens][d_model] in;  y [n_tokens][d_model] out; both bfloat16.
+ * gate and up are [d_ff][d_model] per expert, down is [d_model][d_ff]; one wtype.
+ * ------------------------------------------------------------------------ */
+dip_status dip_expert_mlp(dip_ctx *ctx, const dip_grouped_matrix *gate, const dip_grouped_matrix *up,
+                          const dip_grouped_matrix *down, const void *x, int n_tokens,
+                          const dip_expert_route *route, const dip_expert_work *work, void *y, void *stream);
 
 #ifdef __cplusplus
 }

@@ -15,8 +15,9 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdip.so")
 
-W_F32, W_BF16, W_INT4_G128 = 0, 1, 2
+W_F32, W_BF16, W_INT4_G128, W_FP8_B128 = 0, 1, 2, 3
 MAX_D, MAX_BATCH, INT4_GROUP, CACHE_META_INTS = 32768, 16, 128, 8
+FP8_BLOCK, MAX_EXPERTS, MAX_TOP_K, MAX_TOKENS = 128, 512, 16, 65536
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CUDA, ERR_WORKSPACE = 0, 1, 2, 3, 4
 DEVICE_OK, DEVICE_WAIT_TIMEOUT, DEVICE_TIER_INCONSISTENT = 0, 1, 2
 
@@ -131,6 +132,38 @@ _lib.dip_mlp_step_neuron_pruned.argtypes = [_vp, C.POINTER(NeuronWeightsStruct),
 _lib.dip_sparse_gemv_down_noalloc.restype = _i32
 _lib.dip_sparse_gemv_down_noalloc.argtypes = [C.POINTER(MlpWeightsStruct), _vp, _vp, _i32, _vp, _vp]
 
+
+
+class GroupedMatrixStruct(C.Structure):
+    _fields_ = [("wtype", C.c_int32), ("n_experts", C.c_int32), ("d_out", C.c_int32), ("d_in", C.c_int32),
+                ("values", _vp), ("scales", _vp)]
+
+
+class ExpertRouteStruct(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("n_experts", C.c_int32), ("top_k", C.c_int32), ("reserved", C.c_int32),
+                ("expert", _vp), ("weight", _vp), ("offset", _vp), ("row_token", _vp), ("token_row", _vp)]
+
+
+class ExpertWorkStruct(C.Structure):
+    _fields_ = [("rows", _vp), ("row_scales", _vp), ("h", _vp), ("h_scales", _vp), ("out", _vp)]
+
+
+_lib.dip_route_experts.restype = _i32
+_lib.dip_route_experts.argtypes = [_vp, _vp, _i32, _i32, C.POINTER(ExpertRouteStruct), _vp]
+_lib.dip_stage_rows.restype = _i32
+_lib.dip_stage_rows.argtypes = [_vp, _vp, _i32, _i32, C.POINTER(ExpertRouteStruct), _i32, _vp, _vp, _vp]
+_lib.dip_grouped_product.restype = _i32
+_lib.dip_grouped_product.argtypes = [_vp, C.POINTER(GroupedMatrixStruct), _vp, _vp, _i32, _vp, _vp, _i32, _vp]
+_lib.dip_grouped_gate_up.restype = _i32
+_lib.dip_grouped_gate_up.argtypes = [_vp, C.POINTER(GroupedMatrixStruct), C.POINTER(GroupedMatrixStruct), _vp, _vp, _i32,
+                                     _vp, _vp, _vp, _vp]
+_lib.dip_combine_rows.restype = _i32
+_lib.dip_combine_rows.argtypes = [_vp, _vp, C.POINTER(ExpertRouteStruct), _i32, _vp, _vp]
+_lib.dip_expert_mlp.restype = _i32
+_lib.dip_expert_mlp.argtypes = [_vp, C.POINTER(GroupedMatrixStruct), C.POINTER(GroupedMatrixStruct),
+                                C.POINTER(GroupedMatrixStruct), _vp, _i32, C.POINTER(ExpertRouteStruct),
+                                C.POINTER(ExpertWorkStruct), _vp, _vp]
+
 EXPORTED = ["dip_create", "dip_create_ex", "dip_destroy", "dip_status_string", "dip_last_error", "dip_sm_count",
             "dip_device_status", "dip_reset_device_status", "dip_selftest_bounded_wait", "dip_selftest_block_waits", "dip_stack_step_probed",
             "dip_trace_begin", "dip_trace_reset", "dip_trace_read", "dip_trace_end",
@@ -138,7 +171,9 @@ EXPORTED = ["dip_create", "dip_create_ex", "dip_destroy", "dip_status_string", "
             "dip_sparse_gemv_gate_up", "dip_sparse_gemv_down", "dip_select_gemv_gate_up", "dip_select_gemv_down",
             "dip_mlp_step",
             "dip_residual_rmsnorm", "dip_stack_step", "dip_mlp_step_tiered", "dip_mlp_step_neuron_pruned",
-            "dip_sparse_gemv_down_noalloc"]
+            "dip_sparse_gemv_down_noalloc",
+            "dip_route_experts", "dip_stage_rows", "dip_grouped_product", "dip_grouped_gate_up", "dip_combine_rows",
+            "dip_expert_mlp"]
 
 
 class TraceRecord(C.Structure):
@@ -490,3 +525,224 @@ def dip_sparse_gemv_down_noalloc(w: MlpWeights, h: torch.Tensor, kept_idx: torch
         raise DipError(st, "d_model exceeds the no-allocation entry point's fixed scratch (max 16384)")
     if st != OK:
         raise DipError(st, "dip_sparse_gemv_down_noalloc")
+
+
+# ---- mixtures of SwiGLU blocks, and prompts through a dense one -----------------------------------------------------------
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise DipError(ERR_INVALID_ARG, what)
+
+
+def _tensor(t, dtype, shape, name: str, ctx: Optional[Context] = None) -> None:
+    """t is a contiguous device tensor of that type and shape (None in a shape: any extent), on the context's device."""
+    _need(isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous(), "%s must be a contiguous device tensor" % name)
+    _need(t.dtype == dtype, "%s must be %s, got %s" % (name, dtype, t.dtype))
+    _need(len(t.shape) == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape)),
+          "%s must have the shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    _need(ctx is None or t.device.index == ctx.device, "%s is not on the context's device" % name)
+
+
+def _blocks(d: int) -> int:
+    return (d + FP8_BLOCK - 1) // FP8_BLOCK
+
+
+_ROW_DTYPES = {W_BF16: torch.bfloat16, W_FP8_B128: torch.float8_e4m3fn}
+
+
+class GroupedMatrix:
+    """Matrices [n_experts, d_out, d_in] (or one [d_out, d_in]), bfloat16, or float8_e4m3fn with binary32 scales
+    [n_experts, ceil(d_out / 128), ceil(d_in / 128)].  Nothing is copied: the tensors stay the caller's layout."""
+
+    def __init__(self, values: torch.Tensor, scales: Optional[torch.Tensor] = None):
+        if values.dim() == 2:
+            values, scales = values[None], None if scales is None else scales[None]
+        _need(values.dtype in (torch.bfloat16, torch.float8_e4m3fn), "values must be bfloat16 or float8_e4m3fn")
+        _tensor(values, values.dtype, (None, None, None), "values")
+        self.wtype = W_BF16 if values.dtype == torch.bfloat16 else W_FP8_B128
+        self.n_experts, self.d_out, self.d_in = values.shape
+        _need((scales is not None) == (self.wtype == W_FP8_B128), "scales belong to float8_e4m3fn values, and only to them")
+        if scales is not None:
+            _tensor(scales, torch.float32, (self.n_experts, _blocks(self.d_out), _blocks(self.d_in)), "scales")
+            _need(scales.device == values.device, "values and scales must be on one device")
+        self.values, self.scales, self.device = values, scales, values.device
+        self.struct = GroupedMatrixStruct(self.wtype, self.n_experts, self.d_out, self.d_in, _ptr(values), _ptr(scales))
+
+
+class Rows:
+    """Up to max_rows rows of d values as a grouped product takes them: bfloat16, or e4m3 codes with scales.
+    n_rows of them are in use (what the last call that wrote them wrote)."""
+
+    def __init__(self, max_rows: int, d: int, wtype: int, device):
+        _need(wtype in _ROW_DTYPES, "rows are W_BF16 or W_FP8_B128")
+        self._set(torch.empty((max_rows, d), dtype=_ROW_DTYPES[wtype], device=device),
+                  torch.empty((max_rows, _blocks(d)), device=device) if wtype == W_FP8_B128 else None)
+
+    @classmethod
+    def of(cls, values: torch.Tensor, scales: Optional[torch.Tensor] = None) -> "Rows":
+        """Rows that are there already: all of `values` is in use."""
+        _need(values.dtype in _ROW_DTYPES.values(), "rows are bfloat16 or float8_e4m3fn")
+        _tensor(values, values.dtype, (None, None), "values")
+        _need((scales is not None) == (values.dtype == torch.float8_e4m3fn), "scales belong to float8_e4m3fn rows, and only to them")
+        if scales is not None:
+            _tensor(scales, torch.float32, (values.shape[0], _blocks(values.shape[1])), "scales")
+        self = cls.__new__(cls)
+        self._set(values, scales)
+        self.n_rows = values.shape[0]
+        return self
+
+    def _set(self, values, scales):
+        self.values, self.scales = values, scales
+        self.max_rows, self.d = values.shape
+        self.wtype = W_BF16 if scales is None else W_FP8_B128
+        self.n_rows = 0
+
+    def _check(self, ctx: Context, name: str) -> None:
+        _need(isinstance(self, Rows) and self.values.device.index == ctx.device, "%s must be Rows on the context's device" % name)
+
+
+class ExpertRoute:
+    """A router's decisions for up to max_tokens tokens (device tensors owned here).  After a call with n tokens the
+    first n rows of expert, weight and token_row, all of offset and the first offset[-1] entries of row_token are its."""
+
+    def __init__(self, max_tokens: int, n_experts: int, top_k: int, device):
+        _need(1 <= max_tokens <= MAX_TOKENS, "1 .. %d tokens" % MAX_TOKENS)
+        _need(1 <= n_experts <= MAX_EXPERTS and 1 <= top_k <= min(n_experts, MAX_TOP_K),
+              "1 .. %d experts, of which 1 .. %d are chosen" % (MAX_EXPERTS, MAX_TOP_K))
+        self.max_tokens, self.n_experts, self.top_k = int(max_tokens), int(n_experts), int(top_k)
+        ints = dict(dtype=torch.int32, device=device)
+        self.expert = torch.full((max_tokens, top_k), -1, **ints)
+        self.weight = torch.zeros((max_tokens, top_k), device=device)
+        self.offset = torch.zeros(n_experts + 1, **ints)
+        self.row_token = torch.zeros(max_tokens * top_k, **ints)
+        self.token_row = torch.full((max_tokens, top_k), -1, **ints)
+        self.struct = ExpertRouteStruct(0, self.n_experts, self.top_k, 0, _ptr(self.expert), _ptr(self.weight), _ptr(self.offset),
+                                        _ptr(self.row_token), _ptr(self.token_row))
+
+    @property
+    def n_tokens(self) -> int:
+        return self.struct.n_tokens
+
+    @property
+    def n_rows(self) -> int:
+        """Most rows that the last call's tokens can have."""
+        return self.struct.n_tokens * self.top_k
+
+    def _check(self, ctx: Context) -> None:
+        _need(self.offset.device.index == ctx.device, "the route is not on the context's device")
+
+
+class ExpertWeights:
+    """gate, up [n_experts, d_ff, d_model] and down [n_experts, d_model, d_ff] of a mixture (or of one dense block)."""
+
+    def __init__(self, gate: GroupedMatrix, up: GroupedMatrix, down: GroupedMatrix):
+        shape = lambda m: (m.wtype, m.n_experts, m.d_out, m.d_in, m.device)  # noqa: E731
+        _need(shape(gate) == shape(up) == (down.wtype, down.n_experts, down.d_in, down.d_out, down.device),
+              "gate and up must be alike, and down their transposed shape")
+        self.gate, self.up, self.down = gate, up, down
+        self.wtype, self.n_experts, self.d_model, self.d_ff = gate.wtype, gate.n_experts, gate.d_in, gate.d_out
+
+
+class ExpertWork:
+    """The buffers that dip_expert_mlp needs for up to max_tokens tokens; top_k = 0: without a route."""
+
+    def __init__(self, max_tokens: int, top_k: int, w: ExpertWeights, device):
+        _need(1 <= max_tokens <= MAX_TOKENS and 0 <= top_k <= MAX_TOP_K, "1 .. %d tokens, top_k 0 .. %d" % (MAX_TOKENS, MAX_TOP_K))
+        self.max_rows, self.routed = int(max_tokens) * max(1, int(top_k)), top_k > 0
+        self.wtype, self.d_model, self.d_ff, self.device = w.wtype, w.d_model, w.d_ff, torch.device(device)
+        fp8 = w.wtype == W_FP8_B128
+        self.rows = Rows(self.max_rows, w.d_model, w.wtype, device) if fp8 or self.routed else None
+        self.h = Rows(self.max_rows, w.d_ff, w.wtype, device)
+        self.out = torch.empty((self.max_rows, w.d_model), dtype=torch.bfloat16, device=device) if self.routed else None
+        self.struct = ExpertWorkStruct(_ptr(self.rows.values) if self.rows else None, _ptr(self.rows.scales) if self.rows else None,
+                                       _ptr(self.h.values), _ptr(self.h.scales), _ptr(self.out))
+
+
+def dip_route_experts(ctx: Context, logits: torch.Tensor, route: ExpertRoute, renormalize: bool = True) -> None:
+    """logits [n, n_experts], binary32 or bfloat16, n <= route.max_tokens."""
+    _need(isinstance(logits, torch.Tensor) and logits.dtype in (torch.float32, torch.bfloat16), "logits must be float32 or bfloat16")
+    _tensor(logits, logits.dtype, (None, route.n_experts), "logits", ctx)
+    route._check(ctx)
+    _need(1 <= logits.shape[0] <= route.max_tokens, "the route holds 1 .. %d tokens" % route.max_tokens)
+    route.struct.n_tokens = logits.shape[0]
+    ctx.check(_lib.dip_route_experts(ctx.handle, _ptr(logits), int(logits.dtype == torch.bfloat16), int(bool(renormalize)),
+                                     C.byref(route.struct), _stream()))
+
+
+def _check_route(ctx: Context, route: Optional[ExpertRoute], n_tokens: int) -> None:
+    if route is not None:
+        route._check(ctx)
+        _need(route.n_tokens == n_tokens, "the route is of %d tokens, not %d" % (route.n_tokens, n_tokens))
+
+
+def _check_offset(ctx: Context, offset: Optional[torch.Tensor], n_experts: int) -> None:
+    _need(offset is not None or n_experts == 1, "several experts need the offsets of their groups")
+    if offset is not None:
+        _tensor(offset, torch.int32, (n_experts + 1,), "offset", ctx)
+
+
+def dip_stage_rows(ctx: Context, x: torch.Tensor, rows: Rows, route: Optional[ExpertRoute] = None) -> None:
+    """x [n, d] bfloat16 -> rows: x[t] for every row's token t, or x[r]; quantised if the rows are e4m3."""
+    rows._check(ctx, "rows")
+    _tensor(x, torch.bfloat16, (None, rows.d), "x", ctx)
+    _check_route(ctx, route, x.shape[0])
+    n = x.shape[0] if route is None else route.n_rows
+    _need(1 <= n <= rows.max_rows, "rows for %d, %d are needed" % (rows.max_rows, n))
+    ctx.check(_lib.dip_stage_rows(ctx.handle, _ptr(x), x.shape[0], rows.d, C.byref(route.struct) if route else None, rows.wtype,
+                                  _ptr(rows.values), _ptr(rows.scales), _stream()))
+    rows.n_rows = n
+
+
+def dip_grouped_product(ctx: Context, w: GroupedMatrix, rows: Rows, y: torch.Tensor, offset: Optional[torch.Tensor] = None) -> None:
+    """y [>= rows.n_rows, d_out], bfloat16 or float32; offset int32 [n_experts + 1], None: one expert."""
+    rows._check(ctx, "rows")
+    _need(w.device.index == ctx.device, "the weights are not on the context's device")
+    _need(rows.wtype == w.wtype and rows.d == w.d_in, "rows and weights differ in type or width")
+    _need(isinstance(y, torch.Tensor) and y.dtype in (torch.bfloat16, torch.float32), "y must be bfloat16 or float32")
+    _tensor(y, y.dtype, (None, w.d_out), "y", ctx)
+    _need(1 <= rows.n_rows <= y.shape[0], "y has %d rows for %d" % (y.shape[0], rows.n_rows))
+    _check_offset(ctx, offset, w.n_experts)
+    ctx.check(_lib.dip_grouped_product(ctx.handle, C.byref(w.struct), _ptr(rows.values), _ptr(rows.scales), rows.n_rows, _ptr(offset),
+                                       _ptr(y), int(y.dtype == torch.float32), _stream()))
+
+
+def dip_grouped_gate_up(ctx: Context, gate: GroupedMatrix, up: GroupedMatrix, rows: Rows, h: Rows,
+                        offset: Optional[torch.Tensor] = None) -> None:
+    """h = silu(gate rows) * (up rows), rounded (and for e4m3 quantised) as the next product takes it."""
+    rows._check(ctx, "rows")
+    h._check(ctx, "h")
+    for m in (gate, up):
+        _need(m.device.index == ctx.device, "the weights are not on the context's device")
+        _need(rows.wtype == h.wtype == m.wtype and rows.d == m.d_in and h.d == m.d_out and m.n_experts == gate.n_experts,
+              "rows, h and weights differ in type, width or number of experts")
+    _need(1 <= rows.n_rows <= h.max_rows, "h has %d rows for %d" % (h.max_rows, rows.n_rows))
+    _check_offset(ctx, offset, gate.n_experts)
+    ctx.check(_lib.dip_grouped_gate_up(ctx.handle, C.byref(gate.struct), C.byref(up.struct), _ptr(rows.values), _ptr(rows.scales),
+                                       rows.n_rows, _ptr(offset), _ptr(h.values), _ptr(h.scales), _stream()))
+    h.n_rows = rows.n_rows
+
+
+def dip_combine_rows(ctx: Context, rows: torch.Tensor, route: ExpertRoute, y: torch.Tensor) -> None:
+    """y [n, d] = the weighted sums of rows [>= n * top_k, d]; both bfloat16, n the route's tokens."""
+    route._check(ctx)
+    _need(route.n_tokens >= 1, "the route has no tokens yet")
+    _tensor(y, torch.bfloat16, (route.n_tokens, None), "y", ctx)
+    _tensor(rows, torch.bfloat16, (None, y.shape[1]), "rows", ctx)
+    _need(rows.shape[0] >= route.n_rows, "rows has %d rows for %d" % (rows.shape[0], route.n_rows))
+    ctx.check(_lib.dip_combine_rows(ctx.handle, _ptr(rows), C.byref(route.struct), y.shape[1], _ptr(y), _stream()))
+
+
+def dip_expert_mlp(ctx: Context, w: ExpertWeights, x: torch.Tensor, work: ExpertWork, y: torch.Tensor,
+                   route: Optional[ExpertRoute] = None) -> None:
+    """x [n, d_model] -> y [n, d_model], bfloat16, through the mixture (route) or the one dense block (no route)."""
+    _need(w.gate.device.index == ctx.device, "the weights are not on the context's device")
+    _tensor(x, torch.bfloat16, (None, w.d_model), "x", ctx)
+    _tensor(y, torch.bfloat16, (x.shape[0], w.d_model), "y", ctx)
+    _check_route(ctx, route, x.shape[0])
+    _need(route is None or route.n_experts == w.n_experts, "route and weights differ in their number of experts")
+    _need(route is not None or w.n_experts == 1, "several experts need a route")
+    _need((work.wtype, work.d_model, work.d_ff) == (w.wtype, w.d_model, w.d_ff) and work.h.values.device.index == ctx.device and
+          work.routed == (route is not None), "the buffers are of another shape, type, device or kind of call")
+    n = x.shape[0] if route is None else route.n_rows
+    _need(1 <= n <= work.max_rows, "buffers for %d rows, %d are needed" % (work.max_rows, n))
+    ctx.check(_lib.dip_expert_mlp(ctx.handle, C.byref(w.gate.struct), C.byref(w.up.struct), C.byref(w.down.struct), _ptr(x),
+                                  x.shape[0], C.byref(route.struct) if route else None, C.byref(work.struct), _ptr(y), _stream()))

@@ -60,12 +60,7 @@ template <typename T> dip_status dev_alloc(dip_ctx *ctx, T **p, size_t n)
     return DIP_OK;
 }
 
-// The context exists and its device is the calling thread's current one.
-bool ctx_ok(const dip_ctx *ctx)
-{
-    int dev = -1;
-    return ctx && cudaGetDevice(&dev) == cudaSuccess && dev == ctx->device;
-}
+bool ctx_ok(const dip_ctx *ctx) { return dip_ctx_current(ctx); }
 
 // Shapes within what the context's workspace was sized for.
 bool fits(const dip_ctx *ctx, int d_a, int d_b, int batch)
@@ -161,6 +156,7 @@ dip_status dip_create_ex(dip_ctx **out, int device, const dip_options *opt)
     if ((st = dev_alloc(ctx, &ctx->mask_tmp, (size_t)(ctx->max_d / 32))) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->coarse, vec)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->xt, (size_t)ctx->max_d * 32)) != DIP_OK) return fail(st);
+    if ((st = dev_alloc(ctx, &ctx->route_counts, (size_t)DIP_MAX_TOKENS / DIP_ROUTE_TOKENS * DIP_MAX_EXPERTS)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->status, (size_t)1)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->trace, (size_t)DIP_TRACE_SLOTS * DIP_TRACE_WORDS)) != DIP_OK) return fail(st);
     if (cudaStreamCreateWithFlags(&ctx->tier_fetch, cudaStreamNonBlocking) != cudaSuccess) return fail(DIP_ERR_CUDA);
@@ -220,6 +216,7 @@ dip_status dip_destroy(dip_ctx *ctx)
     cudaFree(ctx->mask_tmp);
     cudaFree(ctx->coarse);
     cudaFree(ctx->xt);
+    cudaFree(ctx->route_counts);
     cudaFree(ctx->status);
     cudaFree(ctx->trace);
     for (int i = 0; i < 2; ++i) {

@@ -14,6 +14,7 @@ constexpr int DIP_TRACE_SLOTS = 1024;
 constexpr uint32_t DIP_MAIL_EMPTY = 0xffffffffu;
 constexpr int DIP_SYNC_WORDS = 2;
 constexpr int DIP_MAIL_FLOATS = 4096;  // boxes per SM: one CTA's segment of sums (INT4: up to 2048, F32 / BF16: 256 per token)
+constexpr int DIP_ROUTE_TOKENS = 128;  // tokens per block of the router
 constexpr int DIP_TRACE_WORDS = 4;   // first start, dependency ready, last end, auxiliary
 
 // Scratch workspace of a context.  All device memory the library itself owns.
@@ -53,6 +54,7 @@ struct dip_ctx {
     uint16_t *coarse;    // [max_batch][max_d] top 16 bits of the rank keys of h, left by the gate/up product
     uint16_t *xt;        // [max_d][32] batched decode: per column, the tokens' values as bfloat16 (16 high, 16 low halves)
     int coarse_min_d;    // smallest d_ff for which the step ranks h from those
+    int32_t *route_counts;   // [DIP_MAX_TOKENS / DIP_ROUTE_TOKENS][DIP_MAX_EXPERTS] the router: rows per token block and expert
     int *status;         // sticky device status word (0 = fine)
     int fuse_select;     // single-token F32 / BF16 steps: the products build their own masks
     // the cache updates run beside the GEMVs: one side stream per cache kind
@@ -129,6 +131,13 @@ static inline cudaError_t dip_launch_pdl(void (*kernel)(KArgs...), dim3 grid, di
     return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
 }
 #endif
+
+// The context exists and its device is the calling thread's current one.
+static inline bool dip_ctx_current(const dip_ctx *ctx)
+{
+    int dev = -1;
+    return ctx && cudaGetDevice(&dev) == cudaSuccess && dev == ctx->device;
+}
 
 static inline bool dip_aligned16(const void *p) { return (((uintptr_t)p) & 15u) == 0; }
 
@@ -278,3 +287,14 @@ dip_status dip_launch_pack(dip_ctx *ctx, int wtype, int d_model, int d_ff,
                            const void *Wg, const void *Wu, const void *Wd,
                            const void *Sg, const void *Su, const void *Sd,
                            const dip_mlp_weights *out, cudaStream_t stream);
+
+// route.cu: the router's choice and grouping; rows into their places; the rows' weighted sums per token.
+dip_status dip_launch_route(dip_ctx *ctx, const void *logits, bool bf16, bool renormalize, const dip_expert_route &r, cudaStream_t stream);
+dip_status dip_launch_stage_rows(dip_ctx *ctx, const void *x, int n_tokens, int d, const dip_expert_route *route, bool fp8,
+                                 void *rows, float *scales, cudaStream_t stream);
+dip_status dip_launch_combine_rows(dip_ctx *ctx, const void *rows, const dip_expert_route &r, int d, void *y, cudaStream_t stream);
+
+// grouped.cu: products of groups of rows.  up != nullptr: out = silu(w rows) * (up rows), FP8: as codes with out_scales.
+dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const dip_grouped_matrix *up, const void *rows,
+                              const float *row_scales, int n_rows, const int32_t *offset, void *out, bool out_f32, float *out_scales,
+                              cudaStream_t stream);

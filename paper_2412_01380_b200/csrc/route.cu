@@ -1,0 +1,338 @@
+// The router of a mixture, and the rows on their way into the grouped products and out of them.
+//
+// Choice: a warp per token holds the token's logits in registers (E / 32 per lane) and takes the largest top_k times: one
+// warp-wide maximum over order-preserving integers, one warp-wide minimum over the indices that hold it (ties: lowest).
+// Grouping: row = first row of the expert + tokens in front that chose it.  A block has DIP_ROUTE_TOKENS tokens and a bit set
+// of them per expert, so a rank within the block is a popcount; nothing depends on the order of atomics.  Up to
+// DIP_ROUTE_TOKENS tokens are one launch.  More are two: the blocks leave their counts, and every block of the second launch
+// adds up the counts in front of its own (blocks^2 * E words out of L2; 16384 tokens, 128 experts: 8 MB).
+// Bound by latency for a token, by the trips to memory between the launches for a prompt.
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+#include "float8.cuh"
+#include "gemv_common.cuh"
+
+namespace {
+
+constexpr int RT_THREADS = 1024, RT_WARPS = RT_THREADS / 32;
+constexpr int RT_WORDS = DIP_ROUTE_TOKENS / 32;
+constexpr uint32_t RT_ALL = 0xffffffffu;
+
+struct RouteParams {
+    const void *logits;
+    int n_tokens, n_experts, top_k, bf16, renormalize;
+    int32_t *expert;
+    float *weight;
+    int32_t *offset, *row_token, *token_row;
+    int32_t *counts;         // [blocks][DIP_MAX_EXPERTS]
+};
+
+struct RouteSmem {
+    uint32_t chosen[DIP_MAX_EXPERTS][RT_WORDS];   // tokens of this block that chose the expert
+    int32_t start[DIP_MAX_EXPERTS];               // first row of this block's tokens in the expert's group
+    int32_t total[DIP_MAX_EXPERTS];
+    int32_t warp_sum[RT_WARPS];
+};
+
+// Order-preserving image of a logit; 0: closed.  (-0 and 0 are equal.)
+__device__ __forceinline__ uint32_t route_key(float v)
+{
+    v += 0.f;
+    if (!(v > -INFINITY)) return 0u;
+    const uint32_t b = __float_as_uint(v);
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float route_value(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key ^ 0x80000000u : ~key); }
+__device__ __forceinline__ float route_part(uint32_t key, float high)
+{
+    if (key == 0u) return 0.f;
+    const float v = route_value(key);
+    return high == INFINITY ? (v == INFINITY ? 1.f : 0.f) : expf(v - high);
+}
+
+// One token, one warp: experts and weights, and the token's bit in the sets of its experts.
+template <int NV>
+__device__ __forceinline__ void route_token(const RouteParams &p, int t, int bit, RouteSmem &s)
+{
+    const int lane = threadIdx.x & 31;
+    uint32_t key[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int e = lane + 32 * i;
+        key[i] = 0u;
+        if (e < p.n_experts) {
+            const size_t at = (size_t)t * p.n_experts + e;
+            key[i] = route_key(p.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p.logits)[at])
+                                      : static_cast<const float *>(p.logits)[at]);
+        }
+    }
+    uint32_t most = 0u;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) most = max(most, key[i]);
+    most = __reduce_max_sync(RT_ALL, most);
+    const float high = route_value(most);
+    float sum = 0.f;
+    if (!p.renormalize) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) sum += route_part(key[i], high);
+    }
+    uint32_t mine = 0u;                           // choice `lane`
+    int mine_e = -1;
+    for (int j = 0; j < p.top_k && most != 0u; ++j) {
+        int at = 0x7fffffff;
+#pragma unroll
+        for (int i = NV - 1; i >= 0; --i)
+            if (key[i] == most) at = lane + 32 * i;
+        const int e = (int)__reduce_min_sync(RT_ALL, (unsigned)at);
+        if (lane == j) {
+            mine = most;
+            mine_e = e;
+        }
+        most = 0u;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (lane + 32 * i == e) key[i] = 0u;
+            most = max(most, key[i]);
+        }
+        most = __reduce_max_sync(RT_ALL, most);
+    }
+    const float part = route_part(mine, high);
+    if (p.renormalize) sum = part;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(RT_ALL, sum, o);
+    if (lane < p.top_k) {
+        p.expert[(size_t)t * p.top_k + lane] = mine_e;
+        p.weight[(size_t)t * p.top_k + lane] = mine_e >= 0 ? part / sum : 0.f;
+        if (mine_e >= 0) atomicOr(&s.chosen[mine_e][bit >> 5], 1u << (bit & 31));
+    }
+}
+
+// start[e] += exclusive prefix of total[0 .. E); block 0 also writes the offsets.  All threads.
+__device__ __forceinline__ void route_offsets(const RouteParams &p, RouteSmem &s)
+{
+    static_assert(RT_THREADS >= DIP_MAX_EXPERTS, "a thread per expert");
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int n = tid < p.n_experts ? s.total[tid] : 0;
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(RT_ALL, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) s.warp_sum[warp] = incl;
+    __syncthreads();
+    const int first = (int)__reduce_add_sync(RT_ALL, lane < warp ? (unsigned)s.warp_sum[lane] : 0u) + incl - n;
+    if (tid < p.n_experts) {
+        s.start[tid] += first;
+        if (blockIdx.x == 0) {
+            p.offset[tid] = first;
+            if (tid == p.n_experts - 1) p.offset[tid + 1] = first + n;
+        }
+    }
+    __syncthreads();
+}
+
+// Rows of this block's choices.
+__device__ __forceinline__ void route_rows(const RouteParams &p, const RouteSmem &s, int t0, int n)
+{
+    for (int i = threadIdx.x; i < n * p.top_k; i += RT_THREADS) {
+        const int bit = i / p.top_k;
+        const size_t at = (size_t)t0 * p.top_k + i;
+        const int e = p.expert[at];
+        int row = -1;
+        if (e >= 0) {
+            row = s.start[e];
+#pragma unroll
+            for (int w = 0; w < RT_WORDS; ++w) {
+                const int below = bit - 32 * w;
+                row += __popc(s.chosen[e][w] & (below >= 32 ? RT_ALL : below > 0 ? (1u << below) - 1u : 0u));
+            }
+            p.row_token[row] = t0 + bit;
+        }
+        p.token_row[at] = row;
+    }
+}
+
+__device__ __forceinline__ void route_clear(const RouteParams &p, RouteSmem &s)
+{
+    for (int i = threadIdx.x; i < p.n_experts * RT_WORDS; i += RT_THREADS) (&s.chosen[0][0])[i] = 0u;
+    for (int i = threadIdx.x; i < p.n_experts; i += RT_THREADS) s.start[i] = s.total[i] = 0;
+    __syncthreads();
+}
+
+template <int NV>
+__global__ void __launch_bounds__(RT_THREADS, 1) route_choose_kernel(const RouteParams p)
+{
+    __shared__ RouteSmem s;
+    const int t0 = blockIdx.x * DIP_ROUTE_TOKENS, n = min(DIP_ROUTE_TOKENS, p.n_tokens - t0);
+    route_clear(p, s);
+    dip_grid_dependency_wait();
+    dip_launch_dependents();
+    for (int i = threadIdx.x >> 5; i < n; i += RT_WARPS) route_token<NV>(p, t0 + i, i, s);
+    __syncthreads();
+    for (int e = threadIdx.x; e < p.n_experts; e += RT_THREADS) {
+        int c = 0;
+#pragma unroll
+        for (int w = 0; w < RT_WORDS; ++w) c += __popc(s.chosen[e][w]);
+        s.total[e] = c;
+        if (gridDim.x > 1) p.counts[(size_t)blockIdx.x * DIP_MAX_EXPERTS + e] = c;
+    }
+    if (gridDim.x > 1) return;
+    __syncthreads();
+    route_offsets(p, s);
+    route_rows(p, s, t0, n);
+}
+
+__global__ void __launch_bounds__(RT_THREADS, 1) route_rows_kernel(const RouteParams p)
+{
+    __shared__ RouteSmem s;
+    const int t0 = blockIdx.x * DIP_ROUTE_TOKENS, n = min(DIP_ROUTE_TOKENS, p.n_tokens - t0);
+    route_clear(p, s);
+    dip_grid_dependency_wait();
+    dip_launch_dependents();
+    for (int i = threadIdx.x; i < n * p.top_k; i += RT_THREADS) {
+        const int e = p.expert[(size_t)t0 * p.top_k + i], bit = i / p.top_k;
+        if (e >= 0) atomicOr(&s.chosen[e][bit >> 5], 1u << (bit & 31));
+    }
+    // all blocks' counts, and those in front of this block
+    const int width = p.n_experts <= 32 ? 32 : p.n_experts <= 64 ? 64 : p.n_experts <= 128 ? 128 : p.n_experts <= 256 ? 256 : 512;
+    const int e = threadIdx.x % width;
+    if (e < p.n_experts) {
+        int total = 0, before = 0;
+#pragma unroll 4
+        for (int b = threadIdx.x / width; b < (int)gridDim.x; b += RT_THREADS / width) {
+            const int c = p.counts[(size_t)b * DIP_MAX_EXPERTS + e];
+            total += c;
+            if (b < (int)blockIdx.x) before += c;
+        }
+        atomicAdd(&s.total[e], total);
+        atomicAdd(&s.start[e], before);
+    }
+    __syncthreads();
+    route_offsets(p, s);
+    route_rows(p, s, t0, n);
+}
+
+// ---- rows into their places ----
+struct StageParams {
+    const uint4 *x;            // [n_tokens][d / 8]
+    int n_tokens, n_rows, d;
+    const int32_t *row_token;  // nullptr: row r is token r
+    const int32_t *end;        // offset + n_experts
+    void *rows;
+    float *scales;
+};
+
+// A piece of a row is 256 columns, eight to a lane: 16 lanes are a block of 128.  A warp per piece.
+template <bool FP8>
+__global__ void __launch_bounds__(256) stage_rows_kernel(const StageParams p)
+{
+    dip_grid_dependency_wait();
+    dip_launch_dependents();
+    const int lane = threadIdx.x & 31, pieces = (p.d + 255) / 256, blocks = (p.d + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
+    const long long n_rows = p.end ? min(*p.end, p.n_rows) : p.n_rows;
+    const long long step = (long long)gridDim.x * 8;
+    for (long long i = blockIdx.x * 8ll + (threadIdx.x >> 5); i < n_rows * pieces; i += step) {
+        const int r = (int)(i / pieces), c = (int)(i % pieces) * 256 + lane * 8;
+        const int t = p.row_token ? p.row_token[r] : r;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (c < p.d && t >= 0 && t < p.n_tokens) v = p.x[((size_t)t * p.d + c) >> 3];
+        if (!FP8) {
+            if (c < p.d) static_cast<uint4 *>(p.rows)[((size_t)r * p.d + c) >> 3] = v;
+            continue;
+        }
+        float f[8];
+        decode16<DIP_W_BF16>(v, f);
+        float amax = 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) amax = fmaxf(amax, fabsf(f[q]));
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(RT_ALL, amax, o));
+        const float scale = fp8_scale(amax);
+        if (c < p.d) {
+            uint2 code;
+            code.x = fp8_codes4(f[0], f[1], f[2], f[3], scale);
+            code.y = fp8_codes4(f[4], f[5], f[6], f[7], scale);
+            static_cast<uint2 *>(p.rows)[((size_t)r * p.d + c) >> 3] = code;
+            if ((lane & 15) == 0) p.scales[(size_t)r * blocks + c / DIP_FP8_BLOCK] = scale;
+        }
+    }
+}
+
+// ---- the rows' weighted sums ----
+struct CombineParams {
+    const uint4 *rows;         // [n_rows][d / 8]
+    uint4 *y;                  // [n_tokens][d / 8]
+    const float *weight;
+    const int32_t *token_row;
+    int n_tokens, top_k, d;
+};
+
+// A thread per eight columns of a token.  Reads every row once: bound by memory.
+__global__ void __launch_bounds__(256) combine_rows_kernel(const CombineParams p)
+{
+    dip_grid_dependency_wait();
+    dip_launch_dependents();
+    const int eights = p.d / 8, n_rows = p.n_tokens * p.top_k;
+    const long long n = (long long)p.n_tokens * eights, step = (long long)gridDim.x * 256;
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += step) {
+        const int t = (int)(i / eights), c = (int)(i % eights);
+        float sum[8] = {};
+#pragma unroll 2
+        for (int j = 0; j < p.top_k; ++j) {
+            const int row = p.token_row[t * p.top_k + j];
+            if (row < 0 || row >= n_rows) continue;
+            const float w = p.weight[t * p.top_k + j];
+            float f[8];
+            decode16<DIP_W_BF16>(p.rows[(size_t)row * eights + c], f);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum[q] = fmaf(w, f[q], sum[q]);
+        }
+        p.y[i] = bf16x8(sum);
+    }
+}
+
+template <int NV>
+cudaError_t launch_choose(const RouteParams &p, int blocks, cudaStream_t stream)
+{
+    return dip_launch_pdl(route_choose_kernel<NV>, dim3(blocks), dim3(RT_THREADS), 0, stream, p);
+}
+
+}  // namespace
+
+dip_status dip_launch_route(dip_ctx *ctx, const void *logits, bool bf16, bool renormalize, const dip_expert_route &r, cudaStream_t stream)
+{
+    const RouteParams p = {logits, r.n_tokens, r.n_experts, r.top_k, bf16, renormalize, r.expert, r.weight, r.offset, r.row_token,
+                           r.token_row, ctx->route_counts};
+    const int blocks = (r.n_tokens + DIP_ROUTE_TOKENS - 1) / DIP_ROUTE_TOKENS, per_lane = (r.n_experts + 31) / 32;
+    DIP_CUDA_TRY(ctx, per_lane <= 1   ? launch_choose<1>(p, blocks, stream)
+                      : per_lane <= 2 ? launch_choose<2>(p, blocks, stream)
+                      : per_lane <= 4 ? launch_choose<4>(p, blocks, stream)
+                      : per_lane <= 8 ? launch_choose<8>(p, blocks, stream)
+                                      : launch_choose<16>(p, blocks, stream));
+    if (blocks > 1) DIP_CUDA_TRY(ctx, dip_launch_pdl(route_rows_kernel, dim3(blocks), dim3(RT_THREADS), 0, stream, p));
+    return DIP_OK;
+}
+
+dip_status dip_launch_stage_rows(dip_ctx *ctx, const void *x, int n_tokens, int d, const dip_expert_route *route, bool fp8,
+                                 void *rows, float *scales, cudaStream_t stream)
+{
+    const int n_rows = route ? n_tokens * route->top_k : n_tokens;
+    const StageParams p = {static_cast<const uint4 *>(x), n_tokens, n_rows, d, route ? route->row_token : nullptr,
+                           route ? route->offset + route->n_experts : nullptr, rows, scales};
+    const long long warps = (long long)n_rows * ((d + 255) / 256);
+    const int ctas = (int)min((warps + 7) / 8, (long long)ctx->sm_count * 8);
+    DIP_CUDA_TRY(ctx, fp8 ? dip_launch_pdl(stage_rows_kernel<true>, dim3(ctas), dim3(256), 0, stream, p)
+                          : dip_launch_pdl(stage_rows_kernel<false>, dim3(ctas), dim3(256), 0, stream, p));
+    return DIP_OK;
+}
+
+dip_status dip_launch_combine_rows(dip_ctx *ctx, const void *rows, const dip_expert_route &r, int d, void *y, cudaStream_t stream)
+{
+    const CombineParams p = {static_cast<const uint4 *>(rows), static_cast<uint4 *>(y), r.weight, r.token_row, r.n_tokens, r.top_k, d};
+    const long long n = (long long)r.n_tokens * (d / 8);
+    const int ctas = (int)min((n + 255) / 256, (long long)ctx->sm_count * 8);
+    DIP_CUDA_TRY(ctx, dip_launch_pdl(combine_rows_kernel, dim3(ctas), dim3(256), 0, stream, p));
+    return DIP_OK;
+}
