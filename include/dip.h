@@ -169,7 +169,8 @@ dip_status dip_selftest_bounded_wait(dip_ctx *ctx, int limit_us, unsigned long l
  * calls synchronise the device; the stamps cost one atomic per CTA.
  *   kind: 1 select (DIP), 2 select (cache-aware), 3 cache update, 4 gate/up GEMV,
  *         5 down GEMV, 6 cache update and slot assignment, 7 reads of the slow tier (two-tier step; parts
- *         of a GEMV's launch, or of one that does both), 9 neuron-major product (Gate / Up pruning).
+ *         of a GEMV's launch, or of one that does both), 9 neuron-major product (Gate / Up pruning),
+ *         10 grouped gate/up product, 11 grouped product.
  * ------------------------------------------------------------------------ */
 typedef struct {
     int32_t kind;

@@ -157,6 +157,8 @@ dip_status dip_create_ex(dip_ctx **out, int device, const dip_options *opt)
     if ((st = dev_alloc(ctx, &ctx->coarse, vec)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->xt, (size_t)ctx->max_d * 32)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->route_counts, (size_t)DIP_MAX_TOKENS / DIP_ROUTE_TOKENS * DIP_MAX_EXPERTS)) != DIP_OK) return fail(st);
+    if ((st = dev_alloc(ctx, &ctx->group_partials, (size_t)ctx->sm_count * 2 * DIP_GROUP_ROWS * DIP_GROUP_COLS)) != DIP_OK) return fail(st);
+    if ((st = dev_alloc(ctx, &ctx->group_tickets, (size_t)ctx->sm_count)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->status, (size_t)1)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->trace, (size_t)DIP_TRACE_SLOTS * DIP_TRACE_WORDS)) != DIP_OK) return fail(st);
     if (cudaStreamCreateWithFlags(&ctx->tier_fetch, cudaStreamNonBlocking) != cudaSuccess) return fail(DIP_ERR_CUDA);
@@ -182,7 +184,8 @@ dip_status dip_create_ex(dip_ctx **out, int device, const dip_options *opt)
         };
         bool ok = set(ctx->mail, empty, mail_bytes) && set(ctx->status, zeros, sizeof(int)) &&
                   set(ctx->readers, zeros, DIP_SYNC_WORDS * sizeof(unsigned int)) && set(ctx->tickets, zeros, sizeof(zeros)) &&
-                  set(ctx->counts, zeros, 8 * sizeof(int32_t));
+                  set(ctx->counts, zeros, 8 * sizeof(int32_t)) && (size_t)ctx->sm_count <= N_TICKETS &&
+                  set(ctx->group_tickets, zeros, (size_t)ctx->sm_count * sizeof(unsigned int));
         ok = cudaStreamSynchronize(ctx->side[0]) == cudaSuccess && ok;
         free(empty);
         if (!ok) return fail(DIP_ERR_CUDA);
@@ -217,6 +220,8 @@ dip_status dip_destroy(dip_ctx *ctx)
     cudaFree(ctx->coarse);
     cudaFree(ctx->xt);
     cudaFree(ctx->route_counts);
+    cudaFree(ctx->group_partials);
+    cudaFree(ctx->group_tickets);
     cudaFree(ctx->status);
     cudaFree(ctx->trace);
     for (int i = 0; i < 2; ++i) {
@@ -271,6 +276,7 @@ dip_status dip_reset_device_status(dip_ctx *ctx, void *stream)
     DIP_CUDA_TRY(ctx, cudaMemsetAsync(ctx->status, 0, sizeof(int), (cudaStream_t)stream));
     // (a launch that gave up a wait leaves behind what comes too late: counts, and sums nobody takes)
     DIP_CUDA_TRY(ctx, cudaMemsetAsync(ctx->readers, 0, DIP_SYNC_WORDS * sizeof(unsigned int), (cudaStream_t)stream));
+    DIP_CUDA_TRY(ctx, cudaMemsetAsync(ctx->group_tickets, 0, (size_t)ctx->sm_count * sizeof(unsigned int), (cudaStream_t)stream));
     DIP_CUDA_TRY(ctx, cudaMemsetAsync(ctx->mail, 0xff, (size_t)ctx->sm_count * DIP_MAIL_FLOATS * sizeof(float), (cudaStream_t)stream));
     return DIP_OK;
 }

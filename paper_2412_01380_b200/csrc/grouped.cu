@@ -1,7 +1,22 @@
-// Products of groups of rows, a group per expert: y[r] = W[e(r)] rows[r], and h = silu(Wg rows) * (Wu rows).
-// Simple form: a block has 16 rows of one expert and 128 outputs, and goes through the input in chunks of 32.
+// Products of groups of rows, a group per expert, on the fifth-generation tensor cores: y[r] = W[e(r)] rows[r], and
+// h[r] = silu(Wg[e(r)] rows[r]) * (Wu[e(r)] rows[r]).  One kernel for a token's one or two rows and for a prompt's thousands.
+//
+// A tile is 128 rows of one expert by 256 rows of its weights (gate/up: the 128 gate and the 128 up rows of the same
+// outputs, so that one thread has both).  Both operands are K-major 128-byte pieces (64 bfloat16, 128 e4m3) that TMA lays
+// into shared memory with the 128-byte swizzle the operand descriptors name; a step of the pipeline is 16 + 32 KB.
+//   warp 0      one thread issues the copies: a ring of GP_STAGES steps
+//   warp 1      one thread issues the MMAs (M = 128, N = 256, four per step) into one of two accumulators of 256 columns
+//   warps 4-11  take the accumulators out: thread = row, a half of the columns for each four warps
+// BF16: an accumulator is a tile, and the next tile's MMAs run while the first is taken out.  FP8: a step is a block of 128
+// input indices, which has scales of its own, so every step's accumulator is taken out and added, times row scale * weight
+// scale, to binary32 sums in registers: 256 multiply-adds per warp scheduler and step against the 512 cycles of its MMAs.
+//
+// Blocks stay: whole rounds of tiles are dealt out one to a block, and what is left over (all of it where there are
+// fewer tiles than SMs, as for a token) is cut along K into equal runs of steps, one per block, in tile order.  A tile's
+// parts meet in the partial sums' workspace; the block that comes last adds them up in order of K, so results do not
+// depend on who that is, and nobody waits.
+#include <cuda.h>
 #include <cuda_bf16.h>
-#include <cuda_fp8.h>
 
 #include "common.cuh"
 #include "float8.cuh"
@@ -9,96 +24,485 @@
 
 namespace {
 
-constexpr int GP_ROWS = 16, GP_COLS = 128, GP_K = 32, GP_THREADS = 256;
+constexpr int GP_ROWS = DIP_GROUP_ROWS, GP_COLS = DIP_GROUP_COLS;
+constexpr int GP_STAGES = 4;
+constexpr int GP_STEP_BYTES = 128;                  // of a row, per step
+constexpr int GP_BOX = 32;                          // rows per copy of the row operand
+constexpr int GP_A_BYTES = GP_ROWS * GP_STEP_BYTES, GP_B_BYTES = GP_COLS * GP_STEP_BYTES;
+constexpr int GP_OUT_WARPS = 8, GP_THREADS = (4 + GP_OUT_WARPS) * 32;
+// registers of a thread of the first four warps and of the others, out of the launch's 168 each: (56 + 2 * 224) / 3
+constexpr int GP_REGS_FEW = 56, GP_REGS_MANY = 224;
+constexpr int GP_TMEM_COLS = 512;
+constexpr int GP_MIN_STEPS = 4;                     // a part of a tile has at least so many
+constexpr int GP_CHUNK = 12;                        // row tiles that go through an expert's weights together
 
 struct GroupedParams {
-    const void *w, *up, *rows;
     const float *w_scales, *up_scales, *row_scales;
-    int n_experts, d_out, d_in, n_rows;
+    int n_experts, d_out, d_in, n_rows, steps;
     const int32_t *offset;
     void *out;
     float *out_scales;
     int out_f32;
+    float *partials;
+    unsigned int *tickets;
+    int *status;
+    unsigned long long wait_limit_ns;
+    unsigned long long *tr;
 };
 
-template <bool FP8>
-__device__ __forceinline__ float grouped_value(const void *p, size_t i)
+struct __align__(1024) GroupedSmem {
+    unsigned char a[GP_STAGES][GP_A_BYTES];
+    unsigned char b[GP_STAGES][GP_B_BYTES];
+    uint64_t full[GP_STAGES], empty[GP_STAGES];     // a step's copies have landed; its MMAs have read them
+    uint64_t sum_full[2], sum_empty[2];             // an accumulator is complete; has been taken out
+    uint64_t drained;
+    uint32_t tmem_base;
+    int last;
+    float amax[2][GP_ROWS];
+    int start[DIP_MAX_EXPERTS + 1];                 // first row of each expert
+    int tiles[DIP_MAX_EXPERTS + 1];                 // row tiles in front of it
+};
+
+__device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, int x, int y, uint64_t *bar)
 {
-    if (FP8) return (float)static_cast<const __nv_fp8_e4m3 *>(p)[i];
-    return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+
+// K-major operand, 128-byte swizzle: groups of 8 rows are 1 KB apart.
+__device__ __forceinline__ uint64_t operand_desc(const void *p)
+{
+    return (uint64_t)((smem_u32(p) & 0x3ffffu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// binary32 sums, K-major operands of M = 128 and N = 256; bfloat16 (kind::f16) or e4m3 (kind::f8f6f4)
+template <bool FP8>
+__device__ __forceinline__ void grouped_mma(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t accumulate)
+{
+    constexpr uint32_t SHAPE = (1u << 4) | ((uint32_t)(GP_COLS >> 3) << 17) | ((uint32_t)(GP_ROWS >> 4) << 24);
+    if (FP8)
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
+                     ::"r"(d_tmem), "l"(a), "l"(b), "r"(SHAPE), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                     ::"r"(d_tmem), "l"(a), "l"(b), "r"(SHAPE | (1u << 7) | (1u << 10)), "r"(accumulate) : "memory");
+}
+
+__device__ __forceinline__ void grouped_commit(uint64_t *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+// 32 columns of this warp's 32 lanes: thread = lane, register = column.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+                 "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+                   "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+                   "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(taddr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+// Barriers of the warps that take sums out; the second also says to all of them alike whether any came with `v`.
+__device__ __forceinline__ void out_barrier() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(GP_OUT_WARPS * 32) : "memory"); }
+__device__ __forceinline__ bool out_barrier_any(bool v)
+{
+    unsigned any;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n barrier.cta.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(any) : "r"((unsigned)v), "n"(GP_OUT_WARPS * 32) : "memory");
+    return any != 0u;
+}
+
+// One run of steps of one tile.
+struct Run {
+    int expert, row0, rows, out0;   // the tile: its first row, its rows, its first output
+    int k0, k1;                     // steps
+    int rest;                       // index among the tiles that are cut, -1: dealt out whole
+};
+
+// The runs of this block, in order.  Every role walks through them for itself.
+template <bool GATED>
+struct Schedule {
+    const GroupedSmem &s;
+    int n_experts, steps, n_cols;
+    int whole;                      // rounds of whole tiles
+    long long units, parts;         // steps of the tiles that are cut, blocks that share them
+    long long at, end;              // this block's units
+
+    __device__ __forceinline__ Schedule(const GroupedSmem &sm, const GroupedParams &p) : s(sm), n_experts(p.n_experts), steps(p.steps)
+    {
+        const int width = GATED ? GP_COLS / 2 : GP_COLS, g = gridDim.x;
+        n_cols = (p.d_out + width - 1) / width;
+        const long long tiles = (long long)s.tiles[n_experts] * n_cols;
+        whole = (int)(tiles / g);
+        units = (tiles - (long long)whole * g) * steps;
+        parts = min((long long)g, max(units / GP_MIN_STEPS, tiles - (long long)whole * g));
+        at = (int)blockIdx.x < parts ? units * blockIdx.x / parts : 0;
+        end = (int)blockIdx.x < parts ? units * (blockIdx.x + 1) / parts : 0;
+    }
+    // first and last block with a part of cut tile `rest`, and which of that block's runs it is
+    __device__ __forceinline__ int block_of(long long unit) const { return (int)(((unit + 1) * parts - 1) / units); }
+    __device__ __forceinline__ int run_of(int block, int rest) const { return (int)(units * block / parts / steps) == rest ? 0 : 1; }
+
+    __device__ __forceinline__ void locate(long long tile, Run &r) const
+    {
+        int lo = 0, hi = n_experts;             // the expert with tiles[e] * n_cols <= tile < tiles[e + 1] * n_cols
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((long long)s.tiles[mid] * n_cols <= tile) lo = mid;
+            else hi = mid;
+        }
+        const int n_rows = s.start[lo + 1] - s.start[lo], row_tiles = s.tiles[lo + 1] - s.tiles[lo];
+        const int l = (int)(tile - (long long)s.tiles[lo] * n_cols), chunk = l / (GP_CHUNK * n_cols);
+        const int here = min(GP_CHUNK, row_tiles - chunk * GP_CHUNK), in = l - chunk * GP_CHUNK * n_cols;
+        const int m = chunk * GP_CHUNK + in % here;
+        r.expert = lo;
+        r.row0 = s.start[lo] + m * GP_ROWS;
+        r.rows = min(GP_ROWS, n_rows - m * GP_ROWS);
+        r.out0 = in / here * (GATED ? GP_COLS / 2 : GP_COLS);
+    }
+    __device__ __forceinline__ bool get(int i, Run &r) const
+    {
+        if (i < whole) {
+            locate((long long)i * gridDim.x + blockIdx.x, r);
+            r.k0 = 0;
+            r.k1 = steps;
+            r.rest = -1;
+            return true;
+        }
+        long long u = at;
+        for (i -= whole; i > 0 && u < end; --i) u = min(end, (u / steps + 1) * steps);
+        if (u >= end) return false;
+        r.rest = (int)(u / steps);
+        locate((long long)whole * gridDim.x + r.rest, r);
+        r.k0 = (int)(u - (long long)r.rest * steps);
+        r.k1 = (int)min((long long)steps, r.k0 + (end - u));
+        return true;
+    }
+};
+
+// first rows and tiles of the experts, by one warp
+__device__ __forceinline__ void grouped_plan(const GroupedParams &p, GroupedSmem &s)
+{
+    const int lane = threadIdx.x & 31, each = (p.n_experts + 32) / 32;      // offsets per lane
+    const int i0 = min(lane * each, p.n_experts + 1), i1 = min(i0 + each, p.n_experts + 1);
+    int most = 0;
+    for (int i = i0; i < i1; ++i) {
+        const int v = p.offset ? min(p.offset[i], p.n_rows) : i ? p.n_rows : 0;
+        most = max(most, v);
+        s.start[i] = most;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, most, o);
+        if (lane >= o) most = max(most, v);
+    }
+    int before = __shfl_up_sync(0xffffffffu, most, 1);
+    if (lane == 0) before = 0;
+    for (int i = i0; i < i1; ++i) s.start[i] = max(s.start[i], before);
+    __syncwarp();
+    int n = 0;
+    for (int i = i0; i < i1; ++i) {
+        s.tiles[i] = n;
+        if (i < p.n_experts) n += (s.start[i + 1] - s.start[i] + GP_ROWS - 1) / GP_ROWS;
+    }
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    for (int i = i0; i < i1; ++i) s.tiles[i] += incl - n;
 }
 
 template <bool FP8, bool GATED>
-__global__ void __launch_bounds__(GP_THREADS) grouped_simple_kernel(const GroupedParams p)
+__global__ void __launch_bounds__(GP_THREADS, 1)
+grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap w_map,
+               const __grid_constant__ CUtensorMap up_map, const GroupedParams p)
 {
-    __shared__ float sx[GP_ROWS][GP_K + 1], sw[GP_COLS][GP_K + 1], su[GATED ? GP_COLS : 1][GP_K + 1];
-    __shared__ float amax[GP_ROWS][16];
-    dip_grid_dependency_wait();
+    extern __shared__ unsigned char gp_smem_raw[];
+    GroupedSmem &s = *reinterpret_cast<GroupedSmem *>((reinterpret_cast<uintptr_t>(gp_smem_raw) + 1023) & ~(uintptr_t)1023);
+    DIP_TRACE_MIN(p.tr, 0);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem_base)),
+                     "n"(GP_TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (tid == 0) {
+        for (int i = 0; i < GP_STAGES; ++i) {
+            mbar_init(&s.full[i], 1);
+            mbar_init(&s.empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s.sum_full[i], 1);
+            mbar_init(&s.sum_empty[i], GP_OUT_WARPS);
+        }
+        mbar_init(&s.drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    dip_grid_dependency_wait();                      // rows and offsets come from the kernels in front
+    DIP_TRACE_MIN(p.tr, 1);
+    if (warp == 0) grouped_plan(p, s);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     dip_launch_dependents();
-    const int tid = threadIdx.x, r = tid >> 4, c = tid & 15, o0 = blockIdx.x * GP_COLS;
-    const int kb = (p.d_in + 127) / 128, ob = (p.d_out + 127) / 128;
-    for (int e = 0, tile = 0, last = 0; e < p.n_experts; ++e) {
-        const int r0 = p.offset ? max(last, min(p.offset[e], p.n_rows)) : 0, r1 = p.offset ? min(p.offset[e + 1], p.n_rows) : p.n_rows;
-        last = max(r0, r1);
-        for (int m = r0; m < r1; m += GP_ROWS, ++tile) {
-            if (tile % gridDim.y != blockIdx.y) continue;
-            float a[8] = {}, b[8] = {};
-            for (int k0 = 0; k0 < p.d_in; k0 += GP_K) {
-                __syncthreads();
-                for (int i = tid; i < GP_ROWS * GP_K; i += GP_THREADS) {
-                    const int row = m + i / GP_K, k = k0 + i % GP_K;
-                    float v = row < r1 ? grouped_value<FP8>(p.rows, (size_t)row * p.d_in + k) : 0.f;
-                    if (FP8 && row < r1) v *= p.row_scales[(size_t)row * kb + k / 128];
-                    sx[i / GP_K][i % GP_K] = v;
-                }
-                for (int i = tid; i < GP_COLS * GP_K; i += GP_THREADS) {
-                    const int o = o0 + i / GP_K, k = k0 + i % GP_K;
-                    const size_t at = ((size_t)e * p.d_out + o) * p.d_in + k, sc = ((size_t)e * ob + o / 128) * kb + k / 128;
-                    float v = 0.f, u = 0.f;
-                    if (o < p.d_out) {
-                        v = grouped_value<FP8>(p.w, at) * (FP8 ? p.w_scales[sc] : 1.f);
-                        if (GATED) u = grouped_value<FP8>(p.up, at) * (FP8 ? p.up_scales[sc] : 1.f);
+    const uint32_t tmem = s.tmem_base;
+    const Schedule<GATED> plan(s, p);
+    const int per_step = FP8 ? GP_STEP_BYTES : GP_STEP_BYTES / 2;
+    bool failed = false;
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(GP_REGS_FEW));
+        if (warp == 0 && lane == 0) {
+            Run r;
+            int g = 0;                               // steps so far
+            for (int i = 0; !failed && plan.get(i, r); ++i) {
+                const int boxes = (r.rows + GP_BOX - 1) / GP_BOX;
+                const int w_row = r.expert * p.d_out + r.out0;
+                // (plain: the tile's second half may lie behind the last output)
+                const bool second = GATED || r.out0 + GP_COLS / 2 < p.d_out;
+                const unsigned bytes = boxes * GP_BOX * GP_STEP_BYTES + (second ? GP_B_BYTES : GP_B_BYTES / 2);
+                for (int k = r.k0; k < r.k1; ++k, ++g) {
+                    const int st = g % GP_STAGES;
+                    if (g >= GP_STAGES && !mbar_wait(&s.empty[st], (g / GP_STAGES - 1) & 1, p.wait_limit_ns)) {
+                        failed = true;
+                        break;
                     }
-                    sw[i / GP_K][i % GP_K] = v;
-                    if (GATED) su[i / GP_K][i % GP_K] = u;
+                    mbar_expect_tx(&s.full[st], bytes);
+                    for (int b = 0; b < boxes; ++b)
+                        tma_load(s.a[st] + b * GP_BOX * GP_STEP_BYTES, &rows_map, k * per_step, r.row0 + b * GP_BOX, &s.full[st]);
+                    tma_load(s.b[st], &w_map, k * per_step, w_row, &s.full[st]);
+                    if (second)
+                        tma_load(s.b[st] + GP_B_BYTES / 2, GATED ? &up_map : &w_map, k * per_step, GATED ? w_row : w_row + GP_COLS / 2,
+                                 &s.full[st]);
                 }
-                __syncthreads();
-                for (int k = 0; k < GP_K; ++k)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        a[j] = fmaf(sx[r][k], sw[c + 16 * j][k], a[j]);
-                        if (GATED) b[j] = fmaf(sx[r][k], su[c + 16 * j][k], b[j]);
-                    }
             }
-            const int row = m + r;
-            float scale = 1.f;
+            // (given up: no copy of this block's is under way when it leaves)
+            if (failed)
+                for (int j = max(0, g - GP_STAGES); j < g; ++j) mbar_wait(&s.full[j % GP_STAGES], (j / GP_STAGES) & 1, p.wait_limit_ns);
+        } else if (warp == 1 && lane == 0) {
+            Run r;
+            int g = 0, n = 0;                        // steps, accumulators so far
+            for (int i = 0; !failed && plan.get(i, r); ++i) {
+                for (int k = r.k0; k < r.k1; ++k, ++g) {
+                    const int st = g % GP_STAGES, buf = n & 1;
+                    const bool first = FP8 || k == r.k0, last = FP8 || k == r.k1 - 1;
+                    if ((first && n >= 2 && !mbar_wait(&s.sum_empty[buf], (n / 2 - 1) & 1, p.wait_limit_ns)) ||
+                        !mbar_wait(&s.full[st], (g / GP_STAGES) & 1, p.wait_limit_ns)) {
+                        failed = true;
+                        break;
+                    }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t a = operand_desc(s.a[st]), b = operand_desc(s.b[st]);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)      // 32 bytes of K each
+                        grouped_mma<FP8>(tmem + buf * GP_COLS, a + 2 * q, b + 2 * q, (first && q == 0) ? 0u : 1u);
+                    grouped_commit(&s.empty[st]);
+                    if (last) {
+                        grouped_commit(&s.sum_full[buf]);
+                        ++n;
+                    }
+                }
+            }
+            if (failed) {
+                grouped_commit(&s.drained);
+                mbar_wait(&s.drained, 0, p.wait_limit_ns);
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(GP_REGS_MANY));
+        const int half = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        // this thread's columns: 64 from col0 on and 64 from col1 on
+        const int col0 = GATED ? 64 * half : 128 * half, col1 = GATED ? 128 + 64 * half : 128 * half + 64;
+        const int in_blocks = (p.d_in + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK, out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
+        int n = 0;
+        Run r;
+        for (int i = 0; !failed && plan.get(i, r); ++i) {
+            float acc[128];
+            if (FP8) {
+#pragma unroll
+                for (int j = 0; j < 128; ++j) acc[j] = 0.f;
+                const float *xs = p.row_scales + (size_t)(r.row0 + min(row, r.rows - 1)) * in_blocks;
+                const int ob = r.out0 / DIP_FP8_BLOCK + (GATED ? 0 : half);
+                const float *ws = p.w_scales + ((size_t)r.expert * out_blocks + min(ob, out_blocks - 1)) * in_blocks;
+                const float *us = GATED ? p.up_scales + ((size_t)r.expert * out_blocks + ob) * in_blocks : ws;
+                for (int k = r.k0; k < r.k1; ++k, ++n) {
+                    const float x = __ldg(xs + k), s0 = x * __ldg(ws + k), s1 = GATED ? x * __ldg(us + k) : s0;
+                    const int buf = n & 1;
+                    if (!mbar_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns)) {
+                        failed = true;
+                        break;
+                    }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[32];
+                        tmem_ld32(lanes + buf * GP_COLS + (c < 2 ? col0 + 32 * c : col1 + 32 * (c - 2)), v);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) acc[32 * c + j] = fmaf(__uint_as_float(v[j]), c < 2 ? s0 : s1, acc[32 * c + j]);
+                    }
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
+                }
+            } else {
+                const int buf = n & 1;
+                if (!mbar_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns)) failed = true;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t v[32];
+                    tmem_ld32(lanes + buf * GP_COLS + (c < 2 ? col0 + 32 * c : col1 + 32 * (c - 2)), v);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) acc[32 * c + j] = __uint_as_float(v[j]);
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
+                ++n;
+            }
+            // (a wait of one warp that runs out takes the others along: they meet at barriers below)
+            failed = out_barrier_any(failed);
+            if (failed) break;
+
+            if (r.k1 - r.k0 < p.steps) {
+                // a part of the tile: the last of its blocks goes on with the sum of all
+                const int b0 = plan.block_of((long long)r.rest * p.steps), b1 = plan.block_of((long long)(r.rest + 1) * p.steps - 1);
+                const size_t mine = (size_t)half * 32 * GP_ROWS + row;
+                float4 *to = reinterpret_cast<float4 *>(p.partials) +
+                             (size_t)(2 * blockIdx.x + plan.run_of(blockIdx.x, r.rest)) * (GP_ROWS * GP_COLS / 4) + mine;
+                if (row < r.rows) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) to[j * GP_ROWS] = make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
+                }
+                __threadfence();
+                out_barrier();
+                if (warp == 4 && lane == 0) {
+                    s.last = atomicAdd(p.tickets + r.rest, 1u) == (unsigned)(b1 - b0);
+                    if (s.last) p.tickets[r.rest] = 0u;
+                    __threadfence();
+                }
+                out_barrier();
+                if (!s.last) continue;
+#pragma unroll
+                for (int j = 0; j < 128; ++j) acc[j] = 0.f;
+                if (row < r.rows) {
+                    for (int b = b0; b <= b1; ++b) {
+                        const float4 *from = reinterpret_cast<const float4 *>(p.partials) +
+                                             (size_t)(2 * b + plan.run_of(b, r.rest)) * (GP_ROWS * GP_COLS / 4) + mine;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float4 v = __ldcg(from + j * GP_ROWS);
+                            acc[4 * j] += v.x;
+                            acc[4 * j + 1] += v.y;
+                            acc[4 * j + 2] += v.z;
+                            acc[4 * j + 3] += v.w;
+                        }
+                    }
+                }
+            }
+
+            const size_t at = (size_t)(r.row0 + row) * p.d_out;
             if (GATED) {
-                float most = 0.f;
+                const int o = r.out0 + 64 * half;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    a[j] = silu_f32(a[j]) * b[j];
-                    if (o0 + c + 16 * j < p.d_out) most = fmaxf(most, fabsf(a[j]));
-                }
+                for (int j = 0; j < 64; ++j) acc[j] = silu_f32(acc[j]) * acc[64 + j];
                 if (FP8) {
-                    amax[r][c] = most;
-                    __syncthreads();
-                    for (int i = 0; i < 16; ++i) most = fmaxf(most, amax[r][i]);
-                    scale = fp8_scale(most);
-                    if (row < r1 && c == 0) p.out_scales[(size_t)row * ob + blockIdx.x] = scale;
-                }
-            }
-            if (row >= r1) continue;
+                    // a block of 128 outputs has a scale: two threads have a half each
+                    float most = 0.f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int o = o0 + c + 16 * j;
-                if (o >= p.d_out) continue;
-                const size_t at = (size_t)row * p.d_out + o;
-                if (GATED && FP8) static_cast<uint8_t *>(p.out)[at] = (uint8_t)fp8_codes4(a[j], 0.f, 0.f, 0.f, scale);
-                else if (p.out_f32) static_cast<float *>(p.out)[at] = a[j];
-                else static_cast<__nv_bfloat16 *>(p.out)[at] = __float2bfloat16_rn(a[j]);
+                    for (int j = 0; j < 64; ++j)
+                        if (o + j < p.d_out) most = fmaxf(most, fabsf(acc[j]));
+                    s.amax[half][row] = most;
+                    out_barrier();
+                    const float scale = fp8_scale(fmaxf(most, s.amax[half ^ 1][row]));
+                    if (row < r.rows) {
+                        if (half == 0) p.out_scales[(size_t)(r.row0 + row) * out_blocks + r.out0 / DIP_FP8_BLOCK] = scale;
+#pragma unroll
+                        for (int j = 0; j < 64; j += 16)
+                            if (o + j < p.d_out)
+                                *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.out) + at + o + j) =
+                                    make_uint4(fp8_codes4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3], scale),
+                                               fp8_codes4(acc[j + 4], acc[j + 5], acc[j + 6], acc[j + 7], scale),
+                                               fp8_codes4(acc[j + 8], acc[j + 9], acc[j + 10], acc[j + 11], scale),
+                                               fp8_codes4(acc[j + 12], acc[j + 13], acc[j + 14], acc[j + 15], scale));
+                    }
+                    out_barrier();                   // (before the next tile's maxima)
+                } else if (row < r.rows) {
+#pragma unroll
+                    for (int j = 0; j < 64; j += 8)
+                        if (o + j < p.d_out) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + at + o + j) = bf16x8(acc + j);
+                }
+            } else if (row < r.rows) {
+                const int o = r.out0 + 128 * half;
+                if (p.out_f32) {
+#pragma unroll
+                    for (int j = 0; j < 128; j += 4)
+                        if (o + j < p.d_out)
+                            *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at + o + j) =
+                                make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 128; j += 8)
+                        if (o + j < p.d_out) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + at + o + j) = bf16x8(acc + j);
+                }
             }
         }
     }
+    if (failed) atomicExch(p.status, 1);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(GP_TMEM_COLS) : "memory");
+    DIP_TRACE_MAX(p.tr, 2);
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder, looked up once (the library does not link against libcuda).
+EncodeTiled encoder()
+{
+    static const EncodeTiled fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return (EncodeTiled)f;
+    }();
+    return fn;
+}
+
+// Pieces of `box` rows by 128 bytes of a row-major [n][d] matrix, laid down with the 128-byte swizzle; zeros outside.
+bool encode(CUtensorMap *map, const void *p, bool fp8, size_t n, int d, int box)
+{
+    const int item = fp8 ? 1 : 2;
+    const cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)n}, strides[1] = {(cuuint64_t)d * item};
+    const cuuint32_t piece[2] = {(cuuint32_t)(GP_STEP_BYTES / item), (cuuint32_t)box}, one[2] = {1, 1};
+    return encoder()(map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(p), dims, strides,
+                     piece, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool FP8, bool GATED>
+cudaError_t launch(dip_ctx *ctx, int ctas, cudaStream_t stream, const CUtensorMap &rows, const CUtensorMap &w, const CUtensorMap &up,
+                   const GroupedParams &p)
+{
+    static dip_per_device_once once;
+    const size_t smem = sizeof(GroupedSmem) + 1024;
+    static_assert(sizeof(GroupedSmem) + 1024 <= 227 * 1024, "fits a CTA's shared memory");
+    const cudaError_t e = dip_raise_smem_limit(once, ctx->device, grouped_kernel<FP8, GATED>, smem);
+    return e != cudaSuccess ? e : dip_launch_pdl(grouped_kernel<FP8, GATED>, dim3(ctas), dim3(GP_THREADS), smem, stream, rows, w, up, p);
 }
 
 }  // namespace
@@ -108,11 +512,36 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
                               cudaStream_t stream)
 {
     const bool fp8 = w.wtype == DIP_W_FP8_B128;
-    const GroupedParams p = {w.values, up ? up->values : nullptr, rows, w.scales, up ? up->scales : nullptr, row_scales, w.n_experts,
-                             w.d_out, w.d_in, n_rows, offset, out, out_scales, out_f32};
-    const dim3 grid((w.d_out + GP_COLS - 1) / GP_COLS, min(64, (n_rows + GP_ROWS - 1) / GP_ROWS + w.n_experts)), block(GP_THREADS);
-    const auto kernel = fp8 ? (up ? grouped_simple_kernel<true, true> : grouped_simple_kernel<true, false>)
-                            : (up ? grouped_simple_kernel<false, true> : grouped_simple_kernel<false, false>);
-    DIP_CUDA_TRY(ctx, dip_launch_pdl(kernel, grid, block, 0, stream, p));
+    const size_t w_rows = (size_t)w.n_experts * w.d_out;
+    CUtensorMap rows_map, w_map, up_map;
+    if (!encoder() || !encode(&rows_map, rows, fp8, n_rows, w.d_in, GP_BOX) || !encode(&w_map, w.values, fp8, w_rows, w.d_in, GP_COLS / 2) ||
+        !encode(&up_map, up ? up->values : w.values, fp8, w_rows, w.d_in, GP_COLS / 2)) {
+        snprintf(ctx->err, sizeof(ctx->err), "cuTensorMapEncodeTiled failed");
+        return DIP_ERR_CUDA;
+    }
+    GroupedParams p = {};
+    p.w_scales = w.scales;
+    p.up_scales = up ? up->scales : nullptr;
+    p.row_scales = row_scales;
+    p.n_experts = w.n_experts;
+    p.d_out = w.d_out;
+    p.d_in = w.d_in;
+    p.n_rows = n_rows;
+    p.steps = (w.d_in * (fp8 ? 1 : 2) + GP_STEP_BYTES - 1) / GP_STEP_BYTES;
+    p.offset = offset;
+    p.out = out;
+    p.out_scales = out_scales;
+    p.out_f32 = out_f32;
+    p.partials = ctx->group_partials;
+    p.tickets = ctx->group_tickets;
+    p.status = ctx->status;
+    p.wait_limit_ns = ctx->wait_limit_ns;
+    p.tr = dip_trace_slot(ctx, up ? 10 : 11);
+    // no more blocks than there can be parts
+    const int width = up ? GP_COLS / 2 : GP_COLS;
+    const long long tiles = (long long)((n_rows + GP_ROWS - 1) / GP_ROWS + min(w.n_experts, n_rows) - 1) * ((w.d_out + width - 1) / width);
+    const int ctas = (int)min((long long)ctx->sm_count, max(tiles, tiles * p.steps / GP_MIN_STEPS));
+    const auto start = fp8 ? (up ? launch<true, true> : launch<true, false>) : (up ? launch<false, true> : launch<false, false>);
+    DIP_CUDA_TRY(ctx, start(ctx, ctas, stream, rows_map, w_map, up_map, p));
     return DIP_OK;
 }
