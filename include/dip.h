@@ -671,10 +671,10 @@ dip_status dip_grouped_gate_up(dip_ctx *ctx, const dip_grouped_matrix *gate, con
 
 /* ------------------------------------------------------------------------
  * dip_combine_rows — y[t] = sum over j of weight[t][j] * rows[token_row[t][j]]
- * in the order of j, binary32 sums, bfloat16 rows and y; a choice that is -1 adds
- * nothing, a token without any gets 0.  d as above.
+ * in the order of j, binary32 rows and sums, y rounded once to bfloat16; a choice
+ * that is -1 adds nothing, a token without any gets 0.  d as above.
  * ------------------------------------------------------------------------ */
-dip_status dip_combine_rows(dip_ctx *ctx, const void *rows, const dip_expert_route *route, int d, void *y, void *stream);
+dip_status dip_combine_rows(dip_ctx *ctx, const float *rows, const dip_expert_route *route, int d, void *y, void *stream);
 
 /* Buffers of dip_expert_mlp for n = n_tokens * top_k rows (n_tokens without a route); the caller's. */
 typedef struct {
@@ -682,7 +682,7 @@ typedef struct {
     float *row_scales;   /* [n][ceil(d_model/128)], FP8 only                                   */
     void *h;             /* [n][d_ff]: bfloat16, or e4m3                                       */
     float *h_scales;     /* [n][ceil(d_ff/128)], FP8 only                                      */
-    void *out;           /* [n][d_model] bfloat16.  NULL without a route                       */
+    float *out;          /* [n][d_model].  NULL without a route                                */
 } dip_expert_work;
 
 /* ------------------------------------------------------------------------

@@ -652,7 +652,7 @@ class ExpertWork:
         fp8 = w.wtype == W_FP8_B128
         self.rows = Rows(self.max_rows, w.d_model, w.wtype, device) if fp8 or self.routed else None
         self.h = Rows(self.max_rows, w.d_ff, w.wtype, device)
-        self.out = torch.empty((self.max_rows, w.d_model), dtype=torch.bfloat16, device=device) if self.routed else None
+        self.out = torch.empty((self.max_rows, w.d_model), device=device) if self.routed else None
         self.struct = ExpertWorkStruct(_ptr(self.rows.values) if self.rows else None, _ptr(self.rows.scales) if self.rows else None,
                                        _ptr(self.h.values), _ptr(self.h.scales), _ptr(self.out))
 
@@ -722,11 +722,11 @@ def dip_grouped_gate_up(ctx: Context, gate: GroupedMatrix, up: GroupedMatrix, ro
 
 
 def dip_combine_rows(ctx: Context, rows: torch.Tensor, route: ExpertRoute, y: torch.Tensor) -> None:
-    """y [n, d] = the weighted sums of rows [>= n * top_k, d]; both bfloat16, n the route's tokens."""
+    """y [n, d] bfloat16 = the weighted sums of rows [>= n * top_k, d], binary32; n the route's tokens."""
     route._check(ctx)
     _need(route.n_tokens >= 1, "the route has no tokens yet")
     _tensor(y, torch.bfloat16, (route.n_tokens, None), "y", ctx)
-    _tensor(rows, torch.bfloat16, (None, y.shape[1]), "rows", ctx)
+    _tensor(rows, torch.float32, (None, y.shape[1]), "rows", ctx)
     _need(rows.shape[0] >= route.n_rows, "rows has %d rows for %d" % (rows.shape[0], route.n_rows))
     ctx.check(_lib.dip_combine_rows(ctx.handle, _ptr(rows), C.byref(route.struct), y.shape[1], _ptr(y), _stream()))
 

@@ -295,7 +295,7 @@ dip_status dip_launch_pack(dip_ctx *ctx, int wtype, int d_model, int d_ff,
 dip_status dip_launch_route(dip_ctx *ctx, const void *logits, bool bf16, bool renormalize, const dip_expert_route &r, cudaStream_t stream);
 dip_status dip_launch_stage_rows(dip_ctx *ctx, const void *x, int n_tokens, int d, const dip_expert_route *route, bool fp8,
                                  void *rows, float *scales, cudaStream_t stream);
-dip_status dip_launch_combine_rows(dip_ctx *ctx, const void *rows, const dip_expert_route &r, int d, void *y, cudaStream_t stream);
+dip_status dip_launch_combine_rows(dip_ctx *ctx, const float *rows, const dip_expert_route &r, int d, void *y, cudaStream_t stream);
 
 // grouped.cu: products of groups of rows.  up != nullptr: out = silu(w rows) * (up rows), FP8: as codes with out_scales.
 dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const dip_grouped_matrix *up, const void *rows,

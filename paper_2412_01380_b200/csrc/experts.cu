@@ -73,7 +73,7 @@ dip_status dip_grouped_gate_up(dip_ctx *ctx, const dip_grouped_matrix *gate, con
     return dip_launch_grouped(ctx, *gate, up, rows, row_scales, n_rows, offset, h, false, h_scales, (cudaStream_t)stream);
 }
 
-dip_status dip_combine_rows(dip_ctx *ctx, const void *rows, const dip_expert_route *route, int d, void *y, void *stream)
+dip_status dip_combine_rows(dip_ctx *ctx, const float *rows, const dip_expert_route *route, int d, void *y, void *stream)
 {
     if (!dip_ctx_current(ctx) || bad(rows) || bad(y) || !route_ok(route) || !width_ok(d)) return DIP_ERR_INVALID_ARG;
     return dip_launch_combine_rows(ctx, rows, *route, d, y, (cudaStream_t)stream);
@@ -103,8 +103,8 @@ dip_status dip_expert_mlp(dip_ctx *ctx, const dip_grouped_matrix *gate, const di
     if ((st = dip_launch_grouped(ctx, *gate, up, staged ? work->rows : x, work->row_scales, n_rows, offset, work->h, false,
                                  work->h_scales, s)) != DIP_OK)
         return st;
-    if ((st = dip_launch_grouped(ctx, *down, nullptr, work->h, work->h_scales, n_rows, offset, route ? work->out : y, false, nullptr,
-                                 s)) != DIP_OK)
+    if ((st = dip_launch_grouped(ctx, *down, nullptr, work->h, work->h_scales, n_rows, offset,
+                                 route ? work->out : y, route != nullptr, nullptr, s)) != DIP_OK)
         return st;
     return route ? dip_launch_combine_rows(ctx, work->out, *route, d, y, s) : DIP_OK;
 }

@@ -4,6 +4,9 @@
 // A tile is 128 rows of one expert by 256 rows of its weights (gate/up: the 128 gate and the 128 up rows of the same
 // outputs, so that one thread has both).  Both operands are K-major 128-byte pieces (64 bfloat16, 128 e4m3) that TMA lays
 // into shared memory with the 128-byte swizzle the operand descriptors name; a step of the pipeline is 16 + 32 KB.
+// A tile of at most GP_FEW rows changes the operands' roles: the weights are the M side (two MMAs of 128) and the rows the
+// N side, as many columns as there are rows (in sixteens).  The loads are the same, but a thread then has one output of a few rows
+// instead of one row of 128 outputs, and what follows the last step takes as long as there are rows.
 //   warp 0      one thread issues the copies: a ring of GP_STAGES steps
 //   warp 1      one thread issues the MMAs (M = 128, N = 256, four per step) into one of two accumulators of 256 columns
 //   warps 4-11  take the accumulators out: thread = row, a half of the columns for each four warps
@@ -27,18 +30,19 @@ namespace {
 constexpr int GP_ROWS = DIP_GROUP_ROWS, GP_COLS = DIP_GROUP_COLS;
 constexpr int GP_STAGES = 4;
 constexpr int GP_STEP_BYTES = 128;                  // of a row, per step
-constexpr int GP_BOX = 32;                          // rows per copy of the row operand
+constexpr int GP_BOX = 32;                          // rows per copy of the rows of a tile of few
 constexpr int GP_A_BYTES = GP_ROWS * GP_STEP_BYTES, GP_B_BYTES = GP_COLS * GP_STEP_BYTES;
 constexpr int GP_OUT_WARPS = 8, GP_THREADS = (4 + GP_OUT_WARPS) * 32;
 // registers of a thread of the first four warps and of the others, out of the launch's 168 each: (56 + 2 * 224) / 3
 constexpr int GP_REGS_FEW = 56, GP_REGS_MANY = 224;
 constexpr int GP_TMEM_COLS = 512;
 constexpr int GP_MIN_STEPS = 4;                     // a part of a tile has at least so many
+constexpr int GP_FEW = 64;                          // rows of a tile that are columns of its sums
 constexpr int GP_CHUNK = 12;                        // row tiles that go through an expert's weights together
 
 struct GroupedParams {
     const float *w_scales, *up_scales, *row_scales;
-    int n_experts, d_out, d_in, n_rows, steps;
+    int n_experts, d_out, d_in, n_rows, steps, n_cols;
     const int32_t *offset;
     void *out;
     float *out_scales;
@@ -58,7 +62,7 @@ struct __align__(1024) GroupedSmem {
     uint64_t drained;
     uint32_t tmem_base;
     int last;
-    float amax[2][GP_ROWS];
+    float amax[4 * GP_FEW > 2 * GP_ROWS ? 4 * GP_FEW : 2 * GP_ROWS];
     int start[DIP_MAX_EXPERTS + 1];                 // first row of each expert
     int tiles[DIP_MAX_EXPERTS + 1];                 // row tiles in front of it
 };
@@ -69,23 +73,43 @@ __device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, int 
                  ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
 }
 
+// A whole warp's bounded wait: all lanes go on alike.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, unsigned parity, unsigned long long limit_ns)
+{
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit_ns));
+}
+
+// One lane of a whole warp.  (A role's warp goes through its loop as a whole and elects a lane where it issues: with the loop in
+// a branch of lane 0, whose operands the compiler cannot know to be uniform, a copy took 180 cycles to issue and an MMA 100.)
+__device__ __forceinline__ bool elect_one()
+{
+    unsigned yes;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+    return yes != 0u;
+}
+
 // K-major operand, 128-byte swizzle: groups of 8 rows are 1 KB apart.
 __device__ __forceinline__ uint64_t operand_desc(const void *p)
 {
     return (uint64_t)((smem_u32(p) & 0x3ffffu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
-// binary32 sums, K-major operands of M = 128 and N = 256; bfloat16 (kind::f16) or e4m3 (kind::f8f6f4)
+// Instruction descriptor: binary32 sums, K-major operands of M = 128 and N = n; bfloat16 or e4m3
 template <bool FP8>
-__device__ __forceinline__ void grouped_mma(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t accumulate)
+__device__ __forceinline__ uint32_t grouped_shape(int n)
 {
-    constexpr uint32_t SHAPE = (1u << 4) | ((uint32_t)(GP_COLS >> 3) << 17) | ((uint32_t)(GP_ROWS >> 4) << 24);
+    return (1u << 4) | (FP8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+
+template <bool FP8>
+__device__ __forceinline__ void grouped_mma(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t shape, uint32_t accumulate)
+{
     if (FP8)
         asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
-                     ::"r"(d_tmem), "l"(a), "l"(b), "r"(SHAPE), "r"(accumulate) : "memory");
+                     ::"r"(d_tmem), "l"(a), "l"(b), "r"(shape), "r"(accumulate) : "memory");
     else
         asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                     ::"r"(d_tmem), "l"(a), "l"(b), "r"(SHAPE | (1u << 7) | (1u << 10)), "r"(accumulate) : "memory");
+                     ::"r"(d_tmem), "l"(a), "l"(b), "r"(shape), "r"(accumulate) : "memory");
 }
 
 __device__ __forceinline__ void grouped_commit(uint64_t *bar)
@@ -106,6 +130,14 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32])
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// Eight columns, without the wait.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
 // Barriers of the warps that take sums out; the second also says to all of them alike whether any came with `v`.
 __device__ __forceinline__ void out_barrier() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(GP_OUT_WARPS * 32) : "memory"); }
 __device__ __forceinline__ bool out_barrier_any(bool v)
@@ -123,63 +155,70 @@ struct Run {
     int rest;                       // index among the tiles that are cut, -1: dealt out whole
 };
 
-// The runs of this block, in order.  Every role walks through them for itself.
+// The runs of this block, in order.  Every role walks through them for itself.  (32 bits hold it all: at most 2^21 tiles, and
+// fewer than a block's worth of cut ones of at most 512 steps.)
 template <bool GATED>
 struct Schedule {
     const GroupedSmem &s;
     int n_experts, steps, n_cols;
     int whole;                      // rounds of whole tiles
-    long long units, parts;         // steps of the tiles that are cut, blocks that share them
-    long long at, end;              // this block's units
+    int units, parts;               // steps of the tiles that are cut, blocks that share them
+    int at, end;                    // this block's units
 
-    __device__ __forceinline__ Schedule(const GroupedSmem &sm, const GroupedParams &p) : s(sm), n_experts(p.n_experts), steps(p.steps)
+    __device__ __forceinline__ Schedule(const GroupedSmem &sm, const GroupedParams &p)
+        : s(sm), n_experts(p.n_experts), steps(p.steps), n_cols(p.n_cols)
     {
-        const int width = GATED ? GP_COLS / 2 : GP_COLS, g = gridDim.x;
-        n_cols = (p.d_out + width - 1) / width;
-        const long long tiles = (long long)s.tiles[n_experts] * n_cols;
-        whole = (int)(tiles / g);
-        units = (tiles - (long long)whole * g) * steps;
-        parts = min((long long)g, max(units / GP_MIN_STEPS, tiles - (long long)whole * g));
-        at = (int)blockIdx.x < parts ? units * blockIdx.x / parts : 0;
-        end = (int)blockIdx.x < parts ? units * (blockIdx.x + 1) / parts : 0;
+        const int g = gridDim.x, tiles = s.tiles[n_experts] * n_cols;
+        whole = tiles / g;
+        const int rest = tiles - whole * g;
+        units = rest * steps;
+        parts = min(g, max(units / GP_MIN_STEPS, rest));
+        const bool mine = (int)blockIdx.x < parts;
+        at = mine ? units * blockIdx.x / parts : 0;
+        end = mine ? units * (blockIdx.x + 1) / parts : 0;
     }
-    // first and last block with a part of cut tile `rest`, and which of that block's runs it is
-    __device__ __forceinline__ int block_of(long long unit) const { return (int)(((unit + 1) * parts - 1) / units); }
-    __device__ __forceinline__ int run_of(int block, int rest) const { return (int)(units * block / parts / steps) == rest ? 0 : 1; }
+    // the block that has a unit, and which of its runs is the one in cut tile `rest`
+    __device__ __forceinline__ int block_of(int unit) const { return ((unit + 1) * parts - 1) / units; }
+    __device__ __forceinline__ int run_of(int block, int rest) const { return units * block / parts / steps == rest ? 0 : 1; }
 
-    __device__ __forceinline__ void locate(long long tile, Run &r) const
+    __device__ __forceinline__ void locate(int tile, Run &r) const
     {
         int lo = 0, hi = n_experts;             // the expert with tiles[e] * n_cols <= tile < tiles[e + 1] * n_cols
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if ((long long)s.tiles[mid] * n_cols <= tile) lo = mid;
+            if (s.tiles[mid] * n_cols <= tile) lo = mid;
             else hi = mid;
         }
         const int n_rows = s.start[lo + 1] - s.start[lo], row_tiles = s.tiles[lo + 1] - s.tiles[lo];
-        const int l = (int)(tile - (long long)s.tiles[lo] * n_cols), chunk = l / (GP_CHUNK * n_cols);
-        const int here = min(GP_CHUNK, row_tiles - chunk * GP_CHUNK), in = l - chunk * GP_CHUNK * n_cols;
-        const int m = chunk * GP_CHUNK + in % here;
+        int in = tile - s.tiles[lo] * n_cols, m = 0, here = row_tiles;
+        if (row_tiles > GP_CHUNK) {
+            m = in / (GP_CHUNK * n_cols) * GP_CHUNK;
+            in -= m * n_cols;
+            here = min(GP_CHUNK, row_tiles - m);
+        }
+        const int col = here == 1 ? in : in / here;
+        m += in - col * here;
         r.expert = lo;
         r.row0 = s.start[lo] + m * GP_ROWS;
         r.rows = min(GP_ROWS, n_rows - m * GP_ROWS);
-        r.out0 = in / here * (GATED ? GP_COLS / 2 : GP_COLS);
+        r.out0 = col * (GATED ? GP_COLS / 2 : GP_COLS);
     }
     __device__ __forceinline__ bool get(int i, Run &r) const
     {
-        if (i < whole) {
-            locate((long long)i * gridDim.x + blockIdx.x, r);
-            r.k0 = 0;
-            r.k1 = steps;
-            r.rest = -1;
-            return true;
+        r.rest = -1;
+        r.k0 = 0;
+        r.k1 = steps;
+        int tile = i * gridDim.x + blockIdx.x;
+        if (i >= whole) {
+            int u = at;
+            for (i -= whole; i > 0 && u < end; --i) u = min(end, (u / steps + 1) * steps);
+            if (u >= end) return false;
+            r.rest = u / steps;
+            r.k0 = u - r.rest * steps;
+            r.k1 = min(steps, r.k0 + (end - u));
+            tile = whole * gridDim.x + r.rest;
         }
-        long long u = at;
-        for (i -= whole; i > 0 && u < end; --i) u = min(end, (u / steps + 1) * steps);
-        if (u >= end) return false;
-        r.rest = (int)(u / steps);
-        locate((long long)whole * gridDim.x + r.rest, r);
-        r.k0 = (int)(u - (long long)r.rest * steps);
-        r.k1 = (int)min((long long)steps, r.k0 + (end - u));
+        locate(tile, r);
         return true;
     }
 };
@@ -218,10 +257,319 @@ __device__ __forceinline__ void grouped_plan(const GroupedParams &p, GroupedSmem
     for (int i = i0; i < i1; ++i) s.tiles[i] += incl - n;
 }
 
+// A part of a cut tile is in the workspace (this thread's share of it): true for the warps of the block that came last.
+template <bool GATED>
+__device__ __forceinline__ bool part_is_last(const GroupedParams &p, GroupedSmem &s, const Schedule<GATED> &plan, const Run &r, int &b0, int &b1)
+{
+    b0 = plan.block_of(r.rest * p.steps);
+    b1 = plan.block_of((r.rest + 1) * p.steps - 1);
+    __threadfence();
+    out_barrier();
+    if (threadIdx.x == GP_THREADS - 1) {
+        s.last = atomicAdd(p.tickets + r.rest, 1u) == (unsigned)(b1 - b0);
+        if (s.last) p.tickets[r.rest] = 0u;
+        __threadfence();
+    }
+    out_barrier();
+    return s.last != 0;
+}
+
+// The sums of a tile of few rows and what becomes of them: thread = output, values = rows.  False: a wait ran out.
+// Plain: half = which 128 outputs; gate/up: the halves share the rows, and a thread has gate and up of its output.
+template <bool FP8, bool GATED>
+__device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem &s, const Schedule<GATED> &plan, const Run &r, uint32_t lanes,
+                                         int half, int place, int &n)
+{
+    constexpr int N = GATED ? GP_FEW / 2 : GP_FEW;   // rows of a thread
+    const int lane = threadIdx.x & 31, per = GATED ? ((r.rows + 1) / 2 + 7) / 8 * 8 : GP_FEW;
+    const int t0 = GATED ? half * per : 0, rows = min(per, r.rows - t0);             // (may be none)
+    const int col = GATED ? t0 : GP_COLS / 2 * half, o = r.out0 + (GATED ? 0 : GP_COLS / 2 * half) + place;
+    const int in_blocks = (p.d_in + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK, out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
+    float a[N], u[GATED ? N : 1];
+    bool ok = true;
+    if (FP8) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) a[j] = 0.f;
+        if (GATED) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) u[j] = 0.f;
+        }
+        // a lane keeps the scales of row t0 + lane (and of the one 32 behind it), and asks for the next step's in good time
+        const int last = r.row0 + r.rows - 1;
+        const float *x0 = p.row_scales + (size_t)min(r.row0 + t0 + lane, last) * in_blocks;
+        const float *x1 = p.row_scales + (size_t)min(r.row0 + t0 + 32 + lane, last) * in_blocks;
+        const size_t at = ((size_t)r.expert * out_blocks + min(r.out0 / DIP_FP8_BLOCK + (GATED ? 0 : half), out_blocks - 1)) * in_blocks;
+        const float *ws = p.w_scales + at, *us = GATED ? p.up_scales + at : ws;
+        float next0 = __ldg(x0 + r.k0), next1 = __ldg(x1 + r.k0), next_w = __ldg(ws + r.k0), next_u = __ldg(us + r.k0);
+        for (int k = r.k0; k < r.k1; ++k, ++n) {
+            const float s0 = next0, s1 = next1, w = next_w, v = next_u;
+            if (k + 1 < r.k1) {
+                next0 = __ldg(x0 + k + 1);
+                if (!GATED) next1 = __ldg(x1 + k + 1);
+                next_w = __ldg(ws + k + 1);
+                if (GATED) next_u = __ldg(us + k + 1);
+            }
+            const int buf = n & 1;
+            if (ok && !warp_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns)) ok = false;
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+            for (int c = 0; c < N / 8; ++c)
+                if (8 * c < rows) {
+                    uint32_t d[8], e[8];
+                    tmem_ld8(lanes + buf * GP_COLS + col + 8 * c, d);
+                    if (GATED) tmem_ld8(lanes + buf * GP_COLS + GP_COLS / 2 + col + 8 * c, e);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float x = __shfl_sync(0xffffffffu, 8 * c + j < 32 ? s0 : s1, (8 * c + j) & 31);
+                        a[8 * c + j] = fmaf(__uint_as_float(d[j]), x * w, a[8 * c + j]);
+                        if (GATED) u[8 * c + j] = fmaf(__uint_as_float(e[j]), x * v, u[8 * c + j]);
+                    }
+                }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
+        }
+    } else {
+        const int buf = n & 1;
+        ok = warp_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+        for (int c = 0; c < N / 8; ++c)
+            if (8 * c < rows) {
+                uint32_t d[8], e[8];
+                tmem_ld8(lanes + buf * GP_COLS + col + 8 * c, d);
+                if (GATED) tmem_ld8(lanes + buf * GP_COLS + GP_COLS / 2 + col + 8 * c, e);
+                tmem_wait_ld();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    a[8 * c + j] = __uint_as_float(d[j]);
+                    if (GATED) u[8 * c + j] = __uint_as_float(e[j]);
+                }
+            }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
+        ++n;
+    }
+    // (a wait of one warp that runs out takes the others along: they meet at barriers below)
+    if (out_barrier_any(!ok)) return false;
+
+    if (r.k1 - r.k0 < p.steps) {
+        // a part of the tile: the last of its blocks goes on with the sum of all.  Parts are [row][256 sums]
+        const size_t mine = (size_t)t0 * GP_COLS + (GATED ? 0 : GP_COLS / 2 * half) + place;
+        float *to = p.partials + (size_t)(2 * blockIdx.x + plan.run_of(blockIdx.x, r.rest)) * (GP_ROWS * GP_COLS) + mine;
+#pragma unroll
+        for (int c = 0; c < N / 8; ++c)
+            if (8 * c < rows) {
+#pragma unroll
+                for (int j = 8 * c; j < 8 * c + 8; ++j)
+                    if (j < rows) {
+                        to[j * GP_COLS] = a[j];
+                        if (GATED) to[j * GP_COLS + GP_COLS / 2] = u[j];
+                    }
+            }
+        int b0, b1;
+        if (!part_is_last(p, s, plan, r, b0, b1)) return true;
+#pragma unroll
+        for (int j = 0; j < N; ++j) a[j] = 0.f;
+        if (GATED) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) u[j] = 0.f;
+        }
+        for (int b = b0; b <= b1; ++b) {
+            const float *from = p.partials + (size_t)(2 * b + plan.run_of(b, r.rest)) * (GP_ROWS * GP_COLS) + mine;
+#pragma unroll
+            for (int c = 0; c < N / 8; ++c)
+                if (8 * c < rows) {
+#pragma unroll
+                    for (int j = 8 * c; j < 8 * c + 8; ++j)
+                        if (j < rows) {
+                            a[j] += __ldcg(from + j * GP_COLS);
+                            if (GATED) u[j] += __ldcg(from + j * GP_COLS + GP_COLS / 2);
+                        }
+                }
+        }
+    }
+
+    const bool there = o < p.d_out;
+    const size_t at = (size_t)(r.row0 + t0) * p.d_out + o;
+    if (GATED) {
+#pragma unroll
+        for (int c = 0; c < N / 8; ++c)
+            if (8 * c < rows) {
+#pragma unroll
+                for (int j = 8 * c; j < 8 * c + 8; ++j) {
+                    a[j] = silu_f32(a[j]) * u[j];
+                    if (FP8) {
+                        const unsigned most = __reduce_max_sync(0xffffffffu, there ? __float_as_uint(fmaxf(fabsf(a[j]), 0.f)) : 0u);
+                        if (lane == 0) s.amax[(threadIdx.x >> 5 & 3) * GP_FEW + t0 + j] = __uint_as_float(most);
+                    }
+                }
+            }
+    }
+    if (GATED && FP8) out_barrier();
+#pragma unroll
+    for (int c = 0; c < N / 8; ++c)
+        if (8 * c < rows) {
+#pragma unroll
+            for (int j = 8 * c; j < 8 * c + 8; ++j)
+                if (j < rows) {
+                    if (GATED && FP8) {
+                        const float *m = s.amax + t0 + j;
+                        const float scale = fp8_scale(fmaxf(fmaxf(m[0], m[GP_FEW]), fmaxf(m[2 * GP_FEW], m[3 * GP_FEW])));
+                        if (there) static_cast<uint8_t *>(p.out)[at + (size_t)j * p.d_out] = (uint8_t)fp8_codes4(a[j], 0.f, 0.f, 0.f, scale);
+                        if (place == 0) p.out_scales[(size_t)(r.row0 + t0 + j) * out_blocks + r.out0 / DIP_FP8_BLOCK] = scale;
+                    } else if (there) {
+                        if (!GATED && p.out_f32) static_cast<float *>(p.out)[at + (size_t)j * p.d_out] = a[j];
+                        else static_cast<__nv_bfloat16 *>(p.out)[at + (size_t)j * p.d_out] = __float2bfloat16_rn(a[j]);
+                    }
+                }
+        }
+    if (GATED && FP8) out_barrier();                 // (before the next tile's maxima)
+    return true;
+}
+
+// The sums of any other tile: thread = row, values = 128 of its columns (gate/up: 64 gate and the 64 up beside them).
+template <bool FP8, bool GATED>
+__device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem &s, const Schedule<GATED> &plan, const Run &r, uint32_t lanes,
+                                          int half, int row, int &n)
+{
+    const int lane = threadIdx.x & 31;
+    const int col0 = GATED ? 64 * half : 128 * half, col1 = GATED ? 128 + 64 * half : 128 * half + 64;    // 64 columns from each
+    const int in_blocks = (p.d_in + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK, out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
+    float acc[128];
+    bool ok = true;
+    if (FP8) {
+#pragma unroll
+        for (int j = 0; j < 128; ++j) acc[j] = 0.f;
+        const float *xs = p.row_scales + (size_t)(r.row0 + min(row, r.rows - 1)) * in_blocks;
+        const size_t at = ((size_t)r.expert * out_blocks + min(r.out0 / DIP_FP8_BLOCK + (GATED ? 0 : half), out_blocks - 1)) * in_blocks;
+        const float *ws = p.w_scales + at, *us = GATED ? p.up_scales + at : ws;
+        float next_x = __ldg(xs + r.k0), next_w = __ldg(ws + r.k0), next_u = __ldg(us + r.k0);
+        for (int k = r.k0; k < r.k1; ++k, ++n) {
+            const float s0 = next_x * next_w, s1 = GATED ? next_x * next_u : s0;
+            if (k + 1 < r.k1) {                      // (asked for a step ahead)
+                next_x = __ldg(xs + k + 1);
+                next_w = __ldg(ws + k + 1);
+                if (GATED) next_u = __ldg(us + k + 1);
+            }
+            const int buf = n & 1;
+            if (!warp_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns)) {
+                ok = false;
+                break;
+            }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t v[32];
+                tmem_ld32(lanes + buf * GP_COLS + (c < 2 ? col0 + 32 * c : col1 + 32 * (c - 2)), v);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) acc[32 * c + j] = fmaf(__uint_as_float(v[j]), c < 2 ? s0 : s1, acc[32 * c + j]);
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
+        }
+    } else {
+        const int buf = n & 1;
+        ok = warp_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            uint32_t v[32];
+            tmem_ld32(lanes + buf * GP_COLS + (c < 2 ? col0 + 32 * c : col1 + 32 * (c - 2)), v);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) acc[32 * c + j] = __uint_as_float(v[j]);
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
+        ++n;
+    }
+    if (out_barrier_any(!ok)) return false;
+
+    if (r.k1 - r.k0 < p.steps) {
+        // parts are [half][column / 4][row][4]
+        const size_t mine = (size_t)half * 32 * GP_ROWS + row;
+        float4 *to = reinterpret_cast<float4 *>(p.partials) +
+                     (size_t)(2 * blockIdx.x + plan.run_of(blockIdx.x, r.rest)) * (GP_ROWS * GP_COLS / 4) + mine;
+        if (row < r.rows) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) to[j * GP_ROWS] = make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
+        }
+        int b0, b1;
+        if (!part_is_last(p, s, plan, r, b0, b1)) return true;
+#pragma unroll
+        for (int j = 0; j < 128; ++j) acc[j] = 0.f;
+        if (row < r.rows) {
+            for (int b = b0; b <= b1; ++b) {
+                const float4 *from = reinterpret_cast<const float4 *>(p.partials) +
+                                     (size_t)(2 * b + plan.run_of(b, r.rest)) * (GP_ROWS * GP_COLS / 4) + mine;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const float4 v = __ldcg(from + j * GP_ROWS);
+                    acc[4 * j] += v.x;
+                    acc[4 * j + 1] += v.y;
+                    acc[4 * j + 2] += v.z;
+                    acc[4 * j + 3] += v.w;
+                }
+            }
+        }
+    }
+
+    const size_t at = (size_t)(r.row0 + row) * p.d_out;
+    if (GATED) {
+        const int o = r.out0 + 64 * half;
+#pragma unroll
+        for (int j = 0; j < 64; ++j) acc[j] = silu_f32(acc[j]) * acc[64 + j];
+        if (FP8) {
+            // a block of 128 outputs has a scale: two threads have a half each
+            float most = 0.f;
+#pragma unroll
+            for (int j = 0; j < 64; ++j)
+                if (o + j < p.d_out) most = fmaxf(most, fabsf(acc[j]));
+            s.amax[half * GP_ROWS + row] = most;
+            out_barrier();
+            const float scale = fp8_scale(fmaxf(most, s.amax[(half ^ 1) * GP_ROWS + row]));
+            if (row < r.rows) {
+                if (half == 0) p.out_scales[(size_t)(r.row0 + row) * out_blocks + r.out0 / DIP_FP8_BLOCK] = scale;
+#pragma unroll
+                for (int j = 0; j < 64; j += 16)
+                    if (o + j < p.d_out)
+                        *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.out) + at + o + j) =
+                            make_uint4(fp8_codes4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3], scale),
+                                       fp8_codes4(acc[j + 4], acc[j + 5], acc[j + 6], acc[j + 7], scale),
+                                       fp8_codes4(acc[j + 8], acc[j + 9], acc[j + 10], acc[j + 11], scale),
+                                       fp8_codes4(acc[j + 12], acc[j + 13], acc[j + 14], acc[j + 15], scale));
+            }
+            out_barrier();                           // (before the next tile's maxima)
+        } else if (row < r.rows) {
+#pragma unroll
+            for (int j = 0; j < 64; j += 8)
+                if (o + j < p.d_out) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + at + o + j) = bf16x8(acc + j);
+        }
+    } else if (row < r.rows) {
+        const int o = r.out0 + 128 * half;
+        if (p.out_f32) {
+#pragma unroll
+            for (int j = 0; j < 128; j += 4)
+                if (o + j < p.d_out)
+                    *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at + o + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 128; j += 8)
+                if (o + j < p.d_out) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + at + o + j) = bf16x8(acc + j);
+        }
+    }
+    return true;
+}
+
 template <bool FP8, bool GATED>
 __global__ void __launch_bounds__(GP_THREADS, 1)
-grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap w_map,
-               const __grid_constant__ CUtensorMap up_map, const GroupedParams p)
+grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap few_map,
+               const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap w2_map, const GroupedParams p)
 {
     extern __shared__ unsigned char gp_smem_raw[];
     GroupedSmem &s = *reinterpret_cast<GroupedSmem *>((reinterpret_cast<uintptr_t>(gp_smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -243,6 +591,10 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
             mbar_init(&s.sum_empty[i], GP_OUT_WARPS);
         }
         mbar_init(&s.drained, 1);
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&rows_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&few_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&w2_map) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     dip_grid_dependency_wait();                      // rows and offsets come from the kernels in front
@@ -259,201 +611,90 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(GP_REGS_FEW));
-        if (warp == 0 && lane == 0) {
+        if (warp == 0) {
             Run r;
             int g = 0;                               // steps so far
             for (int i = 0; !failed && plan.get(i, r); ++i) {
-                const int boxes = (r.rows + GP_BOX - 1) / GP_BOX;
+                const bool few = r.rows <= GP_FEW, both = r.rows > GP_BOX;
                 const int w_row = r.expert * p.d_out + r.out0;
                 // (plain: the tile's second half may lie behind the last output)
                 const bool second = GATED || r.out0 + GP_COLS / 2 < p.d_out;
-                const unsigned bytes = boxes * GP_BOX * GP_STEP_BYTES + (second ? GP_B_BYTES : GP_B_BYTES / 2);
-                for (int k = r.k0; k < r.k1; ++k, ++g) {
+                const unsigned bytes = (few ? (both ? 2 : 1) * GP_BOX * GP_STEP_BYTES : GP_A_BYTES) + (second ? GP_B_BYTES : GP_B_BYTES / 2);
+                int x = r.k0 * per_step;
+                for (int k = r.k0; k < r.k1; ++k, ++g, x += per_step) {
                     const int st = g % GP_STAGES;
-                    if (g >= GP_STAGES && !mbar_wait(&s.empty[st], (g / GP_STAGES - 1) & 1, p.wait_limit_ns)) {
+                    if (g >= GP_STAGES && !warp_wait(&s.empty[st], (g / GP_STAGES - 1) & 1, p.wait_limit_ns)) {
                         failed = true;
                         break;
                     }
-                    mbar_expect_tx(&s.full[st], bytes);
-                    for (int b = 0; b < boxes; ++b)
-                        tma_load(s.a[st] + b * GP_BOX * GP_STEP_BYTES, &rows_map, k * per_step, r.row0 + b * GP_BOX, &s.full[st]);
-                    tma_load(s.b[st], &w_map, k * per_step, w_row, &s.full[st]);
-                    if (second)
-                        tma_load(s.b[st] + GP_B_BYTES / 2, GATED ? &up_map : &w_map, k * per_step, GATED ? w_row : w_row + GP_COLS / 2,
-                                 &s.full[st]);
+                    if (elect_one()) {
+                        mbar_expect_tx(&s.full[st], bytes);
+                        if (GATED) {
+                            tma_load(s.b[st], &w_map, x, w_row, &s.full[st]);
+                            tma_load(s.b[st] + GP_B_BYTES / 2, &w2_map, x, w_row, &s.full[st]);
+                        } else {
+                            tma_load(s.b[st], second ? &w2_map : &w_map, x, w_row, &s.full[st]);
+                        }
+                        tma_load(s.a[st], few ? &few_map : &rows_map, x, r.row0, &s.full[st]);
+                        if (few && both) tma_load(s.a[st] + GP_BOX * GP_STEP_BYTES, &few_map, x, r.row0 + GP_BOX, &s.full[st]);
+                    }
+                    __syncwarp();
                 }
             }
             // (given up: no copy of this block's is under way when it leaves)
             if (failed)
-                for (int j = max(0, g - GP_STAGES); j < g; ++j) mbar_wait(&s.full[j % GP_STAGES], (j / GP_STAGES) & 1, p.wait_limit_ns);
-        } else if (warp == 1 && lane == 0) {
+                for (int j = max(0, g - GP_STAGES); j < g; ++j) warp_wait(&s.full[j % GP_STAGES], (j / GP_STAGES) & 1, p.wait_limit_ns);
+        } else if (warp == 1) {
             Run r;
             int g = 0, n = 0;                        // steps, accumulators so far
             for (int i = 0; !failed && plan.get(i, r); ++i) {
+                const bool few = r.rows <= GP_FEW;
+                const uint32_t shape = grouped_shape<FP8>(few ? (r.rows + 15) / 16 * 16 : GP_COLS);
                 for (int k = r.k0; k < r.k1; ++k, ++g) {
                     const int st = g % GP_STAGES, buf = n & 1;
                     const bool first = FP8 || k == r.k0, last = FP8 || k == r.k1 - 1;
-                    if ((first && n >= 2 && !mbar_wait(&s.sum_empty[buf], (n / 2 - 1) & 1, p.wait_limit_ns)) ||
-                        !mbar_wait(&s.full[st], (g / GP_STAGES) & 1, p.wait_limit_ns)) {
+                    if ((first && n >= 2 && !warp_wait(&s.sum_empty[buf], (n / 2 - 1) & 1, p.wait_limit_ns)) ||
+                        !warp_wait(&s.full[st], (g / GP_STAGES) & 1, p.wait_limit_ns)) {
                         failed = true;
                         break;
                     }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t a = operand_desc(s.a[st]), b = operand_desc(s.b[st]);
+                    const uint32_t to = tmem + buf * GP_COLS;
+                    if (elect_one()) {
+                        if (!few) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)      // 32 bytes of K each
-                        grouped_mma<FP8>(tmem + buf * GP_COLS, a + 2 * q, b + 2 * q, (first && q == 0) ? 0u : 1u);
-                    grouped_commit(&s.empty[st]);
-                    if (last) {
-                        grouped_commit(&s.sum_full[buf]);
-                        ++n;
+                            for (int q = 0; q < 4; ++q)          // 32 bytes of K each
+                                grouped_mma<FP8>(to, a + 2 * q, b + 2 * q, shape, (first && q == 0) ? 0u : 1u);
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                grouped_mma<FP8>(to, b + 2 * q, a + 2 * q, shape, (first && q == 0) ? 0u : 1u);
+                                grouped_mma<FP8>(to + GP_COLS / 2, b + (GP_B_BYTES / 2 >> 4) + 2 * q, a + 2 * q, shape, (first && q == 0) ? 0u : 1u);
+                            }
+                        }
+                        grouped_commit(&s.empty[st]);
+                        if (last) grouped_commit(&s.sum_full[buf]);
                     }
+                    __syncwarp();
+                    if (last) ++n;
                 }
             }
             if (failed) {
-                grouped_commit(&s.drained);
-                mbar_wait(&s.drained, 0, p.wait_limit_ns);
+                if (elect_one()) grouped_commit(&s.drained);
+                __syncwarp();
+                warp_wait(&s.drained, 0, p.wait_limit_ns);
             }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(GP_REGS_MANY));
-        const int half = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
+        const int half = (warp - 4) >> 2, place = (warp & 3) * 32 + lane;        // lane of tensor memory
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        // this thread's columns: 64 from col0 on and 64 from col1 on
-        const int col0 = GATED ? 64 * half : 128 * half, col1 = GATED ? 128 + 64 * half : 128 * half + 64;
-        const int in_blocks = (p.d_in + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK, out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
-        int n = 0;
+        int n = 0;                                   // accumulators so far
         Run r;
         for (int i = 0; !failed && plan.get(i, r); ++i) {
-            float acc[128];
-            if (FP8) {
-#pragma unroll
-                for (int j = 0; j < 128; ++j) acc[j] = 0.f;
-                const float *xs = p.row_scales + (size_t)(r.row0 + min(row, r.rows - 1)) * in_blocks;
-                const int ob = r.out0 / DIP_FP8_BLOCK + (GATED ? 0 : half);
-                const float *ws = p.w_scales + ((size_t)r.expert * out_blocks + min(ob, out_blocks - 1)) * in_blocks;
-                const float *us = GATED ? p.up_scales + ((size_t)r.expert * out_blocks + ob) * in_blocks : ws;
-                for (int k = r.k0; k < r.k1; ++k, ++n) {
-                    const float x = __ldg(xs + k), s0 = x * __ldg(ws + k), s1 = GATED ? x * __ldg(us + k) : s0;
-                    const int buf = n & 1;
-                    if (!mbar_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns)) {
-                        failed = true;
-                        break;
-                    }
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t v[32];
-                        tmem_ld32(lanes + buf * GP_COLS + (c < 2 ? col0 + 32 * c : col1 + 32 * (c - 2)), v);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) acc[32 * c + j] = fmaf(__uint_as_float(v[j]), c < 2 ? s0 : s1, acc[32 * c + j]);
-                    }
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
-                }
-            } else {
-                const int buf = n & 1;
-                if (!mbar_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns)) failed = true;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t v[32];
-                    tmem_ld32(lanes + buf * GP_COLS + (c < 2 ? col0 + 32 * c : col1 + 32 * (c - 2)), v);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) acc[32 * c + j] = __uint_as_float(v[j]);
-                }
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
-                ++n;
-            }
-            // (a wait of one warp that runs out takes the others along: they meet at barriers below)
-            failed = out_barrier_any(failed);
-            if (failed) break;
-
-            if (r.k1 - r.k0 < p.steps) {
-                // a part of the tile: the last of its blocks goes on with the sum of all
-                const int b0 = plan.block_of((long long)r.rest * p.steps), b1 = plan.block_of((long long)(r.rest + 1) * p.steps - 1);
-                const size_t mine = (size_t)half * 32 * GP_ROWS + row;
-                float4 *to = reinterpret_cast<float4 *>(p.partials) +
-                             (size_t)(2 * blockIdx.x + plan.run_of(blockIdx.x, r.rest)) * (GP_ROWS * GP_COLS / 4) + mine;
-                if (row < r.rows) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) to[j * GP_ROWS] = make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
-                }
-                __threadfence();
-                out_barrier();
-                if (warp == 4 && lane == 0) {
-                    s.last = atomicAdd(p.tickets + r.rest, 1u) == (unsigned)(b1 - b0);
-                    if (s.last) p.tickets[r.rest] = 0u;
-                    __threadfence();
-                }
-                out_barrier();
-                if (!s.last) continue;
-#pragma unroll
-                for (int j = 0; j < 128; ++j) acc[j] = 0.f;
-                if (row < r.rows) {
-                    for (int b = b0; b <= b1; ++b) {
-                        const float4 *from = reinterpret_cast<const float4 *>(p.partials) +
-                                             (size_t)(2 * b + plan.run_of(b, r.rest)) * (GP_ROWS * GP_COLS / 4) + mine;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float4 v = __ldcg(from + j * GP_ROWS);
-                            acc[4 * j] += v.x;
-                            acc[4 * j + 1] += v.y;
-                            acc[4 * j + 2] += v.z;
-                            acc[4 * j + 3] += v.w;
-                        }
-                    }
-                }
-            }
-
-            const size_t at = (size_t)(r.row0 + row) * p.d_out;
-            if (GATED) {
-                const int o = r.out0 + 64 * half;
-#pragma unroll
-                for (int j = 0; j < 64; ++j) acc[j] = silu_f32(acc[j]) * acc[64 + j];
-                if (FP8) {
-                    // a block of 128 outputs has a scale: two threads have a half each
-                    float most = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 64; ++j)
-                        if (o + j < p.d_out) most = fmaxf(most, fabsf(acc[j]));
-                    s.amax[half][row] = most;
-                    out_barrier();
-                    const float scale = fp8_scale(fmaxf(most, s.amax[half ^ 1][row]));
-                    if (row < r.rows) {
-                        if (half == 0) p.out_scales[(size_t)(r.row0 + row) * out_blocks + r.out0 / DIP_FP8_BLOCK] = scale;
-#pragma unroll
-                        for (int j = 0; j < 64; j += 16)
-                            if (o + j < p.d_out)
-                                *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.out) + at + o + j) =
-                                    make_uint4(fp8_codes4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3], scale),
-                                               fp8_codes4(acc[j + 4], acc[j + 5], acc[j + 6], acc[j + 7], scale),
-                                               fp8_codes4(acc[j + 8], acc[j + 9], acc[j + 10], acc[j + 11], scale),
-                                               fp8_codes4(acc[j + 12], acc[j + 13], acc[j + 14], acc[j + 15], scale));
-                    }
-                    out_barrier();                   // (before the next tile's maxima)
-                } else if (row < r.rows) {
-#pragma unroll
-                    for (int j = 0; j < 64; j += 8)
-                        if (o + j < p.d_out) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + at + o + j) = bf16x8(acc + j);
-                }
-            } else if (row < r.rows) {
-                const int o = r.out0 + 128 * half;
-                if (p.out_f32) {
-#pragma unroll
-                    for (int j = 0; j < 128; j += 4)
-                        if (o + j < p.d_out)
-                            *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at + o + j) =
-                                make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 128; j += 8)
-                        if (o + j < p.d_out) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + at + o + j) = bf16x8(acc + j);
-                }
-            }
+            if (r.rows <= GP_FEW) failed = !take_few<FP8, GATED>(p, s, plan, r, lanes, half, place, n);
+            else failed = !take_tile<FP8, GATED>(p, s, plan, r, lanes, half, place, n);
         }
     }
     if (failed) atomicExch(p.status, 1);
@@ -495,14 +736,14 @@ bool encode(CUtensorMap *map, const void *p, bool fp8, size_t n, int d, int box)
 }
 
 template <bool FP8, bool GATED>
-cudaError_t launch(dip_ctx *ctx, int ctas, cudaStream_t stream, const CUtensorMap &rows, const CUtensorMap &w, const CUtensorMap &up,
-                   const GroupedParams &p)
+cudaError_t launch(dip_ctx *ctx, int ctas, cudaStream_t stream, const CUtensorMap (&m)[4], const GroupedParams &p)
 {
     static dip_per_device_once once;
     const size_t smem = sizeof(GroupedSmem) + 1024;
     static_assert(sizeof(GroupedSmem) + 1024 <= 227 * 1024, "fits a CTA's shared memory");
     const cudaError_t e = dip_raise_smem_limit(once, ctx->device, grouped_kernel<FP8, GATED>, smem);
-    return e != cudaSuccess ? e : dip_launch_pdl(grouped_kernel<FP8, GATED>, dim3(ctas), dim3(GP_THREADS), smem, stream, rows, w, up, p);
+    return e != cudaSuccess ? e : dip_launch_pdl(grouped_kernel<FP8, GATED>, dim3(ctas), dim3(GP_THREADS), smem, stream, m[0], m[1],
+                                              m[2], m[3], p);
 }
 
 }  // namespace
@@ -513,9 +754,11 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
 {
     const bool fp8 = w.wtype == DIP_W_FP8_B128;
     const size_t w_rows = (size_t)w.n_experts * w.d_out;
-    CUtensorMap rows_map, w_map, up_map;
-    if (!encoder() || !encode(&rows_map, rows, fp8, n_rows, w.d_in, GP_BOX) || !encode(&w_map, w.values, fp8, w_rows, w.d_in, GP_COLS / 2) ||
-        !encode(&up_map, up ? up->values : w.values, fp8, w_rows, w.d_in, GP_COLS / 2)) {
+    // the rows, whole tiles of them and few; a half of a tile's weights; the other half (gate/up), or both at once
+    CUtensorMap maps[4];
+    if (!encoder() || !encode(&maps[0], rows, fp8, n_rows, w.d_in, GP_ROWS) || !encode(&maps[1], rows, fp8, n_rows, w.d_in, GP_BOX) ||
+        !encode(&maps[2], w.values, fp8, w_rows, w.d_in, GP_COLS / 2) ||
+        !encode(&maps[3], up ? up->values : w.values, fp8, w_rows, w.d_in, up ? GP_COLS / 2 : GP_COLS)) {
         snprintf(ctx->err, sizeof(ctx->err), "cuTensorMapEncodeTiled failed");
         return DIP_ERR_CUDA;
     }
@@ -528,6 +771,7 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
     p.d_in = w.d_in;
     p.n_rows = n_rows;
     p.steps = (w.d_in * (fp8 ? 1 : 2) + GP_STEP_BYTES - 1) / GP_STEP_BYTES;
+    p.n_cols = (w.d_out + (up ? GP_COLS / 2 : GP_COLS) - 1) / (up ? GP_COLS / 2 : GP_COLS);
     p.offset = offset;
     p.out = out;
     p.out_scales = out_scales;
@@ -538,10 +782,9 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
     p.wait_limit_ns = ctx->wait_limit_ns;
     p.tr = dip_trace_slot(ctx, up ? 10 : 11);
     // no more blocks than there can be parts
-    const int width = up ? GP_COLS / 2 : GP_COLS;
-    const long long tiles = (long long)((n_rows + GP_ROWS - 1) / GP_ROWS + min(w.n_experts, n_rows) - 1) * ((w.d_out + width - 1) / width);
+    const long long tiles = (long long)((n_rows + GP_ROWS - 1) / GP_ROWS + min(w.n_experts, n_rows) - 1) * p.n_cols;
     const int ctas = (int)min((long long)ctx->sm_count, max(tiles, tiles * p.steps / GP_MIN_STEPS));
     const auto start = fp8 ? (up ? launch<true, true> : launch<true, false>) : (up ? launch<false, true> : launch<false, false>);
-    DIP_CUDA_TRY(ctx, start(ctx, ctas, stream, rows_map, w_map, up_map, p));
+    DIP_CUDA_TRY(ctx, start(ctx, ctas, stream, maps, p));
     return DIP_OK;
 }

@@ -284,7 +284,8 @@ def steps(ctx, w, x, route):
     n = x.shape[0] * (route.top_k if route else 1)
     offset = route.offset if route else None
     rows, h = dip.Rows(n, w.d_model, w.wtype, "cuda"), dip.Rows(n, w.d_ff, w.wtype, "cuda")
-    out, y = (torch.zeros((m, w.d_model), device="cuda", dtype=torch.bfloat16) for m in (n, x.shape[0]))
+    out = torch.zeros((n, w.d_model), device="cuda", dtype=torch.float32 if route else torch.bfloat16)
+    y = torch.zeros((x.shape[0], w.d_model), device="cuda", dtype=torch.bfloat16)
     dip.dip_stage_rows(ctx, x, rows, route=route)
     dip.dip_grouped_gate_up(ctx, w.gate, w.up, rows, h, offset=offset)
     dip.dip_grouped_product(ctx, w.down, h, out, offset=offset)
@@ -315,7 +316,6 @@ def test_mixture(ctx, wtype, tokens, experts, top_k, d_model, d_ff):
     # the last product and the weighted sum on the h that the kernels left; the first product has its own tests
     n = int(r.offset[-1])
     want, bound = eu.product64(*down, eu.values64(h.values, h.scales), r.offset)
-    bound = eu.rounded(want, bound, torch.bfloat16)
     eu.assert_within(out[:n], want[:n], bound[:n], "out")
     at, there = r.token_row.long().clamp_min(0), (r.token_row >= 0)[:, :, None]
     share = r.weight.double()[:, :, None]
@@ -345,7 +345,7 @@ def test_combine_is_the_weighted_sum_in_order(ctx):
     z = torch.randn((50, 9), generator=gen_of(1), device="cuda")
     z[7], z[8, 1:] = -math.inf, -math.inf
     dip.dip_route_experts(ctx, z, r, renormalize=False)
-    rows = torch.randn((200, 96), generator=gen_of(2), device="cuda").bfloat16()
+    rows = torch.randn((200, 96), generator=gen_of(2), device="cuda")
     rows[int(r.offset[-1]):] = math.nan
     y = nan_like((50, 96), torch.bfloat16)
     dip.dip_combine_rows(ctx, rows, r, y)
