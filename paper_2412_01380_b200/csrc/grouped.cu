@@ -1,20 +1,24 @@
 // Products of groups of rows, a group per expert, on the fifth-generation tensor cores: y[r] = W[e(r)] rows[r], and
 // h[r] = silu(Wg[e(r)] rows[r]) * (Wu[e(r)] rows[r]).  One kernel for a token's one or two rows and for a prompt's thousands.
 //
-// A tile is 128 rows of one expert by 256 rows of its weights (gate/up: the 128 gate and the 128 up rows of the same
+// A block's tile is 128 rows of one expert by 256 rows of its weights (gate/up: the 128 gate and the 128 up rows of the same
 // outputs, so that one thread has both).  Both operands are K-major 128-byte pieces (64 bfloat16, 128 e4m3) that TMA lays
-// into shared memory with the 128-byte swizzle the operand descriptors name; a step of the pipeline is 16 + 32 KB.
-// A tile of at most GP_FEW rows changes the operands' roles: the weights are the M side (two MMAs of 128) and the rows the
-// N side, as many columns as there are rows (in sixteens).  The loads are the same, but a thread then has one output of a few rows
-// instead of one row of 128 outputs, and what follows the last step takes as long as there are rows.
-//   warp 0      one thread issues the copies: a ring of GP_STAGES steps
-//   warp 1      one thread issues the MMAs (M = 128, N = 256, four per step) into one of two accumulators of 256 columns
-//   warps 4-11  take the accumulators out: thread = row, a half of the columns for each four warps
+// into shared memory with the 128-byte swizzle the operand descriptors name.
+//   PAIR   two blocks of a cluster share a tile of 256 rows: each loads its 128 rows and half of the weights, and the first one's
+//          MMAs (cta_group::2, M = 256) read both halves.  Per step and SM 32 KB come in and 32 KB are read, which shared
+//          memory does in the 512 cycles that the MMAs take.  (Alone it is 48 and 48 KB: 768 cycles, measured 785.)
+//   single a block by itself.  A tile of at most GP_FEW rows changes the operands' roles: the weights are the M side (two MMAs of
+//          128) and the rows the N side, as many columns as there are rows (in sixteens).  The loads are the same, but a thread
+//          then has one output of a few rows instead of one row of 64 outputs, and what follows the last step takes as long as there
+//          are rows.
+//   warp 0      issues the copies: a ring of steps
+//   warp 1      issues the MMAs (N = 256, four per step) into one of two accumulators of 256 columns
+//   warps 4-19  take the accumulators out: thread = row, a quarter of the columns for each four warps
 // BF16: an accumulator is a tile, and the next tile's MMAs run while the first is taken out.  FP8: a step is a block of 128
 // input indices, which has scales of its own, so every step's accumulator is taken out and added, times row scale * weight
 // scale, to binary32 sums in registers: 256 multiply-adds per warp scheduler and step against the 512 cycles of its MMAs.
 //
-// Blocks stay: whole rounds of tiles are dealt out one to a block, and what is left over (all of it where there are
+// Blocks stay: whole rounds of tiles are dealt out one to a block (or pair), and what is left over (all of it where there are
 // fewer tiles than SMs, as for a token) is cut along K into equal runs of steps, one per block, in tile order.  A tile's
 // parts meet in the partial sums' workspace; the block that comes last adds them up in order of K, so results do not
 // depend on who that is, and nobody waits.
@@ -28,17 +32,18 @@
 namespace {
 
 constexpr int GP_ROWS = DIP_GROUP_ROWS, GP_COLS = DIP_GROUP_COLS;
-constexpr int GP_STAGES = 4;
 constexpr int GP_STEP_BYTES = 128;                  // of a row, per step
 constexpr int GP_BOX = 32;                          // rows per copy of the rows of a tile of few
 constexpr int GP_A_BYTES = GP_ROWS * GP_STEP_BYTES, GP_B_BYTES = GP_COLS * GP_STEP_BYTES;
-constexpr int GP_OUT_WARPS = 8, GP_THREADS = (4 + GP_OUT_WARPS) * 32;
-// registers of a thread of the first four warps and of the others, out of the launch's 168 each: (56 + 2 * 224) / 3
-constexpr int GP_REGS_FEW = 56, GP_REGS_MANY = 224;
+constexpr int GP_OUT_WARPS = 16, GP_THREADS = (4 + GP_OUT_WARPS) * 32;
+// registers of a thread of the first four warps and of the others, out of the launch's 96 each: (64 + 4 * 104) / 5
+constexpr int GP_REGS_FEW = 64, GP_REGS_MANY = 104;
 constexpr int GP_TMEM_COLS = 512;
 constexpr int GP_MIN_STEPS = 4;                     // a part of a tile has at least so many
 constexpr int GP_FEW = 64;                          // rows of a tile that are columns of its sums
 constexpr int GP_CHUNK = 12;                        // row tiles that go through an expert's weights together
+template <bool PAIR> constexpr int GP_STAGES = PAIR ? 5 : 4;
+template <bool PAIR> constexpr int GP_PIECE = PAIR ? 64 : 32;      // bytes of a row that leave together
 
 struct GroupedParams {
     const float *w_scales, *up_scales, *row_scales;
@@ -54,23 +59,35 @@ struct GroupedParams {
     unsigned long long *tr;
 };
 
-struct __align__(1024) GroupedSmem {
-    unsigned char a[GP_STAGES][GP_A_BYTES];
-    unsigned char b[GP_STAGES][GP_B_BYTES];
-    uint64_t full[GP_STAGES], empty[GP_STAGES];     // a step's copies have landed; its MMAs have read them
-    uint64_t sum_full[2], sum_empty[2];             // an accumulator is complete; has been taken out
-    uint64_t drained;
-    uint32_t tmem_base;
-    int last;
-    float amax[4 * GP_FEW > 2 * GP_ROWS ? 4 * GP_FEW : 2 * GP_ROWS];
+struct GroupedPlan {
     int start[DIP_MAX_EXPERTS + 1];                 // first row of each expert
     int tiles[DIP_MAX_EXPERTS + 1];                 // row tiles in front of it
 };
 
+template <bool PAIR>
+struct __align__(1024) GroupedSmem {
+    unsigned char a[GP_STAGES<PAIR>][GP_A_BYTES];
+    unsigned char b[GP_STAGES<PAIR>][PAIR ? GP_B_BYTES / 2 : GP_B_BYTES];
+    unsigned char out[GP_OUT_WARPS][32 * GP_PIECE<PAIR>];
+    uint64_t full[GP_STAGES<PAIR>], empty[GP_STAGES<PAIR>];        // a step's copies have landed; its MMAs have read them
+    uint64_t sum_full[2], sum_empty[2];             // an accumulator is complete; has been taken out
+    uint64_t drained;
+    uint32_t tmem_base;
+    int last;
+    float amax[4 * GP_ROWS];
+    GroupedPlan plan;
+};
+
+// PAIR: into this block's shared memory, counted by the first block's barrier (whose address has the block's bit clear).
+template <bool PAIR>
 __device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, int x, int y, uint64_t *bar)
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+    if (PAIR)
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar) & 0xfeffffffu) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
 }
 
 // A whole warp's bounded wait: all lanes go on alike.
@@ -94,43 +111,62 @@ __device__ __forceinline__ uint64_t operand_desc(const void *p)
     return (uint64_t)((smem_u32(p) & 0x3ffffu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
-// Instruction descriptor: binary32 sums, K-major operands of M = 128 and N = n; bfloat16 or e4m3
-template <bool FP8>
+// Instruction descriptor: binary32 sums, K-major operands of M = 128 (PAIR: 256) and N = n; bfloat16 or e4m3
+template <bool FP8, bool PAIR>
 __device__ __forceinline__ uint32_t grouped_shape(int n)
 {
-    return (1u << 4) | (FP8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+    return (1u << 4) | (FP8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(n >> 3) << 17) | ((PAIR ? 16u : 8u) << 24);
 }
 
-template <bool FP8>
+template <bool FP8, bool PAIR>
 __device__ __forceinline__ void grouped_mma(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t shape, uint32_t accumulate)
 {
-    if (FP8)
-        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
-                     ::"r"(d_tmem), "l"(a), "l"(b), "r"(shape), "r"(accumulate) : "memory");
-    else
-        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                     ::"r"(d_tmem), "l"(a), "l"(b), "r"(shape), "r"(accumulate) : "memory");
+#define GP_MMA(group, kind)                                                                                                         \
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::" group ".kind::" kind " [%0], %1, %2, %3, p;\n}" \
+                 ::"r"(d_tmem), "l"(a), "l"(b), "r"(shape), "r"(accumulate) : "memory")
+    if (FP8 && PAIR) GP_MMA("2", "f8f6f4");
+    else if (FP8) GP_MMA("1", "f8f6f4");
+    else if (PAIR) GP_MMA("2", "f16");
+    else GP_MMA("1", "f16");
+#undef GP_MMA
 }
 
+// Arrives at the barrier (PAIR: at both blocks') once the MMAs so far are through.
+template <bool PAIR>
 __device__ __forceinline__ void grouped_commit(uint64_t *bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    if (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
-// 32 columns of this warp's 32 lanes: thread = lane, register = column.
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32])
+// Arrives at the first block's barrier.
+template <bool PAIR>
+__device__ __forceinline__ void arrive_first(uint64_t *bar)
 {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
-                 "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
-                   "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
-                   "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-                 : "r"(taddr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    if (PAIR)
+        asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, 0;\n mbarrier.arrive.shared::cluster.b64 _, [r];\n}"
+                     ::"r"(smem_u32(bar)) : "memory");
+    else
+        mbar_arrive(bar);
 }
 
-// Eight columns, without the wait.
+__device__ __forceinline__ void pair_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Sixteen columns of this warp's 32 lanes, without the wait: thread = lane, register = column.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr));
+}
+// Eight.
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8])
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
@@ -157,29 +193,37 @@ struct Run {
 
 // The runs of this block, in order.  Every role walks through them for itself.  (32 bits hold it all: at most 2^21 tiles, and
 // fewer than a block's worth of cut ones of at most 512 steps.)
-template <bool GATED>
+template <bool GATED, bool PAIR>
 struct Schedule {
-    const GroupedSmem &s;
+    static constexpr int ROWS = PAIR ? 2 * GP_ROWS : GP_ROWS;
+    const GroupedPlan &s;
     int n_experts, steps, n_cols;
+    int block, blocks;              // this block or pair, and how many there are
     int whole;                      // rounds of whole tiles
     int units, parts;               // steps of the tiles that are cut, blocks that share them
     int at, end;                    // this block's units
 
-    __device__ __forceinline__ Schedule(const GroupedSmem &sm, const GroupedParams &p)
-        : s(sm), n_experts(p.n_experts), steps(p.steps), n_cols(p.n_cols)
+    __device__ __forceinline__ Schedule(const GroupedPlan &plan, const GroupedParams &p)
+        : s(plan), n_experts(p.n_experts), steps(p.steps), n_cols(p.n_cols), block(PAIR ? blockIdx.x >> 1 : blockIdx.x),
+          blocks(PAIR ? gridDim.x >> 1 : gridDim.x)
     {
-        const int g = gridDim.x, tiles = s.tiles[n_experts] * n_cols;
-        whole = tiles / g;
-        const int rest = tiles - whole * g;
+        const int tiles = s.tiles[n_experts] * n_cols;
+        whole = tiles / blocks;
+        const int rest = tiles - whole * blocks;
         units = rest * steps;
-        parts = min(g, max(units / GP_MIN_STEPS, rest));
-        const bool mine = (int)blockIdx.x < parts;
-        at = mine ? units * blockIdx.x / parts : 0;
-        end = mine ? units * (blockIdx.x + 1) / parts : 0;
+        parts = min(blocks, max(units / GP_MIN_STEPS, rest));
+        const bool mine = block < parts;
+        at = mine ? units * block / parts : 0;
+        end = mine ? units * (block + 1) / parts : 0;
     }
     // the block that has a unit, and which of its runs is the one in cut tile `rest`
     __device__ __forceinline__ int block_of(int unit) const { return ((unit + 1) * parts - 1) / units; }
-    __device__ __forceinline__ int run_of(int block, int rest) const { return units * block / parts / steps == rest ? 0 : 1; }
+    __device__ __forceinline__ int run_of(int b, int rest) const { return units * b / parts / steps == rest ? 0 : 1; }
+    // where block b (of this one's kind in its pair) leaves its part of the cut tile, in floats
+    __device__ __forceinline__ size_t part_at(int b, int rest) const
+    {
+        return (size_t)(2 * (PAIR ? 2 * b + (int)(blockIdx.x & 1) : b) + run_of(b, rest)) * (GP_ROWS * GP_COLS);
+    }
 
     __device__ __forceinline__ void locate(int tile, Run &r) const
     {
@@ -199,8 +243,8 @@ struct Schedule {
         const int col = here == 1 ? in : in / here;
         m += in - col * here;
         r.expert = lo;
-        r.row0 = s.start[lo] + m * GP_ROWS;
-        r.rows = min(GP_ROWS, n_rows - m * GP_ROWS);
+        r.row0 = s.start[lo] + m * ROWS;
+        r.rows = min(ROWS, n_rows - m * ROWS);
         r.out0 = col * (GATED ? GP_COLS / 2 : GP_COLS);
     }
     __device__ __forceinline__ bool get(int i, Run &r) const
@@ -208,7 +252,7 @@ struct Schedule {
         r.rest = -1;
         r.k0 = 0;
         r.k1 = steps;
-        int tile = i * gridDim.x + blockIdx.x;
+        int tile = i * blocks + block;
         if (i >= whole) {
             int u = at;
             for (i -= whole; i > 0 && u < end; --i) u = min(end, (u / steps + 1) * steps);
@@ -216,7 +260,7 @@ struct Schedule {
             r.rest = u / steps;
             r.k0 = u - r.rest * steps;
             r.k1 = min(steps, r.k0 + (end - u));
-            tile = whole * gridDim.x + r.rest;
+            tile = whole * blocks + r.rest;
         }
         locate(tile, r);
         return true;
@@ -224,7 +268,7 @@ struct Schedule {
 };
 
 // first rows and tiles of the experts, by one warp
-__device__ __forceinline__ void grouped_plan(const GroupedParams &p, GroupedSmem &s)
+__device__ __forceinline__ void grouped_plan(const GroupedParams &p, int tile_rows, GroupedPlan &s)
 {
     const int lane = threadIdx.x & 31, each = (p.n_experts + 32) / 32;      // offsets per lane
     const int i0 = min(lane * each, p.n_experts + 1), i1 = min(i0 + each, p.n_experts + 1);
@@ -246,7 +290,7 @@ __device__ __forceinline__ void grouped_plan(const GroupedParams &p, GroupedSmem
     int n = 0;
     for (int i = i0; i < i1; ++i) {
         s.tiles[i] = n;
-        if (i < p.n_experts) n += (s.start[i + 1] - s.start[i] + GP_ROWS - 1) / GP_ROWS;
+        if (i < p.n_experts) n += (s.start[i + 1] - s.start[i] + tile_rows - 1) / tile_rows;
     }
     int incl = n;
 #pragma unroll
@@ -258,16 +302,18 @@ __device__ __forceinline__ void grouped_plan(const GroupedParams &p, GroupedSmem
 }
 
 // A part of a cut tile is in the workspace (this thread's share of it): true for the warps of the block that came last.
-template <bool GATED>
-__device__ __forceinline__ bool part_is_last(const GroupedParams &p, GroupedSmem &s, const Schedule<GATED> &plan, const Run &r, int &b0, int &b1)
+template <bool GATED, bool PAIR>
+__device__ __forceinline__ bool part_is_last(const GroupedParams &p, GroupedSmem<PAIR> &s, const Schedule<GATED, PAIR> &plan, const Run &r,
+                                             int &b0, int &b1)
 {
     b0 = plan.block_of(r.rest * p.steps);
     b1 = plan.block_of((r.rest + 1) * p.steps - 1);
     __threadfence();
     out_barrier();
     if (threadIdx.x == GP_THREADS - 1) {
-        s.last = atomicAdd(p.tickets + r.rest, 1u) == (unsigned)(b1 - b0);
-        if (s.last) p.tickets[r.rest] = 0u;
+        unsigned int *ticket = p.tickets + (PAIR ? 2 * r.rest + (int)(blockIdx.x & 1) : r.rest);
+        s.last = atomicAdd(ticket, 1u) == (unsigned)(b1 - b0);
+        if (s.last) *ticket = 0u;
         __threadfence();
     }
     out_barrier();
@@ -275,15 +321,17 @@ __device__ __forceinline__ bool part_is_last(const GroupedParams &p, GroupedSmem
 }
 
 // The sums of a tile of few rows and what becomes of them: thread = output, values = rows.  False: a wait ran out.
-// Plain: half = which 128 outputs; gate/up: the halves share the rows, and a thread has gate and up of its output.
+// The warps' quarters share the rows; plain: two quarters each for the first and the second 128 outputs; gate/up: a thread has gate
+// and up of its output.
 template <bool FP8, bool GATED>
-__device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem &s, const Schedule<GATED> &plan, const Run &r, uint32_t lanes,
-                                         int half, int place, int &n)
+__device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<false> &s, const Schedule<GATED, false> &plan, const Run &r,
+                                         uint32_t lanes, int quarter, int place, int &n)
 {
-    constexpr int N = GATED ? GP_FEW / 2 : GP_FEW;   // rows of a thread
-    const int lane = threadIdx.x & 31, per = GATED ? ((r.rows + 1) / 2 + 7) / 8 * 8 : GP_FEW;
-    const int t0 = GATED ? half * per : 0, rows = min(per, r.rows - t0);             // (may be none)
-    const int col = GATED ? t0 : GP_COLS / 2 * half, o = r.out0 + (GATED ? 0 : GP_COLS / 2 * half) + place;
+    constexpr int SHARES = GATED ? 4 : 2, N = GP_FEW / SHARES;                     // rows of a thread: at most N
+    const int lane = threadIdx.x & 31, per = ((r.rows + SHARES - 1) / SHARES + 7) / 8 * 8;
+    const int t0 = (GATED ? quarter : quarter >> 1) * per, rows = min(per, r.rows - t0);      // (may be none)
+    const int side = GATED ? 0 : GP_COLS / 2 * (quarter & 1), o = r.out0 + side + place;
+    const uint32_t sums = lanes + side + t0;
     const int in_blocks = (p.d_in + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK, out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
     float a[N], u[GATED ? N : 1];
     bool ok = true;
@@ -294,35 +342,34 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem &s,
 #pragma unroll
             for (int j = 0; j < N; ++j) u[j] = 0.f;
         }
-        // a lane keeps the scales of row t0 + lane (and of the one 32 behind it), and asks for the next step's in good time
-        const int last = r.row0 + r.rows - 1;
-        const float *x0 = p.row_scales + (size_t)min(r.row0 + t0 + lane, last) * in_blocks;
-        const float *x1 = p.row_scales + (size_t)min(r.row0 + t0 + 32 + lane, last) * in_blocks;
-        const size_t at = ((size_t)r.expert * out_blocks + min(r.out0 / DIP_FP8_BLOCK + (GATED ? 0 : half), out_blocks - 1)) * in_blocks;
+        // a lane keeps the scale of row t0 + lane, and asks for the next step's in good time
+        const float *xs = p.row_scales + (size_t)min(r.row0 + t0 + lane, r.row0 + r.rows - 1) * in_blocks;
+        const size_t at = ((size_t)r.expert * out_blocks + min((r.out0 + side) / DIP_FP8_BLOCK, out_blocks - 1)) * in_blocks;
         const float *ws = p.w_scales + at, *us = GATED ? p.up_scales + at : ws;
-        float next0 = __ldg(x0 + r.k0), next1 = __ldg(x1 + r.k0), next_w = __ldg(ws + r.k0), next_u = __ldg(us + r.k0);
+        float next_x = __ldg(xs + r.k0), next_w = __ldg(ws + r.k0), next_u = __ldg(us + r.k0);
         for (int k = r.k0; k < r.k1; ++k, ++n) {
-            const float s0 = next0, s1 = next1, w = next_w, v = next_u;
+            const float sx = next_x, w = next_w, v = next_u;
             if (k + 1 < r.k1) {
-                next0 = __ldg(x0 + k + 1);
-                if (!GATED) next1 = __ldg(x1 + k + 1);
+                next_x = __ldg(xs + k + 1);
                 next_w = __ldg(ws + k + 1);
                 if (GATED) next_u = __ldg(us + k + 1);
             }
             const int buf = n & 1;
-            if (ok && !warp_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns)) ok = false;
-            if (!ok) break;
+            if (!warp_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns)) {
+                ok = false;
+                break;
+            }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
             for (int c = 0; c < N / 8; ++c)
                 if (8 * c < rows) {
                     uint32_t d[8], e[8];
-                    tmem_ld8(lanes + buf * GP_COLS + col + 8 * c, d);
-                    if (GATED) tmem_ld8(lanes + buf * GP_COLS + GP_COLS / 2 + col + 8 * c, e);
+                    tmem_ld8(sums + buf * GP_COLS + 8 * c, d);
+                    if (GATED) tmem_ld8(sums + buf * GP_COLS + GP_COLS / 2 + 8 * c, e);
                     tmem_wait_ld();
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float x = __shfl_sync(0xffffffffu, 8 * c + j < 32 ? s0 : s1, (8 * c + j) & 31);
+                        const float x = __shfl_sync(0xffffffffu, sx, 8 * c + j);
                         a[8 * c + j] = fmaf(__uint_as_float(d[j]), x * w, a[8 * c + j]);
                         if (GATED) u[8 * c + j] = fmaf(__uint_as_float(e[j]), x * v, u[8 * c + j]);
                     }
@@ -339,8 +386,8 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem &s,
         for (int c = 0; c < N / 8; ++c)
             if (8 * c < rows) {
                 uint32_t d[8], e[8];
-                tmem_ld8(lanes + buf * GP_COLS + col + 8 * c, d);
-                if (GATED) tmem_ld8(lanes + buf * GP_COLS + GP_COLS / 2 + col + 8 * c, e);
+                tmem_ld8(sums + buf * GP_COLS + 8 * c, d);
+                if (GATED) tmem_ld8(sums + buf * GP_COLS + GP_COLS / 2 + 8 * c, e);
                 tmem_wait_ld();
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -358,8 +405,8 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem &s,
 
     if (r.k1 - r.k0 < p.steps) {
         // a part of the tile: the last of its blocks goes on with the sum of all.  Parts are [row][256 sums]
-        const size_t mine = (size_t)t0 * GP_COLS + (GATED ? 0 : GP_COLS / 2 * half) + place;
-        float *to = p.partials + (size_t)(2 * blockIdx.x + plan.run_of(blockIdx.x, r.rest)) * (GP_ROWS * GP_COLS) + mine;
+        const size_t mine = (size_t)t0 * GP_COLS + side + place;
+        float *to = p.partials + plan.part_at(plan.block, r.rest) + mine;
 #pragma unroll
         for (int c = 0; c < N / 8; ++c)
             if (8 * c < rows) {
@@ -379,7 +426,7 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem &s,
             for (int j = 0; j < N; ++j) u[j] = 0.f;
         }
         for (int b = b0; b <= b1; ++b) {
-            const float *from = p.partials + (size_t)(2 * b + plan.run_of(b, r.rest)) * (GP_ROWS * GP_COLS) + mine;
+            const float *from = p.partials + plan.part_at(b, r.rest) + mine;
 #pragma unroll
             for (int c = 0; c < N / 8; ++c)
                 if (8 * c < rows) {
@@ -431,21 +478,42 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem &s,
     return true;
 }
 
-// The sums of any other tile: thread = row, values = 128 of its columns (gate/up: 64 gate and the 64 up beside them).
-template <bool FP8, bool GATED>
-__device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem &s, const Schedule<GATED> &plan, const Run &r, uint32_t lanes,
-                                          int half, int row, int &n)
+// A piece of this warp's 32 rows leaves by way of shared memory: each thread brings GP_PIECE bytes of its row, and the warp writes
+// whole pieces row after row (a thread writing 16 bytes of its own row at a time touched 32 lines per instruction: 6000 cycles for
+// a tile of 256 bfloat16 columns).  to: the piece of lane 0's row, `pitch` bytes from row to row; only rows below n, bytes below `bytes`.
+template <bool PAIR>
+__device__ __forceinline__ void leave(unsigned char *stage, const uint4 *v, char *to, size_t pitch, int n, int bytes)
+{
+    constexpr int Q = GP_PIECE<PAIR> / 16, ROWS = 32 / Q, SHIFT = PAIR ? 1 : 2;       // 16-byte parts of a piece, rows per pass
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < Q; ++q) *reinterpret_cast<uint4 *>(stage + lane * GP_PIECE<PAIR> + ((q ^ (lane >> SHIFT & (Q - 1))) << 4)) = v[q];
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        const int row = i * ROWS + lane / Q, q = lane % Q;
+        const uint4 w = *reinterpret_cast<const uint4 *>(stage + row * GP_PIECE<PAIR> + ((q ^ (row >> SHIFT & (Q - 1))) << 4));
+        if (row < n && 16 * q < bytes) *reinterpret_cast<uint4 *>(to + row * pitch + 16 * q) = w;
+    }
+}
+
+// The sums of any other tile: thread = row, values = 64 of its columns (gate/up: 32 gate and the 32 up beside them).
+// row0, rows: this block's rows of the tile (may be none).
+template <bool FP8, bool GATED, bool PAIR>
+__device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<PAIR> &s, const Schedule<GATED, PAIR> &plan, const Run &r,
+                                          int row0, int rows, uint32_t lanes, int quarter, int row, int &n)
 {
     const int lane = threadIdx.x & 31;
-    const int col0 = GATED ? 64 * half : 128 * half, col1 = GATED ? 128 + 64 * half : 128 * half + 64;    // 64 columns from each
+    const int col0 = GATED ? 32 * quarter : 64 * quarter, col1 = GATED ? GP_COLS / 2 + col0 : col0 + 32;      // 32 columns from each
     const int in_blocks = (p.d_in + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK, out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
-    float acc[128];
+    float acc[64];
     bool ok = true;
     if (FP8) {
 #pragma unroll
-        for (int j = 0; j < 128; ++j) acc[j] = 0.f;
-        const float *xs = p.row_scales + (size_t)(r.row0 + min(row, r.rows - 1)) * in_blocks;
-        const size_t at = ((size_t)r.expert * out_blocks + min(r.out0 / DIP_FP8_BLOCK + (GATED ? 0 : half), out_blocks - 1)) * in_blocks;
+        for (int j = 0; j < 64; ++j) acc[j] = 0.f;
+        const float *xs = p.row_scales + (size_t)max(0, min(row0 + row, r.row0 + r.rows - 1)) * in_blocks;
+        const size_t at = ((size_t)r.expert * out_blocks + min((r.out0 + (GATED ? 0 : col0)) / DIP_FP8_BLOCK, out_blocks - 1)) * in_blocks;
         const float *ws = p.w_scales + at, *us = GATED ? p.up_scales + at : ws;
         float next_x = __ldg(xs + r.k0), next_w = __ldg(ws + r.k0), next_u = __ldg(us + r.k0);
         for (int k = r.k0; k < r.k1; ++k, ++n) {
@@ -463,14 +531,15 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem &s
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                uint32_t v[32];
-                tmem_ld32(lanes + buf * GP_COLS + (c < 2 ? col0 + 32 * c : col1 + 32 * (c - 2)), v);
+                uint32_t v[16];
+                tmem_ld16(lanes + buf * GP_COLS + (c < 2 ? col0 + 16 * c : col1 + 16 * (c - 2)), v);
+                tmem_wait_ld();
 #pragma unroll
-                for (int j = 0; j < 32; ++j) acc[32 * c + j] = fmaf(__uint_as_float(v[j]), c < 2 ? s0 : s1, acc[32 * c + j]);
+                for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(__uint_as_float(v[j]), c < 2 ? s0 : s1, acc[16 * c + j]);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
+            if (lane == 0) arrive_first<PAIR>(&s.sum_empty[buf]);
         }
     } else {
         const int buf = n & 1;
@@ -478,37 +547,36 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem &s
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            uint32_t v[32];
-            tmem_ld32(lanes + buf * GP_COLS + (c < 2 ? col0 + 32 * c : col1 + 32 * (c - 2)), v);
+            uint32_t v[16];
+            tmem_ld16(lanes + buf * GP_COLS + (c < 2 ? col0 + 16 * c : col1 + 16 * (c - 2)), v);
+            tmem_wait_ld();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) acc[32 * c + j] = __uint_as_float(v[j]);
+            for (int j = 0; j < 16; ++j) acc[16 * c + j] = __uint_as_float(v[j]);
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
+        if (lane == 0) arrive_first<PAIR>(&s.sum_empty[buf]);
         ++n;
     }
     if (out_barrier_any(!ok)) return false;
 
     if (r.k1 - r.k0 < p.steps) {
-        // parts are [half][column / 4][row][4]
-        const size_t mine = (size_t)half * 32 * GP_ROWS + row;
-        float4 *to = reinterpret_cast<float4 *>(p.partials) +
-                     (size_t)(2 * blockIdx.x + plan.run_of(blockIdx.x, r.rest)) * (GP_ROWS * GP_COLS / 4) + mine;
-        if (row < r.rows) {
+        // parts are [quarter][column / 4][row][4]
+        const size_t mine = (size_t)quarter * 16 * GP_ROWS + row;
+        float4 *to = reinterpret_cast<float4 *>(p.partials + plan.part_at(plan.block, r.rest)) + mine;
+        if (row < rows) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) to[j * GP_ROWS] = make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
+            for (int j = 0; j < 16; ++j) to[j * GP_ROWS] = make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
         }
         int b0, b1;
         if (!part_is_last(p, s, plan, r, b0, b1)) return true;
 #pragma unroll
-        for (int j = 0; j < 128; ++j) acc[j] = 0.f;
-        if (row < r.rows) {
+        for (int j = 0; j < 64; ++j) acc[j] = 0.f;
+        if (row < rows) {
             for (int b = b0; b <= b1; ++b) {
-                const float4 *from = reinterpret_cast<const float4 *>(p.partials) +
-                                     (size_t)(2 * b + plan.run_of(b, r.rest)) * (GP_ROWS * GP_COLS / 4) + mine;
+                const float4 *from = reinterpret_cast<const float4 *>(p.partials + plan.part_at(b, r.rest)) + mine;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
+                for (int j = 0; j < 16; ++j) {
                     const float4 v = __ldcg(from + j * GP_ROWS);
                     acc[4 * j] += v.x;
                     acc[4 * j + 1] += v.y;
@@ -519,76 +587,97 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem &s
         }
     }
 
-    const size_t at = (size_t)(r.row0 + row) * p.d_out;
+    const int first = row & ~31, n_here = rows - first;              // this warp's rows
+    unsigned char *stage = s.out[(threadIdx.x >> 5) - 4];
     if (GATED) {
-        const int o = r.out0 + 64 * half;
+        const int o = r.out0 + 32 * quarter;
 #pragma unroll
-        for (int j = 0; j < 64; ++j) acc[j] = silu_f32(acc[j]) * acc[64 + j];
+        for (int j = 0; j < 32; ++j) acc[j] = silu_f32(acc[j]) * acc[32 + j];
         if (FP8) {
-            // a block of 128 outputs has a scale: two threads have a half each
+            // a block of 128 outputs has a scale: four threads have a quarter each
             float most = 0.f;
 #pragma unroll
-            for (int j = 0; j < 64; ++j)
-                if (o + j < p.d_out) most = fmaxf(most, fabsf(acc[j]));
-            s.amax[half * GP_ROWS + row] = most;
+            for (int j = 0; j < 32; ++j)
+                if (o < p.d_out) most = fmaxf(most, fabsf(acc[j]));
+            s.amax[quarter * GP_ROWS + row] = most;
             out_barrier();
-            const float scale = fp8_scale(fmaxf(most, s.amax[(half ^ 1) * GP_ROWS + row]));
-            if (row < r.rows) {
-                if (half == 0) p.out_scales[(size_t)(r.row0 + row) * out_blocks + r.out0 / DIP_FP8_BLOCK] = scale;
+            const float *m = s.amax + row;
+            const float scale = fp8_scale(fmaxf(fmaxf(m[0], m[GP_ROWS]), fmaxf(m[2 * GP_ROWS], m[3 * GP_ROWS])));
+            if (row < rows) {
+                if (quarter == 0) p.out_scales[(size_t)(row0 + row) * out_blocks + r.out0 / DIP_FP8_BLOCK] = scale;
+                if (o < p.d_out) {
+                    uint4 *to = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.out) + (size_t)(row0 + row) * p.d_out + o);
 #pragma unroll
-                for (int j = 0; j < 64; j += 16)
-                    if (o + j < p.d_out)
-                        *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.out) + at + o + j) =
-                            make_uint4(fp8_codes4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3], scale),
-                                       fp8_codes4(acc[j + 4], acc[j + 5], acc[j + 6], acc[j + 7], scale),
-                                       fp8_codes4(acc[j + 8], acc[j + 9], acc[j + 10], acc[j + 11], scale),
-                                       fp8_codes4(acc[j + 12], acc[j + 13], acc[j + 14], acc[j + 15], scale));
+                    for (int j = 0; j < 32; j += 16)
+                        to[j / 16] = make_uint4(fp8_codes4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3], scale),
+                                                fp8_codes4(acc[j + 4], acc[j + 5], acc[j + 6], acc[j + 7], scale),
+                                                fp8_codes4(acc[j + 8], acc[j + 9], acc[j + 10], acc[j + 11], scale),
+                                                fp8_codes4(acc[j + 12], acc[j + 13], acc[j + 14], acc[j + 15], scale));
+                }
             }
             out_barrier();                           // (before the next tile's maxima)
-        } else if (row < r.rows) {
-#pragma unroll
-            for (int j = 0; j < 64; j += 8)
-                if (o + j < p.d_out) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + at + o + j) = bf16x8(acc + j);
+            return true;
         }
-    } else if (row < r.rows) {
-        const int o = r.out0 + 128 * half;
-        if (p.out_f32) {
+    }
+    // (widths are multiples of 32 outputs)
+    const int item = !GATED && p.out_f32 ? 4 : 2, o = r.out0 + (GATED ? 32 : 64) * quarter, left = max(0, p.d_out - o) * item;
+    char *to = static_cast<char *>(p.out) + ((size_t)(row0 + first) * p.d_out + o) * item;
+    const size_t pitch = (size_t)p.d_out * item;
+    constexpr int B = GP_PIECE<PAIR>;
+    if (item == 4) {
 #pragma unroll
-            for (int j = 0; j < 128; j += 4)
-                if (o + j < p.d_out)
-                    *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at + o + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
-        } else {
+        for (int c = 0; c < 256 / B; ++c) {
+            uint4 v[B / 16];
 #pragma unroll
-            for (int j = 0; j < 128; j += 8)
-                if (o + j < p.d_out) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + at + o + j) = bf16x8(acc + j);
+            for (int q = 0; q < B / 16; ++q) {
+                const float *f = acc + c * (B / 4) + 4 * q;
+                v[q] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+            }
+            leave<PAIR>(stage, v, to + c * B, pitch, n_here, left - c * B);
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < (GATED ? 64 : 128) / B; ++c) {
+            uint4 v[B / 16];
+#pragma unroll
+            for (int q = 0; q < B / 16; ++q) v[q] = bf16x8(acc + c * (B / 2) + 8 * q);
+            leave<PAIR>(stage, v, to + c * B, pitch, n_here, left - c * B);
         }
     }
     return true;
 }
 
-template <bool FP8, bool GATED>
+template <bool FP8, bool GATED, bool PAIR>
 __global__ void __launch_bounds__(GP_THREADS, 1)
 grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap few_map,
                const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap w2_map, const GroupedParams p)
 {
     extern __shared__ unsigned char gp_smem_raw[];
-    GroupedSmem &s = *reinterpret_cast<GroupedSmem *>((reinterpret_cast<uintptr_t>(gp_smem_raw) + 1023) & ~(uintptr_t)1023);
+    GroupedSmem<PAIR> &s = *reinterpret_cast<GroupedSmem<PAIR> *>((reinterpret_cast<uintptr_t>(gp_smem_raw) + 1023) & ~(uintptr_t)1023);
+    constexpr int STAGES = GP_STAGES<PAIR>;
     DIP_TRACE_MIN(p.tr, 0);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = PAIR ? blockIdx.x & 1 : 0;      // (clusters are two neighbouring blocks)
 
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem_base)),
-                     "n"(GP_TMEM_COLS) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem_base)),
+                         "n"(GP_TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem_base)),
+                         "n"(GP_TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     if (tid == 0) {
-        for (int i = 0; i < GP_STAGES; ++i) {
+        for (int i = 0; i < STAGES; ++i) {
             mbar_init(&s.full[i], 1);
             mbar_init(&s.empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.sum_full[i], 1);
-            mbar_init(&s.sum_empty[i], GP_OUT_WARPS);
+            mbar_init(&s.sum_empty[i], PAIR ? 2 * GP_OUT_WARPS : GP_OUT_WARPS);
         }
         mbar_init(&s.drained, 1);
         asm volatile("prefetch.tensormap [%0];" ::"l"(&rows_map) : "memory");
@@ -599,14 +688,15 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
     }
     dip_grid_dependency_wait();                      // rows and offsets come from the kernels in front
     DIP_TRACE_MIN(p.tr, 1);
-    if (warp == 0) grouped_plan(p, s);
+    if (warp == 0) grouped_plan(p, Schedule<GATED, PAIR>::ROWS, s.plan);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (PAIR) pair_barrier();                        // (the other block's barriers are set up)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     dip_launch_dependents();
     const uint32_t tmem = s.tmem_base;
-    const Schedule<GATED> plan(s, p);
-    const int per_step = FP8 ? GP_STEP_BYTES : GP_STEP_BYTES / 2;
+    const Schedule<GATED, PAIR> plan(s.plan, p);
+    constexpr int PER_STEP = FP8 ? GP_STEP_BYTES : GP_STEP_BYTES / 2;
     bool failed = false;
 
     if (warp < 4) {
@@ -615,46 +705,53 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
             Run r;
             int g = 0;                               // steps so far
             for (int i = 0; !failed && plan.get(i, r); ++i) {
-                const bool few = r.rows <= GP_FEW, both = r.rows > GP_BOX;
-                const int w_row = r.expert * p.d_out + r.out0;
-                // (plain: the tile's second half may lie behind the last output)
-                const bool second = GATED || r.out0 + GP_COLS / 2 < p.d_out;
-                const unsigned bytes = (few ? (both ? 2 : 1) * GP_BOX * GP_STEP_BYTES : GP_A_BYTES) + (second ? GP_B_BYTES : GP_B_BYTES / 2);
-                int x = r.k0 * per_step;
-                for (int k = r.k0; k < r.k1; ++k, ++g, x += per_step) {
-                    const int st = g % GP_STAGES;
-                    if (g >= GP_STAGES && !warp_wait(&s.empty[st], (g / GP_STAGES - 1) & 1, p.wait_limit_ns)) {
+                const bool few = !PAIR && r.rows <= GP_FEW, both = r.rows > GP_BOX;
+                const int w_row = r.expert * p.d_out + r.out0, row0 = r.row0 + rank * GP_ROWS;
+                // (single, plain: the tile's second half may lie behind the last output; PAIR: the second block may have no rows)
+                const bool second = GATED || r.out0 + GP_COLS / 2 < p.d_out, some = rank * GP_ROWS < r.rows;
+                const unsigned bytes = PAIR ? GP_B_BYTES + (r.rows > GP_ROWS ? 2 : 1) * GP_A_BYTES
+                                            : (few ? (both ? 2 : 1) * GP_BOX * GP_STEP_BYTES : GP_A_BYTES) + (second ? GP_B_BYTES : GP_B_BYTES / 2);
+                int x = r.k0 * PER_STEP;
+                for (int k = r.k0; k < r.k1; ++k, ++g, x += PER_STEP) {
+                    const int st = g % STAGES;
+                    if (g >= STAGES && !warp_wait(&s.empty[st], (g / STAGES - 1) & 1, p.wait_limit_ns)) {
                         failed = true;
                         break;
                     }
                     if (elect_one()) {
-                        mbar_expect_tx(&s.full[st], bytes);
-                        if (GATED) {
-                            tma_load(s.b[st], &w_map, x, w_row, &s.full[st]);
-                            tma_load(s.b[st] + GP_B_BYTES / 2, &w2_map, x, w_row, &s.full[st]);
+                        if (rank == 0) mbar_expect_tx(&s.full[st], bytes);
+                        if (PAIR) {
+                            if (GATED) tma_load<PAIR>(s.b[st], rank ? &w2_map : &w_map, x, w_row, &s.full[st]);
+                            else tma_load<PAIR>(s.b[st], &w_map, x, w_row + rank * (GP_COLS / 2), &s.full[st]);
+                            if (some) tma_load<PAIR>(s.a[st], &rows_map, x, row0, &s.full[st]);
                         } else {
-                            tma_load(s.b[st], second ? &w2_map : &w_map, x, w_row, &s.full[st]);
+                            if (GATED) {
+                                tma_load<PAIR>(s.b[st], &w_map, x, w_row, &s.full[st]);
+                                tma_load<PAIR>(s.b[st] + GP_B_BYTES / 2, &w2_map, x, w_row, &s.full[st]);
+                            } else {
+                                tma_load<PAIR>(s.b[st], second ? &w2_map : &w_map, x, w_row, &s.full[st]);
+                            }
+                            tma_load<PAIR>(s.a[st], few ? &few_map : &rows_map, x, r.row0, &s.full[st]);
+                            if (few && both) tma_load<PAIR>(s.a[st] + GP_BOX * GP_STEP_BYTES, &few_map, x, r.row0 + GP_BOX, &s.full[st]);
                         }
-                        tma_load(s.a[st], few ? &few_map : &rows_map, x, r.row0, &s.full[st]);
-                        if (few && both) tma_load(s.a[st] + GP_BOX * GP_STEP_BYTES, &few_map, x, r.row0 + GP_BOX, &s.full[st]);
                     }
                     __syncwarp();
                 }
             }
-            // (given up: no copy of this block's is under way when it leaves)
-            if (failed)
-                for (int j = max(0, g - GP_STAGES); j < g; ++j) warp_wait(&s.full[j % GP_STAGES], (j / GP_STAGES) & 1, p.wait_limit_ns);
-        } else if (warp == 1) {
+            // (given up: no copy of this block's is under way when it leaves; the second block's count at the first one's barriers)
+            if (failed && rank == 0)
+                for (int j = max(0, g - STAGES); j < g; ++j) warp_wait(&s.full[j % STAGES], (j / STAGES) & 1, p.wait_limit_ns);
+        } else if (warp == 1 && rank == 0) {
             Run r;
             int g = 0, n = 0;                        // steps, accumulators so far
             for (int i = 0; !failed && plan.get(i, r); ++i) {
-                const bool few = r.rows <= GP_FEW;
-                const uint32_t shape = grouped_shape<FP8>(few ? (r.rows + 15) / 16 * 16 : GP_COLS);
+                const bool few = !PAIR && r.rows <= GP_FEW;
+                const uint32_t shape = grouped_shape<FP8, PAIR>(few ? (r.rows + 15) / 16 * 16 : GP_COLS);
                 for (int k = r.k0; k < r.k1; ++k, ++g) {
-                    const int st = g % GP_STAGES, buf = n & 1;
+                    const int st = g % STAGES, buf = n & 1;
                     const bool first = FP8 || k == r.k0, last = FP8 || k == r.k1 - 1;
                     if ((first && n >= 2 && !warp_wait(&s.sum_empty[buf], (n / 2 - 1) & 1, p.wait_limit_ns)) ||
-                        !warp_wait(&s.full[st], (g / GP_STAGES) & 1, p.wait_limit_ns)) {
+                        !warp_wait(&s.full[st], (g / STAGES) & 1, p.wait_limit_ns)) {
                         failed = true;
                         break;
                     }
@@ -665,44 +762,54 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
                         if (!few) {
 #pragma unroll
                             for (int q = 0; q < 4; ++q)          // 32 bytes of K each
-                                grouped_mma<FP8>(to, a + 2 * q, b + 2 * q, shape, (first && q == 0) ? 0u : 1u);
+                                grouped_mma<FP8, PAIR>(to, a + 2 * q, b + 2 * q, shape, (first && q == 0) ? 0u : 1u);
                         } else {
 #pragma unroll
                             for (int q = 0; q < 4; ++q) {
-                                grouped_mma<FP8>(to, b + 2 * q, a + 2 * q, shape, (first && q == 0) ? 0u : 1u);
-                                grouped_mma<FP8>(to + GP_COLS / 2, b + (GP_B_BYTES / 2 >> 4) + 2 * q, a + 2 * q, shape, (first && q == 0) ? 0u : 1u);
+                                grouped_mma<FP8, PAIR>(to, b + 2 * q, a + 2 * q, shape, (first && q == 0) ? 0u : 1u);
+                                grouped_mma<FP8, PAIR>(to + GP_COLS / 2, b + (GP_B_BYTES / 2 >> 4) + 2 * q, a + 2 * q, shape,
+                                                       (first && q == 0) ? 0u : 1u);
                             }
                         }
-                        grouped_commit(&s.empty[st]);
-                        if (last) grouped_commit(&s.sum_full[buf]);
+                        grouped_commit<PAIR>(&s.empty[st]);
+                        if (last) grouped_commit<PAIR>(&s.sum_full[buf]);
                     }
                     __syncwarp();
                     if (last) ++n;
                 }
             }
             if (failed) {
-                if (elect_one()) grouped_commit(&s.drained);
+                if (elect_one()) grouped_commit<PAIR>(&s.drained);
                 __syncwarp();
                 warp_wait(&s.drained, 0, p.wait_limit_ns);
             }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(GP_REGS_MANY));
-        const int half = (warp - 4) >> 2, place = (warp & 3) * 32 + lane;        // lane of tensor memory
+        const int quarter = (warp - 4) >> 2, place = (warp & 3) * 32 + lane;     // lane of tensor memory
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         int n = 0;                                   // accumulators so far
         Run r;
         for (int i = 0; !failed && plan.get(i, r); ++i) {
-            if (r.rows <= GP_FEW) failed = !take_few<FP8, GATED>(p, s, plan, r, lanes, half, place, n);
-            else failed = !take_tile<FP8, GATED>(p, s, plan, r, lanes, half, place, n);
+            if constexpr (!PAIR) {
+                if (r.rows <= GP_FEW) {
+                    failed = !take_few<FP8, GATED>(p, s, plan, r, lanes, quarter, place, n);
+                    continue;
+                }
+            }
+            failed = !take_tile<FP8, GATED, PAIR>(p, s, plan, r, r.row0 + rank * GP_ROWS, min(GP_ROWS, r.rows - rank * GP_ROWS), lanes, quarter,
+                                                  place, n);
         }
     }
     if (failed) atomicExch(p.status, 1);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (PAIR) pair_barrier();                        // (the first block's MMAs have read this block's memory, all has arrived at its barriers)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (warp == 1)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(GP_TMEM_COLS) : "memory");
+    if (warp == 1) {
+        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(GP_TMEM_COLS) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(GP_TMEM_COLS) : "memory");
+    }
     DIP_TRACE_MAX(p.tr, 2);
 }
 
@@ -735,26 +842,51 @@ bool encode(CUtensorMap *map, const void *p, bool fp8, size_t n, int d, int box)
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool FP8, bool GATED>
+template <bool FP8, bool GATED, bool PAIR>
 cudaError_t launch(dip_ctx *ctx, int ctas, cudaStream_t stream, const CUtensorMap (&m)[4], const GroupedParams &p)
 {
     static dip_per_device_once once;
-    const size_t smem = sizeof(GroupedSmem) + 1024;
-    static_assert(sizeof(GroupedSmem) + 1024 <= 227 * 1024, "fits a CTA's shared memory");
-    const cudaError_t e = dip_raise_smem_limit(once, ctx->device, grouped_kernel<FP8, GATED>, smem);
-    return e != cudaSuccess ? e : dip_launch_pdl(grouped_kernel<FP8, GATED>, dim3(ctas), dim3(GP_THREADS), smem, stream, m[0], m[1],
-                                              m[2], m[3], p);
+    const auto kernel = grouped_kernel<FP8, GATED, PAIR>;
+    const size_t smem = sizeof(GroupedSmem<PAIR>) + 1024;
+    static_assert(sizeof(GroupedSmem<PAIR>) + 1024 <= 227 * 1024, "fits a CTA's shared memory");
+    const cudaError_t e = dip_raise_smem_limit(once, ctx->device, kernel, smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(GP_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = PAIR ? 2 : 1;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], p);
+}
+
+template <bool FP8, bool GATED>
+cudaError_t launch(bool pair, dip_ctx *ctx, int ctas, cudaStream_t stream, const CUtensorMap (&m)[4], const GroupedParams &p)
+{
+    return pair ? launch<FP8, GATED, true>(ctx, ctas, stream, m, p) : launch<FP8, GATED, false>(ctx, ctas, stream, m, p);
 }
 
 }  // namespace
+
+// Pairs from this many rows per expert on (the average over as many experts as can have any).
+constexpr int GP_PAIR_ROWS = 192;
 
 dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const dip_grouped_matrix *up, const void *rows,
                               const float *row_scales, int n_rows, const int32_t *offset, void *out, bool out_f32, float *out_scales,
                               cudaStream_t stream)
 {
     const bool fp8 = w.wtype == DIP_W_FP8_B128;
+    const int met = min(w.n_experts, n_rows);
+    const bool pair = n_rows >= GP_PAIR_ROWS * met && ctx->sm_count % 2 == 0;
     const size_t w_rows = (size_t)w.n_experts * w.d_out;
-    // the rows, whole tiles of them and few; a half of a tile's weights; the other half (gate/up), or both at once
+    // the rows, whole tiles of them and few; half of a tile's weights; the other half (gate/up), or both at once
     CUtensorMap maps[4];
     if (!encoder() || !encode(&maps[0], rows, fp8, n_rows, w.d_in, GP_ROWS) || !encode(&maps[1], rows, fp8, n_rows, w.d_in, GP_BOX) ||
         !encode(&maps[2], w.values, fp8, w_rows, w.d_in, GP_COLS / 2) ||
@@ -762,6 +894,7 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
         snprintf(ctx->err, sizeof(ctx->err), "cuTensorMapEncodeTiled failed");
         return DIP_ERR_CUDA;
     }
+    const int width = up ? GP_COLS / 2 : GP_COLS, tile_rows = pair ? 2 * GP_ROWS : GP_ROWS;
     GroupedParams p = {};
     p.w_scales = w.scales;
     p.up_scales = up ? up->scales : nullptr;
@@ -771,7 +904,7 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
     p.d_in = w.d_in;
     p.n_rows = n_rows;
     p.steps = (w.d_in * (fp8 ? 1 : 2) + GP_STEP_BYTES - 1) / GP_STEP_BYTES;
-    p.n_cols = (w.d_out + (up ? GP_COLS / 2 : GP_COLS) - 1) / (up ? GP_COLS / 2 : GP_COLS);
+    p.n_cols = (w.d_out + width - 1) / width;
     p.offset = offset;
     p.out = out;
     p.out_scales = out_scales;
@@ -782,9 +915,10 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
     p.wait_limit_ns = ctx->wait_limit_ns;
     p.tr = dip_trace_slot(ctx, up ? 10 : 11);
     // no more blocks than there can be parts
-    const long long tiles = (long long)((n_rows + GP_ROWS - 1) / GP_ROWS + min(w.n_experts, n_rows) - 1) * p.n_cols;
-    const int ctas = (int)min((long long)ctx->sm_count, max(tiles, tiles * p.steps / GP_MIN_STEPS));
+    const long long tiles = (long long)((n_rows + tile_rows - 1) / tile_rows + met - 1) * p.n_cols;
+    const long long most = max(tiles, tiles * p.steps / GP_MIN_STEPS);
+    const int ctas = pair ? 2 * (int)min((long long)ctx->sm_count / 2, most) : (int)min((long long)ctx->sm_count, most);
     const auto start = fp8 ? (up ? launch<true, true> : launch<true, false>) : (up ? launch<false, true> : launch<false, false>);
-    DIP_CUDA_TRY(ctx, start(ctx, ctas, stream, maps, p));
+    DIP_CUDA_TRY(ctx, start(pair, ctx, ctas, stream, maps, p));
     return DIP_OK;
 }
