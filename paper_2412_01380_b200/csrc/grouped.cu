@@ -13,10 +13,10 @@
 //          are rows.
 //   warp 0      issues the copies: a ring of steps
 //   warp 1      issues the MMAs (N = 256, four per step) into one of two accumulators of 256 columns
-//   warps 4-19  take the accumulators out: thread = row, a quarter of the columns for each four warps
+//   the others  take the accumulators out: thread = row, and each four warps have a share of the columns
 // BF16: an accumulator is a tile, and the next tile's MMAs run while the first is taken out.  FP8: a step is a block of 128
 // input indices, which has scales of its own, so every step's accumulator is taken out and added, times row scale * weight
-// scale, to binary32 sums in registers: 256 multiply-adds per warp scheduler and step against the 512 cycles of its MMAs.
+// scale, to binary32 sums in registers: 256 columns per warp scheduler and step against the 512 cycles of its MMAs.
 //
 // Blocks stay: whole rounds of tiles are dealt out one to a block (or pair), and what is left over (all of it where there are
 // fewer tiles than SMs, as for a token) is cut along K into equal runs of steps, one per block, in tile order.  A tile's
@@ -35,11 +35,17 @@ constexpr int GP_ROWS = DIP_GROUP_ROWS, GP_COLS = DIP_GROUP_COLS;
 constexpr int GP_STEP_BYTES = 128;                  // of a row, per step
 constexpr int GP_BOX = 32;                          // rows per copy of the rows of a tile of few
 constexpr int GP_A_BYTES = GP_ROWS * GP_STEP_BYTES, GP_B_BYTES = GP_COLS * GP_STEP_BYTES;
-constexpr int GP_OUT_WARPS = 16, GP_THREADS = (4 + GP_OUT_WARPS) * 32;
-// registers of a thread of the first four warps and of the others, out of the launch's 96 each: (64 + 4 * 104) / 5
-constexpr int GP_REGS_FEW = 64, GP_REGS_MANY = 104;
+// Warps that take sums out.  FP8 keeps a tile's sums in registers over all steps, and two warps per scheduler with 128 of them each
+// can have two loads of 32 accumulator columns in hand; BF16 only has to get rid of a tile.
+template <bool FP8> constexpr int GP_OUT_WARPS = FP8 ? 8 : 16;
+template <bool FP8> constexpr int GP_THREADS = (4 + GP_OUT_WARPS<FP8>) * 32;
+// registers of a thread of the first four warps and of the others; in all what the launch has: (56 + 2 * 224) / 3 = 168 each, or
+// (64 + 4 * 104) / 5 = 96
+template <bool FP8> constexpr int GP_REGS_FEW = FP8 ? 56 : 64;
+template <bool FP8> constexpr int GP_REGS_MANY = FP8 ? 224 : 104;
 constexpr int GP_TMEM_COLS = 512;
 constexpr int GP_MIN_STEPS = 4;                     // a part of a tile has at least so many
+constexpr int GP_JOIN_FEW = 8, GP_JOIN = 20;        // steps' worth of time that a cut tile's parts take to meet (few rows; others)
 constexpr int GP_FEW = 64;                          // rows of a tile that are columns of its sums
 constexpr int GP_CHUNK = 12;                        // row tiles that go through an expert's weights together
 template <bool PAIR> constexpr int GP_STAGES = PAIR ? 5 : 4;
@@ -62,13 +68,14 @@ struct GroupedParams {
 struct GroupedPlan {
     int start[DIP_MAX_EXPERTS + 1];                 // first row of each expert
     int tiles[DIP_MAX_EXPERTS + 1];                 // row tiles in front of it
+    int most;                                       // rows of the largest group
 };
 
-template <bool PAIR>
+template <bool FP8, bool PAIR>
 struct __align__(1024) GroupedSmem {
     unsigned char a[GP_STAGES<PAIR>][GP_A_BYTES];
     unsigned char b[GP_STAGES<PAIR>][PAIR ? GP_B_BYTES / 2 : GP_B_BYTES];
-    unsigned char out[GP_OUT_WARPS][32 * GP_PIECE<PAIR>];
+    unsigned char out[GP_OUT_WARPS<FP8>][32 * GP_PIECE<PAIR>];
     uint64_t full[GP_STAGES<PAIR>], empty[GP_STAGES<PAIR>];        // a step's copies have landed; its MMAs have read them
     uint64_t sum_full[2], sum_empty[2];             // an accumulator is complete; has been taken out
     uint64_t drained;
@@ -158,29 +165,66 @@ __device__ __forceinline__ void pair_barrier()
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Sixteen columns of this warp's 32 lanes, without the wait: thread = lane, register = column.
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
+// 8, 16 or 32 columns of this warp's 32 lanes: thread = lane, register = column.  The wait names the registers, so that nothing
+// uses them before it.
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]),
+                   "+r"(r[7])::"memory");
+}
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[16])
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
                    "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(taddr));
 }
-// Eight.
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8])
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[16])
 {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]),
+                   "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]),
+                   "+r"(r[15])::"memory");
 }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+                 "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+                   "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+                   "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]),
+                   "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                   "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                   "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
+}
+
+// (a0, a1) += (d0, d1) * s, in one instruction.
+__device__ __forceinline__ void fma2(float &a0, float &a1, uint32_t d0, uint32_t d1, float s)
+{
+    asm("{\n .reg .b64 a, d, f;\n mov.b64 a, {%0, %1};\n mov.b64 d, {%2, %3};\n mov.b64 f, {%4, %4};\n fma.rn.f32x2 a, d, f, a;\n"
+        " mov.b64 {%0, %1}, a;\n}" : "+f"(a0), "+f"(a1) : "r"(d0), "r"(d1), "f"(s));
+}
 
 // Barriers of the warps that take sums out; the second also says to all of them alike whether any came with `v`.
-__device__ __forceinline__ void out_barrier() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(GP_OUT_WARPS * 32) : "memory"); }
+template <bool FP8>
+__device__ __forceinline__ void out_barrier() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(GP_OUT_WARPS<FP8> * 32) : "memory"); }
+template <bool FP8>
 __device__ __forceinline__ bool out_barrier_any(bool v)
 {
     unsigned any;
     asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n barrier.cta.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(any) : "r"((unsigned)v), "n"(GP_OUT_WARPS * 32) : "memory");
+                 : "=r"(any) : "r"((unsigned)v), "n"(GP_OUT_WARPS<FP8> * 32) : "memory");
     return any != 0u;
 }
 
@@ -212,6 +256,7 @@ struct Schedule {
         const int rest = tiles - whole * blocks;
         units = rest * steps;
         parts = min(blocks, max(units / GP_MIN_STEPS, rest));
+        if (parts > rest && units / parts + (s.most <= GP_FEW ? GP_JOIN_FEW : GP_JOIN) >= steps) parts = rest;      // (they stay whole)
         const bool mine = block < parts;
         at = mine ? units * block / parts : 0;
         end = mine ? units * (block + 1) / parts : 0;
@@ -287,11 +332,16 @@ __device__ __forceinline__ void grouped_plan(const GroupedParams &p, int tile_ro
     if (lane == 0) before = 0;
     for (int i = i0; i < i1; ++i) s.start[i] = max(s.start[i], before);
     __syncwarp();
-    int n = 0;
+    int n = 0, rows = 0;
     for (int i = i0; i < i1; ++i) {
         s.tiles[i] = n;
-        if (i < p.n_experts) n += (s.start[i + 1] - s.start[i] + tile_rows - 1) / tile_rows;
+        if (i >= p.n_experts) break;
+        const int here = s.start[i + 1] - s.start[i];
+        n += (here + tile_rows - 1) / tile_rows;
+        rows = max(rows, here);
     }
+    rows = __reduce_max_sync(0xffffffffu, rows);
+    if (lane == 0) s.most = rows;
     int incl = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -302,35 +352,35 @@ __device__ __forceinline__ void grouped_plan(const GroupedParams &p, int tile_ro
 }
 
 // A part of a cut tile is in the workspace (this thread's share of it): true for the warps of the block that came last.
-template <bool GATED, bool PAIR>
-__device__ __forceinline__ bool part_is_last(const GroupedParams &p, GroupedSmem<PAIR> &s, const Schedule<GATED, PAIR> &plan, const Run &r,
+template <bool FP8, bool GATED, bool PAIR>
+__device__ __forceinline__ bool part_is_last(const GroupedParams &p, GroupedSmem<FP8, PAIR> &s, const Schedule<GATED, PAIR> &plan, const Run &r,
                                              int &b0, int &b1)
 {
     b0 = plan.block_of(r.rest * p.steps);
     b1 = plan.block_of((r.rest + 1) * p.steps - 1);
     __threadfence();
-    out_barrier();
-    if (threadIdx.x == GP_THREADS - 1) {
+    out_barrier<FP8>();
+    if (threadIdx.x == GP_THREADS<FP8> - 1) {
         unsigned int *ticket = p.tickets + (PAIR ? 2 * r.rest + (int)(blockIdx.x & 1) : r.rest);
         s.last = atomicAdd(ticket, 1u) == (unsigned)(b1 - b0);
         if (s.last) *ticket = 0u;
         __threadfence();
     }
-    out_barrier();
+    out_barrier<FP8>();
     return s.last != 0;
 }
 
 // The sums of a tile of few rows and what becomes of them: thread = output, values = rows.  False: a wait ran out.
-// The warps' quarters share the rows; plain: two quarters each for the first and the second 128 outputs; gate/up: a thread has gate
-// and up of its output.
+// Each four warps have a share of the rows; plain: the first or the second 128 outputs of a share; gate/up: a thread has gate and up of
+// its output.
 template <bool FP8, bool GATED>
-__device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<false> &s, const Schedule<GATED, false> &plan, const Run &r,
-                                         uint32_t lanes, int quarter, int place, int &n)
+__device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<FP8, false> &s, const Schedule<GATED, false> &plan, const Run &r,
+                                         uint32_t lanes, int share, int place, int &n)
 {
-    constexpr int SHARES = GATED ? 4 : 2, N = GP_FEW / SHARES;                     // rows of a thread: at most N
+    constexpr int SHARES = GP_OUT_WARPS<FP8> / (GATED ? 4 : 8), N = GP_FEW / SHARES;         // rows of a thread: at most N
     const int lane = threadIdx.x & 31, per = ((r.rows + SHARES - 1) / SHARES + 7) / 8 * 8;
-    const int t0 = (GATED ? quarter : quarter >> 1) * per, rows = min(per, r.rows - t0);      // (may be none)
-    const int side = GATED ? 0 : GP_COLS / 2 * (quarter & 1), o = r.out0 + side + place;
+    const int t0 = (GATED ? share : share >> 1) * per, rows = min(per, r.rows - t0);      // (may be none)
+    const int side = GATED ? 0 : GP_COLS / 2 * (share & 1), o = r.out0 + side + place;
     const uint32_t sums = lanes + side + t0;
     const int in_blocks = (p.d_in + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK, out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
     float a[N], u[GATED ? N : 1];
@@ -342,15 +392,17 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<fal
 #pragma unroll
             for (int j = 0; j < N; ++j) u[j] = 0.f;
         }
-        // a lane keeps the scale of row t0 + lane, and asks for the next step's in good time
+        // a lane keeps the scales of row t0 + lane and of the one 32 behind it, and asks for the next step's in good time
         const float *xs = p.row_scales + (size_t)min(r.row0 + t0 + lane, r.row0 + r.rows - 1) * in_blocks;
+        const float *ys = p.row_scales + (size_t)min(r.row0 + t0 + 32 + lane, r.row0 + r.rows - 1) * in_blocks;
         const size_t at = ((size_t)r.expert * out_blocks + min((r.out0 + side) / DIP_FP8_BLOCK, out_blocks - 1)) * in_blocks;
         const float *ws = p.w_scales + at, *us = GATED ? p.up_scales + at : ws;
-        float next_x = __ldg(xs + r.k0), next_w = __ldg(ws + r.k0), next_u = __ldg(us + r.k0);
+        float next_x = __ldg(xs + r.k0), next_w = __ldg(ws + r.k0), next_u = __ldg(us + r.k0), next_y = __ldg(ys + r.k0);
         for (int k = r.k0; k < r.k1; ++k, ++n) {
-            const float sx = next_x, w = next_w, v = next_u;
+            const float sx = next_x, sy = next_y, w = next_w, v = next_u;
             if (k + 1 < r.k1) {
                 next_x = __ldg(xs + k + 1);
+                if (N > 32) next_y = __ldg(ys + k + 1);
                 next_w = __ldg(ws + k + 1);
                 if (GATED) next_u = __ldg(us + k + 1);
             }
@@ -364,12 +416,15 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<fal
             for (int c = 0; c < N / 8; ++c)
                 if (8 * c < rows) {
                     uint32_t d[8], e[8];
-                    tmem_ld8(sums + buf * GP_COLS + 8 * c, d);
-                    if (GATED) tmem_ld8(sums + buf * GP_COLS + GP_COLS / 2 + 8 * c, e);
-                    tmem_wait_ld();
+                    tmem_ld(sums + buf * GP_COLS + 8 * c, d);
+                    if (GATED) {
+                        tmem_ld(sums + buf * GP_COLS + GP_COLS / 2 + 8 * c, e);
+                        tmem_wait(e);
+                    }
+                    tmem_wait(d);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float x = __shfl_sync(0xffffffffu, sx, 8 * c + j);
+                        const float x = __shfl_sync(0xffffffffu, c < 4 ? sx : sy, (8 * c + j) & 31);
                         a[8 * c + j] = fmaf(__uint_as_float(d[j]), x * w, a[8 * c + j]);
                         if (GATED) u[8 * c + j] = fmaf(__uint_as_float(e[j]), x * v, u[8 * c + j]);
                     }
@@ -386,9 +441,12 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<fal
         for (int c = 0; c < N / 8; ++c)
             if (8 * c < rows) {
                 uint32_t d[8], e[8];
-                tmem_ld8(sums + buf * GP_COLS + 8 * c, d);
-                if (GATED) tmem_ld8(sums + buf * GP_COLS + GP_COLS / 2 + 8 * c, e);
-                tmem_wait_ld();
+                tmem_ld(sums + buf * GP_COLS + 8 * c, d);
+                if (GATED) {
+                    tmem_ld(sums + buf * GP_COLS + GP_COLS / 2 + 8 * c, e);
+                    tmem_wait(e);
+                }
+                tmem_wait(d);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     a[8 * c + j] = __uint_as_float(d[j]);
@@ -401,7 +459,7 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<fal
         ++n;
     }
     // (a wait of one warp that runs out takes the others along: they meet at barriers below)
-    if (out_barrier_any(!ok)) return false;
+    if (out_barrier_any<FP8>(!ok)) return false;
 
     if (r.k1 - r.k0 < p.steps) {
         // a part of the tile: the last of its blocks goes on with the sum of all.  Parts are [row][256 sums]
@@ -456,7 +514,7 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<fal
                 }
             }
     }
-    if (GATED && FP8) out_barrier();
+    if (GATED && FP8) out_barrier<FP8>();
 #pragma unroll
     for (int c = 0; c < N / 8; ++c)
         if (8 * c < rows) {
@@ -474,7 +532,7 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<fal
                     }
                 }
         }
-    if (GATED && FP8) out_barrier();                 // (before the next tile's maxima)
+    if (GATED && FP8) out_barrier<FP8>();                 // (before the next tile's maxima)
     return true;
 }
 
@@ -498,20 +556,21 @@ __device__ __forceinline__ void leave(unsigned char *stage, const uint4 *v, char
     }
 }
 
-// The sums of any other tile: thread = row, values = 64 of its columns (gate/up: 32 gate and the 32 up beside them).
-// row0, rows: this block's rows of the tile (may be none).
+// The sums of any other tile: thread = row, values = its share of the columns (gate/up: half of them gate, the others the up beside
+// them).  row0, rows: this block's rows of the tile (may be none).
 template <bool FP8, bool GATED, bool PAIR>
-__device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<PAIR> &s, const Schedule<GATED, PAIR> &plan, const Run &r,
-                                          int row0, int rows, uint32_t lanes, int quarter, int row, int &n)
+__device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<FP8, PAIR> &s, const Schedule<GATED, PAIR> &plan, const Run &r,
+                                          int row0, int rows, uint32_t lanes, int share, int row, int &n)
 {
+    constexpr int SHARES = GP_OUT_WARPS<FP8> / 4, C = GP_COLS / SHARES, H = C / 2;
     const int lane = threadIdx.x & 31;
-    const int col0 = GATED ? 32 * quarter : 64 * quarter, col1 = GATED ? GP_COLS / 2 + col0 : col0 + 32;      // 32 columns from each
+    const int col0 = GATED ? H * share : C * share, col1 = GATED ? GP_COLS / 2 + col0 : col0 + H;      // H columns from each
     const int in_blocks = (p.d_in + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK, out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
-    float acc[64];
+    float acc[C];
     bool ok = true;
-    if (FP8) {
+    if constexpr (FP8) {
 #pragma unroll
-        for (int j = 0; j < 64; ++j) acc[j] = 0.f;
+        for (int j = 0; j < C; ++j) acc[j] = 0.f;
         const float *xs = p.row_scales + (size_t)max(0, min(row0 + row, r.row0 + r.rows - 1)) * in_blocks;
         const size_t at = ((size_t)r.expert * out_blocks + min((r.out0 + (GATED ? 0 : col0)) / DIP_FP8_BLOCK, out_blocks - 1)) * in_blocks;
         const float *ws = p.w_scales + at, *us = GATED ? p.up_scales + at : ws;
@@ -529,27 +588,34 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<PA
                 break;
             }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            // one load of 32 columns is under way while the one in front is added
+            uint32_t v[2][32];
+            tmem_ld(lanes + buf * GP_COLS + col0, v[0]);
+            tmem_wait(v[0]);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[16];
-                tmem_ld16(lanes + buf * GP_COLS + (c < 2 ? col0 + 16 * c : col1 + 16 * (c - 2)), v);
-                tmem_wait_ld();
+            for (int c = 0; c < C / 32; ++c) {
+                if (c + 1 < C / 32) {
+                    tmem_ld(lanes + buf * GP_COLS + (32 * (c + 1) < H ? col0 + 32 * (c + 1) : col1 + 32 * (c + 1) - H), v[(c + 1) & 1]);
+                } else {                             // all of it is in registers
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) arrive_first<PAIR>(&s.sum_empty[buf]);
+                }
 #pragma unroll
-                for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(__uint_as_float(v[j]), c < 2 ? s0 : s1, acc[16 * c + j]);
+                for (int j = 0; j < 32; j += 2)
+                    fma2(acc[32 * c + j], acc[32 * c + j + 1], v[c & 1][j], v[c & 1][j + 1], 32 * c < H ? s0 : s1);
+                if (c + 1 < C / 32) tmem_wait(v[(c + 1) & 1]);
             }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) arrive_first<PAIR>(&s.sum_empty[buf]);
         }
     } else {
         const int buf = n & 1;
         ok = warp_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < C / 16; ++c) {
             uint32_t v[16];
-            tmem_ld16(lanes + buf * GP_COLS + (c < 2 ? col0 + 16 * c : col1 + 16 * (c - 2)), v);
-            tmem_wait_ld();
+            tmem_ld(lanes + buf * GP_COLS + (16 * c < H ? col0 + 16 * c : col1 + 16 * c - H), v);
+            tmem_wait(v);
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[16 * c + j] = __uint_as_float(v[j]);
         }
@@ -558,25 +624,25 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<PA
         if (lane == 0) arrive_first<PAIR>(&s.sum_empty[buf]);
         ++n;
     }
-    if (out_barrier_any(!ok)) return false;
+    if (out_barrier_any<FP8>(!ok)) return false;
 
     if (r.k1 - r.k0 < p.steps) {
-        // parts are [quarter][column / 4][row][4]
-        const size_t mine = (size_t)quarter * 16 * GP_ROWS + row;
+        // parts are [share][column / 4][row][4]
+        const size_t mine = (size_t)share * (C / 4) * GP_ROWS + row;
         float4 *to = reinterpret_cast<float4 *>(p.partials + plan.part_at(plan.block, r.rest)) + mine;
         if (row < rows) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) to[j * GP_ROWS] = make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
+            for (int j = 0; j < C / 4; ++j) to[j * GP_ROWS] = make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
         }
         int b0, b1;
         if (!part_is_last(p, s, plan, r, b0, b1)) return true;
 #pragma unroll
-        for (int j = 0; j < 64; ++j) acc[j] = 0.f;
+        for (int j = 0; j < C; ++j) acc[j] = 0.f;
         if (row < rows) {
             for (int b = b0; b <= b1; ++b) {
                 const float4 *from = reinterpret_cast<const float4 *>(p.partials + plan.part_at(b, r.rest)) + mine;
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
+                for (int j = 0; j < C / 4; ++j) {
                     const float4 v = __ldcg(from + j * GP_ROWS);
                     acc[4 * j] += v.x;
                     acc[4 * j + 1] += v.y;
@@ -590,43 +656,43 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<PA
     const int first = row & ~31, n_here = rows - first;              // this warp's rows
     unsigned char *stage = s.out[(threadIdx.x >> 5) - 4];
     if (GATED) {
-        const int o = r.out0 + 32 * quarter;
+        const int o = r.out0 + H * share;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) acc[j] = silu_f32(acc[j]) * acc[32 + j];
+        for (int j = 0; j < H; ++j) acc[j] = silu_f32(acc[j]) * acc[H + j];
         if (FP8) {
-            // a block of 128 outputs has a scale: four threads have a quarter each
+            // a block of 128 outputs has a scale: two threads have a half each (widths are multiples of 32 outputs)
             float most = 0.f;
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (o < p.d_out) most = fmaxf(most, fabsf(acc[j]));
-            s.amax[quarter * GP_ROWS + row] = most;
-            out_barrier();
-            const float *m = s.amax + row;
-            const float scale = fp8_scale(fmaxf(fmaxf(m[0], m[GP_ROWS]), fmaxf(m[2 * GP_ROWS], m[3 * GP_ROWS])));
-            if (row < rows) {
-                if (quarter == 0) p.out_scales[(size_t)(row0 + row) * out_blocks + r.out0 / DIP_FP8_BLOCK] = scale;
-                if (o < p.d_out) {
-                    uint4 *to = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.out) + (size_t)(row0 + row) * p.d_out + o);
+            for (int j = 0; j < H; ++j)
+                if (o + (j & ~31) < p.d_out) most = fmaxf(most, fabsf(acc[j]));
+            s.amax[share * GP_ROWS + row] = most;
+            out_barrier<FP8>();
+            const float scale = fp8_scale(fmaxf(most, s.amax[(share ^ 1) * GP_ROWS + row]));
+            if (row < rows && share == 0) p.out_scales[(size_t)(row0 + row) * out_blocks + r.out0 / DIP_FP8_BLOCK] = scale;
+            char *to = static_cast<char *>(p.out) + (size_t)(row0 + first) * p.d_out + o;
+            constexpr int B = GP_PIECE<PAIR>;
 #pragma unroll
-                    for (int j = 0; j < 32; j += 16)
-                        to[j / 16] = make_uint4(fp8_codes4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3], scale),
-                                                fp8_codes4(acc[j + 4], acc[j + 5], acc[j + 6], acc[j + 7], scale),
-                                                fp8_codes4(acc[j + 8], acc[j + 9], acc[j + 10], acc[j + 11], scale),
-                                                fp8_codes4(acc[j + 12], acc[j + 13], acc[j + 14], acc[j + 15], scale));
+            for (int c = 0; c < H / B; ++c) {
+                uint4 v[B / 16];
+#pragma unroll
+                for (int q = 0; q < B / 16; ++q) {
+                    const float *f = acc + c * B + 16 * q;
+                    v[q] = make_uint4(fp8_codes4(f[0], f[1], f[2], f[3], scale), fp8_codes4(f[4], f[5], f[6], f[7], scale),
+                                      fp8_codes4(f[8], f[9], f[10], f[11], scale), fp8_codes4(f[12], f[13], f[14], f[15], scale));
                 }
+                leave<PAIR>(stage, v, to + c * B, p.d_out, n_here, p.d_out - o - c * B);
             }
-            out_barrier();                           // (before the next tile's maxima)
+            out_barrier<FP8>();                      // (before the next tile's maxima)
             return true;
         }
     }
-    // (widths are multiples of 32 outputs)
-    const int item = !GATED && p.out_f32 ? 4 : 2, o = r.out0 + (GATED ? 32 : 64) * quarter, left = max(0, p.d_out - o) * item;
+    const int item = !GATED && p.out_f32 ? 4 : 2, o = r.out0 + (GATED ? H : C) * share, left = (p.d_out - o) * item;
     char *to = static_cast<char *>(p.out) + ((size_t)(row0 + first) * p.d_out + o) * item;
     const size_t pitch = (size_t)p.d_out * item;
     constexpr int B = GP_PIECE<PAIR>;
     if (item == 4) {
 #pragma unroll
-        for (int c = 0; c < 256 / B; ++c) {
+        for (int c = 0; c < 4 * C / B; ++c) {
             uint4 v[B / 16];
 #pragma unroll
             for (int q = 0; q < B / 16; ++q) {
@@ -637,7 +703,7 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<PA
         }
     } else {
 #pragma unroll
-        for (int c = 0; c < (GATED ? 64 : 128) / B; ++c) {
+        for (int c = 0; c < 2 * (GATED ? H : C) / B; ++c) {
             uint4 v[B / 16];
 #pragma unroll
             for (int q = 0; q < B / 16; ++q) v[q] = bf16x8(acc + c * (B / 2) + 8 * q);
@@ -648,12 +714,13 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<PA
 }
 
 template <bool FP8, bool GATED, bool PAIR>
-__global__ void __launch_bounds__(GP_THREADS, 1)
+__global__ void __launch_bounds__(GP_THREADS<FP8>, 1)
 grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap few_map,
                const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap w2_map, const GroupedParams p)
 {
     extern __shared__ unsigned char gp_smem_raw[];
-    GroupedSmem<PAIR> &s = *reinterpret_cast<GroupedSmem<PAIR> *>((reinterpret_cast<uintptr_t>(gp_smem_raw) + 1023) & ~(uintptr_t)1023);
+    using Smem = GroupedSmem<FP8, PAIR>;
+    Smem &s = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(gp_smem_raw) + 1023) & ~(uintptr_t)1023);
     constexpr int STAGES = GP_STAGES<PAIR>;
     DIP_TRACE_MIN(p.tr, 0);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -677,7 +744,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.sum_full[i], 1);
-            mbar_init(&s.sum_empty[i], PAIR ? 2 * GP_OUT_WARPS : GP_OUT_WARPS);
+            mbar_init(&s.sum_empty[i], (PAIR ? 2 : 1) * GP_OUT_WARPS<FP8>);
         }
         mbar_init(&s.drained, 1);
         asm volatile("prefetch.tensormap [%0];" ::"l"(&rows_map) : "memory");
@@ -700,7 +767,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
     bool failed = false;
 
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(GP_REGS_FEW));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(GP_REGS_FEW<FP8>));
         if (warp == 0) {
             Run r;
             int g = 0;                               // steps so far
@@ -785,19 +852,19 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(GP_REGS_MANY));
-        const int quarter = (warp - 4) >> 2, place = (warp & 3) * 32 + lane;     // lane of tensor memory
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(GP_REGS_MANY<FP8>));
+        const int share = (warp - 4) >> 2, place = (warp & 3) * 32 + lane;     // lane of tensor memory
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         int n = 0;                                   // accumulators so far
         Run r;
         for (int i = 0; !failed && plan.get(i, r); ++i) {
             if constexpr (!PAIR) {
                 if (r.rows <= GP_FEW) {
-                    failed = !take_few<FP8, GATED>(p, s, plan, r, lanes, quarter, place, n);
+                    failed = !take_few<FP8, GATED>(p, s, plan, r, lanes, share, place, n);
                     continue;
                 }
             }
-            failed = !take_tile<FP8, GATED, PAIR>(p, s, plan, r, r.row0 + rank * GP_ROWS, min(GP_ROWS, r.rows - rank * GP_ROWS), lanes, quarter,
+            failed = !take_tile<FP8, GATED, PAIR>(p, s, plan, r, r.row0 + rank * GP_ROWS, min(GP_ROWS, r.rows - rank * GP_ROWS), lanes, share,
                                                   place, n);
         }
     }
@@ -847,13 +914,13 @@ cudaError_t launch(dip_ctx *ctx, int ctas, cudaStream_t stream, const CUtensorMa
 {
     static dip_per_device_once once;
     const auto kernel = grouped_kernel<FP8, GATED, PAIR>;
-    const size_t smem = sizeof(GroupedSmem<PAIR>) + 1024;
-    static_assert(sizeof(GroupedSmem<PAIR>) + 1024 <= 227 * 1024, "fits a CTA's shared memory");
+    const size_t smem = sizeof(GroupedSmem<FP8, PAIR>) + 1024;
+    static_assert(sizeof(GroupedSmem<FP8, PAIR>) + 1024 <= 227 * 1024, "fits a CTA's shared memory");
     const cudaError_t e = dip_raise_smem_limit(once, ctx->device, kernel, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
-    cfg.blockDim = dim3(GP_THREADS);
+    cfg.blockDim = dim3(GP_THREADS<FP8>);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
