@@ -12,7 +12,9 @@
 //          then has one output of a few rows instead of one row of 64 outputs, and what follows the last step takes as long as there
 //          are rows.
 //   warp 0      issues the copies: a ring of steps
-//   warp 1      issues the MMAs (N = 256, four per step) into one of two accumulators of 256 columns
+//   warp 1      issues the MMAs (N = 256, four per step) into one of two accumulators of 256 columns; GP_SPLIT: warps 1 and 2 those of
+//               a half each
+//   warp 3      FP8: brings the rows' scales, eight steps at a time, into a ring of their own
 //   the others  take the accumulators out: thread = row, and each four warps have a share of the columns
 // BF16: an accumulator is a tile, and the next tile's MMAs run while the first is taken out.  FP8: a step is a block of 128
 // input indices, which has scales of its own, so every step's accumulator is taken out and added, times row scale * weight
@@ -46,8 +48,13 @@ template <bool FP8> constexpr int GP_REGS_MANY = FP8 ? 224 : 104;
 constexpr int GP_TMEM_COLS = 512;
 constexpr int GP_MIN_STEPS = 4;                     // a part of a tile has at least so many
 constexpr int GP_JOIN_FEW = 8, GP_JOIN = 20;        // steps' worth of time that a cut tile's parts take to meet (few rows; others)
+constexpr int GP_SCALE_STEPS = 8, GP_SCALE_SLOTS = 4;   // steps of scales that come together, and how many such groups there is room for
 constexpr int GP_FEW = 64;                          // rows of a tile that are columns of its sums
 constexpr int GP_CHUNK = 12;                        // row tiles that go through an expert's weights together
+// 8-bit pairs make and take out a step's accumulator in halves, with a warp for each half's MMAs: one warp that waits for two halves and
+// issues both needs some 900 cycles a step, and the way from an MMA by its warps' registers back to the next MMA into the
+// same columns, across the pair, has two steps to fit into.  The halves read the rows twice: 80 KB of shared memory per step, 640 cycles.
+template <bool FP8, bool PAIR> constexpr bool GP_SPLIT = FP8 && PAIR;
 template <bool PAIR> constexpr int GP_STAGES = PAIR ? 5 : 4;
 template <bool PAIR> constexpr int GP_PIECE = PAIR ? 64 : 32;      // bytes of a row that leave together
 
@@ -69,6 +76,8 @@ struct GroupedPlan {
     int start[DIP_MAX_EXPERTS + 1];                 // first row of each expert
     int tiles[DIP_MAX_EXPERTS + 1];                 // row tiles in front of it
     int most;                                       // rows of the largest group
+    int whole;                                      // rounds of whole tiles
+    int units, parts;                               // steps of the tiles that are cut, blocks that share them
 };
 
 template <bool FP8, bool PAIR>
@@ -77,10 +86,14 @@ struct __align__(1024) GroupedSmem {
     unsigned char b[GP_STAGES<PAIR>][PAIR ? GP_B_BYTES / 2 : GP_B_BYTES];
     unsigned char out[GP_OUT_WARPS<FP8>][32 * GP_PIECE<PAIR>];
     uint64_t full[GP_STAGES<PAIR>], empty[GP_STAGES<PAIR>];        // a step's copies have landed; its MMAs have read them
-    uint64_t sum_full[2], sum_empty[2];             // an accumulator is complete; has been taken out
-    uint64_t drained;
+    uint64_t sum_full[2][2], sum_empty[2][2];       // an accumulator (GP_SPLIT: a half of it) is complete; has been taken out
+    uint64_t scale_full[GP_SCALE_SLOTS], scale_empty[GP_SCALE_SLOTS];
+    uint64_t drained[2];
+    float row_scale[FP8 ? GP_SCALE_SLOTS * GP_SCALE_STEPS : 1][FP8 ? GP_ROWS : 1];
+    float2 w_scale[GP_SCALE_SLOTS * GP_SCALE_STEPS];     // of a tile's two blocks of weights (gate/up: one of each)
     uint32_t tmem_base;
     int last;
+    int fail;
     float amax[4 * GP_ROWS];
     GroupedPlan plan;
 };
@@ -97,10 +110,48 @@ __device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, int 
                      ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
 }
 
+// Four bytes to shared memory, asynchronously.
+__device__ __forceinline__ void copy4(float *dst, const float *src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+
+// Whether the phase with the given parity is through (waits a little if it is not).
+__device__ __forceinline__ bool try_wait(uint32_t bar, unsigned parity)
+{
+    unsigned ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0u;
+}
+
 // A whole warp's bounded wait: all lanes go on alike.
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, unsigned parity, unsigned long long limit_ns)
 {
+    if (__all_sync(0xffffffffu, try_wait(smem_u32(bar), parity))) return true;
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit_ns));
+}
+
+// The same for those who go on in any case: once a wait has run out, s.fail says so to the others, and nothing waits any more.
+// (What a step costs these warps beside its arithmetic is what bounds 8-bit products; they have no control flow for failures.)
+template <typename Smem>
+__device__ __forceinline__ void wait_on(uint32_t bar, unsigned parity, Smem &s, int *status, unsigned long long limit_ns)
+{
+    if (!try_wait(bar, parity)) {
+        unsigned long long t0 = 0;
+        for (unsigned i = 1; !*(volatile int *)&s.fail && !try_wait(bar, parity); ++i) {
+            if (i & 63u) continue;
+            const unsigned long long now = dip_gtime();
+            if (t0 == 0) {
+                t0 = now;
+            } else if (now - t0 > limit_ns) {
+                *(volatile int *)&s.fail = 1;
+                atomicExch(status, 1);
+                break;
+            }
+        }
+    }
+    __syncwarp();
 }
 
 // One lane of a whole warp.  (A role's warp goes through its loop as a whole and elects a lane where it issues: with the loop in
@@ -149,15 +200,16 @@ __device__ __forceinline__ void grouped_commit(uint64_t *bar)
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
-// Arrives at the first block's barrier.
+// One lane of the warp arrives at the first block's barrier.  (Predicated: a branch and its way back together took 190 cycles.)
 template <bool PAIR>
-__device__ __forceinline__ void arrive_first(uint64_t *bar)
+__device__ __forceinline__ void arrive_first(uint32_t bar, int lane)
 {
     if (PAIR)
-        asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, 0;\n mbarrier.arrive.shared::cluster.b64 _, [r];\n}"
-                     ::"r"(smem_u32(bar)) : "memory");
+        asm volatile("{\n .reg .pred p;\n .reg .b32 r;\n setp.eq.s32 p, %1, 0;\n mapa.shared::cluster.u32 r, %0, 0;\n"
+                     " @p mbarrier.arrive.shared::cluster.b64 _, [r];\n}" ::"r"(bar), "r"(lane) : "memory");
     else
-        mbar_arrive(bar);
+        asm volatile("{\n .reg .pred p;\n setp.eq.s32 p, %1, 0;\n @p mbarrier.arrive.shared::cta.b64 _, [%0];\n}"
+                     ::"r"(bar), "r"(lane) : "memory");
 }
 
 __device__ __forceinline__ void pair_barrier()
@@ -216,17 +268,9 @@ __device__ __forceinline__ void fma2(float &a0, float &a1, uint32_t d0, uint32_t
         " mov.b64 {%0, %1}, a;\n}" : "+f"(a0), "+f"(a1) : "r"(d0), "r"(d1), "f"(s));
 }
 
-// Barriers of the warps that take sums out; the second also says to all of them alike whether any came with `v`.
+// Barrier of the warps that take sums out.
 template <bool FP8>
 __device__ __forceinline__ void out_barrier() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(GP_OUT_WARPS<FP8> * 32) : "memory"); }
-template <bool FP8>
-__device__ __forceinline__ bool out_barrier_any(bool v)
-{
-    unsigned any;
-    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n barrier.cta.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(any) : "r"((unsigned)v), "n"(GP_OUT_WARPS<FP8> * 32) : "memory");
-    return any != 0u;
-}
 
 // One run of steps of one tile.
 struct Run {
@@ -235,35 +279,29 @@ struct Run {
     int rest;                       // index among the tiles that are cut, -1: dealt out whole
 };
 
-// The runs of this block, in order.  Every role walks through them for itself.  (32 bits hold it all: at most 2^21 tiles, and
-// fewer than a block's worth of cut ones of at most 512 steps.)
+// The runs of this block, in order.  Every role walks through them for itself, and keeps nothing of this in registers meanwhile.
+// (32 bits hold it all: at most 2^21 tiles, and fewer than a block's worth of cut ones of at most 512 steps.)
 template <bool GATED, bool PAIR>
 struct Schedule {
     static constexpr int ROWS = PAIR ? 2 * GP_ROWS : GP_ROWS;
-    const GroupedPlan &s;
-    int n_experts, steps, n_cols;
-    int block, blocks;              // this block or pair, and how many there are
-    int whole;                      // rounds of whole tiles
-    int units, parts;               // steps of the tiles that are cut, blocks that share them
-    int at, end;                    // this block's units
+    const GroupedParams &p;
+    volatile GroupedPlan &s;
 
-    __device__ __forceinline__ Schedule(const GroupedPlan &plan, const GroupedParams &p)
-        : s(plan), n_experts(p.n_experts), steps(p.steps), n_cols(p.n_cols), block(PAIR ? blockIdx.x >> 1 : blockIdx.x),
-          blocks(PAIR ? gridDim.x >> 1 : gridDim.x)
+    __device__ __forceinline__ int block() const { return PAIR ? blockIdx.x >> 1 : blockIdx.x; }
+    __device__ __forceinline__ int blocks() const { return PAIR ? gridDim.x >> 1 : gridDim.x; }
+    // by one thread, once the experts' rows and tiles are known
+    __device__ __forceinline__ void divide() const
     {
-        const int tiles = s.tiles[n_experts] * n_cols;
-        whole = tiles / blocks;
-        const int rest = tiles - whole * blocks;
-        units = rest * steps;
-        parts = min(blocks, max(units / GP_MIN_STEPS, rest));
-        if (parts > rest && units / parts + (s.most <= GP_FEW ? GP_JOIN_FEW : GP_JOIN) >= steps) parts = rest;      // (they stay whole)
-        const bool mine = block < parts;
-        at = mine ? units * block / parts : 0;
-        end = mine ? units * (block + 1) / parts : 0;
+        const int tiles = s.tiles[p.n_experts] * p.n_cols, whole = tiles / blocks(), rest = tiles - whole * blocks(), units = rest * p.steps;
+        int parts = min(blocks(), max(units / GP_MIN_STEPS, rest));
+        if (parts > rest && units / parts + (s.most <= GP_FEW ? GP_JOIN_FEW : GP_JOIN) >= p.steps) parts = rest;      // (they stay whole)
+        s.whole = whole;
+        s.units = units;
+        s.parts = parts;
     }
     // the block that has a unit, and which of its runs is the one in cut tile `rest`
-    __device__ __forceinline__ int block_of(int unit) const { return ((unit + 1) * parts - 1) / units; }
-    __device__ __forceinline__ int run_of(int b, int rest) const { return units * b / parts / steps == rest ? 0 : 1; }
+    __device__ __forceinline__ int block_of(int unit) const { return ((unit + 1) * s.parts - 1) / s.units; }
+    __device__ __forceinline__ int run_of(int b, int rest) const { return s.units * b / s.parts / p.steps == rest ? 0 : 1; }
     // where block b (of this one's kind in its pair) leaves its part of the cut tile, in floats
     __device__ __forceinline__ size_t part_at(int b, int rest) const
     {
@@ -272,17 +310,17 @@ struct Schedule {
 
     __device__ __forceinline__ void locate(int tile, Run &r) const
     {
-        int lo = 0, hi = n_experts;             // the expert with tiles[e] * n_cols <= tile < tiles[e + 1] * n_cols
+        int lo = 0, hi = p.n_experts;             // the expert with tiles[e] * p.n_cols <= tile < tiles[e + 1] * p.n_cols
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (s.tiles[mid] * n_cols <= tile) lo = mid;
+            if (s.tiles[mid] * p.n_cols <= tile) lo = mid;
             else hi = mid;
         }
         const int n_rows = s.start[lo + 1] - s.start[lo], row_tiles = s.tiles[lo + 1] - s.tiles[lo];
-        int in = tile - s.tiles[lo] * n_cols, m = 0, here = row_tiles;
+        int in = tile - s.tiles[lo] * p.n_cols, m = 0, here = row_tiles;
         if (row_tiles > GP_CHUNK) {
-            m = in / (GP_CHUNK * n_cols) * GP_CHUNK;
-            in -= m * n_cols;
+            m = in / (GP_CHUNK * p.n_cols) * GP_CHUNK;
+            in -= m * p.n_cols;
             here = min(GP_CHUNK, row_tiles - m);
         }
         const int col = here == 1 ? in : in / here;
@@ -294,18 +332,22 @@ struct Schedule {
     }
     __device__ __forceinline__ bool get(int i, Run &r) const
     {
+        const int whole = s.whole;
         r.rest = -1;
         r.k0 = 0;
-        r.k1 = steps;
-        int tile = i * blocks + block;
+        r.k1 = p.steps;
+        int tile = i * blocks() + block();
         if (i >= whole) {
-            int u = at;
-            for (i -= whole; i > 0 && u < end; --i) u = min(end, (u / steps + 1) * steps);
+            const int units = s.units, parts = s.parts;
+            if (block() >= parts) return false;
+            int u = units * block() / parts;
+            const int end = units * (block() + 1) / parts;
+            for (i -= whole; i > 0 && u < end; --i) u = min(end, (u / p.steps + 1) * p.steps);
             if (u >= end) return false;
-            r.rest = u / steps;
-            r.k0 = u - r.rest * steps;
-            r.k1 = min(steps, r.k0 + (end - u));
-            tile = whole * blocks + r.rest;
+            r.rest = u / p.steps;
+            r.k0 = u - r.rest * p.steps;
+            r.k1 = min(p.steps, r.k0 + (end - u));
+            tile = whole * blocks() + r.rest;
         }
         locate(tile, r);
         return true;
@@ -370,11 +412,11 @@ __device__ __forceinline__ bool part_is_last(const GroupedParams &p, GroupedSmem
     return s.last != 0;
 }
 
-// The sums of a tile of few rows and what becomes of them: thread = output, values = rows.  False: a wait ran out.
+// The sums of a tile of few rows and what becomes of them: thread = output, values = rows.
 // Each four warps have a share of the rows; plain: the first or the second 128 outputs of a share; gate/up: a thread has gate and up of
 // its output.
 template <bool FP8, bool GATED>
-__device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<FP8, false> &s, const Schedule<GATED, false> &plan, const Run &r,
+__device__ __forceinline__ void take_few(const GroupedParams &p, GroupedSmem<FP8, false> &s, const Schedule<GATED, false> &plan, const Run &r,
                                          uint32_t lanes, int share, int place, int &n)
 {
     constexpr int SHARES = GP_OUT_WARPS<FP8> / (GATED ? 4 : 8), N = GP_FEW / SHARES;         // rows of a thread: at most N
@@ -384,7 +426,6 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<FP8
     const uint32_t sums = lanes + side + t0;
     const int in_blocks = (p.d_in + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK, out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
     float a[N], u[GATED ? N : 1];
-    bool ok = true;
     if (FP8) {
 #pragma unroll
         for (int j = 0; j < N; ++j) a[j] = 0.f;
@@ -407,10 +448,7 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<FP8
                 if (GATED) next_u = __ldg(us + k + 1);
             }
             const int buf = n & 1;
-            if (!warp_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns)) {
-                ok = false;
-                break;
-            }
+            wait_on(smem_u32(&s.sum_full[buf][0]), (n / 2) & 1, s, p.status, p.wait_limit_ns);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
             for (int c = 0; c < N / 8; ++c)
@@ -431,11 +469,11 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<FP8
                 }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
+            if (lane == 0) mbar_arrive(&s.sum_empty[buf][0]);
         }
     } else {
         const int buf = n & 1;
-        ok = warp_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns);
+        wait_on(smem_u32(&s.sum_full[buf][0]), (n / 2) & 1, s, p.status, p.wait_limit_ns);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
         for (int c = 0; c < N / 8; ++c)
@@ -455,16 +493,14 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<FP8
             }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s.sum_empty[buf]);
+        if (lane == 0) mbar_arrive(&s.sum_empty[buf][0]);
         ++n;
     }
-    // (a wait of one warp that runs out takes the others along: they meet at barriers below)
-    if (out_barrier_any<FP8>(!ok)) return false;
 
     if (r.k1 - r.k0 < p.steps) {
         // a part of the tile: the last of its blocks goes on with the sum of all.  Parts are [row][256 sums]
         const size_t mine = (size_t)t0 * GP_COLS + side + place;
-        float *to = p.partials + plan.part_at(plan.block, r.rest) + mine;
+        float *to = p.partials + plan.part_at(plan.block(), r.rest) + mine;
 #pragma unroll
         for (int c = 0; c < N / 8; ++c)
             if (8 * c < rows) {
@@ -476,7 +512,7 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<FP8
                     }
             }
         int b0, b1;
-        if (!part_is_last(p, s, plan, r, b0, b1)) return true;
+        if (!part_is_last(p, s, plan, r, b0, b1)) return;
 #pragma unroll
         for (int j = 0; j < N; ++j) a[j] = 0.f;
         if (GATED) {
@@ -533,7 +569,6 @@ __device__ __forceinline__ bool take_few(const GroupedParams &p, GroupedSmem<FP8
                 }
         }
     if (GATED && FP8) out_barrier<FP8>();                 // (before the next tile's maxima)
-    return true;
 }
 
 // A piece of this warp's 32 rows leaves by way of shared memory: each thread brings GP_PIECE bytes of its row, and the warp writes
@@ -556,60 +591,64 @@ __device__ __forceinline__ void leave(unsigned char *stage, const uint4 *v, char
     }
 }
 
-// The sums of any other tile: thread = row, values = its share of the columns (gate/up: half of them gate, the others the up beside
-// them).  row0, rows: this block's rows of the tile (may be none).
+// The sums of any other tile: thread = row, values = its share of the columns, in two groups: H from the tile's output first on and H from
+// second on (gate/up: gate, and the up of the same outputs).  row0, rows: this block's rows of the tile (may be none).
 template <bool FP8, bool GATED, bool PAIR>
-__device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<FP8, PAIR> &s, const Schedule<GATED, PAIR> &plan, const Run &r,
-                                          int row0, int rows, uint32_t lanes, int share, int row, int &n)
+__device__ __forceinline__ void take_tile(const GroupedParams &p, GroupedSmem<FP8, PAIR> &s, const Schedule<GATED, PAIR> &plan, const Run &r,
+                                          int row0, int rows, uint32_t lanes, int share, int row, int &n, int &groups)
 {
     constexpr int SHARES = GP_OUT_WARPS<FP8> / 4, C = GP_COLS / SHARES, H = C / 2;
+    // the groups' columns; halves of a pair's accumulator have the first (second) half of both blocks' weights
+    constexpr bool SPLIT = GP_SPLIT<FP8, PAIR>;
     const int lane = threadIdx.x & 31;
-    const int col0 = GATED ? H * share : C * share, col1 = GATED ? GP_COLS / 2 + col0 : col0 + H;      // H columns from each
-    const int in_blocks = (p.d_in + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK, out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
+    const int first = GATED || SPLIT ? H * share : C * share, second = GATED ? first : SPLIT ? GP_COLS / 2 + first : first + H;
+    const int col0 = SPLIT ? C * share : first, col1 = GATED && !SPLIT ? GP_COLS / 2 + col0 : col0 + H;
+    const int out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
     float acc[C];
-    bool ok = true;
     if constexpr (FP8) {
 #pragma unroll
         for (int j = 0; j < C; ++j) acc[j] = 0.f;
-        const float *xs = p.row_scales + (size_t)max(0, min(row0 + row, r.row0 + r.rows - 1)) * in_blocks;
-        const size_t at = ((size_t)r.expert * out_blocks + min((r.out0 + (GATED ? 0 : col0)) / DIP_FP8_BLOCK, out_blocks - 1)) * in_blocks;
-        const float *ws = p.w_scales + at, *us = GATED ? p.up_scales + at : ws;
-        float next_x = __ldg(xs + r.k0), next_w = __ldg(ws + r.k0), next_u = __ldg(us + r.k0);
-        for (int k = r.k0; k < r.k1; ++k, ++n) {
-            const float s0 = next_x * next_w, s1 = GATED ? next_x * next_u : s0;
-            if (k + 1 < r.k1) {                      // (asked for a step ahead)
-                next_x = __ldg(xs + k + 1);
-                next_w = __ldg(ws + k + 1);
-                if (GATED) next_u = __ldg(us + k + 1);
-            }
-            const int buf = n & 1;
-            if (!warp_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns)) {
-                ok = false;
-                break;
-            }
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            // one load of 32 columns is under way while the one in front is added
-            uint32_t v[2][32];
-            tmem_ld(lanes + buf * GP_COLS + col0, v[0]);
-            tmem_wait(v[0]);
+        // (which of the tile's two blocks of weights a group of columns belongs to)
+        const bool block0 = !GATED && !SPLIT && share == 1, block1 = GATED || SPLIT || share == 1;
+        const uint32_t full = smem_u32(&s.sum_full[0][SPLIT ? share : 0]), empty = smem_u32(&s.sum_empty[0][SPLIT ? share : 0]);
+        constexpr uint32_t NEXT = sizeof(s.sum_full[0]);             // from one accumulator's barrier to the other's
+        for (int left = r.k1 - r.k0; left > 0; left -= GP_SCALE_STEPS, ++groups) {
+            const int slot = groups % GP_SCALE_SLOTS;
+            wait_on(smem_u32(&s.scale_full[slot]), (groups / GP_SCALE_SLOTS) & 1, s, p.status, p.wait_limit_ns);
+            const float *xs = &s.row_scale[slot * GP_SCALE_STEPS][row];
+            const float2 *ws = &s.w_scale[slot * GP_SCALE_STEPS];
+            const int end = n + min(left, GP_SCALE_STEPS);
+            for (; n < end; ++n, xs += GP_ROWS, ++ws) {
+                const float x = *xs;
+                const float2 w = *ws;
+                const float s0 = x * (block0 ? w.y : w.x), s1 = x * (block1 ? w.y : w.x);
+                const int buf = n & 1;
+                wait_on(full + buf * NEXT, (n >> 1) & 1, s, p.status, p.wait_limit_ns);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                // one load is under way while the one in front is added
+                const uint32_t from = lanes + buf * GP_COLS;
+                uint32_t v[2][32];
+                tmem_ld(from + col0, v[0]);
 #pragma unroll
-            for (int c = 0; c < C / 32; ++c) {
-                if (c + 1 < C / 32) {
-                    tmem_ld(lanes + buf * GP_COLS + (32 * (c + 1) < H ? col0 + 32 * (c + 1) : col1 + 32 * (c + 1) - H), v[(c + 1) & 1]);
-                } else {                             // all of it is in registers
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) arrive_first<PAIR>(&s.sum_empty[buf]);
+                for (int c = 0; c < C / 32; ++c) {
+                    tmem_wait(v[c & 1]);
+                    if (c + 1 < C / 32) {
+                        tmem_ld(from + (32 * (c + 1) < H ? col0 + 32 * (c + 1) : col1 + 32 * (c + 1) - H), v[(c + 1) & 1]);
+                    } else {                         // all of it is in registers
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        arrive_first<PAIR>(empty + buf * NEXT, lane);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) fma2(acc[32 * c + j], acc[32 * c + j + 1], v[c & 1][j], v[c & 1][j + 1], 32 * c < H ? s0 : s1);
                 }
-#pragma unroll
-                for (int j = 0; j < 32; j += 2)
-                    fma2(acc[32 * c + j], acc[32 * c + j + 1], v[c & 1][j], v[c & 1][j + 1], 32 * c < H ? s0 : s1);
-                if (c + 1 < C / 32) tmem_wait(v[(c + 1) & 1]);
             }
+            __syncwarp();
+            arrive_first<false>(smem_u32(&s.scale_empty[slot]), lane);
         }
     } else {
         const int buf = n & 1;
-        ok = warp_wait(&s.sum_full[buf], (n / 2) & 1, p.wait_limit_ns);
+        wait_on(smem_u32(&s.sum_full[buf][0]), (n / 2) & 1, s, p.status, p.wait_limit_ns);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
         for (int c = 0; c < C / 16; ++c) {
@@ -621,21 +660,20 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<FP
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (lane == 0) arrive_first<PAIR>(&s.sum_empty[buf]);
+        arrive_first<PAIR>(smem_u32(&s.sum_empty[buf][0]), lane);
         ++n;
     }
-    if (out_barrier_any<FP8>(!ok)) return false;
 
     if (r.k1 - r.k0 < p.steps) {
         // parts are [share][column / 4][row][4]
         const size_t mine = (size_t)share * (C / 4) * GP_ROWS + row;
-        float4 *to = reinterpret_cast<float4 *>(p.partials + plan.part_at(plan.block, r.rest)) + mine;
+        float4 *to = reinterpret_cast<float4 *>(p.partials + plan.part_at(plan.block(), r.rest)) + mine;
         if (row < rows) {
 #pragma unroll
             for (int j = 0; j < C / 4; ++j) to[j * GP_ROWS] = make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
         }
         int b0, b1;
-        if (!part_is_last(p, s, plan, r, b0, b1)) return true;
+        if (!part_is_last(p, s, plan, r, b0, b1)) return;
 #pragma unroll
         for (int j = 0; j < C; ++j) acc[j] = 0.f;
         if (row < rows) {
@@ -653,10 +691,10 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<FP
         }
     }
 
-    const int first = row & ~31, n_here = rows - first;              // this warp's rows
+    const int warp_row = row & ~31, n_here = rows - warp_row;        // this warp's rows
     unsigned char *stage = s.out[(threadIdx.x >> 5) - 4];
     if (GATED) {
-        const int o = r.out0 + H * share;
+        const int o = r.out0 + first;
 #pragma unroll
         for (int j = 0; j < H; ++j) acc[j] = silu_f32(acc[j]) * acc[H + j];
         if (FP8) {
@@ -669,7 +707,7 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<FP
             out_barrier<FP8>();
             const float scale = fp8_scale(fmaxf(most, s.amax[(share ^ 1) * GP_ROWS + row]));
             if (row < rows && share == 0) p.out_scales[(size_t)(row0 + row) * out_blocks + r.out0 / DIP_FP8_BLOCK] = scale;
-            char *to = static_cast<char *>(p.out) + (size_t)(row0 + first) * p.d_out + o;
+            char *to = static_cast<char *>(p.out) + (size_t)(row0 + warp_row) * p.d_out + o;
             constexpr int B = GP_PIECE<PAIR>;
 #pragma unroll
             for (int c = 0; c < H / B; ++c) {
@@ -683,34 +721,37 @@ __device__ __forceinline__ bool take_tile(const GroupedParams &p, GroupedSmem<FP
                 leave<PAIR>(stage, v, to + c * B, p.d_out, n_here, p.d_out - o - c * B);
             }
             out_barrier<FP8>();                      // (before the next tile's maxima)
-            return true;
+            return;
         }
     }
-    const int item = !GATED && p.out_f32 ? 4 : 2, o = r.out0 + (GATED ? H : C) * share, left = (p.d_out - o) * item;
-    char *to = static_cast<char *>(p.out) + ((size_t)(row0 + first) * p.d_out + o) * item;
+    const int item = !GATED && p.out_f32 ? 4 : 2;
     const size_t pitch = (size_t)p.d_out * item;
+    char *to = static_cast<char *>(p.out) + ((size_t)(row0 + warp_row) * p.d_out + r.out0) * item;
     constexpr int B = GP_PIECE<PAIR>;
-    if (item == 4) {
 #pragma unroll
-        for (int c = 0; c < 4 * C / B; ++c) {
-            uint4 v[B / 16];
+    for (int g = 0; g < (GATED ? 1 : 2); ++g) {
+        const int o = g ? second : first, left = (p.d_out - r.out0 - o) * item;
+        if (item == 4) {
 #pragma unroll
-            for (int q = 0; q < B / 16; ++q) {
-                const float *f = acc + c * (B / 4) + 4 * q;
-                v[q] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+            for (int c = 0; c < 4 * H / B; ++c) {
+                uint4 v[B / 16];
+#pragma unroll
+                for (int q = 0; q < B / 16; ++q) {
+                    const float *f = acc + g * H + c * (B / 4) + 4 * q;
+                    v[q] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                }
+                leave<PAIR>(stage, v, to + o * 4 + c * B, pitch, n_here, left - c * B);
             }
-            leave<PAIR>(stage, v, to + c * B, pitch, n_here, left - c * B);
-        }
-    } else {
+        } else {
 #pragma unroll
-        for (int c = 0; c < 2 * (GATED ? H : C) / B; ++c) {
-            uint4 v[B / 16];
+            for (int c = 0; c < 2 * H / B; ++c) {
+                uint4 v[B / 16];
 #pragma unroll
-            for (int q = 0; q < B / 16; ++q) v[q] = bf16x8(acc + c * (B / 2) + 8 * q);
-            leave<PAIR>(stage, v, to + c * B, pitch, n_here, left - c * B);
+                for (int q = 0; q < B / 16; ++q) v[q] = bf16x8(acc + g * H + c * (B / 2) + 8 * q);
+                leave<PAIR>(stage, v, to + o * 2 + c * B, pitch, n_here, left - c * B);
+            }
         }
     }
-    return true;
 }
 
 template <bool FP8, bool GATED, bool PAIR>
@@ -740,13 +781,19 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
     if (tid == 0) {
         for (int i = 0; i < STAGES; ++i) {
             mbar_init(&s.full[i], 1);
-            mbar_init(&s.empty[i], 1);
+            mbar_init(&s.empty[i], GP_SPLIT<FP8, PAIR> ? 2 : 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&s.sum_full[i], 1);
-            mbar_init(&s.sum_empty[i], (PAIR ? 2 : 1) * GP_OUT_WARPS<FP8>);
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&s.sum_full[i >> 1][i & 1], 1);
+            mbar_init(&s.sum_empty[i >> 1][i & 1], (PAIR ? 2 : 1) * GP_OUT_WARPS<FP8> / (GP_SPLIT<FP8, PAIR> ? 2 : 1));
         }
-        mbar_init(&s.drained, 1);
+        for (int i = 0; i < GP_SCALE_SLOTS; ++i) {
+            mbar_init(&s.scale_full[i], 32);
+            mbar_init(&s.scale_empty[i], GP_OUT_WARPS<FP8>);
+        }
+        mbar_init(&s.drained[0], 1);
+        mbar_init(&s.drained[1], 1);
+        s.fail = 0;
         asm volatile("prefetch.tensormap [%0];" ::"l"(&rows_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&few_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
@@ -755,14 +802,18 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
     }
     dip_grid_dependency_wait();                      // rows and offsets come from the kernels in front
     DIP_TRACE_MIN(p.tr, 1);
-    if (warp == 0) grouped_plan(p, Schedule<GATED, PAIR>::ROWS, s.plan);
+    const Schedule<GATED, PAIR> plan = {p, s.plan};
+    if (warp == 0) {
+        grouped_plan(p, plan.ROWS, s.plan);
+        __syncwarp();
+        if (lane == 0) plan.divide();
+    }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (PAIR) pair_barrier();                        // (the other block's barriers are set up)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     dip_launch_dependents();
     const uint32_t tmem = s.tmem_base;
-    const Schedule<GATED, PAIR> plan(s.plan, p);
     constexpr int PER_STEP = FP8 ? GP_STEP_BYTES : GP_STEP_BYTES / 2;
     bool failed = false;
 
@@ -808,23 +859,56 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
             // (given up: no copy of this block's is under way when it leaves; the second block's count at the first one's barriers)
             if (failed && rank == 0)
                 for (int j = max(0, g - STAGES); j < g; ++j) warp_wait(&s.full[j % STAGES], (j / STAGES) & 1, p.wait_limit_ns);
-        } else if (warp == 1 && rank == 0) {
+        } else if (FP8 && warp == 3) {
+            // four rows a lane; the first lanes the weights' scales
+            const int out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
+            Run r;
+            int g = 0;                               // groups so far
+            for (int i = 0; !failed && plan.get(i, r); ++i) {
+                if (!PAIR && r.rows <= GP_FEW) continue;
+                const int last_row = r.row0 + r.rows - 1, ob = r.out0 / DIP_FP8_BLOCK + (GATED ? 0 : lane & 1);
+                const float *x[4];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) x[m] = p.row_scales + (size_t)min(r.row0 + rank * GP_ROWS + 32 * m + lane, last_row) * p.steps;
+                const float *ws = (GATED && (lane & 1) ? p.up_scales : p.w_scales) + ((size_t)r.expert * out_blocks + min(ob, out_blocks - 1)) * p.steps;
+                for (int k0 = r.k0; k0 < r.k1; k0 += GP_SCALE_STEPS, ++g) {
+                    const int slot = g % GP_SCALE_SLOTS;
+                    if (g >= GP_SCALE_SLOTS && !warp_wait(&s.scale_empty[slot], (g / GP_SCALE_SLOTS - 1) & 1, p.wait_limit_ns)) {
+                        failed = true;
+                        break;
+                    }
+#pragma unroll
+                    for (int q = 0; q < GP_SCALE_STEPS; ++q) {
+                        const int k = min(k0 + q, r.k1 - 1);
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) copy4(&s.row_scale[slot * GP_SCALE_STEPS + q][32 * m + lane], x[m] + k);
+                    }
+                    if (lane < 2 * GP_SCALE_STEPS)
+                        copy4(reinterpret_cast<float *>(s.w_scale) + slot * 2 * GP_SCALE_STEPS + lane, ws + min(k0 + (lane >> 1), r.k1 - 1));
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&s.scale_full[slot])) : "memory");
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+        } else if ((warp == 1 || (GP_SPLIT<FP8, PAIR> && warp == 2)) && rank == 0) {
+            constexpr bool SPLIT = GP_SPLIT<FP8, PAIR>;
+            const int half = warp - 1;
             Run r;
             int g = 0, n = 0;                        // steps, accumulators so far
             for (int i = 0; !failed && plan.get(i, r); ++i) {
                 const bool few = !PAIR && r.rows <= GP_FEW;
-                const uint32_t shape = grouped_shape<FP8, PAIR>(few ? (r.rows + 15) / 16 * 16 : GP_COLS);
+                const uint32_t shape = grouped_shape<FP8, PAIR>(few ? (r.rows + 15) / 16 * 16 : SPLIT ? GP_COLS / 2 : GP_COLS);
                 for (int k = r.k0; k < r.k1; ++k, ++g) {
                     const int st = g % STAGES, buf = n & 1;
                     const bool first = FP8 || k == r.k0, last = FP8 || k == r.k1 - 1;
-                    if ((first && n >= 2 && !warp_wait(&s.sum_empty[buf], (n / 2 - 1) & 1, p.wait_limit_ns)) ||
+                    if ((first && n >= 2 && !warp_wait(&s.sum_empty[buf][half], (n / 2 - 1) & 1, p.wait_limit_ns)) ||
                         !warp_wait(&s.full[st], (g / STAGES) & 1, p.wait_limit_ns)) {
                         failed = true;
                         break;
                     }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t a = operand_desc(s.a[st]), b = operand_desc(s.b[st]);
-                    const uint32_t to = tmem + buf * GP_COLS;
+                    // a half of N = 128 is 64 rows of each block's weights
+                    const uint64_t a = operand_desc(s.a[st]), b = operand_desc(s.b[st]) + (SPLIT ? half * (64 * GP_STEP_BYTES >> 4) : 0);
+                    const uint32_t to = tmem + buf * GP_COLS + (SPLIT ? half * (GP_COLS / 2) : 0);
                     if (elect_one()) {
                         if (!few) {
 #pragma unroll
@@ -839,36 +923,39 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
                             }
                         }
                         grouped_commit<PAIR>(&s.empty[st]);
-                        if (last) grouped_commit<PAIR>(&s.sum_full[buf]);
+                        if (last) grouped_commit<PAIR>(&s.sum_full[buf][half]);
                     }
                     __syncwarp();
                     if (last) ++n;
                 }
             }
             if (failed) {
-                if (elect_one()) grouped_commit<PAIR>(&s.drained);
+                if (elect_one()) grouped_commit<PAIR>(&s.drained[half]);
                 __syncwarp();
-                warp_wait(&s.drained, 0, p.wait_limit_ns);
+                warp_wait(&s.drained[half], 0, p.wait_limit_ns);
             }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(GP_REGS_MANY<FP8>));
         const int share = (warp - 4) >> 2, place = (warp & 3) * 32 + lane;     // lane of tensor memory
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        int n = 0;                                   // accumulators so far
+        int n = 0, groups = 0;                       // accumulators, groups of scales so far
         Run r;
-        for (int i = 0; !failed && plan.get(i, r); ++i) {
+        for (int i = 0; plan.get(i, r); ++i) {
             if constexpr (!PAIR) {
                 if (r.rows <= GP_FEW) {
-                    failed = !take_few<FP8, GATED>(p, s, plan, r, lanes, share, place, n);
+                    take_few<FP8, GATED>(p, s, plan, r, lanes, share, place, n);
                     continue;
                 }
             }
-            failed = !take_tile<FP8, GATED, PAIR>(p, s, plan, r, r.row0 + rank * GP_ROWS, min(GP_ROWS, r.rows - rank * GP_ROWS), lanes, share,
-                                                  place, n);
+            take_tile<FP8, GATED, PAIR>(p, s, plan, r, r.row0 + rank * GP_ROWS, min(GP_ROWS, r.rows - rank * GP_ROWS), lanes, share, place, n,
+                                         groups);
         }
     }
-    if (failed) atomicExch(p.status, 1);
+    if (failed) {
+        *(volatile int *)&s.fail = 1;
+        atomicExch(p.status, 1);
+    }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (PAIR) pair_barrier();                        // (the first block's MMAs have read this block's memory, all has arrived at its barriers)
