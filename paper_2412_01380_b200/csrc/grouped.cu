@@ -7,12 +7,12 @@
 //   PAIR   two blocks of a cluster share a tile of 256 rows: each loads its 128 rows and half of the weights, and the first one's
 //          MMAs (cta_group::2, M = 256) read both halves.  Per step and SM 32 KB come in and 32 KB are read, which shared
 //          memory does in the 512 cycles that the MMAs take.  (Alone it is 48 and 48 KB: 768 cycles, measured 785.)
-//   single a block by itself.  A tile of at most GP_FEW rows changes the operands' roles: the weights are the M side (two MMAs of
-//          128) and the rows the N side, as many columns as there are rows (in sixteens).  The loads are the same, but a thread
-//          then has one output of a few rows instead of one row of 64 outputs, and what follows the last step takes as long as there
-//          are rows.
+//   whole  a block by itself.
+//   few    the same for groups of few rows, tiles of at most 64: the operands change their roles.  The weights are the M side (two
+//          MMAs of 128) and the rows the N side, as many columns as there are rows (in sixteens).  The loads are alike, but a thread then
+//          has one output of a few rows instead of one row of 64 outputs, and what follows the last step takes as long as there are rows.
 //   warp 0      issues the copies: a ring of steps
-//   warp 1      issues the MMAs (N = 256, four per step) into one of two accumulators of 256 columns; GP_SPLIT: warps 1 and 2 those of
+//   warp 1      issues the MMAs (N = 256, four per step) into one of two accumulators of 256 columns; SPLIT: warps 1 and 2 those of
 //               a half each
 //   warp 3      FP8: brings the rows' scales, eight steps at a time, into a ring of their own
 //   the others  take the accumulators out: thread = row, and each four warps have a share of the columns
@@ -37,26 +37,31 @@ constexpr int GP_ROWS = DIP_GROUP_ROWS, GP_COLS = DIP_GROUP_COLS;
 constexpr int GP_STEP_BYTES = 128;                  // of a row, per step
 constexpr int GP_BOX = 32;                          // rows per copy of the rows of a tile of few
 constexpr int GP_A_BYTES = GP_ROWS * GP_STEP_BYTES, GP_B_BYTES = GP_COLS * GP_STEP_BYTES;
-// Warps that take sums out.  FP8 keeps a tile's sums in registers over all steps, and two warps per scheduler with 128 of them each
-// can have two loads of 32 accumulator columns in hand; BF16 only has to get rid of a tile.
-template <bool FP8> constexpr int GP_OUT_WARPS = FP8 ? 8 : 16;
-template <bool FP8> constexpr int GP_THREADS = (4 + GP_OUT_WARPS<FP8>) * 32;
-// registers of a thread of the first four warps and of the others; in all what the launch has: (56 + 2 * 224) / 3 = 168 each, or
-// (64 + 4 * 104) / 5 = 96
-template <bool FP8> constexpr int GP_REGS_FEW = FP8 ? 56 : 64;
-template <bool FP8> constexpr int GP_REGS_MANY = FP8 ? 224 : 104;
 constexpr int GP_TMEM_COLS = 512;
 constexpr int GP_MIN_STEPS = 4;                     // a part of a tile has at least so many
 constexpr int GP_JOIN_FEW = 8, GP_JOIN = 20;        // steps' worth of time that a cut tile's parts take to meet (few rows; others)
 constexpr int GP_SCALE_STEPS = 8, GP_SCALE_SLOTS = 4;   // steps of scales that come together, and how many such groups there is room for
 constexpr int GP_FEW = 64;                          // rows of a tile that are columns of its sums
 constexpr int GP_CHUNK = 12;                        // row tiles that go through an expert's weights together
-// 8-bit pairs make and take out a step's accumulator in halves, with a warp for each half's MMAs: one warp that waits for two halves and
-// issues both needs some 900 cycles a step, and the way from an MMA by its warps' registers back to the next MMA into the
-// same columns, across the pair, has two steps to fit into.  The halves read the rows twice: 80 KB of shared memory per step, 640 cycles.
-template <bool FP8, bool PAIR> constexpr bool GP_SPLIT = FP8 && PAIR;
-template <bool PAIR> constexpr int GP_STAGES = PAIR ? 5 : 4;
-template <bool PAIR> constexpr int GP_PIECE = PAIR ? 64 : 32;      // bytes of a row that leave together
+enum { GP_FEW_ROWS, GP_WHOLE, GP_PAIR };            // see above
+template <bool FP8_, bool GATED_, int MODE> struct Kind {
+    static constexpr bool FP8 = FP8_, GATED = GATED_, PAIR = MODE == GP_PAIR, FEW = MODE == GP_FEW_ROWS;
+    static constexpr int TILE_ROWS = PAIR ? 2 * GP_ROWS : FEW ? GP_FEW : GP_ROWS;
+    static constexpr int A_BYTES = (FEW ? GP_FEW : GP_ROWS) * GP_STEP_BYTES, B_BYTES = PAIR ? GP_B_BYTES / 2 : GP_B_BYTES;
+    static constexpr int STAGES = PAIR || FEW ? 5 : 4;
+    static constexpr int PIECE = PAIR ? 64 : 32;     // bytes of a row that leave together
+    // 8-bit pairs make and take out a step's accumulator in halves, with a warp for each half's MMAs: one warp that waits for two halves
+    // and issues both needs some 900 cycles a step, and the way from an MMA by its warps' registers back to the next MMA into the
+    // same columns, across the pair, has two steps to fit into.  The halves read the rows twice: 80 KB of shared memory per step, 640
+    // cycles.
+    static constexpr bool SPLIT = FP8 && PAIR;
+    // Warps that take sums out.  FP8 keeps a tile's sums in registers over all steps, and two warps per scheduler with 128 of them
+    // each can have two loads of 32 accumulator columns in hand; BF16 only has to get rid of a tile.
+    static constexpr int OUT_WARPS = FP8 || FEW ? 8 : 16, THREADS = (4 + OUT_WARPS) * 32;
+    // registers of a thread of the first four warps and of the others; in all what the launch has: (56 + 2 * 224) / 3 = (40 + 2 * 232) / 3 = 168 each, or
+    // (64 + 4 * 104) / 5 = 96
+    static constexpr int REGS_FEW = FP8 ? (PAIR ? 56 : 40) : 64, REGS_MANY = FP8 ? (PAIR ? 224 : 232) : 104;
+};
 
 struct GroupedParams {
     const float *w_scales, *up_scales, *row_scales;
@@ -75,21 +80,21 @@ struct GroupedParams {
 struct GroupedPlan {
     int start[DIP_MAX_EXPERTS + 1];                 // first row of each expert
     int tiles[DIP_MAX_EXPERTS + 1];                 // row tiles in front of it
-    int most;                                       // rows of the largest group
     int whole;                                      // rounds of whole tiles
     int units, parts;                               // steps of the tiles that are cut, blocks that share them
 };
 
-template <bool FP8, bool PAIR>
+template <class K>
 struct __align__(1024) GroupedSmem {
-    unsigned char a[GP_STAGES<PAIR>][GP_A_BYTES];
-    unsigned char b[GP_STAGES<PAIR>][PAIR ? GP_B_BYTES / 2 : GP_B_BYTES];
-    unsigned char out[GP_OUT_WARPS<FP8>][32 * GP_PIECE<PAIR>];
-    uint64_t full[GP_STAGES<PAIR>], empty[GP_STAGES<PAIR>];        // a step's copies have landed; its MMAs have read them
-    uint64_t sum_full[2][2], sum_empty[2][2];       // an accumulator (GP_SPLIT: a half of it) is complete; has been taken out
+    static constexpr bool RING = K::FP8 && !K::FEW;
+    unsigned char a[K::STAGES][K::A_BYTES];
+    unsigned char b[K::STAGES][K::B_BYTES];
+    unsigned char out[K::FEW ? 1 : K::OUT_WARPS][32 * K::PIECE];
+    uint64_t full[K::STAGES], empty[K::STAGES];     // a step's copies have landed; its MMAs have read them
+    uint64_t sum_full[2][2], sum_empty[2][2];       // an accumulator (SPLIT: a half of it) is complete; has been taken out
     uint64_t scale_full[GP_SCALE_SLOTS], scale_empty[GP_SCALE_SLOTS];
     uint64_t drained[2];
-    float row_scale[FP8 ? GP_SCALE_SLOTS * GP_SCALE_STEPS : 1][FP8 ? GP_ROWS : 1];
+    float row_scale[RING ? GP_SCALE_SLOTS * GP_SCALE_STEPS : 1][RING ? GP_ROWS : 1];
     float2 w_scale[GP_SCALE_SLOTS * GP_SCALE_STEPS];     // of a tile's two blocks of weights (gate/up: one of each)
     uint32_t tmem_base;
     int last;
@@ -108,6 +113,11 @@ __device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, int 
     else
         asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                      ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+
+__device__ __forceinline__ void tma_prefetch(const CUtensorMap *map, int x, int y)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
 }
 
 // Four bytes to shared memory, asynchronously.
@@ -269,8 +279,8 @@ __device__ __forceinline__ void fma2(float &a0, float &a1, uint32_t d0, uint32_t
 }
 
 // Barrier of the warps that take sums out.
-template <bool FP8>
-__device__ __forceinline__ void out_barrier() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(GP_OUT_WARPS<FP8> * 32) : "memory"); }
+template <class K>
+__device__ __forceinline__ void out_barrier() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(K::OUT_WARPS * 32) : "memory"); }
 
 // One run of steps of one tile.
 struct Run {
@@ -281,9 +291,10 @@ struct Run {
 
 // The runs of this block, in order.  Every role walks through them for itself, and keeps nothing of this in registers meanwhile.
 // (32 bits hold it all: at most 2^21 tiles, and fewer than a block's worth of cut ones of at most 512 steps.)
-template <bool GATED, bool PAIR>
+template <class K>
 struct Schedule {
-    static constexpr int ROWS = PAIR ? 2 * GP_ROWS : GP_ROWS;
+    static constexpr bool GATED = K::GATED, PAIR = K::PAIR;
+    static constexpr int ROWS = K::TILE_ROWS;
     const GroupedParams &p;
     volatile GroupedPlan &s;
 
@@ -294,7 +305,7 @@ struct Schedule {
     {
         const int tiles = s.tiles[p.n_experts] * p.n_cols, whole = tiles / blocks(), rest = tiles - whole * blocks(), units = rest * p.steps;
         int parts = min(blocks(), max(units / GP_MIN_STEPS, rest));
-        if (parts > rest && units / parts + (s.most <= GP_FEW ? GP_JOIN_FEW : GP_JOIN) >= p.steps) parts = rest;      // (they stay whole)
+        if (parts > rest && units / parts + (K::FEW ? GP_JOIN_FEW : GP_JOIN) >= p.steps) parts = rest;      // (they stay whole)
         s.whole = whole;
         s.units = units;
         s.parts = parts;
@@ -374,16 +385,11 @@ __device__ __forceinline__ void grouped_plan(const GroupedParams &p, int tile_ro
     if (lane == 0) before = 0;
     for (int i = i0; i < i1; ++i) s.start[i] = max(s.start[i], before);
     __syncwarp();
-    int n = 0, rows = 0;
+    int n = 0;
     for (int i = i0; i < i1; ++i) {
         s.tiles[i] = n;
-        if (i >= p.n_experts) break;
-        const int here = s.start[i + 1] - s.start[i];
-        n += (here + tile_rows - 1) / tile_rows;
-        rows = max(rows, here);
+        if (i < p.n_experts) n += (s.start[i + 1] - s.start[i] + tile_rows - 1) / tile_rows;
     }
-    rows = __reduce_max_sync(0xffffffffu, rows);
-    if (lane == 0) s.most = rows;
     int incl = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -394,32 +400,32 @@ __device__ __forceinline__ void grouped_plan(const GroupedParams &p, int tile_ro
 }
 
 // A part of a cut tile is in the workspace (this thread's share of it): true for the warps of the block that came last.
-template <bool FP8, bool GATED, bool PAIR>
-__device__ __forceinline__ bool part_is_last(const GroupedParams &p, GroupedSmem<FP8, PAIR> &s, const Schedule<GATED, PAIR> &plan, const Run &r,
-                                             int &b0, int &b1)
+template <class K>
+__device__ __forceinline__ bool part_is_last(const GroupedParams &p, GroupedSmem<K> &s, const Schedule<K> &plan, const Run &r, int &b0, int &b1)
 {
     b0 = plan.block_of(r.rest * p.steps);
     b1 = plan.block_of((r.rest + 1) * p.steps - 1);
     __threadfence();
-    out_barrier<FP8>();
-    if (threadIdx.x == GP_THREADS<FP8> - 1) {
-        unsigned int *ticket = p.tickets + (PAIR ? 2 * r.rest + (int)(blockIdx.x & 1) : r.rest);
+    out_barrier<K>();
+    if (threadIdx.x == K::THREADS - 1) {
+        unsigned int *ticket = p.tickets + (K::PAIR ? 2 * r.rest + (int)(blockIdx.x & 1) : r.rest);
         s.last = atomicAdd(ticket, 1u) == (unsigned)(b1 - b0);
         if (s.last) *ticket = 0u;
         __threadfence();
     }
-    out_barrier<FP8>();
+    out_barrier<K>();
     return s.last != 0;
 }
 
 // The sums of a tile of few rows and what becomes of them: thread = output, values = rows.
 // Each four warps have a share of the rows; plain: the first or the second 128 outputs of a share; gate/up: a thread has gate and up of
 // its output.
-template <bool FP8, bool GATED>
-__device__ __forceinline__ void take_few(const GroupedParams &p, GroupedSmem<FP8, false> &s, const Schedule<GATED, false> &plan, const Run &r,
-                                         uint32_t lanes, int share, int place, int &n)
+template <class K>
+__device__ __forceinline__ void take_few(const GroupedParams &p, GroupedSmem<K> &s, const Schedule<K> &plan, const Run &r, uint32_t lanes,
+                                         int share, int place, int &n)
 {
-    constexpr int SHARES = GP_OUT_WARPS<FP8> / (GATED ? 4 : 8), N = GP_FEW / SHARES;         // rows of a thread: at most N
+    constexpr bool FP8 = K::FP8, GATED = K::GATED;
+    constexpr int SHARES = K::OUT_WARPS / (GATED ? 4 : 8), N = GP_FEW / SHARES;         // rows of a thread: at most N
     const int lane = threadIdx.x & 31, per = ((r.rows + SHARES - 1) / SHARES + 7) / 8 * 8;
     const int t0 = (GATED ? share : share >> 1) * per, rows = min(per, r.rows - t0);      // (may be none)
     const int side = GATED ? 0 : GP_COLS / 2 * (share & 1), o = r.out0 + side + place;
@@ -550,7 +556,7 @@ __device__ __forceinline__ void take_few(const GroupedParams &p, GroupedSmem<FP8
                 }
             }
     }
-    if (GATED && FP8) out_barrier<FP8>();
+    if (GATED && FP8) out_barrier<K>();
 #pragma unroll
     for (int c = 0; c < N / 8; ++c)
         if (8 * c < rows) {
@@ -568,38 +574,38 @@ __device__ __forceinline__ void take_few(const GroupedParams &p, GroupedSmem<FP8
                     }
                 }
         }
-    if (GATED && FP8) out_barrier<FP8>();                 // (before the next tile's maxima)
+    if (GATED && FP8) out_barrier<K>();                 // (before the next tile's maxima)
 }
 
-// A piece of this warp's 32 rows leaves by way of shared memory: each thread brings GP_PIECE bytes of its row, and the warp writes
+// A piece of this warp's 32 rows leaves by way of shared memory: each thread brings PIECE bytes of its row, and the warp writes
 // whole pieces row after row (a thread writing 16 bytes of its own row at a time touched 32 lines per instruction: 6000 cycles for
 // a tile of 256 bfloat16 columns).  to: the piece of lane 0's row, `pitch` bytes from row to row; only rows below n, bytes below `bytes`.
-template <bool PAIR>
+template <class K>
 __device__ __forceinline__ void leave(unsigned char *stage, const uint4 *v, char *to, size_t pitch, int n, int bytes)
 {
-    constexpr int Q = GP_PIECE<PAIR> / 16, ROWS = 32 / Q, SHIFT = PAIR ? 1 : 2;       // 16-byte parts of a piece, rows per pass
+    constexpr int Q = K::PIECE / 16, ROWS = 32 / Q, SHIFT = K::PIECE == 64 ? 1 : 2;       // 16-byte parts of a piece, rows per pass
     const int lane = threadIdx.x & 31;
     __syncwarp();
 #pragma unroll
-    for (int q = 0; q < Q; ++q) *reinterpret_cast<uint4 *>(stage + lane * GP_PIECE<PAIR> + ((q ^ (lane >> SHIFT & (Q - 1))) << 4)) = v[q];
+    for (int q = 0; q < Q; ++q) *reinterpret_cast<uint4 *>(stage + lane * K::PIECE + ((q ^ (lane >> SHIFT & (Q - 1))) << 4)) = v[q];
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
         const int row = i * ROWS + lane / Q, q = lane % Q;
-        const uint4 w = *reinterpret_cast<const uint4 *>(stage + row * GP_PIECE<PAIR> + ((q ^ (row >> SHIFT & (Q - 1))) << 4));
+        const uint4 w = *reinterpret_cast<const uint4 *>(stage + row * K::PIECE + ((q ^ (row >> SHIFT & (Q - 1))) << 4));
         if (row < n && 16 * q < bytes) *reinterpret_cast<uint4 *>(to + row * pitch + 16 * q) = w;
     }
 }
 
 // The sums of any other tile: thread = row, values = its share of the columns, in two groups: H from the tile's output first on and H from
 // second on (gate/up: gate, and the up of the same outputs).  row0, rows: this block's rows of the tile (may be none).
-template <bool FP8, bool GATED, bool PAIR>
-__device__ __forceinline__ void take_tile(const GroupedParams &p, GroupedSmem<FP8, PAIR> &s, const Schedule<GATED, PAIR> &plan, const Run &r,
-                                          int row0, int rows, uint32_t lanes, int share, int row, int &n, int &groups)
+template <class K>
+__device__ __forceinline__ void take_tile(const GroupedParams &p, GroupedSmem<K> &s, const Schedule<K> &plan, const Run &r, int row0, int rows,
+                                          uint32_t lanes, int share, int row, int &n, int &groups)
 {
-    constexpr int SHARES = GP_OUT_WARPS<FP8> / 4, C = GP_COLS / SHARES, H = C / 2;
+    constexpr bool FP8 = K::FP8, GATED = K::GATED, PAIR = K::PAIR, SPLIT = K::SPLIT;
+    constexpr int SHARES = K::OUT_WARPS / 4, C = GP_COLS / SHARES, H = C / 2;
     // the groups' columns; halves of a pair's accumulator have the first (second) half of both blocks' weights
-    constexpr bool SPLIT = GP_SPLIT<FP8, PAIR>;
     const int lane = threadIdx.x & 31;
     const int first = GATED || SPLIT ? H * share : C * share, second = GATED ? first : SPLIT ? GP_COLS / 2 + first : first + H;
     const int col0 = SPLIT ? C * share : first, col1 = GATED && !SPLIT ? GP_COLS / 2 + col0 : col0 + H;
@@ -704,11 +710,11 @@ __device__ __forceinline__ void take_tile(const GroupedParams &p, GroupedSmem<FP
             for (int j = 0; j < H; ++j)
                 if (o + (j & ~31) < p.d_out) most = fmaxf(most, fabsf(acc[j]));
             s.amax[share * GP_ROWS + row] = most;
-            out_barrier<FP8>();
+            out_barrier<K>();
             const float scale = fp8_scale(fmaxf(most, s.amax[(share ^ 1) * GP_ROWS + row]));
             if (row < rows && share == 0) p.out_scales[(size_t)(row0 + row) * out_blocks + r.out0 / DIP_FP8_BLOCK] = scale;
             char *to = static_cast<char *>(p.out) + (size_t)(row0 + warp_row) * p.d_out + o;
-            constexpr int B = GP_PIECE<PAIR>;
+            constexpr int B = K::PIECE;
 #pragma unroll
             for (int c = 0; c < H / B; ++c) {
                 uint4 v[B / 16];
@@ -718,16 +724,16 @@ __device__ __forceinline__ void take_tile(const GroupedParams &p, GroupedSmem<FP
                     v[q] = make_uint4(fp8_codes4(f[0], f[1], f[2], f[3], scale), fp8_codes4(f[4], f[5], f[6], f[7], scale),
                                       fp8_codes4(f[8], f[9], f[10], f[11], scale), fp8_codes4(f[12], f[13], f[14], f[15], scale));
                 }
-                leave<PAIR>(stage, v, to + c * B, p.d_out, n_here, p.d_out - o - c * B);
+                leave<K>(stage, v, to + c * B, p.d_out, n_here, p.d_out - o - c * B);
             }
-            out_barrier<FP8>();                      // (before the next tile's maxima)
+            out_barrier<K>();                      // (before the next tile's maxima)
             return;
         }
     }
     const int item = !GATED && p.out_f32 ? 4 : 2;
     const size_t pitch = (size_t)p.d_out * item;
     char *to = static_cast<char *>(p.out) + ((size_t)(row0 + warp_row) * p.d_out + r.out0) * item;
-    constexpr int B = GP_PIECE<PAIR>;
+    constexpr int B = K::PIECE;
 #pragma unroll
     for (int g = 0; g < (GATED ? 1 : 2); ++g) {
         const int o = g ? second : first, left = (p.d_out - r.out0 - o) * item;
@@ -740,7 +746,7 @@ __device__ __forceinline__ void take_tile(const GroupedParams &p, GroupedSmem<FP
                     const float *f = acc + g * H + c * (B / 4) + 4 * q;
                     v[q] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
                 }
-                leave<PAIR>(stage, v, to + o * 4 + c * B, pitch, n_here, left - c * B);
+                leave<K>(stage, v, to + o * 4 + c * B, pitch, n_here, left - c * B);
             }
         } else {
 #pragma unroll
@@ -748,21 +754,22 @@ __device__ __forceinline__ void take_tile(const GroupedParams &p, GroupedSmem<FP
                 uint4 v[B / 16];
 #pragma unroll
                 for (int q = 0; q < B / 16; ++q) v[q] = bf16x8(acc + g * H + c * (B / 2) + 8 * q);
-                leave<PAIR>(stage, v, to + o * 2 + c * B, pitch, n_here, left - c * B);
+                leave<K>(stage, v, to + o * 2 + c * B, pitch, n_here, left - c * B);
             }
         }
     }
 }
 
-template <bool FP8, bool GATED, bool PAIR>
-__global__ void __launch_bounds__(GP_THREADS<FP8>, 1)
-grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap few_map,
-               const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap w2_map, const GroupedParams p)
+template <class K>
+__global__ void __launch_bounds__(K::THREADS, 1)
+grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap w_map,
+               const __grid_constant__ CUtensorMap w2_map, const GroupedParams p)
 {
+    constexpr bool FP8 = K::FP8, GATED = K::GATED, PAIR = K::PAIR, FEW = K::FEW, SPLIT = K::SPLIT;
     extern __shared__ unsigned char gp_smem_raw[];
-    using Smem = GroupedSmem<FP8, PAIR>;
+    using Smem = GroupedSmem<K>;
     Smem &s = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(gp_smem_raw) + 1023) & ~(uintptr_t)1023);
-    constexpr int STAGES = GP_STAGES<PAIR>;
+    constexpr int STAGES = K::STAGES, PER_STEP = FP8 ? GP_STEP_BYTES : GP_STEP_BYTES / 2;
     DIP_TRACE_MIN(p.tr, 0);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = PAIR ? blockIdx.x & 1 : 0;      // (clusters are two neighbouring blocks)
@@ -781,54 +788,73 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
     if (tid == 0) {
         for (int i = 0; i < STAGES; ++i) {
             mbar_init(&s.full[i], 1);
-            mbar_init(&s.empty[i], GP_SPLIT<FP8, PAIR> ? 2 : 1);
+            mbar_init(&s.empty[i], SPLIT ? 2 : 1);
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(&s.sum_full[i >> 1][i & 1], 1);
-            mbar_init(&s.sum_empty[i >> 1][i & 1], (PAIR ? 2 : 1) * GP_OUT_WARPS<FP8> / (GP_SPLIT<FP8, PAIR> ? 2 : 1));
+            mbar_init(&s.sum_empty[i >> 1][i & 1], (PAIR ? 2 : 1) * K::OUT_WARPS / (SPLIT ? 2 : 1));
         }
         for (int i = 0; i < GP_SCALE_SLOTS; ++i) {
             mbar_init(&s.scale_full[i], 32);
-            mbar_init(&s.scale_empty[i], GP_OUT_WARPS<FP8>);
+            mbar_init(&s.scale_empty[i], K::OUT_WARPS);
         }
         mbar_init(&s.drained[0], 1);
         mbar_init(&s.drained[1], 1);
         s.fail = 0;
         asm volatile("prefetch.tensormap [%0];" ::"l"(&rows_map) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&few_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&w2_map) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    dip_grid_dependency_wait();                      // rows and offsets come from the kernels in front
+    // rows and offsets come from the kernels in front; weights do too, as far as the library can know, so before they are through it only
+    // asks L2 for the first ones, where there are no offsets to wait for
+    const Schedule<K> plan = {p, s.plan};
+    if (warp != 0 || p.offset) dip_grid_dependency_wait();
     DIP_TRACE_MIN(p.tr, 1);
-    const Schedule<GATED, PAIR> plan = {p, s.plan};
     if (warp == 0) {
+        __syncwarp();
         grouped_plan(p, plan.ROWS, s.plan);
         __syncwarp();
         if (lane == 0) plan.divide();
+        __syncwarp();
+        if (!p.offset) {
+            Run r;
+            if (FEW && plan.get(0, r) && elect_one()) {
+                for (int k = r.k0; k < min(r.k0 + STAGES, r.k1); ++k) {
+                    tma_prefetch(&w_map, k * PER_STEP, r.out0);
+                    tma_prefetch(GATED ? &w2_map : &w_map, k * PER_STEP, GATED ? r.out0 : r.out0 + GP_COLS / 2);
+                }
+            }
+            __syncwarp();
+            dip_grid_dependency_wait();
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    if (PAIR) pair_barrier();                        // (the other block's barriers are set up)
+    if (PAIR) {
+        __syncthreads();
+        pair_barrier();                              // (the other block's barriers are set up)
+    } else if (warp == 0) {                          // (goes on to its copies)
+        asm volatile("barrier.cta.arrive 2, %0;" ::"n"(K::THREADS) : "memory");
+    } else {
+        asm volatile("barrier.cta.sync 2, %0;" ::"n"(K::THREADS) : "memory");
+    }
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     dip_launch_dependents();
-    const uint32_t tmem = s.tmem_base;
-    constexpr int PER_STEP = FP8 ? GP_STEP_BYTES : GP_STEP_BYTES / 2;
+    const uint32_t tmem = s.tmem_base;               // (warp 0 has no use for it)
     bool failed = false;
 
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(GP_REGS_FEW<FP8>));
+        if (!FEW) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(K::REGS_FEW));
         if (warp == 0) {
             Run r;
             int g = 0;                               // steps so far
             for (int i = 0; !failed && plan.get(i, r); ++i) {
-                const bool few = !PAIR && r.rows <= GP_FEW, both = r.rows > GP_BOX;
+                const bool both = r.rows > GP_BOX;               // (few)
                 const int w_row = r.expert * p.d_out + r.out0, row0 = r.row0 + rank * GP_ROWS;
-                // (single, plain: the tile's second half may lie behind the last output; PAIR: the second block may have no rows)
+                // (plain: the tile's second half may lie behind the last output; PAIR: the second block may have no rows)
                 const bool second = GATED || r.out0 + GP_COLS / 2 < p.d_out, some = rank * GP_ROWS < r.rows;
                 const unsigned bytes = PAIR ? GP_B_BYTES + (r.rows > GP_ROWS ? 2 : 1) * GP_A_BYTES
-                                            : (few ? (both ? 2 : 1) * GP_BOX * GP_STEP_BYTES : GP_A_BYTES) + (second ? GP_B_BYTES : GP_B_BYTES / 2);
+                                            : (FEW ? (both ? 2 : 1) * GP_BOX * GP_STEP_BYTES : GP_A_BYTES) + (second ? GP_B_BYTES : GP_B_BYTES / 2);
                 int x = r.k0 * PER_STEP;
                 for (int k = r.k0; k < r.k1; ++k, ++g, x += PER_STEP) {
                     const int st = g % STAGES;
@@ -849,8 +875,8 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
                             } else {
                                 tma_load<PAIR>(s.b[st], second ? &w2_map : &w_map, x, w_row, &s.full[st]);
                             }
-                            tma_load<PAIR>(s.a[st], few ? &few_map : &rows_map, x, r.row0, &s.full[st]);
-                            if (few && both) tma_load<PAIR>(s.a[st] + GP_BOX * GP_STEP_BYTES, &few_map, x, r.row0 + GP_BOX, &s.full[st]);
+                            tma_load<PAIR>(s.a[st], &rows_map, x, r.row0, &s.full[st]);
+                            if (FEW && both) tma_load<PAIR>(s.a[st] + GP_BOX * GP_STEP_BYTES, &rows_map, x, r.row0 + GP_BOX, &s.full[st]);
                         }
                     }
                     __syncwarp();
@@ -859,13 +885,12 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
             // (given up: no copy of this block's is under way when it leaves; the second block's count at the first one's barriers)
             if (failed && rank == 0)
                 for (int j = max(0, g - STAGES); j < g; ++j) warp_wait(&s.full[j % STAGES], (j / STAGES) & 1, p.wait_limit_ns);
-        } else if (FP8 && warp == 3) {
+        } else if (Smem::RING && warp == 3) {
             // four rows a lane; the first lanes the weights' scales
             const int out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
             Run r;
             int g = 0;                               // groups so far
             for (int i = 0; !failed && plan.get(i, r); ++i) {
-                if (!PAIR && r.rows <= GP_FEW) continue;
                 const int last_row = r.row0 + r.rows - 1, ob = r.out0 / DIP_FP8_BLOCK + (GATED ? 0 : lane & 1);
                 const float *x[4];
 #pragma unroll
@@ -889,14 +914,12 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
                 }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
-        } else if ((warp == 1 || (GP_SPLIT<FP8, PAIR> && warp == 2)) && rank == 0) {
-            constexpr bool SPLIT = GP_SPLIT<FP8, PAIR>;
+        } else if ((warp == 1 || (SPLIT && warp == 2)) && rank == 0) {
             const int half = warp - 1;
             Run r;
             int g = 0, n = 0;                        // steps, accumulators so far
             for (int i = 0; !failed && plan.get(i, r); ++i) {
-                const bool few = !PAIR && r.rows <= GP_FEW;
-                const uint32_t shape = grouped_shape<FP8, PAIR>(few ? (r.rows + 15) / 16 * 16 : SPLIT ? GP_COLS / 2 : GP_COLS);
+                const uint32_t shape = grouped_shape<FP8, PAIR>(FEW ? (r.rows + 15) / 16 * 16 : SPLIT ? GP_COLS / 2 : GP_COLS);
                 for (int k = r.k0; k < r.k1; ++k, ++g) {
                     const int st = g % STAGES, buf = n & 1;
                     const bool first = FP8 || k == r.k0, last = FP8 || k == r.k1 - 1;
@@ -910,7 +933,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
                     const uint64_t a = operand_desc(s.a[st]), b = operand_desc(s.b[st]) + (SPLIT ? half * (64 * GP_STEP_BYTES >> 4) : 0);
                     const uint32_t to = tmem + buf * GP_COLS + (SPLIT ? half * (GP_COLS / 2) : 0);
                     if (elect_one()) {
-                        if (!few) {
+                        if (!FEW) {
 #pragma unroll
                             for (int q = 0; q < 4; ++q)          // 32 bytes of K each
                                 grouped_mma<FP8, PAIR>(to, a + 2 * q, b + 2 * q, shape, (first && q == 0) ? 0u : 1u);
@@ -936,20 +959,14 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(GP_REGS_MANY<FP8>));
+        if (!FEW) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(K::REGS_MANY));
         const int share = (warp - 4) >> 2, place = (warp & 3) * 32 + lane;     // lane of tensor memory
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         int n = 0, groups = 0;                       // accumulators, groups of scales so far
         Run r;
         for (int i = 0; plan.get(i, r); ++i) {
-            if constexpr (!PAIR) {
-                if (r.rows <= GP_FEW) {
-                    take_few<FP8, GATED>(p, s, plan, r, lanes, share, place, n);
-                    continue;
-                }
-            }
-            take_tile<FP8, GATED, PAIR>(p, s, plan, r, r.row0 + rank * GP_ROWS, min(GP_ROWS, r.rows - rank * GP_ROWS), lanes, share, place, n,
-                                         groups);
+            if constexpr (FEW) take_few<K>(p, s, plan, r, lanes, share, place, n);
+            else take_tile<K>(p, s, plan, r, r.row0 + rank * GP_ROWS, min(GP_ROWS, r.rows - rank * GP_ROWS), lanes, share, place, n, groups);
         }
     }
     if (failed) {
@@ -996,41 +1013,43 @@ bool encode(CUtensorMap *map, const void *p, bool fp8, size_t n, int d, int box)
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool FP8, bool GATED, bool PAIR>
-cudaError_t launch(dip_ctx *ctx, int ctas, cudaStream_t stream, const CUtensorMap (&m)[4], const GroupedParams &p)
+template <class K>
+cudaError_t launch(dip_ctx *ctx, int ctas, cudaStream_t stream, const CUtensorMap (&m)[3], const GroupedParams &p)
 {
     static dip_per_device_once once;
-    const auto kernel = grouped_kernel<FP8, GATED, PAIR>;
-    const size_t smem = sizeof(GroupedSmem<FP8, PAIR>) + 1024;
-    static_assert(sizeof(GroupedSmem<FP8, PAIR>) + 1024 <= 227 * 1024, "fits a CTA's shared memory");
+    const auto kernel = grouped_kernel<K>;
+    const size_t smem = sizeof(GroupedSmem<K>) + 1024;
+    static_assert(sizeof(GroupedSmem<K>) + 1024 <= 227 * 1024, "fits a CTA's shared memory");
     const cudaError_t e = dip_raise_smem_limit(once, ctx->device, kernel, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
-    cfg.blockDim = dim3(GP_THREADS<FP8>);
+    cfg.blockDim = dim3(K::THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = PAIR ? 2 : 1;
+    attr[1].val.clusterDim.x = K::PAIR ? 2 : 1;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], p);
+    return cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], p);
 }
 
 template <bool FP8, bool GATED>
-cudaError_t launch(bool pair, dip_ctx *ctx, int ctas, cudaStream_t stream, const CUtensorMap (&m)[4], const GroupedParams &p)
+cudaError_t launch(int mode, dip_ctx *ctx, int ctas, cudaStream_t stream, const CUtensorMap (&m)[3], const GroupedParams &p)
 {
-    return pair ? launch<FP8, GATED, true>(ctx, ctas, stream, m, p) : launch<FP8, GATED, false>(ctx, ctas, stream, m, p);
+    return mode == GP_PAIR    ? launch<Kind<FP8, GATED, GP_PAIR>>(ctx, ctas, stream, m, p)
+           : mode == GP_WHOLE ? launch<Kind<FP8, GATED, GP_WHOLE>>(ctx, ctas, stream, m, p)
+                              : launch<Kind<FP8, GATED, GP_FEW_ROWS>>(ctx, ctas, stream, m, p);
 }
 
 }  // namespace
 
-// Pairs from this many rows per expert on (the average over as many experts as can have any).
-constexpr int GP_PAIR_ROWS = 192;
+// Few up to, and pairs from this many rows per expert on (the average over as many experts as can have any).
+constexpr int GP_FEW_UP_TO = 32, GP_PAIR_ROWS = 192;
 
 dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const dip_grouped_matrix *up, const void *rows,
                               const float *row_scales, int n_rows, const int32_t *offset, void *out, bool out_f32, float *out_scales,
@@ -1038,17 +1057,17 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
 {
     const bool fp8 = w.wtype == DIP_W_FP8_B128;
     const int met = min(w.n_experts, n_rows);
-    const bool pair = n_rows >= GP_PAIR_ROWS * met && ctx->sm_count % 2 == 0;
+    const int mode = n_rows <= GP_FEW_UP_TO * met ? GP_FEW_ROWS : n_rows >= GP_PAIR_ROWS * met && ctx->sm_count % 2 == 0 ? GP_PAIR : GP_WHOLE;
     const size_t w_rows = (size_t)w.n_experts * w.d_out;
-    // the rows, whole tiles of them and few; half of a tile's weights; the other half (gate/up), or both at once
-    CUtensorMap maps[4];
-    if (!encoder() || !encode(&maps[0], rows, fp8, n_rows, w.d_in, GP_ROWS) || !encode(&maps[1], rows, fp8, n_rows, w.d_in, GP_BOX) ||
-        !encode(&maps[2], w.values, fp8, w_rows, w.d_in, GP_COLS / 2) ||
-        !encode(&maps[3], up ? up->values : w.values, fp8, w_rows, w.d_in, up ? GP_COLS / 2 : GP_COLS)) {
+    // the rows; half of a tile's weights; the other half (gate/up), or both at once
+    CUtensorMap maps[3];
+    if (!encoder() || !encode(&maps[0], rows, fp8, n_rows, w.d_in, mode == GP_FEW_ROWS ? GP_BOX : GP_ROWS) ||
+        !encode(&maps[1], w.values, fp8, w_rows, w.d_in, GP_COLS / 2) ||
+        !encode(&maps[2], up ? up->values : w.values, fp8, w_rows, w.d_in, up ? GP_COLS / 2 : GP_COLS)) {
         snprintf(ctx->err, sizeof(ctx->err), "cuTensorMapEncodeTiled failed");
         return DIP_ERR_CUDA;
     }
-    const int width = up ? GP_COLS / 2 : GP_COLS, tile_rows = pair ? 2 * GP_ROWS : GP_ROWS;
+    const int width = up ? GP_COLS / 2 : GP_COLS, tile_rows = mode == GP_PAIR ? 2 * GP_ROWS : mode == GP_WHOLE ? GP_ROWS : GP_FEW;
     GroupedParams p = {};
     p.w_scales = w.scales;
     p.up_scales = up ? up->scales : nullptr;
@@ -1071,8 +1090,8 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
     // no more blocks than there can be parts
     const long long tiles = (long long)((n_rows + tile_rows - 1) / tile_rows + met - 1) * p.n_cols;
     const long long most = max(tiles, tiles * p.steps / GP_MIN_STEPS);
-    const int ctas = pair ? 2 * (int)min((long long)ctx->sm_count / 2, most) : (int)min((long long)ctx->sm_count, most);
+    const int ctas = mode == GP_PAIR ? 2 * (int)min((long long)ctx->sm_count / 2, most) : (int)min((long long)ctx->sm_count, most);
     const auto start = fp8 ? (up ? launch<true, true> : launch<true, false>) : (up ? launch<false, true> : launch<false, false>);
-    DIP_CUDA_TRY(ctx, start(pair, ctx, ctas, stream, maps, p));
+    DIP_CUDA_TRY(ctx, start(mode, ctx, ctas, stream, maps, p));
     return DIP_OK;
 }
