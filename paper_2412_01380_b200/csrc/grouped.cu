@@ -40,6 +40,7 @@ constexpr int GP_A_BYTES = GP_ROWS * GP_STEP_BYTES, GP_B_BYTES = GP_COLS * GP_ST
 constexpr int GP_TMEM_COLS = 512;
 constexpr int GP_MIN_STEPS = 4;                     // a part of a tile has at least so many
 constexpr int GP_JOIN_FEW = 8, GP_JOIN = 20;        // steps' worth of time that a cut tile's parts take to meet (few rows; others)
+constexpr int GP_TWO_RUNS = 6;                      // steps' worth of time that a block loses between two runs
 constexpr int GP_SCALE_STEPS = 8, GP_SCALE_SLOTS = 4;   // steps of scales that come together, and how many such groups there is room for
 constexpr int GP_FEW = 64;                          // rows of a tile that are columns of its sums
 constexpr int GP_CHUNK = 12;                        // row tiles that go through an expert's weights together
@@ -305,6 +306,9 @@ struct Schedule {
     {
         const int tiles = s.tiles[p.n_experts] * p.n_cols, whole = tiles / blocks(), rest = tiles - whole * blocks(), units = rest * p.steps;
         int parts = min(blocks(), max(units / GP_MIN_STEPS, rest));
+        // runs within one tile each, where that makes them hardly longer: a block with two has a tile's end in the middle of its steps
+        const int each = rest ? parts / rest : 1;
+        if (parts > rest && (p.steps + each - 1) / each <= units / parts + GP_TWO_RUNS) parts = rest * each;
         if (parts > rest && units / parts + (K::FEW ? GP_JOIN_FEW : GP_JOIN) >= p.steps) parts = rest;      // (they stay whole)
         s.whole = whole;
         s.units = units;
