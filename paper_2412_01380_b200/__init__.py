@@ -528,18 +528,20 @@ def dip_sparse_gemv_down_noalloc(w: MlpWeights, h: torch.Tensor, kept_idx: torch
 
 
 # ---- mixtures of SwiGLU blocks, and prompts through a dense one -----------------------------------------------------------
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise DipError(ERR_INVALID_ARG, what)
+def _refuse(what: str, *args) -> None:
+    raise DipError(ERR_INVALID_ARG, what % args if args else what)
 
 
-def _tensor(t, dtype, shape, name: str, ctx: Optional[Context] = None) -> None:
-    """t is a contiguous device tensor of that type and shape (None in a shape: any extent), on the context's device."""
-    _need(isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous(), "%s must be a contiguous device tensor" % name)
-    _need(t.dtype == dtype, "%s must be %s, got %s" % (name, dtype, t.dtype))
-    _need(len(t.shape) == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape)),
-          "%s must have the shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    _need(ctx is None or t.device.index == ctx.device, "%s is not on the context's device" % name)
+def _matrix(t, dtype, n: Optional[int], d: Optional[int], name: str, device: int) -> None:
+    """t is a contiguous [n, d] tensor (None: any extent) of that type on that device.  Called several times per launch of a few
+    microseconds: no message is formed unless it is needed."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
+        _refuse("%s must be a tensor of %s", name, dtype)
+    if t.get_device() != device or not t.is_contiguous():
+        _refuse("%s must be contiguous and on device %d", name, device)
+    s = t.shape
+    if len(s) != 2 or (n is not None and s[0] != n) or (d is not None and s[1] != d):
+        _refuse("%s must have the shape %s, got %s", name, (n, d), tuple(s))
 
 
 def _blocks(d: int) -> int:
@@ -556,16 +558,21 @@ class GroupedMatrix:
     def __init__(self, values: torch.Tensor, scales: Optional[torch.Tensor] = None):
         if values.dim() == 2:
             values, scales = values[None], None if scales is None else scales[None]
-        _need(values.dtype in (torch.bfloat16, torch.float8_e4m3fn), "values must be bfloat16 or float8_e4m3fn")
-        _tensor(values, values.dtype, (None, None, None), "values")
+        if values.dim() != 3 or values.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            _refuse("values must be [n_experts, d_out, d_in], bfloat16 or float8_e4m3fn")
         self.wtype = W_BF16 if values.dtype == torch.bfloat16 else W_FP8_B128
         self.n_experts, self.d_out, self.d_in = values.shape
-        _need((scales is not None) == (self.wtype == W_FP8_B128), "scales belong to float8_e4m3fn values, and only to them")
+        if (scales is not None) != (self.wtype == W_FP8_B128):
+            _refuse("scales belong to float8_e4m3fn values, and only to them")
+        if not values.is_cuda or not values.is_contiguous():
+            _refuse("values must be a contiguous device tensor")
         if scales is not None:
-            _tensor(scales, torch.float32, (self.n_experts, _blocks(self.d_out), _blocks(self.d_in)), "scales")
-            _need(scales.device == values.device, "values and scales must be on one device")
-        self.values, self.scales, self.device = values, scales, values.device
+            if (scales.dtype != torch.float32 or scales.device != values.device or not scales.is_contiguous() or
+                    tuple(scales.shape) != (self.n_experts, _blocks(self.d_out), _blocks(self.d_in))):
+                _refuse("scales must be contiguous float32 [n_experts, ceil(d_out / 128), ceil(d_in / 128)] beside the values")
+        self.values, self.scales, self.device = values, scales, values.get_device()
         self.struct = GroupedMatrixStruct(self.wtype, self.n_experts, self.d_out, self.d_in, _ptr(values), _ptr(scales))
+        self.ref = C.byref(self.struct)
 
 
 class Rows:
@@ -573,18 +580,20 @@ class Rows:
     n_rows of them are in use (what the last call that wrote them wrote)."""
 
     def __init__(self, max_rows: int, d: int, wtype: int, device):
-        _need(wtype in _ROW_DTYPES, "rows are W_BF16 or W_FP8_B128")
+        if wtype not in _ROW_DTYPES:
+            _refuse("rows are W_BF16 or W_FP8_B128")
         self._set(torch.empty((max_rows, d), dtype=_ROW_DTYPES[wtype], device=device),
                   torch.empty((max_rows, _blocks(d)), device=device) if wtype == W_FP8_B128 else None)
 
     @classmethod
     def of(cls, values: torch.Tensor, scales: Optional[torch.Tensor] = None) -> "Rows":
         """Rows that are there already: all of `values` is in use."""
-        _need(values.dtype in _ROW_DTYPES.values(), "rows are bfloat16 or float8_e4m3fn")
-        _tensor(values, values.dtype, (None, None), "values")
-        _need((scales is not None) == (values.dtype == torch.float8_e4m3fn), "scales belong to float8_e4m3fn rows, and only to them")
+        if values.dim() != 2 or values.dtype not in _ROW_DTYPES.values() or not values.is_cuda or not values.is_contiguous():
+            _refuse("rows are a contiguous bfloat16 or float8_e4m3fn device tensor [n, d]")
+        if (scales is not None) != (values.dtype == torch.float8_e4m3fn):
+            _refuse("scales belong to float8_e4m3fn rows, and only to them")
         if scales is not None:
-            _tensor(scales, torch.float32, (values.shape[0], _blocks(values.shape[1])), "scales")
+            _matrix(scales, torch.float32, values.shape[0], _blocks(values.shape[1]), "scales", values.get_device())
         self = cls.__new__(cls)
         self._set(values, scales)
         self.n_rows = values.shape[0]
@@ -595,9 +604,7 @@ class Rows:
         self.max_rows, self.d = values.shape
         self.wtype = W_BF16 if scales is None else W_FP8_B128
         self.n_rows = 0
-
-    def _check(self, ctx: Context, name: str) -> None:
-        _need(isinstance(self, Rows) and self.values.device.index == ctx.device, "%s must be Rows on the context's device" % name)
+        self.device, self.ptr, self.scales_ptr = values.get_device(), _ptr(values), _ptr(scales)
 
 
 class ExpertRoute:
@@ -605,9 +612,10 @@ class ExpertRoute:
     first n rows of expert, weight and token_row, all of offset and the first offset[-1] entries of row_token are its."""
 
     def __init__(self, max_tokens: int, n_experts: int, top_k: int, device):
-        _need(1 <= max_tokens <= MAX_TOKENS, "1 .. %d tokens" % MAX_TOKENS)
-        _need(1 <= n_experts <= MAX_EXPERTS and 1 <= top_k <= min(n_experts, MAX_TOP_K),
-              "1 .. %d experts, of which 1 .. %d are chosen" % (MAX_EXPERTS, MAX_TOP_K))
+        if not 1 <= max_tokens <= MAX_TOKENS:
+            _refuse("1 .. %d tokens", MAX_TOKENS)
+        if not (1 <= n_experts <= MAX_EXPERTS and 1 <= top_k <= min(n_experts, MAX_TOP_K)):
+            _refuse("1 .. %d experts, of which 1 .. %d are chosen", MAX_EXPERTS, MAX_TOP_K)
         self.max_tokens, self.n_experts, self.top_k = int(max_tokens), int(n_experts), int(top_k)
         ints = dict(dtype=torch.int32, device=device)
         self.expert = torch.full((max_tokens, top_k), -1, **ints)
@@ -615,8 +623,10 @@ class ExpertRoute:
         self.offset = torch.zeros(n_experts + 1, **ints)
         self.row_token = torch.zeros(max_tokens * top_k, **ints)
         self.token_row = torch.full((max_tokens, top_k), -1, **ints)
+        self.device = self.offset.get_device()
         self.struct = ExpertRouteStruct(0, self.n_experts, self.top_k, 0, _ptr(self.expert), _ptr(self.weight), _ptr(self.offset),
                                         _ptr(self.row_token), _ptr(self.token_row))
+        self.ref = C.byref(self.struct)
 
     @property
     def n_tokens(self) -> int:
@@ -627,18 +637,15 @@ class ExpertRoute:
         """Most rows that the last call's tokens can have."""
         return self.struct.n_tokens * self.top_k
 
-    def _check(self, ctx: Context) -> None:
-        _need(self.offset.device.index == ctx.device, "the route is not on the context's device")
-
 
 class ExpertWeights:
     """gate, up [n_experts, d_ff, d_model] and down [n_experts, d_model, d_ff] of a mixture (or of one dense block)."""
 
     def __init__(self, gate: GroupedMatrix, up: GroupedMatrix, down: GroupedMatrix):
         shape = lambda m: (m.wtype, m.n_experts, m.d_out, m.d_in, m.device)  # noqa: E731
-        _need(shape(gate) == shape(up) == (down.wtype, down.n_experts, down.d_in, down.d_out, down.device),
-              "gate and up must be alike, and down their transposed shape")
-        self.gate, self.up, self.down = gate, up, down
+        if not shape(gate) == shape(up) == (down.wtype, down.n_experts, down.d_in, down.d_out, down.device):
+            _refuse("gate and up must be alike, and down their transposed shape")
+        self.gate, self.up, self.down, self.device = gate, up, down, gate.device
         self.wtype, self.n_experts, self.d_model, self.d_ff = gate.wtype, gate.n_experts, gate.d_in, gate.d_out
 
 
@@ -646,103 +653,118 @@ class ExpertWork:
     """The buffers that dip_expert_mlp needs for up to max_tokens tokens; top_k = 0: without a route."""
 
     def __init__(self, max_tokens: int, top_k: int, w: ExpertWeights, device):
-        _need(1 <= max_tokens <= MAX_TOKENS and 0 <= top_k <= MAX_TOP_K, "1 .. %d tokens, top_k 0 .. %d" % (MAX_TOKENS, MAX_TOP_K))
+        if not (1 <= max_tokens <= MAX_TOKENS and 0 <= top_k <= MAX_TOP_K):
+            _refuse("1 .. %d tokens, top_k 0 .. %d", MAX_TOKENS, MAX_TOP_K)
         self.max_rows, self.routed = int(max_tokens) * max(1, int(top_k)), top_k > 0
-        self.wtype, self.d_model, self.d_ff, self.device = w.wtype, w.d_model, w.d_ff, torch.device(device)
+        self.wtype, self.d_model, self.d_ff = w.wtype, w.d_model, w.d_ff
         fp8 = w.wtype == W_FP8_B128
         self.rows = Rows(self.max_rows, w.d_model, w.wtype, device) if fp8 or self.routed else None
         self.h = Rows(self.max_rows, w.d_ff, w.wtype, device)
         self.out = torch.empty((self.max_rows, w.d_model), device=device) if self.routed else None
-        self.struct = ExpertWorkStruct(_ptr(self.rows.values) if self.rows else None, _ptr(self.rows.scales) if self.rows else None,
-                                       _ptr(self.h.values), _ptr(self.h.scales), _ptr(self.out))
+        self.device = self.h.device
+        self.struct = ExpertWorkStruct(self.rows.ptr if self.rows else None, self.rows.scales_ptr if self.rows else None,
+                                       self.h.ptr, self.h.scales_ptr, _ptr(self.out))
+        self.ref = C.byref(self.struct)
 
 
 def dip_route_experts(ctx: Context, logits: torch.Tensor, route: ExpertRoute, renormalize: bool = True) -> None:
     """logits [n, n_experts], binary32 or bfloat16, n <= route.max_tokens."""
-    _need(isinstance(logits, torch.Tensor) and logits.dtype in (torch.float32, torch.bfloat16), "logits must be float32 or bfloat16")
-    _tensor(logits, logits.dtype, (None, route.n_experts), "logits", ctx)
-    route._check(ctx)
-    _need(1 <= logits.shape[0] <= route.max_tokens, "the route holds 1 .. %d tokens" % route.max_tokens)
-    route.struct.n_tokens = logits.shape[0]
-    ctx.check(_lib.dip_route_experts(ctx.handle, _ptr(logits), int(logits.dtype == torch.bfloat16), int(bool(renormalize)),
-                                     C.byref(route.struct), _stream()))
+    bf16 = isinstance(logits, torch.Tensor) and logits.dtype is torch.bfloat16
+    _matrix(logits, torch.bfloat16 if bf16 else torch.float32, None, route.n_experts, "logits", ctx.device)
+    n = logits.shape[0]
+    if not 1 <= n <= route.max_tokens:
+        _refuse("the route holds 1 .. %d tokens", route.max_tokens)
+    if route.device != ctx.device:
+        _refuse("the route is not on the context's device")
+    route.struct.n_tokens = n
+    ctx.check(_lib.dip_route_experts(ctx.handle, logits.data_ptr(), bf16, bool(renormalize), route.ref, _stream()))
 
 
 def _check_route(ctx: Context, route: Optional[ExpertRoute], n_tokens: int) -> None:
-    if route is not None:
-        route._check(ctx)
-        _need(route.n_tokens == n_tokens, "the route is of %d tokens, not %d" % (route.n_tokens, n_tokens))
+    if route is not None and (route.device != ctx.device or route.struct.n_tokens != n_tokens):
+        _refuse("the route must be on the context's device and of %d tokens, it is of %d", n_tokens, route.struct.n_tokens)
 
 
 def _check_offset(ctx: Context, offset: Optional[torch.Tensor], n_experts: int) -> None:
-    _need(offset is not None or n_experts == 1, "several experts need the offsets of their groups")
-    if offset is not None:
-        _tensor(offset, torch.int32, (n_experts + 1,), "offset", ctx)
+    if offset is None:
+        if n_experts != 1:
+            _refuse("several experts need the offsets of their groups")
+    elif (offset.dtype is not torch.int32 or offset.get_device() != ctx.device or not offset.is_contiguous() or
+          offset.shape != (n_experts + 1,)):
+        _refuse("offset must be contiguous int32 [%d] on the context's device", n_experts + 1)
 
 
 def dip_stage_rows(ctx: Context, x: torch.Tensor, rows: Rows, route: Optional[ExpertRoute] = None) -> None:
     """x [n, d] bfloat16 -> rows: x[t] for every row's token t, or x[r]; quantised if the rows are e4m3."""
-    rows._check(ctx, "rows")
-    _tensor(x, torch.bfloat16, (None, rows.d), "x", ctx)
-    _check_route(ctx, route, x.shape[0])
-    n = x.shape[0] if route is None else route.n_rows
-    _need(1 <= n <= rows.max_rows, "rows for %d, %d are needed" % (rows.max_rows, n))
-    ctx.check(_lib.dip_stage_rows(ctx.handle, _ptr(x), x.shape[0], rows.d, C.byref(route.struct) if route else None, rows.wtype,
-                                  _ptr(rows.values), _ptr(rows.scales), _stream()))
+    _matrix(x, torch.bfloat16, None, rows.d, "x", ctx.device)
+    n_tokens = n = x.shape[0]
+    if route is not None:
+        _check_route(ctx, route, n_tokens)
+        n *= route.top_k
+    if rows.device != ctx.device or not 1 <= n <= rows.max_rows:
+        _refuse("rows must be on the context's device and hold %d, they hold %d", n, rows.max_rows)
+    ctx.check(_lib.dip_stage_rows(ctx.handle, x.data_ptr(), n_tokens, rows.d, route.ref if route is not None else None, rows.wtype,
+                                  rows.ptr, rows.scales_ptr, _stream()))
     rows.n_rows = n
 
 
 def dip_grouped_product(ctx: Context, w: GroupedMatrix, rows: Rows, y: torch.Tensor, offset: Optional[torch.Tensor] = None) -> None:
     """y [>= rows.n_rows, d_out], bfloat16 or float32; offset int32 [n_experts + 1], None: one expert."""
-    rows._check(ctx, "rows")
-    _need(w.device.index == ctx.device, "the weights are not on the context's device")
-    _need(rows.wtype == w.wtype and rows.d == w.d_in, "rows and weights differ in type or width")
-    _need(isinstance(y, torch.Tensor) and y.dtype in (torch.bfloat16, torch.float32), "y must be bfloat16 or float32")
-    _tensor(y, y.dtype, (None, w.d_out), "y", ctx)
-    _need(1 <= rows.n_rows <= y.shape[0], "y has %d rows for %d" % (y.shape[0], rows.n_rows))
+    if rows.device != ctx.device or w.device != ctx.device or rows.wtype != w.wtype or rows.d != w.d_in:
+        _refuse("rows and weights must be on the context's device and agree in type and width")
+    f32 = isinstance(y, torch.Tensor) and y.dtype is torch.float32
+    _matrix(y, torch.float32 if f32 else torch.bfloat16, None, w.d_out, "y", ctx.device)
+    if not 1 <= rows.n_rows <= y.shape[0]:
+        _refuse("y has %d rows for %d", y.shape[0], rows.n_rows)
     _check_offset(ctx, offset, w.n_experts)
-    ctx.check(_lib.dip_grouped_product(ctx.handle, C.byref(w.struct), _ptr(rows.values), _ptr(rows.scales), rows.n_rows, _ptr(offset),
-                                       _ptr(y), int(y.dtype == torch.float32), _stream()))
+    ctx.check(_lib.dip_grouped_product(ctx.handle, w.ref, rows.ptr, rows.scales_ptr, rows.n_rows, _ptr(offset), y.data_ptr(), f32,
+                                       _stream()))
 
 
 def dip_grouped_gate_up(ctx: Context, gate: GroupedMatrix, up: GroupedMatrix, rows: Rows, h: Rows,
                         offset: Optional[torch.Tensor] = None) -> None:
     """h = silu(gate rows) * (up rows), rounded (and for e4m3 quantised) as the next product takes it."""
-    rows._check(ctx, "rows")
-    h._check(ctx, "h")
     for m in (gate, up):
-        _need(m.device.index == ctx.device, "the weights are not on the context's device")
-        _need(rows.wtype == h.wtype == m.wtype and rows.d == m.d_in and h.d == m.d_out and m.n_experts == gate.n_experts,
-              "rows, h and weights differ in type, width or number of experts")
-    _need(1 <= rows.n_rows <= h.max_rows, "h has %d rows for %d" % (h.max_rows, rows.n_rows))
+        if (not rows.device == h.device == m.device == ctx.device or not rows.wtype == h.wtype == m.wtype or rows.d != m.d_in or
+                h.d != m.d_out or m.n_experts != gate.n_experts):
+            _refuse("rows, h and weights must be on the context's device and agree in type, width and number of experts")
+    if not 1 <= rows.n_rows <= h.max_rows:
+        _refuse("h has %d rows for %d", h.max_rows, rows.n_rows)
     _check_offset(ctx, offset, gate.n_experts)
-    ctx.check(_lib.dip_grouped_gate_up(ctx.handle, C.byref(gate.struct), C.byref(up.struct), _ptr(rows.values), _ptr(rows.scales),
-                                       rows.n_rows, _ptr(offset), _ptr(h.values), _ptr(h.scales), _stream()))
+    ctx.check(_lib.dip_grouped_gate_up(ctx.handle, gate.ref, up.ref, rows.ptr, rows.scales_ptr, rows.n_rows, _ptr(offset),
+                                       h.ptr, h.scales_ptr, _stream()))
     h.n_rows = rows.n_rows
 
 
 def dip_combine_rows(ctx: Context, rows: torch.Tensor, route: ExpertRoute, y: torch.Tensor) -> None:
     """y [n, d] bfloat16 = the weighted sums of rows [>= n * top_k, d], binary32; n the route's tokens."""
-    route._check(ctx)
-    _need(route.n_tokens >= 1, "the route has no tokens yet")
-    _tensor(y, torch.bfloat16, (route.n_tokens, None), "y", ctx)
-    _tensor(rows, torch.float32, (None, y.shape[1]), "rows", ctx)
-    _need(rows.shape[0] >= route.n_rows, "rows has %d rows for %d" % (rows.shape[0], route.n_rows))
-    ctx.check(_lib.dip_combine_rows(ctx.handle, _ptr(rows), C.byref(route.struct), y.shape[1], _ptr(y), _stream()))
+    n = route.struct.n_tokens
+    if route.device != ctx.device or n < 1:
+        _refuse("the route must be on the context's device and have tokens")
+    _matrix(y, torch.bfloat16, n, None, "y", ctx.device)
+    _matrix(rows, torch.float32, None, y.shape[1], "rows", ctx.device)
+    if rows.shape[0] < n * route.top_k:
+        _refuse("rows has %d rows for %d", rows.shape[0], n * route.top_k)
+    ctx.check(_lib.dip_combine_rows(ctx.handle, rows.data_ptr(), route.ref, y.shape[1], y.data_ptr(), _stream()))
 
 
 def dip_expert_mlp(ctx: Context, w: ExpertWeights, x: torch.Tensor, work: ExpertWork, y: torch.Tensor,
                    route: Optional[ExpertRoute] = None) -> None:
     """x [n, d_model] -> y [n, d_model], bfloat16, through the mixture (route) or the one dense block (no route)."""
-    _need(w.gate.device.index == ctx.device, "the weights are not on the context's device")
-    _tensor(x, torch.bfloat16, (None, w.d_model), "x", ctx)
-    _tensor(y, torch.bfloat16, (x.shape[0], w.d_model), "y", ctx)
-    _check_route(ctx, route, x.shape[0])
-    _need(route is None or route.n_experts == w.n_experts, "route and weights differ in their number of experts")
-    _need(route is not None or w.n_experts == 1, "several experts need a route")
-    _need((work.wtype, work.d_model, work.d_ff) == (w.wtype, w.d_model, w.d_ff) and work.h.values.device.index == ctx.device and
-          work.routed == (route is not None), "the buffers are of another shape, type, device or kind of call")
-    n = x.shape[0] if route is None else route.n_rows
-    _need(1 <= n <= work.max_rows, "buffers for %d rows, %d are needed" % (work.max_rows, n))
-    ctx.check(_lib.dip_expert_mlp(ctx.handle, C.byref(w.gate.struct), C.byref(w.up.struct), C.byref(w.down.struct), _ptr(x),
-                                  x.shape[0], C.byref(route.struct) if route else None, C.byref(work.struct), _ptr(y), _stream()))
+    _matrix(x, torch.bfloat16, None, w.d_model, "x", ctx.device)
+    n_tokens = n = x.shape[0]
+    _matrix(y, torch.bfloat16, n_tokens, w.d_model, "y", ctx.device)
+    if w.device != ctx.device or (work.wtype, work.d_model, work.d_ff, work.device) != (w.wtype, w.d_model, w.d_ff, ctx.device):
+        _refuse("weights and buffers must be on the context's device, and of one shape and type")
+    if route is None:
+        if w.n_experts != 1:
+            _refuse("several experts need a route")
+    else:
+        _check_route(ctx, route, n_tokens)
+        if route.n_experts != w.n_experts:
+            _refuse("route and weights differ in their number of experts")
+        n *= route.top_k
+    if work.routed != (route is not None) or not 1 <= n <= work.max_rows:
+        _refuse("buffers for %d rows %s a route, %d are needed", work.max_rows, "with" if work.routed else "without", n)
+    ctx.check(_lib.dip_expert_mlp(ctx.handle, w.gate.ref, w.up.ref, w.down.ref, x.data_ptr(), n_tokens,
+                                  route.ref if route is not None else None, work.ref, y.data_ptr(), _stream()))

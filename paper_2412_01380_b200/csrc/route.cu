@@ -51,60 +51,100 @@ __device__ __forceinline__ float route_part(uint32_t key, float high)
     return high == INFINITY ? (v == INFINITY ? 1.f : 0.f) : expf(v - high);
 }
 
-// One token, one warp: experts and weights, and the token's bit in the sets of its experts.
-template <int NV>
-__device__ __forceinline__ void route_token(const RouteParams &p, int t, int bit, RouteSmem &s)
+// Tokens t0 + 32 m (m < M, below n) of a block, one warp: experts and weights, and the tokens' bits in the sets of their experts.  M of
+// them side by side, because one alone waits: for its logits, and for each choice's two trips through all lanes.
+template <int NV, int M>
+__device__ __forceinline__ void route_tokens(const RouteParams &p, int first, int bit0, int n, RouteSmem &s)
 {
     const int lane = threadIdx.x & 31;
-    uint32_t key[NV];
+    uint32_t key[M][NV], most[M];
+    float raw[M][NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int e = lane + 32 * i;
-        key[i] = 0u;
-        if (e < p.n_experts) {
-            const size_t at = (size_t)t * p.n_experts + e;
-            key[i] = route_key(p.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p.logits)[at])
-                                      : static_cast<const float *>(p.logits)[at]);
-        }
-    }
-    uint32_t most = 0u;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) most = max(most, key[i]);
-    most = __reduce_max_sync(RT_ALL, most);
-    const float high = route_value(most);
-    float sum = 0.f;
-    if (!p.renormalize) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) sum += route_part(key[i], high);
-    }
-    uint32_t mine = 0u;                           // choice `lane`
-    int mine_e = -1;
-    for (int j = 0; j < p.top_k && most != 0u; ++j) {
-        int at = 0x7fffffff;
-#pragma unroll
-        for (int i = NV - 1; i >= 0; --i)
-            if (key[i] == most) at = lane + 32 * i;
-        const int e = (int)__reduce_min_sync(RT_ALL, (unsigned)at);
-        if (lane == j) {
-            mine = most;
-            mine_e = e;
-        }
-        most = 0u;
+    for (int m = 0; m < M; ++m)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (lane + 32 * i == e) key[i] = 0u;
-            most = max(most, key[i]);
+            const int e = lane + 32 * i;
+            raw[m][i] = -INFINITY;
+            if (e < p.n_experts && bit0 + 32 * m < n) {
+                const size_t at = (size_t)(first + bit0 + 32 * m) * p.n_experts + e;
+                raw[m][i] = p.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p.logits)[at]) : static_cast<const float *>(p.logits)[at];
+            }
         }
-        most = __reduce_max_sync(RT_ALL, most);
-    }
-    const float part = route_part(mine, high);
-    if (p.renormalize) sum = part;
+    float high[M], sum[M];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(RT_ALL, sum, o);
-    if (lane < p.top_k) {
-        p.expert[(size_t)t * p.top_k + lane] = mine_e;
-        p.weight[(size_t)t * p.top_k + lane] = mine_e >= 0 ? part / sum : 0.f;
-        if (mine_e >= 0) atomicOr(&s.chosen[mine_e][bit >> 5], 1u << (bit & 31));
+    for (int m = 0; m < M; ++m) {
+        most[m] = 0u;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            key[m][i] = route_key(raw[m][i]);
+            most[m] = max(most[m], key[m][i]);
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m) most[m] = __reduce_max_sync(RT_ALL, most[m]);
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        high[m] = route_value(most[m]);
+        sum[m] = 0.f;
+        if (!p.renormalize) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) sum[m] += route_part(key[m][i], high[m]);
+        }
+    }
+    uint32_t mine[M];                             // choice `lane`
+    int mine_e[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        mine[m] = 0u;
+        mine_e[m] = -1;
+    }
+    for (int j = 0; j < p.top_k; ++j) {
+        unsigned at[M];
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            at[m] = 0x7fffffffu;
+#pragma unroll
+            for (int i = NV - 1; i >= 0; --i)
+                if (key[m][i] == most[m]) at[m] = lane + 32 * i;
+        }
+#pragma unroll
+        for (int m = 0; m < M; ++m) at[m] = __reduce_min_sync(RT_ALL, at[m]);
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const int e = most[m] ? (int)at[m] : -1;          // (no expert is left: closed ones have the key 0)
+            if (lane == j) {
+                mine[m] = most[m];
+                mine_e[m] = e;
+            }
+            most[m] = 0u;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (lane + 32 * i == e) key[m][i] = 0u;
+                most[m] = max(most[m], key[m][i]);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < M; ++m) most[m] = __reduce_max_sync(RT_ALL, most[m]);
+    }
+    float part[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        part[m] = route_part(mine[m], high[m]);
+        if (p.renormalize) sum[m] = part[m];
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int m = 0; m < M; ++m) sum[m] += __shfl_xor_sync(RT_ALL, sum[m], o);
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        const int bit = bit0 + 32 * m;
+        if (lane < p.top_k && bit < n) {
+            const size_t to = (size_t)(first + bit) * p.top_k + lane;
+            p.expert[to] = mine_e[m];
+            p.weight[to] = mine_e[m] >= 0 ? part[m] / sum[m] : 0.f;
+            if (mine_e[m] >= 0) atomicOr(&s.chosen[mine_e[m]][bit >> 5], 1u << (bit & 31));
+        }
     }
 }
 
@@ -169,7 +209,15 @@ __global__ void __launch_bounds__(RT_THREADS, 1) route_choose_kernel(const Route
     route_clear(p, s);
     dip_grid_dependency_wait();
     dip_launch_dependents();
-    for (int i = threadIdx.x >> 5; i < n; i += RT_WARPS) route_token<NV>(p, t0 + i, i, s);
+    const int warp = threadIdx.x >> 5;
+    static_assert(DIP_ROUTE_TOKENS == 4 * RT_WARPS, "four tokens a warp");
+    if (n <= RT_WARPS) {
+        if (warp < n) route_tokens<NV, 1>(p, t0, warp, n, s);
+    } else if (NV <= 8) {
+        route_tokens<NV, 4>(p, t0, warp, n, s);
+    } else {                                      // (registers: 64 each at 1024 threads)
+        for (int bit = warp; bit < n; bit += RT_WARPS) route_tokens<NV, 1>(p, t0, bit, n, s);
+    }
     __syncthreads();
     for (int e = threadIdx.x; e < p.n_experts; e += RT_THREADS) {
         int c = 0;
@@ -200,7 +248,7 @@ __global__ void __launch_bounds__(RT_THREADS, 1) route_rows_kernel(const RoutePa
     const int e = threadIdx.x % width;
     if (e < p.n_experts) {
         int total = 0, before = 0;
-#pragma unroll 4
+#pragma unroll 8
         for (int b = threadIdx.x / width; b < (int)gridDim.x; b += RT_THREADS / width) {
             const int c = p.counts[(size_t)b * DIP_MAX_EXPERTS + e];
             total += c;
