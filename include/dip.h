@@ -92,8 +92,9 @@ typedef struct dip_ctx dip_ctx;   /* opaque; owns scratch workspace on one devic
  *                      way the masks are the same bits.
  *   wait_limit_us      bound of every in-kernel wait on an asynchronous copy, in microseconds (0 =
  *                      one second); see dip_device_status.  Waits on another thread block of the
- *                      same launch, which products with row parts make in the normal course, have
- *                      this bound or one second, whichever is longer.
+ *                      same launch, which products with row parts make in the normal course, and
+ *                      those between the warps of a grouped product, have this bound or one
+ *                      second, whichever is longer.
  *   select_in_product  0 = default: in a single-token step each product kernel builds the mask of its
  *                      own input (every thread block selects for itself and goes straight on to its
  *                      rows; the last block also writes the mask; in a down launch that carries
@@ -114,7 +115,7 @@ typedef struct {
 } dip_options;
 
 /* Create a context on `device` (a CUDA ordinal).  Allocates the scratch
- * workspace (about 50 MB at the default sizes) with cudaMalloc; no other call
+ * workspace (about 60 MB at the default sizes) with cudaMalloc; no other call
  * allocates.  *out is NULL on failure.  The calling thread's current device is
  * left as it was.  Every later call on the context must be made with `device`
  * current (DIP_ERR_INVALID_ARG otherwise). */

@@ -9,7 +9,7 @@
 
 namespace {
 
-constexpr size_t PARTIALS_FLOATS = (size_t)8 << 20;   // 32 MB of split-row partial sums
+constexpr size_t PARTIALS_FLOATS = (size_t)8 << 20;   // 32 MB of split-row partial sums at least
 constexpr int N_TICKETS = 4096;
 
 bool dims_ok(int wtype, int d_model, int d_ff)
@@ -133,7 +133,8 @@ dip_status dip_create_ex(dip_ctx **out, int device, const dip_options *opt)
     // (blocks wait for one another whenever a product has row parts: a short limit is not for them)
     ctx->block_wait_ns = ctx->wait_limit_ns > 1000000000ull ? ctx->wait_limit_ns : 1000000000ull;
     // split-row partial sums: up to one part per SM of a whole output row per token
-    ctx->partials_floats = PARTIALS_FLOATS;
+    const size_t group_parts = (size_t)ctx->sm_count * 2 * DIP_GROUP_ROWS * DIP_GROUP_COLS;
+    ctx->partials_floats = group_parts > PARTIALS_FLOATS ? group_parts : PARTIALS_FLOATS;
     ctx->n_tickets = N_TICKETS;
     const size_t vec = (size_t)ctx->max_batch * ctx->max_d;
     if ((st = dev_alloc(ctx, &ctx->partials, ctx->partials_floats)) != DIP_OK) return fail(st);
@@ -157,7 +158,6 @@ dip_status dip_create_ex(dip_ctx **out, int device, const dip_options *opt)
     if ((st = dev_alloc(ctx, &ctx->coarse, vec)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->xt, (size_t)ctx->max_d * 32)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->route_counts, (size_t)DIP_MAX_TOKENS / DIP_ROUTE_TOKENS * DIP_MAX_EXPERTS)) != DIP_OK) return fail(st);
-    if ((st = dev_alloc(ctx, &ctx->group_partials, (size_t)ctx->sm_count * 2 * DIP_GROUP_ROWS * DIP_GROUP_COLS)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->group_tickets, (size_t)ctx->sm_count)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->status, (size_t)1)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->trace, (size_t)DIP_TRACE_SLOTS * DIP_TRACE_WORDS)) != DIP_OK) return fail(st);
@@ -220,7 +220,6 @@ dip_status dip_destroy(dip_ctx *ctx)
     cudaFree(ctx->coarse);
     cudaFree(ctx->xt);
     cudaFree(ctx->route_counts);
-    cudaFree(ctx->group_partials);
     cudaFree(ctx->group_tickets);
     cudaFree(ctx->status);
     cudaFree(ctx->trace);

@@ -28,7 +28,7 @@ struct dip_ctx {
     int gemv_direct;     // one token, F32/BF16: plain-load kernel instead of the copy ring
     unsigned long long wait_limit_ns;   // bound of every in-kernel wait on an asynchronous copy
     unsigned long long block_wait_ns;   // and on other blocks of the launch
-    // split-row partial sums of the two GEMVs (binary32)
+    // split-row partial sums of the two GEMVs (binary32); the grouped products' parts of tiles, [sm_count][2][DIP_GROUP_ROWS][DIP_GROUP_COLS]
     float *partials;
     size_t partials_floats;
     float *mail;         // [sm_count][DIP_MAIL_FLOATS] row parts on their way to the CTA that adds them up
@@ -56,7 +56,6 @@ struct dip_ctx {
     uint16_t *xt;        // [max_d][32] batched decode: per column, the tokens' values as bfloat16 (16 high, 16 low halves)
     int coarse_min_d;    // smallest d_ff for which the step ranks h from those
     int32_t *route_counts;   // [DIP_MAX_TOKENS / DIP_ROUTE_TOKENS][DIP_MAX_EXPERTS] the router: rows per token block and expert
-    float *group_partials;   // [sm_count][2][DIP_GROUP_ROWS][DIP_GROUP_COLS] the grouped products' parts of tiles
     unsigned int *group_tickets; // [sm_count] parts of a tile that are there, zero between launches
     int *status;         // sticky device status word (0 = fine)
     int fuse_select;     // single-token F32 / BF16 steps: the products build their own masks

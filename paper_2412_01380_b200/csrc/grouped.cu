@@ -74,7 +74,7 @@ struct GroupedParams {
     float *partials;
     unsigned int *tickets;
     int *status;
-    unsigned long long wait_limit_ns;
+    unsigned long long copy_wait_ns, wait_limit_ns;      // on a copy; on other warps
     unsigned long long *tr;
 };
 
@@ -888,7 +888,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
             }
             // (given up: no copy of this block's is under way when it leaves; the second block's count at the first one's barriers)
             if (failed && rank == 0)
-                for (int j = max(0, g - STAGES); j < g; ++j) warp_wait(&s.full[j % STAGES], (j / STAGES) & 1, p.wait_limit_ns);
+                for (int j = max(0, g - STAGES); j < g; ++j) warp_wait(&s.full[j % STAGES], (j / STAGES) & 1, p.copy_wait_ns);
         } else if (Smem::RING && warp == 3) {
             // four rows a lane; the first lanes the weights' scales
             const int out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
@@ -928,7 +928,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
                     const int st = g % STAGES, buf = n & 1;
                     const bool first = FP8 || k == r.k0, last = FP8 || k == r.k1 - 1;
                     if ((first && n >= 2 && !warp_wait(&s.sum_empty[buf][half], (n / 2 - 1) & 1, p.wait_limit_ns)) ||
-                        !warp_wait(&s.full[st], (g / STAGES) & 1, p.wait_limit_ns)) {
+                        !warp_wait(&s.full[st], (g / STAGES) & 1, p.copy_wait_ns)) {
                         failed = true;
                         break;
                     }
@@ -1086,10 +1086,11 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
     p.out = out;
     p.out_scales = out_scales;
     p.out_f32 = out_f32;
-    p.partials = ctx->group_partials;
+    p.partials = ctx->partials;
     p.tickets = ctx->group_tickets;
     p.status = ctx->status;
-    p.wait_limit_ns = ctx->wait_limit_ns;
+    p.copy_wait_ns = ctx->wait_limit_ns;
+    p.wait_limit_ns = ctx->block_wait_ns;
     p.tr = dip_trace_slot(ctx, up ? 10 : 11);
     // no more blocks than there can be parts
     const long long tiles = (long long)((n_rows + tile_rows - 1) / tile_rows + met - 1) * p.n_cols;
