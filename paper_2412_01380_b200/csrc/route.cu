@@ -2,12 +2,13 @@
 //
 // Choice: a warp per token holds the token's logits in registers (E / 32 per lane) and takes the largest top_k times: one
 // warp-wide maximum over order-preserving integers, one warp-wide minimum over the indices that hold it (ties: lowest).  A bfloat16
-// logit's integer has 16 bits and shares a word with its index, which makes one maximum of both (16384 tokens, 8 of 128 experts:
-// 15.6 us with two).
-// Grouping: row = first row of the expert + tokens in front that chose it.  A block has DIP_ROUTE_TOKENS tokens and a bit set
-// of them per expert, so a rank within the block is a popcount; nothing depends on the order of atomics.  Up to
-// DIP_ROUTE_TOKENS tokens are one launch.  More are two: the blocks leave their counts, and every block of the second launch
-// adds up the counts in front of its own (blocks^2 * E words out of L2; 16384 tokens, 128 experts: 8 MB).
+// logit's integer has 16 bits and shares a word with its index, which makes one maximum of both.  Up to four logits a lane are sorted
+// first, so that a choice takes a lane's first one and shifts the others up.
+// Grouping: row = first row of the expert + tokens in front that chose it.  A block has up to DIP_ROUTE_TOKENS tokens and a bit set
+// of them per expert, so a rank within the block is a popcount; nothing depends on the order of atomics.  A token per warp of one
+// block is one launch.  More are two: the blocks leave their counts, and every block of the second launch
+// adds up the counts in front of its own (blocks^2 * E words out of L2; 16384 tokens, 128 experts: 8 MB).  Blocks have a token per
+// warp, and four from 128 blocks on, which keeps that in bounds (128 tokens in one block took 10.5 us).
 // Bound by latency for a token, by the trips to memory between the launches for a prompt.
 #include <cuda_bf16.h>
 
@@ -23,7 +24,7 @@ constexpr uint32_t RT_ALL = 0xffffffffu;
 
 struct RouteParams {
     const void *logits;
-    int n_tokens, n_experts, top_k, renormalize;
+    int n_tokens, n_experts, top_k, renormalize, block_tokens;
     int32_t *expert;
     float *weight;
     int32_t *offset, *row_token, *token_row;
@@ -58,6 +59,21 @@ template <bool BF16>
 __device__ __forceinline__ uint32_t unpacked(uint32_t key)
 {
     return !BF16 || key == 0u ? key : (key & 0x80000000u) ? key & 0xffff0000u : key | 0xffffu;
+}
+
+// The greater of two keys first; among equals the lower index (bfloat16 keys have it in them).
+template <bool BF16>
+__device__ __forceinline__ void first_greater(uint32_t &a, uint32_t &b, int &ia, int &ib)
+{
+    const uint32_t hi = max(a, b), lo = min(a, b);
+    if (!BF16) {
+        const bool swap = b > a || (b == a && ib < ia);
+        const int i = ia;
+        ia = swap ? ib : ia;
+        ib = swap ? i : ib;
+    }
+    a = hi;
+    b = lo;
 }
 
 // Tokens t0 + 32 m (m < M, below n) of a block, one warp: experts and weights, and the tokens' bits in the sets of their experts.  M of
@@ -103,11 +119,21 @@ __device__ __forceinline__ void route_tokens(const RouteParams &p, int first, in
     }
     uint32_t mine[M];                             // choice `lane`
     int mine_e[M];
+    int index[M][NV];                             // (BF16: in the keys)
 #pragma unroll
     for (int m = 0; m < M; ++m) {
         mine[m] = 0u;
         mine_e[m] = -1;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) index[m][i] = lane + 32 * i;
+        if (NV == 2) first_greater<BF16>(key[m][0], key[m][NV - 1], index[m][0], index[m][NV - 1]);
+        if (NV == 4) {
+            constexpr int a[5] = {0, 2, 0, 1, 1}, b[5] = {1, 3, 2, 3, 2};
+#pragma unroll
+            for (int q = 0; q < 5; ++q) first_greater<BF16>(key[m][a[q] % NV], key[m][b[q] % NV], index[m][a[q] % NV], index[m][b[q] % NV]);
+        }
     }
+    constexpr bool SORTED = NV <= 4;
     for (int j = 0; j < p.top_k; ++j) {
         unsigned at[M];
 #pragma unroll
@@ -116,8 +142,8 @@ __device__ __forceinline__ void route_tokens(const RouteParams &p, int first, in
             if (!BF16) {
                 at[m] = 0x7fffffffu;
 #pragma unroll
-                for (int i = NV - 1; i >= 0; --i)
-                    if (key[m][i] == most[m]) at[m] = lane + 32 * i;
+                for (int i = SORTED ? 0 : NV - 1; i >= 0; --i)
+                    if (key[m][i] == most[m]) at[m] = index[m][i];
             }
         }
         if (!BF16) {
@@ -131,11 +157,22 @@ __device__ __forceinline__ void route_tokens(const RouteParams &p, int first, in
                 mine[m] = most[m];
                 mine_e[m] = e;
             }
-            most[m] = 0u;
+            if (SORTED) {
+                if ((e & 31) == lane) {                       // (with none left: zeros move up)
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (lane + 32 * i == e) key[m][i] = 0u;
-                most[m] = max(most[m], key[m][i]);
+                    for (int i = 0; i < NV; ++i) {
+                        key[m][i] = i + 1 < NV ? key[m][(i + 1) % NV] : 0u;
+                        index[m][i] = index[m][(i + 1) % NV];
+                    }
+                }
+                most[m] = key[m][0];
+            } else {
+                most[m] = 0u;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (index[m][i] == e) key[m][i] = 0u;
+                    most[m] = max(most[m], key[m][i]);
+                }
             }
         }
 #pragma unroll
@@ -220,7 +257,7 @@ template <int NV, bool BF16>
 __global__ void __launch_bounds__(RT_THREADS, 1) route_choose_kernel(const RouteParams p)
 {
     __shared__ RouteSmem s;
-    const int t0 = blockIdx.x * DIP_ROUTE_TOKENS, n = min(DIP_ROUTE_TOKENS, p.n_tokens - t0);
+    const int t0 = blockIdx.x * p.block_tokens, n = min(p.block_tokens, p.n_tokens - t0);
     route_clear(p, s);
     dip_grid_dependency_wait();
     dip_launch_dependents();
@@ -250,7 +287,7 @@ __global__ void __launch_bounds__(RT_THREADS, 1) route_choose_kernel(const Route
 __global__ void __launch_bounds__(RT_THREADS, 1) route_rows_kernel(const RouteParams p)
 {
     __shared__ RouteSmem s;
-    const int t0 = blockIdx.x * DIP_ROUTE_TOKENS, n = min(DIP_ROUTE_TOKENS, p.n_tokens - t0);
+    const int t0 = blockIdx.x * p.block_tokens, n = min(p.block_tokens, p.n_tokens - t0);
     route_clear(p, s);
     dip_grid_dependency_wait();
     dip_launch_dependents();
@@ -384,9 +421,10 @@ cudaError_t launch_choose(const RouteParams &p, bool bf16, int blocks, cudaStrea
 
 dip_status dip_launch_route(dip_ctx *ctx, const void *logits, bool bf16, bool renormalize, const dip_expert_route &r, cudaStream_t stream)
 {
-    const RouteParams p = {logits, r.n_tokens, r.n_experts, r.top_k, renormalize, r.expert, r.weight, r.offset, r.row_token,
+    const int block_tokens = r.n_tokens <= 128 * RT_WARPS ? RT_WARPS : DIP_ROUTE_TOKENS;
+    const RouteParams p = {logits, r.n_tokens, r.n_experts, r.top_k, renormalize, block_tokens, r.expert, r.weight, r.offset, r.row_token,
                            r.token_row, ctx->route_counts};
-    const int blocks = (r.n_tokens + DIP_ROUTE_TOKENS - 1) / DIP_ROUTE_TOKENS, per_lane = (r.n_experts + 31) / 32;
+    const int blocks = (r.n_tokens + block_tokens - 1) / block_tokens, per_lane = (r.n_experts + 31) / 32;
     const auto choose = per_lane <= 1   ? launch_choose<1>
                         : per_lane <= 2 ? launch_choose<2>
                         : per_lane <= 4 ? launch_choose<4>
