@@ -157,7 +157,7 @@ dip_status dip_create_ex(dip_ctx **out, int device, const dip_options *opt)
     if ((st = dev_alloc(ctx, &ctx->mask_tmp, (size_t)(ctx->max_d / 32))) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->coarse, vec)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->xt, (size_t)ctx->max_d * 32)) != DIP_OK) return fail(st);
-    if ((st = dev_alloc(ctx, &ctx->route_counts, (size_t)DIP_MAX_TOKENS / DIP_ROUTE_TOKENS * DIP_MAX_EXPERTS)) != DIP_OK) return fail(st);
+    if ((st = dev_alloc(ctx, &ctx->route_counts, ((size_t)DIP_MAX_TOKENS / DIP_ROUTE_TOKENS + 1) * DIP_MAX_EXPERTS)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->group_tickets, (size_t)ctx->sm_count)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->status, (size_t)1)) != DIP_OK) return fail(st);
     if ((st = dev_alloc(ctx, &ctx->trace, (size_t)DIP_TRACE_SLOTS * DIP_TRACE_WORDS)) != DIP_OK) return fail(st);

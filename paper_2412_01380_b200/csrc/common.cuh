@@ -14,7 +14,7 @@ constexpr int DIP_TRACE_SLOTS = 1024;
 constexpr uint32_t DIP_MAIL_EMPTY = 0xffffffffu;
 constexpr int DIP_SYNC_WORDS = 2;
 constexpr int DIP_MAIL_FLOATS = 4096;  // boxes per SM: one CTA's segment of sums (INT4: up to 2048, F32 / BF16: 256 per token)
-constexpr int DIP_ROUTE_TOKENS = 128;  // tokens per block of the router
+constexpr int DIP_ROUTE_TOKENS = 128;  // most tokens per block of the router
 constexpr int DIP_GROUP_ROWS = 128, DIP_GROUP_COLS = 256;   // a tile of a grouped product
 constexpr int DIP_TRACE_WORDS = 4;   // first start, dependency ready, last end, auxiliary
 
@@ -55,7 +55,7 @@ struct dip_ctx {
     uint16_t *coarse;    // [max_batch][max_d] top 16 bits of the rank keys of h, left by the gate/up product
     uint16_t *xt;        // [max_d][32] batched decode: per column, the tokens' values as bfloat16 (16 high, 16 low halves)
     int coarse_min_d;    // smallest d_ff for which the step ranks h from those
-    int32_t *route_counts;   // [DIP_MAX_TOKENS / DIP_ROUTE_TOKENS][DIP_MAX_EXPERTS] the router: rows per token block and expert
+    int32_t *route_counts;   // [DIP_MAX_TOKENS / DIP_ROUTE_TOKENS + 1][DIP_MAX_EXPERTS] the router: rows per token block and expert
     unsigned int *group_tickets; // [sm_count] parts of a tile that are there, zero between launches
     int *status;         // sticky device status word (0 = fine)
     int fuse_select;     // single-token F32 / BF16 steps: the products build their own masks

@@ -8,7 +8,8 @@
 // of them per expert, so a rank within the block is a popcount; nothing depends on the order of atomics.  A token per warp of one
 // block is one launch.  More are two: the blocks leave their counts, and every block of the second launch
 // adds up the counts in front of its own (blocks^2 * E words out of L2; 16384 tokens, 128 experts: 8 MB).  Blocks have a token per
-// warp, and four from 128 blocks on, which keeps that in bounds (128 tokens in one block took 10.5 us).
+// warp, and four from 128 blocks on, which keeps that in bounds (128 tokens in one block took 10.5 us, in four 5.3).  From
+// 128 blocks of four on a launch in between does the adding (65536 tokens, 256 experts: 108 us without).
 // Bound by latency for a token, by the trips to memory between the launches for a prompt.
 #include <cuda_bf16.h>
 
@@ -24,7 +25,7 @@ constexpr uint32_t RT_ALL = 0xffffffffu;
 
 struct RouteParams {
     const void *logits;
-    int n_tokens, n_experts, top_k, renormalize, block_tokens;
+    int n_tokens, n_experts, top_k, renormalize, block_tokens, added;
     int32_t *expert;
     float *weight;
     int32_t *offset, *row_token, *token_row;
@@ -284,6 +285,35 @@ __global__ void __launch_bounds__(RT_THREADS, 1) route_choose_kernel(const Route
     route_rows(p, s, t0, n);
 }
 
+// counts[b][e] becomes the sum of those in front of it, and the row behind the last the sum of all.  A block per 32 experts, a lane each;
+// a warp has every 32nd part of the rows.
+__global__ void __launch_bounds__(RT_THREADS, 1) route_add_kernel(const RouteParams p, int blocks)
+{
+    __shared__ int32_t part[RT_WARPS][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane, each = (blocks + RT_WARPS - 1) / RT_WARPS;
+    const int b0 = min(warp * each, blocks), b1 = min(b0 + each, blocks);
+    int32_t *c = p.counts + min(e, DIP_MAX_EXPERTS - 1);
+    dip_grid_dependency_wait();
+    dip_launch_dependents();
+    int sum = 0;
+#pragma unroll 4
+    for (int b = b0; b < b1; ++b) sum += c[(size_t)b * DIP_MAX_EXPERTS];
+    part[warp][lane] = sum;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < RT_WARPS; ++w) {
+        if (w == warp) before = all;
+        all += part[w][lane];
+    }
+    if (e >= p.n_experts) return;
+    for (int b = b0; b < b1; ++b) {
+        const int n = c[(size_t)b * DIP_MAX_EXPERTS];
+        c[(size_t)b * DIP_MAX_EXPERTS] = before;
+        before += n;
+    }
+    if (warp == 0) c[(size_t)blocks * DIP_MAX_EXPERTS] = all;
+}
+
 __global__ void __launch_bounds__(RT_THREADS, 1) route_rows_kernel(const RouteParams p)
 {
     __shared__ RouteSmem s;
@@ -298,7 +328,12 @@ __global__ void __launch_bounds__(RT_THREADS, 1) route_rows_kernel(const RoutePa
     // all blocks' counts, and those in front of this block
     const int width = p.n_experts <= 32 ? 32 : p.n_experts <= 64 ? 64 : p.n_experts <= 128 ? 128 : p.n_experts <= 256 ? 256 : 512;
     const int e = threadIdx.x % width;
-    if (e < p.n_experts) {
+    if (p.added) {
+        if (threadIdx.x < p.n_experts) {
+            s.start[threadIdx.x] = p.counts[(size_t)blockIdx.x * DIP_MAX_EXPERTS + threadIdx.x];
+            s.total[threadIdx.x] = p.counts[(size_t)gridDim.x * DIP_MAX_EXPERTS + threadIdx.x];
+        }
+    } else if (e < p.n_experts) {
         int total = 0, before = 0;
 #pragma unroll 8
         for (int b = threadIdx.x / width; b < (int)gridDim.x; b += RT_THREADS / width) {
@@ -422,15 +457,17 @@ cudaError_t launch_choose(const RouteParams &p, bool bf16, int blocks, cudaStrea
 dip_status dip_launch_route(dip_ctx *ctx, const void *logits, bool bf16, bool renormalize, const dip_expert_route &r, cudaStream_t stream)
 {
     const int block_tokens = r.n_tokens <= 128 * RT_WARPS ? RT_WARPS : DIP_ROUTE_TOKENS;
-    const RouteParams p = {logits, r.n_tokens, r.n_experts, r.top_k, renormalize, block_tokens, r.expert, r.weight, r.offset, r.row_token,
-                           r.token_row, ctx->route_counts};
     const int blocks = (r.n_tokens + block_tokens - 1) / block_tokens, per_lane = (r.n_experts + 31) / 32;
+    const bool add = blocks > 128;
+    const RouteParams p = {logits, r.n_tokens, r.n_experts, r.top_k, renormalize, block_tokens, add, r.expert, r.weight, r.offset, r.row_token,
+                           r.token_row, ctx->route_counts};
     const auto choose = per_lane <= 1   ? launch_choose<1>
                         : per_lane <= 2 ? launch_choose<2>
                         : per_lane <= 4 ? launch_choose<4>
                         : per_lane <= 8 ? launch_choose<8>
                                         : launch_choose<16>;
     DIP_CUDA_TRY(ctx, choose(p, bf16, blocks, stream));
+    if (add) DIP_CUDA_TRY(ctx, dip_launch_pdl(route_add_kernel, dim3(per_lane), dim3(RT_THREADS), 0, stream, p, blocks));
     if (blocks > 1) DIP_CUDA_TRY(ctx, dip_launch_pdl(route_rows_kernel, dim3(blocks), dim3(RT_THREADS), 0, stream, p));
     return DIP_OK;
 }

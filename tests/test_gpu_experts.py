@@ -97,6 +97,26 @@ def test_route_one_expert_takes_all(ctx):
     check_route(ctx, z, 1, True)
 
 
+@pytest.mark.parametrize("tokens,experts,top_k", [(20000, 40, 2), (65536, 8, 1), (16385, 500, 16)])
+def test_route_of_many_tokens(ctx, tokens, experts, top_k):
+    """Many blocks: against a sort (the token by token form takes minutes)."""
+    z = torch.randn((tokens, experts), generator=gen_of(tokens), device="cuda")
+    z[::7] = -math.inf
+    r = dip.ExpertRoute(tokens, experts, top_k, "cuda")
+    dip.dip_route_experts(ctx, z, r)
+    expert = torch.argsort(z, dim=1, descending=True, stable=True)[:, :top_k].int()
+    expert[::7] = -1
+    assert torch.equal(r.expert, expert)
+    key = torch.where(expert < 0, experts, expert).flatten().long()
+    order = torch.argsort(key, stable=True)
+    offset = torch.searchsorted(key[order], torch.arange(experts + 1, device="cuda")).int()
+    assert torch.equal(r.offset, offset)
+    n = int(offset[-1])
+    assert torch.equal(r.row_token[:n], (order // top_k)[:n].int())
+    row = torch.empty_like(order).scatter_(0, order, torch.arange(order.numel(), device="cuda"))
+    assert torch.equal(r.token_row.flatten(), torch.where(key == experts, -1, row).int())
+
+
 def test_route_is_used_again_with_fewer_tokens(ctx):
     r = dip.ExpertRoute(300, 12, 3, "cuda")
     z = torch.randn((300, 12), generator=gen_of(8), device="cuda")
