@@ -620,6 +620,9 @@ __device__ __forceinline__ void take_tile(const GroupedParams &p, GroupedSmem<K>
         for (int j = 0; j < C; ++j) acc[j] = 0.f;
         // (which of the tile's two blocks of weights a group of columns belongs to)
         const bool block0 = !GATED && !SPLIT && share == 1, block1 = GATED || SPLIT || share == 1;
+        // (registers: with 32 columns gate/up keeps some of its own in memory and a prompt's product of 5120 to 17920 takes 476 us instead
+        // of 441; plain products have the room, and take 675 instead of 701)
+        constexpr int L = GATED ? 16 : 32;
         const uint32_t full = smem_u32(&s.sum_full[0][SPLIT ? share : 0]), empty = smem_u32(&s.sum_empty[0][SPLIT ? share : 0]);
         constexpr uint32_t NEXT = sizeof(s.sum_full[0]);             // from one accumulator's barrier to the other's
         for (int left = r.k1 - r.k0; left > 0; left -= GP_SCALE_STEPS, ++groups) {
@@ -635,22 +638,22 @@ __device__ __forceinline__ void take_tile(const GroupedParams &p, GroupedSmem<K>
                 const int buf = n & 1;
                 wait_on(full + buf * NEXT, (n >> 1) & 1, s, p.status, p.wait_limit_ns);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                // one load is under way while the one in front is added
+                // one load is under way while the one in front is added (of L columns)
                 const uint32_t from = lanes + buf * GP_COLS;
-                uint32_t v[2][32];
+                uint32_t v[2][L];
                 tmem_ld(from + col0, v[0]);
 #pragma unroll
-                for (int c = 0; c < C / 32; ++c) {
+                for (int c = 0; c < C / L; ++c) {
                     tmem_wait(v[c & 1]);
-                    if (c + 1 < C / 32) {
-                        tmem_ld(from + (32 * (c + 1) < H ? col0 + 32 * (c + 1) : col1 + 32 * (c + 1) - H), v[(c + 1) & 1]);
+                    if (c + 1 < C / L) {
+                        tmem_ld(from + (L * (c + 1) < H ? col0 + L * (c + 1) : col1 + L * (c + 1) - H), v[(c + 1) & 1]);
                     } else {                         // all of it is in registers
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
                         arrive_first<PAIR>(empty + buf * NEXT, lane);
                     }
 #pragma unroll
-                    for (int j = 0; j < 32; j += 2) fma2(acc[32 * c + j], acc[32 * c + j + 1], v[c & 1][j], v[c & 1][j + 1], 32 * c < H ? s0 : s1);
+                    for (int j = 0; j < L; j += 2) fma2(acc[L * c + j], acc[L * c + j + 1], v[c & 1][j], v[c & 1][j + 1], L * c < H ? s0 : s1);
                 }
             }
             __syncwarp();
