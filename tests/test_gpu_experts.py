@@ -217,6 +217,26 @@ def test_grouped_product_sizes(ctx, wtype, d_in, d_out):
     check_product(ctx, wtype, [3, 0, 17], d_in, d_out, seed=d_in)
 
 
+# few rows per expert, some, and many: one of them a tile and a row more, or a row short of one
+LOADS = {"few": [3, 0, 17], "more_than_a_tile_of_few": [1, 64, 0, 65, 2], "some": [70, 0, 90], "some_uneven": [129, 1, 30],
+         "many": [400, 0, 250], "many_uneven": [256, 255, 513, 1, 0, 700]}
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("wtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("name", list(LOADS))
+@pytest.mark.parametrize("d_in,d_out", [(8192, 352), (1056, 1184)])
+def test_grouped_product_loads(ctx, wtype, name, d_in, d_out, dtype):
+    """Long inputs are cut along K: the tiles' parts meet."""
+    check_product(ctx, wtype, LOADS[name], d_in, d_out, dtype, extra=2)
+
+
+@pytest.mark.parametrize("wtype", ["bf16", "fp8"])
+def test_more_tiles_than_fit_at_once(ctx, wtype):
+    check_product(ctx, wtype, [500, 20, 900, 0, 130], 160, 5216)
+    check_product(ctx, wtype, [1, 2, 0, 1] * 16, 96, 5120)
+
+
 @pytest.mark.parametrize("wtype", ["bf16", "fp8"])
 @pytest.mark.parametrize("rows", [1, 2, 31, 33, 200, 1000])
 def test_dense_product(ctx, wtype, rows):
@@ -284,6 +304,13 @@ def test_gate_up_groups(ctx, wtype, name):
 @pytest.mark.parametrize("d_in,d_out", [(32, 32), (64, 96), (1056, 128), (4096, 160), (256, 2816)])
 def test_gate_up_sizes(ctx, wtype, d_in, d_out):
     check_gate_up(ctx, wtype, [2, 0, 40], d_in, d_out, seed=d_out)
+
+
+@pytest.mark.parametrize("wtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("name", list(LOADS))
+@pytest.mark.parametrize("d_in,d_out", [(8192, 160), (288, 1440)])
+def test_gate_up_loads(ctx, wtype, name, d_in, d_out):
+    check_gate_up(ctx, wtype, LOADS[name], d_in, d_out)
 
 
 @pytest.mark.parametrize("wtype", ["bf16", "fp8"])
@@ -411,6 +438,88 @@ def test_same_bits_again_on_another_stream_and_from_a_graph(ctx, wtype, tokens):
     y.zero_()
     call()
     assert torch.equal(y, again) and not torch.equal(y, first)
+
+
+@pytest.mark.parametrize("wtype", ["bf16", "fp8"])
+def test_two_contexts_at_once(ctx, wtype):
+    """Each context has its own workspace: products whose tiles are cut, side by side on two streams."""
+    g = gen_of(14)
+    m = dip.GroupedMatrix(*eu.matrix(g, wtype == "fp8", 4, 416, 8192))
+    rows = [dip.Rows.of(*eu.rows_of(g, wtype == "fp8", 40, 8192)) for _ in range(2)]
+    o = eu.offsets([5, 30, 0, 5])
+    alone = []
+    for r in rows:
+        y = torch.zeros((40, 416), device="cuda", dtype=torch.bfloat16)
+        dip.dip_grouped_product(ctx, m, r, y, offset=o)
+        alone.append(y)
+    other = dip.Context(0)
+    torch.cuda.synchronize()
+    streams, both = [torch.cuda.Stream() for _ in range(2)], [torch.zeros_like(y) for y in alone]
+    for _ in range(20):
+        for s, c, r, y in zip(streams, (ctx, other), rows, both):
+            with torch.cuda.stream(s):
+                dip.dip_grouped_product(c, m, r, y, offset=o)
+    torch.cuda.synchronize()
+    assert other.device_status() == dip.DEVICE_OK
+    other.close()
+    for a, b in zip(alone, both):
+        assert torch.equal(a, b)
+
+
+def test_two_graphs_of_one_context(ctx):
+    """They share its workspace and run one after the other."""
+    g = gen_of(15)
+    w = [weights(g, fp8, 8, 256, 2080)[3] for fp8 in (False, True)]
+    x = torch.randn((9, 256), generator=g, device="cuda").bfloat16()
+    z = torch.randn((9, 8), generator=g, device="cuda")
+    route = [dip.ExpertRoute(9, 8, 3, "cuda") for _ in w]
+    work, y = [dip.ExpertWork(9, 3, v, "cuda") for v in w], [torch.zeros_like(x) for _ in w]
+
+    def call(i):
+        dip.dip_route_experts(ctx, z, route[i])
+        dip.dip_expert_mlp(ctx, w[i], x, work[i], y[i], route=route[i])
+
+    graphs = []
+    for i in range(2):
+        call(i)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            call(i)
+    want = [v.clone() for v in y]
+    for i in (0, 1, 1, 0, 1):
+        y[i].zero_()
+        graphs[i].replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y[0], want[0]) and torch.equal(y[1], want[1])
+
+
+def test_a_prompt_and_then_decode_steps(ctx):
+    """A model's use: its prompt goes through the dense block at once, its tokens step by step through the packed one, on one
+    context.  A step that keeps every column is the same block; its h stays binary32, the dense block's is rounded once."""
+    d_model, d_ff, g = 512, 1376, gen_of(16)
+    gate, up = (torch.randn((d_ff, d_model), generator=g, device="cuda").mul_(0.05).bfloat16() for _ in range(2))
+    down = torch.randn((d_model, d_ff), generator=g, device="cuda").mul_(0.05).bfloat16()
+    packed = dip.dip_pack_weights(ctx, dip.W_BF16, d_model, d_ff, gate, up, down)
+    w = dip.ExpertWeights(*(dip.GroupedMatrix(m) for m in (gate, up, down)))
+    x = torch.randn((40, d_model), generator=g, device="cuda").bfloat16()
+    y = torch.zeros_like(x)
+    dip.dip_expert_mlp(ctx, w, x, dip.ExpertWork(40, 0, w, "cuda"), y)
+    steps = torch.zeros((40, d_model), device="cuda")
+    for t in range(0, 40, 8):
+        dip.dip_mlp_step(ctx, packed, x[t].float(), d_model, d_ff, 1.0, None, None, steps[t])
+        dip.dip_mlp_step(ctx, packed, x[t + 1:t + 8].float(), d_model, d_ff, 1.0, None, None, steps[t + 1:t + 8])
+    h = x.double() @ gate.double().t()
+    h = h * torch.sigmoid(h) * (x.double() @ up.double().t())
+    want = h @ down.double().t()
+    mass = h.abs() @ down.double().abs().t()
+    # half a step of h, half a step of y, and binary32 sums over d_model and d_ff
+    eu.assert_within(y, want, mass * (2.0 ** -8 + 2.0 ** -11) + want.abs() * 2.0 ** -8, "prompt")
+    # (a batch stands for each value by two bfloat16: 2^-16)
+    eu.assert_within(steps, want, mass * 2.0 ** -11, "steps")
+    again = torch.zeros_like(x)
+    dip.dip_expert_mlp(ctx, w, x, dip.ExpertWork(40, 0, w, "cuda"), again)
+    assert torch.equal(y, again)
 
 
 # ---- refusals that need a context --------------------------------------------------------------------------------------
