@@ -39,7 +39,9 @@ constexpr int GP_BOX = 32;                          // rows per copy of the rows
 constexpr int GP_A_BYTES = GP_ROWS * GP_STEP_BYTES, GP_B_BYTES = GP_COLS * GP_STEP_BYTES;
 constexpr int GP_TMEM_COLS = 512;
 constexpr int GP_MIN_STEPS = 4;                     // a part of a tile has at least so many
-constexpr int GP_JOIN_FEW = 8, GP_JOIN = 20;        // steps' worth of time that a cut tile's parts take to meet (few rows; others)
+// Steps' worth of time that a cut tile's parts take to meet: written, counted, read and added (7 us for a tile of 128 rows; 3.5 us for one row,
+// and as many steps more as there are rows.  8 rows each for 16 experts, 4096 to 2048: 50.7 us with whole tiles, 56.5 cut).
+constexpr int GP_JOIN_FEW = 8, GP_JOIN = 20;
 constexpr int GP_TWO_RUNS = 6;                      // steps' worth of time that a block loses between two runs
 constexpr int GP_SCALE_STEPS = 8, GP_SCALE_SLOTS = 4;   // steps of scales that come together, and how many such groups there is room for
 constexpr int GP_FEW = 64;                          // rows of a tile that are columns of its sums
@@ -59,14 +61,14 @@ template <bool FP8_, bool GATED_, int MODE> struct Kind {
     // Warps that take sums out.  FP8 keeps a tile's sums in registers over all steps, and two warps per scheduler with 128 of them
     // each can have two loads of 32 accumulator columns in hand; BF16 only has to get rid of a tile.
     static constexpr int OUT_WARPS = FP8 || FEW ? 8 : 16, THREADS = (4 + OUT_WARPS) * 32;
-    // registers of a thread of the first four warps and of the others; in all what the launch has: (56 + 2 * 224) / 3 = (40 + 2 * 232) / 3 = 168 each, or
-    // (64 + 4 * 104) / 5 = 96
+    // registers of a thread of the first four warps and of the others; in all what the launch has:
+    // (56 + 2 * 224) / 3 = (40 + 2 * 232) / 3 = 168 each, or (64 + 4 * 104) / 5 = 96
     static constexpr int REGS_FEW = FP8 ? (PAIR ? 56 : 40) : 64, REGS_MANY = FP8 ? (PAIR ? 224 : 232) : 104;
 };
 
 struct GroupedParams {
     const float *w_scales, *up_scales, *row_scales;
-    int n_experts, d_out, d_in, n_rows, steps, n_cols;
+    int n_experts, d_out, d_in, n_rows, steps, n_cols, join;
     const int32_t *offset;
     void *out;
     float *out_scales;
@@ -309,7 +311,7 @@ struct Schedule {
         // runs within one tile each, where that makes them hardly longer: a block with two has a tile's end in the middle of its steps
         const int each = rest ? parts / rest : 1;
         if (parts > rest && (p.steps + each - 1) / each <= units / parts + GP_TWO_RUNS) parts = rest * each;
-        if (parts > rest && units / parts + (K::FEW ? GP_JOIN_FEW : GP_JOIN) >= p.steps) parts = rest;      // (they stay whole)
+        if (parts > rest && units / parts + p.join >= p.steps) parts = rest;      // (they stay whole)
         s.whole = whole;
         s.units = units;
         s.parts = parts;
@@ -421,8 +423,7 @@ __device__ __forceinline__ bool part_is_last(const GroupedParams &p, GroupedSmem
     return s.last != 0;
 }
 
-// The sums of a tile of few rows and what becomes of them: thread = output, values = rows.
-// Each four warps have a share of the rows; plain: the first or the second 128 outputs of a share; gate/up: a thread has gate and up of
+// The sums of a tile of few rows and what becomes of them: thread = output, values = rows.  Each four warps have a share of the rows; plain: the first or the second 128 outputs of a share; gate/up: a thread has gate and up of
 // its output.
 template <class K>
 __device__ __forceinline__ void take_few(const GroupedParams &p, GroupedSmem<K> &s, const Schedule<K> &plan, const Run &r, uint32_t lanes,
@@ -1055,8 +1056,12 @@ cudaError_t launch(int mode, dip_ctx *ctx, int ctas, cudaStream_t stream, const 
 
 }  // namespace
 
-// Few up to, and pairs from this many rows per expert on (the average over as many experts as can have any).
-constexpr int GP_FEW_UP_TO = 32, GP_PAIR_ROWS = 192;
+// Few up to, and pairs from this many rows per expert on (the average over as many experts as can have any).  In us, few / whole tiles:
+// 8 rows for each of 32 experts, 1024 to 1024, 18.8 / 19.3 (8-bit 10.2 / 11.5), 32 rows 20.3 / 19.8 (12.9 / 11.7); one expert, 4096 to 5120, 8 rows
+// 18.3 / 26.9 (16.2 / 22.0), 24 rows 29.0 / 25.6 (24.8 / 22.8).  Whole tiles / pairs: 100 rows for each of 64 experts, gate/up of 2048 to 1408, 139 / 164;
+// 16 experts, 4096 to 4096, 150 rows 116 / 123, 200 rows 149 / 145; 1024 rows for each of 8, gate/up of 4096 to 14336, 1648 / 1430 (8-bit
+// 1304 / 1255).
+constexpr int GP_FEW_UP_TO = 12, GP_PAIR_ROWS = 192;
 
 dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const dip_grouped_matrix *up, const void *rows,
                               const float *row_scales, int n_rows, const int32_t *offset, void *out, bool out_f32, float *out_scales,
@@ -1085,6 +1090,7 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
     p.n_rows = n_rows;
     p.steps = (w.d_in * (fp8 ? 1 : 2) + GP_STEP_BYTES - 1) / GP_STEP_BYTES;
     p.n_cols = (w.d_out + width - 1) / width;
+    p.join = mode == GP_FEW_ROWS ? GP_JOIN_FEW + n_rows / met : GP_JOIN;
     p.offset = offset;
     p.out = out;
     p.out_scales = out_scales;

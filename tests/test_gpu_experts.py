@@ -218,7 +218,7 @@ def test_grouped_product_sizes(ctx, wtype, d_in, d_out):
 
 
 # few rows per expert, some, and many: one of them a tile and a row more, or a row short of one
-LOADS = {"few": [3, 0, 17], "more_than_a_tile_of_few": [1, 64, 0, 65, 2], "some": [70, 0, 90], "some_uneven": [129, 1, 30],
+LOADS = {"few": [3, 0, 17], "few_uneven": [130, 0, 3, 0, 0, 1, 0, 0, 0, 0, 0, 2], "more_than_a_tile_of_few": [1, 64, 0, 65, 2], "some": [70, 0, 90], "some_uneven": [129, 1, 30],
          "many": [400, 0, 250], "many_uneven": [256, 255, 513, 1, 0, 700]}
 
 
