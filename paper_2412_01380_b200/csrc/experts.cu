@@ -28,6 +28,15 @@ bool rows_ok(int wtype, const void *rows, const float *scales)
     return !bad(rows) && (wtype == DIP_W_FP8_B128 ? !bad(scales) : !scales);
 }
 
+// What a call reads and what it writes share memory.
+bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + b_bytes && y < x + a_bytes;
+}
+
+size_t row_bytes(int wtype, int n, int d) { return (size_t)n * d * (wtype == DIP_W_FP8_B128 ? 1 : 2); }
+
 bool n_rows_ok(int n) { return n >= 1 && n <= DIP_MAX_TOKENS * DIP_MAX_TOP_K; }
 
 bool same_shape(const dip_grouped_matrix *a, const dip_grouped_matrix *b)
@@ -52,6 +61,8 @@ dip_status dip_stage_rows(dip_ctx *ctx, const void *x, int n_tokens, int d, cons
     if (!dip_ctx_current(ctx) || bad(x) || n_tokens < 1 || n_tokens > DIP_MAX_TOKENS || !width_ok(d)) return DIP_ERR_INVALID_ARG;
     if ((wtype != DIP_W_BF16 && wtype != DIP_W_FP8_B128) || !rows_ok(wtype, rows, scales)) return DIP_ERR_INVALID_ARG;
     if (route && (!route_ok(route) || route->n_tokens != n_tokens)) return DIP_ERR_INVALID_ARG;
+    if (overlap(x, row_bytes(DIP_W_BF16, n_tokens, d), rows, row_bytes(wtype, route ? n_tokens * route->top_k : n_tokens, d)))
+        return DIP_ERR_INVALID_ARG;
     return dip_launch_stage_rows(ctx, x, n_tokens, d, route, wtype == DIP_W_FP8_B128, rows, scales, (cudaStream_t)stream);
 }
 
@@ -61,6 +72,7 @@ dip_status dip_grouped_product(dip_ctx *ctx, const dip_grouped_matrix *w, const 
     if (!dip_ctx_current(ctx) || !matrix_ok(w) || !rows_ok(w->wtype, rows, row_scales) || !n_rows_ok(n_rows) || bad(y))
         return DIP_ERR_INVALID_ARG;
     if (offset ? !dip_aligned16(offset) : w->n_experts != 1) return DIP_ERR_INVALID_ARG;
+    if (overlap(rows, row_bytes(w->wtype, n_rows, w->d_in), y, (size_t)n_rows * w->d_out * (y_f32 ? 4 : 2))) return DIP_ERR_INVALID_ARG;
     return dip_launch_grouped(ctx, *w, nullptr, rows, row_scales, n_rows, offset, y, y_f32 != 0, nullptr, (cudaStream_t)stream);
 }
 
@@ -70,6 +82,7 @@ dip_status dip_grouped_gate_up(dip_ctx *ctx, const dip_grouped_matrix *gate, con
     if (!dip_ctx_current(ctx) || !matrix_ok(gate) || !matrix_ok(up) || !same_shape(gate, up)) return DIP_ERR_INVALID_ARG;
     if (!rows_ok(gate->wtype, rows, row_scales) || !rows_ok(gate->wtype, h, h_scales) || !n_rows_ok(n_rows)) return DIP_ERR_INVALID_ARG;
     if (offset ? !dip_aligned16(offset) : gate->n_experts != 1) return DIP_ERR_INVALID_ARG;
+    if (overlap(rows, row_bytes(gate->wtype, n_rows, gate->d_in), h, row_bytes(gate->wtype, n_rows, gate->d_out))) return DIP_ERR_INVALID_ARG;
     return dip_launch_grouped(ctx, *gate, up, rows, row_scales, n_rows, offset, h, false, h_scales, (cudaStream_t)stream);
 }
 
@@ -97,6 +110,11 @@ dip_status dip_expert_mlp(dip_ctx *ctx, const dip_grouped_matrix *gate, const di
         return DIP_ERR_INVALID_ARG;
     const cudaStream_t s = (cudaStream_t)stream;
     const int n_rows = route ? n_tokens * route->top_k : n_tokens;
+    const size_t x_bytes = row_bytes(DIP_W_BF16, n_tokens, d), h_bytes = row_bytes(wtype, n_rows, gate->d_out);
+    if ((staged && overlap(x, x_bytes, work->rows, row_bytes(wtype, n_rows, d))) ||
+        overlap(work->h, h_bytes, staged ? work->rows : x, row_bytes(wtype, n_rows, d)) ||
+        overlap(work->h, h_bytes, route ? (const void *)work->out : y, (size_t)n_rows * d * (route ? 4 : 2)))
+        return DIP_ERR_INVALID_ARG;
     const int32_t *offset = route ? route->offset : nullptr;
     dip_status st = DIP_OK;
     if (staged && (st = dip_launch_stage_rows(ctx, x, n_tokens, d, route, fp8, work->rows, work->row_scales, s)) != DIP_OK) return st;

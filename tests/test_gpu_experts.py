@@ -540,6 +540,11 @@ def test_refused_calls_launch_nothing(ctx):
     for out in (y[:4], y.half(), y.t(), torch.zeros((5, 32), device="cuda", dtype=torch.bfloat16), y.cpu()):
         with pytest.raises(dip.DipError):
             dip.dip_grouped_product(ctx, m, rows, out, offset=o)
+    square = dip.GroupedMatrix(eu.matrix(g, False, 1, 96, 96)[0])
+    with pytest.raises(dip.DipError):                              # in place: rows that others still read
+        dip.dip_grouped_product(ctx, square, rows, rows.values)
+    with pytest.raises(dip.DipError):
+        dip.dip_stage_rows(ctx, rows.values, rows)
     with pytest.raises(dip.DipError):                              # 48 columns: no multiple of 32
         narrow = dip.GroupedMatrix(torch.zeros((2, 64, 48), device="cuda", dtype=torch.bfloat16))
         dip.dip_grouped_product(ctx, narrow, dip.Rows.of(torch.zeros((5, 48), device="cuda", dtype=torch.bfloat16)), y, offset=o)
