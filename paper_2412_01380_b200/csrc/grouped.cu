@@ -998,7 +998,7 @@ using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t,
                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// The driver's encoder, looked up once (the library does not link against libcuda).
+// The CUDA driver's encoder, looked up once (the library does not link against libcuda).
 EncodeTiled encoder()
 {
     static const EncodeTiled fn = [] {
@@ -1030,6 +1030,13 @@ cudaError_t launch(dip_ctx *ctx, int ctas, cudaStream_t stream, const CUtensorMa
     const auto kernel = grouped_kernel<K>;
     const size_t smem = sizeof(GroupedSmem<K>) + 1024;
     static_assert(sizeof(GroupedSmem<K>) + 1024 <= 227 * 1024, "fits a CTA's shared memory");
+    // (the warps that take sums out would wait for ever for registers that the launch does not have)
+    static const bool enough = [&] {
+        cudaFuncAttributes a;
+        return K::FEW || (cudaFuncGetAttributes(&a, kernel) == cudaSuccess &&
+                          a.numRegs * (4 + K::OUT_WARPS) >= K::REGS_FEW * 4 + K::REGS_MANY * K::OUT_WARPS);
+    }();
+    if (!enough) return cudaErrorLaunchOutOfResources;
     const cudaError_t e = dip_raise_smem_limit(once, ctx->device, kernel, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
