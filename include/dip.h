@@ -589,7 +589,8 @@ dip_status dip_sparse_gemv_down_noalloc(const dip_mlp_weights *w, const float *h
  * (offset [n_experts + 1], device int32, not decreasing, offset[0] = 0; an offset below
  * one in front of it counts as that one, what lies outside [0, n_rows] is cut off).  Rows behind offset[n_experts] are not
  * read and not written.  offset == NULL: one expert, and all rows are its own.
- * What a product reads and what it writes must not overlap (DIP_ERR_INVALID_ARG).
+ * What a call writes must not overlap what it reads (rows, scales, weights, offsets, routes) or what else it writes
+ * (DIP_ERR_INVALID_ARG); dip_expert_mlp may write over a buffer that is used up by then, so y may be x.
  *
  * Weights are the matrices as checkpoints have them, row-major
  * [n_experts][d_out][d_in]; d_out and d_in are multiples of 32, at least 32 and at

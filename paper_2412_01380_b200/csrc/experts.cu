@@ -1,4 +1,6 @@
 // C ABI of the router, the grouped products and the expert block (include/dip.h): argument validation and composition.
+#include <initializer_list>
+
 #include "common.cuh"
 
 namespace {
@@ -28,14 +30,77 @@ bool rows_ok(int wtype, const void *rows, const float *scales)
     return !bad(rows) && (wtype == DIP_W_FP8_B128 ? !bad(scales) : !scales);
 }
 
-// What a call reads and what it writes share memory.
-bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+// A call's buffer; NULL: it has none.
+struct Range {
+    const void *p;
+    size_t bytes;
+};
+
+bool meet(const Range &a, const Range &b)
 {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return x < y + b_bytes && y < x + a_bytes;
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
 }
 
+// Whether what is written shares memory with what is read.
+bool over(std::initializer_list<Range> written, std::initializer_list<Range> read)
+{
+    for (const Range &w : written)
+        for (const Range &r : read)
+            if (meet(w, r)) return true;
+    return false;
+}
+
+// The same, or with something else that is written.
+bool clash(std::initializer_list<Range> written, std::initializer_list<Range> read)
+{
+    for (const Range *w = written.begin(); w != written.end(); ++w)
+        for (const Range *o = written.begin(); o != w; ++o)
+            if (meet(*w, *o)) return true;
+    return over(written, read);
+}
+
+size_t blocks(int d) { return ((size_t)d + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK; }
 size_t row_bytes(int wtype, int n, int d) { return (size_t)n * d * (wtype == DIP_W_FP8_B128 ? 1 : 2); }
+Range row_scales_of(const float *scales, int n, int d) { return {scales, (size_t)n * blocks(d) * sizeof(float)}; }
+
+Range values_of(const dip_grouped_matrix *w)
+{
+    return {w ? w->values : nullptr, w ? (size_t)w->n_experts * row_bytes(w->wtype, w->d_out, w->d_in) : 0};
+}
+Range scales_of(const dip_grouped_matrix *w)
+{
+    return {w ? w->scales : nullptr, w ? (size_t)w->n_experts * blocks(w->d_out) * blocks(w->d_in) * sizeof(float) : 0};
+}
+
+size_t choice_bytes(const dip_expert_route *r) { return r ? (size_t)r->n_tokens * r->top_k * 4 : 0; }
+Range offset_of(const int32_t *offset, int n_experts) { return {offset, ((size_t)n_experts + 1) * sizeof(int32_t)}; }
+
+// Of one launch each: its blocks run in any order, so what one of them writes may still be read (or written) by others.
+bool stage_clash(const void *x, int n_tokens, int d, const dip_expert_route *r, int wtype, const void *rows, const float *scales)
+{
+    const int n = r ? n_tokens * r->top_k : n_tokens;
+    const size_t c = choice_bytes(r);
+    return clash({{rows, row_bytes(wtype, n, d)}, row_scales_of(scales, n, d)},
+                 {{x, row_bytes(DIP_W_BF16, n_tokens, d)}, {r ? r->expert : nullptr, c}, {r ? r->weight : nullptr, c},
+                  offset_of(r ? r->offset : nullptr, r ? r->n_experts : 0), {r ? r->row_token : nullptr, c}, {r ? r->token_row : nullptr, c}});
+}
+
+bool product_clash(const dip_grouped_matrix *w, const dip_grouped_matrix *up, const void *rows, const float *row_scales, int n,
+                   const int32_t *offset, const void *out, size_t out_bytes, const float *out_scales)
+{
+    return clash({{out, out_bytes}, row_scales_of(out_scales, n, w->d_out)},
+                 {{rows, row_bytes(w->wtype, n, w->d_in)}, row_scales_of(row_scales, n, w->d_in), values_of(w), scales_of(w),
+                  values_of(up), scales_of(up), offset_of(offset, w->n_experts)});
+}
+
+bool combine_clash(const float *rows, const dip_expert_route *r, int d, const void *y)
+{
+    const size_t c = choice_bytes(r);
+    return over({{y, row_bytes(DIP_W_BF16, r->n_tokens, d)}},
+                {{rows, (size_t)r->n_tokens * r->top_k * d * sizeof(float)}, {r->expert, c}, {r->weight, c}, offset_of(r->offset, r->n_experts),
+                 {r->row_token, c}, {r->token_row, c}});
+}
 
 bool n_rows_ok(int n) { return n >= 1 && n <= DIP_MAX_TOKENS * DIP_MAX_TOP_K; }
 
@@ -52,6 +117,10 @@ dip_status dip_route_experts(dip_ctx *ctx, const void *logits, int logits_bf16, 
                              void *stream)
 {
     if (!dip_ctx_current(ctx) || bad(logits) || !route_ok(route)) return DIP_ERR_INVALID_ARG;
+    const size_t c = choice_bytes(route);
+    if (clash({{route->expert, c}, {route->weight, c}, offset_of(route->offset, route->n_experts), {route->row_token, c}, {route->token_row, c}},
+              {{logits, (size_t)route->n_tokens * route->n_experts * (logits_bf16 ? 2 : 4)}}))
+        return DIP_ERR_INVALID_ARG;
     return dip_launch_route(ctx, logits, logits_bf16 != 0, renormalize != 0, *route, (cudaStream_t)stream);
 }
 
@@ -61,8 +130,7 @@ dip_status dip_stage_rows(dip_ctx *ctx, const void *x, int n_tokens, int d, cons
     if (!dip_ctx_current(ctx) || bad(x) || n_tokens < 1 || n_tokens > DIP_MAX_TOKENS || !width_ok(d)) return DIP_ERR_INVALID_ARG;
     if ((wtype != DIP_W_BF16 && wtype != DIP_W_FP8_B128) || !rows_ok(wtype, rows, scales)) return DIP_ERR_INVALID_ARG;
     if (route && (!route_ok(route) || route->n_tokens != n_tokens)) return DIP_ERR_INVALID_ARG;
-    if (overlap(x, row_bytes(DIP_W_BF16, n_tokens, d), rows, row_bytes(wtype, route ? n_tokens * route->top_k : n_tokens, d)))
-        return DIP_ERR_INVALID_ARG;
+    if (stage_clash(x, n_tokens, d, route, wtype, rows, scales)) return DIP_ERR_INVALID_ARG;
     return dip_launch_stage_rows(ctx, x, n_tokens, d, route, wtype == DIP_W_FP8_B128, rows, scales, (cudaStream_t)stream);
 }
 
@@ -72,7 +140,8 @@ dip_status dip_grouped_product(dip_ctx *ctx, const dip_grouped_matrix *w, const 
     if (!dip_ctx_current(ctx) || !matrix_ok(w) || !rows_ok(w->wtype, rows, row_scales) || !n_rows_ok(n_rows) || bad(y))
         return DIP_ERR_INVALID_ARG;
     if (offset ? !dip_aligned16(offset) : w->n_experts != 1) return DIP_ERR_INVALID_ARG;
-    if (overlap(rows, row_bytes(w->wtype, n_rows, w->d_in), y, (size_t)n_rows * w->d_out * (y_f32 ? 4 : 2))) return DIP_ERR_INVALID_ARG;
+    if (product_clash(w, nullptr, rows, row_scales, n_rows, offset, y, (size_t)n_rows * w->d_out * (y_f32 ? 4 : 2), nullptr))
+        return DIP_ERR_INVALID_ARG;
     return dip_launch_grouped(ctx, *w, nullptr, rows, row_scales, n_rows, offset, y, y_f32 != 0, nullptr, (cudaStream_t)stream);
 }
 
@@ -82,13 +151,15 @@ dip_status dip_grouped_gate_up(dip_ctx *ctx, const dip_grouped_matrix *gate, con
     if (!dip_ctx_current(ctx) || !matrix_ok(gate) || !matrix_ok(up) || !same_shape(gate, up)) return DIP_ERR_INVALID_ARG;
     if (!rows_ok(gate->wtype, rows, row_scales) || !rows_ok(gate->wtype, h, h_scales) || !n_rows_ok(n_rows)) return DIP_ERR_INVALID_ARG;
     if (offset ? !dip_aligned16(offset) : gate->n_experts != 1) return DIP_ERR_INVALID_ARG;
-    if (overlap(rows, row_bytes(gate->wtype, n_rows, gate->d_in), h, row_bytes(gate->wtype, n_rows, gate->d_out))) return DIP_ERR_INVALID_ARG;
+    if (product_clash(gate, up, rows, row_scales, n_rows, offset, h, row_bytes(gate->wtype, n_rows, gate->d_out), h_scales))
+        return DIP_ERR_INVALID_ARG;
     return dip_launch_grouped(ctx, *gate, up, rows, row_scales, n_rows, offset, h, false, h_scales, (cudaStream_t)stream);
 }
 
 dip_status dip_combine_rows(dip_ctx *ctx, const float *rows, const dip_expert_route *route, int d, void *y, void *stream)
 {
-    if (!dip_ctx_current(ctx) || bad(rows) || bad(y) || !route_ok(route) || !width_ok(d)) return DIP_ERR_INVALID_ARG;
+    if (!dip_ctx_current(ctx) || bad(rows) || bad(y) || !route_ok(route) || !width_ok(d) || combine_clash(rows, route, d, y))
+        return DIP_ERR_INVALID_ARG;
     return dip_launch_combine_rows(ctx, rows, *route, d, y, (cudaStream_t)stream);
 }
 
@@ -110,12 +181,22 @@ dip_status dip_expert_mlp(dip_ctx *ctx, const dip_grouped_matrix *gate, const di
         return DIP_ERR_INVALID_ARG;
     const cudaStream_t s = (cudaStream_t)stream;
     const int n_rows = route ? n_tokens * route->top_k : n_tokens;
-    const size_t x_bytes = row_bytes(DIP_W_BF16, n_tokens, d), h_bytes = row_bytes(wtype, n_rows, gate->d_out);
-    if ((staged && overlap(x, x_bytes, work->rows, row_bytes(wtype, n_rows, d))) ||
-        overlap(work->h, h_bytes, staged ? work->rows : x, row_bytes(wtype, n_rows, d)) ||
-        overlap(work->h, h_bytes, route ? (const void *)work->out : y, (size_t)n_rows * d * (route ? 4 : 2)))
-        return DIP_ERR_INVALID_ARG;
     const int32_t *offset = route ? route->offset : nullptr;
+    // each launch by itself, and what an early one writes with what a later one reads; a buffer that is used up may be written again
+    // (y over x, say)
+    const void *rows = staged ? work->rows : x, *last = route ? (const void *)work->out : y;
+    const float *row_scales = fp8 ? work->row_scales : nullptr;
+    const size_t c = choice_bytes(route), y_bytes = row_bytes(DIP_W_BF16, n_tokens, d), last_bytes = (size_t)n_rows * d * (route ? 4 : 2);
+    if ((staged && stage_clash(x, n_tokens, d, route, wtype, work->rows, row_scales)) ||
+        product_clash(gate, up, rows, row_scales, n_rows, offset, work->h, row_bytes(wtype, n_rows, gate->d_out), work->h_scales) ||
+        product_clash(down, nullptr, work->h, work->h_scales, n_rows, offset, last, last_bytes, nullptr) ||
+        (route && combine_clash(work->out, route, d, y)) ||
+        over({{staged ? work->rows : nullptr, row_bytes(wtype, n_rows, d)}, row_scales_of(row_scales, n_rows, d),
+              {work->h, row_bytes(wtype, n_rows, gate->d_out)}, row_scales_of(work->h_scales, n_rows, gate->d_out), {last, last_bytes}, {y, y_bytes}},
+             {values_of(gate), scales_of(gate), values_of(up), scales_of(up), values_of(down), scales_of(down),
+              {route ? route->expert : nullptr, c}, {route ? route->weight : nullptr, c}, {route ? route->row_token : nullptr, c},
+              {route ? route->token_row : nullptr, c}, offset_of(offset, gate->n_experts)}))
+        return DIP_ERR_INVALID_ARG;
     dip_status st = DIP_OK;
     if (staged && (st = dip_launch_stage_rows(ctx, x, n_tokens, d, route, fp8, work->rows, work->row_scales, s)) != DIP_OK) return st;
     if ((st = dip_launch_grouped(ctx, *gate, up, staged ? work->rows : x, work->row_scales, n_rows, offset, work->h, false,

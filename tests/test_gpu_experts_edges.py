@@ -1,0 +1,79 @@
+"""Uses of the router, the grouped products and the expert block at the edge of what a call takes: buffers that share memory."""
+import pytest
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no CUDA device", allow_module_level=True)
+
+import paper_2412_01380_b200 as dip
+import expert_util as eu
+
+pytestmark = pytest.mark.gpu
+WTYPES = {"bf16": dip.W_BF16, "fp8": dip.W_FP8_B128}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = dip.Context(0)
+    yield c
+    assert c.device_status() == dip.DEVICE_OK
+    c.close()
+
+
+def gen_of(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def block(g, fp8, experts, d_model, d_ff):
+    gate, up = (dip.GroupedMatrix(*eu.matrix(g, fp8, experts, d_ff, d_model)) for _ in range(2))
+    return dip.ExpertWeights(gate, up, dip.GroupedMatrix(*eu.matrix(g, fp8, experts, d_model, d_ff)))
+
+
+def test_calls_that_write_what_they_read_are_refused(ctx):
+    g = gen_of(1)
+    w = block(g, True, 3, 256, 256)
+    rows, h = dip.Rows.of(*eu.rows_of(g, True, 9, 256)), dip.Rows(9, 256, dip.W_FP8_B128, "cuda")
+    h.values.view(torch.uint8).fill_(3)
+    o, scales = eu.offsets([4, 0, 5]), rows.scales.clone()
+
+    def refused(fn, *args, **kw):
+        with pytest.raises(dip.DipError) as e:
+            fn(ctx, *args, **kw)
+        assert e.value.status == dip.ERR_INVALID_ARG
+
+    # an 8-bit h whose scales, or whose codes, are where the rows' scales are (256 to 256: they have the same shape)
+    same = dip.Rows.of(h.values, rows.scales)
+    refused(dip.dip_grouped_gate_up, w.gate, w.up, rows, same, offset=o)
+    both = torch.zeros(9 * 256 + 64, dtype=torch.uint8, device="cuda")
+    codes, their = both[:9 * 256].view(torch.float8_e4m3fn).view(9, 256), both[9 * 256 - 16:9 * 256 + 56].view(torch.float32).view(9, 2)
+    refused(dip.dip_grouped_gate_up, w.gate, w.up, dip.Rows.of(rows.values, their), dip.Rows.of(codes, h.scales), offset=o)
+    # weighted sums in place, inside the rows
+    route = dip.ExpertRoute(4, 3, 2, "cuda")
+    dip.dip_route_experts(ctx, torch.randn((4, 3), generator=g, device="cuda"), route)
+    out = torch.randn((8, 256), generator=g, device="cuda")
+    before = out.clone()
+    for first in (0, 3):
+        refused(dip.dip_combine_rows, out, route, out.view(torch.bfloat16).view(16, 256)[first:first + 4])
+    work = dip.ExpertWork(4, 2, w, "cuda")
+    x = torch.randn((4, 256), generator=g, device="cuda").bfloat16()
+    refused(dip.dip_expert_mlp, w, x, work, work.out.view(torch.bfloat16).view(16, 256)[4:8], route=route)
+    torch.cuda.synchronize()
+    assert torch.equal(rows.scales, scales) and torch.equal(out, before) and (h.values.view(torch.uint8) == 3).all()
+
+
+@pytest.mark.parametrize("wtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("top_k", [0, 2])
+def test_the_block_in_place(ctx, wtype, top_k):
+    """y over x: x is used up when y is written."""
+    g = gen_of(2)
+    w = block(g, wtype == "fp8", 5 if top_k else 1, 288, 416)
+    x = torch.randn((70, 288), generator=g, device="cuda").bfloat16()
+    work, y, route = dip.ExpertWork(70, top_k, w, "cuda"), torch.zeros_like(x), None
+    if top_k:
+        route = dip.ExpertRoute(70, 5, top_k, "cuda")
+        dip.dip_route_experts(ctx, torch.randn((70, 5), generator=g, device="cuda"), route)
+    dip.dip_expert_mlp(ctx, w, x, work, y, route=route)
+    dip.dip_expert_mlp(ctx, w, x, work, x, route=route)
+    assert torch.equal(x, y)
