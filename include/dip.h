@@ -157,6 +157,13 @@ dip_status dip_reset_device_status(dip_ctx *ctx, void *stream);
  * usable.  waited_ns (device uint64, may be NULL) receives how long the kernel waited.
  * 1 <= limit_us <= 1000000. */
 dip_status dip_selftest_bounded_wait(dip_ctx *ctx, int limit_us, unsigned long long *waited_ns, void *stream);
+/* The same for the waits inside a grouped product (diagnostics): DIP_SELFTEST_GROUP_CASES small kernels, one after the other, in each of which a
+ * warp waits in vain, the block gives up, and, before it leaves, waits for the copies that would be under way (none is; a
+ * warp that stands for them counts them off after the limit and as long again, 0.1 s at most).  report: device uint64 [DIP_SELFTEST_GROUP_CASES][2], per case the
+ * copies that came, and those that had come when the block was ready to leave: the same number.  The status word
+ * becomes DIP_DEVICE_WAIT_TIMEOUT.  1 <= limit_us <= 1000000. */
+enum { DIP_SELFTEST_GROUP_CASES = 8 };
+dip_status dip_selftest_group_waits(dip_ctx *ctx, int limit_us, unsigned long long *report, void *stream);
 
 /* ------------------------------------------------------------------------
  * Timeline of the library's own kernels (diagnostics; off by default).  Between

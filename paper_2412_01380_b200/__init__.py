@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libdip.so")
 W_F32, W_BF16, W_INT4_G128, W_FP8_B128 = 0, 1, 2, 3
 MAX_D, MAX_BATCH, INT4_GROUP, CACHE_META_INTS = 32768, 16, 128, 8
 FP8_BLOCK, MAX_EXPERTS, MAX_TOP_K, MAX_TOKENS = 128, 512, 16, 65536
+SELFTEST_GROUP_CASES = 8
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CUDA, ERR_WORKSPACE = 0, 1, 2, 3, 4
 DEVICE_OK, DEVICE_WAIT_TIMEOUT, DEVICE_TIER_INCONSISTENT = 0, 1, 2
 
@@ -63,6 +64,8 @@ _lib.dip_reset_device_status.restype = _i32
 _lib.dip_reset_device_status.argtypes = [_vp, _vp]
 _lib.dip_selftest_bounded_wait.restype = _i32
 _lib.dip_selftest_bounded_wait.argtypes = [_vp, _i32, _vp, _vp]
+_lib.dip_selftest_group_waits.restype = _i32
+_lib.dip_selftest_group_waits.argtypes = [_vp, _i32, _vp, _vp]
 _lib.dip_selftest_block_waits.restype = _i32
 _lib.dip_selftest_block_waits.argtypes = [_vp, _i32, C.POINTER(CacheStateStruct), _vp, _vp]
 _lib.dip_destroy.restype = _i32
@@ -165,7 +168,7 @@ _lib.dip_expert_mlp.argtypes = [_vp, C.POINTER(GroupedMatrixStruct), C.POINTER(G
                                 C.POINTER(ExpertWorkStruct), _vp, _vp]
 
 EXPORTED = ["dip_create", "dip_create_ex", "dip_destroy", "dip_status_string", "dip_last_error", "dip_sm_count",
-            "dip_device_status", "dip_reset_device_status", "dip_selftest_bounded_wait", "dip_selftest_block_waits", "dip_stack_step_probed",
+            "dip_device_status", "dip_reset_device_status", "dip_selftest_bounded_wait", "dip_selftest_block_waits", "dip_selftest_group_waits", "dip_stack_step_probed",
             "dip_trace_begin", "dip_trace_reset", "dip_trace_read", "dip_trace_end",
             "dip_packed_bytes", "dip_pack_weights", "dip_mask_topk", "dip_ca_mask",
             "dip_sparse_gemv_gate_up", "dip_sparse_gemv_down", "dip_select_gemv_gate_up", "dip_select_gemv_down",
@@ -253,6 +256,13 @@ class Context:
     def selftest_bounded_wait(self, limit_us: int, waited_ns: Optional[torch.Tensor] = None) -> None:
         """Enqueue the tiny kernel whose bounded wait runs out (device status becomes 1)."""
         self.check(_lib.dip_selftest_bounded_wait(self.handle, int(limit_us), _ptr(waited_ns), _stream()))
+
+    def selftest_group_waits(self, limit_us: int, report: torch.Tensor) -> None:
+        """report: contiguous int64 [SELFTEST_GROUP_CASES, 2] on the context's device."""
+        if (report.dtype is not torch.int64 or report.get_device() != self.device or not report.is_contiguous() or
+                report.shape != (SELFTEST_GROUP_CASES, 2)):
+            raise DipError(ERR_INVALID_ARG, "report must be contiguous int64 [%d, 2] on the context's device" % SELFTEST_GROUP_CASES)
+        self.check(_lib.dip_selftest_group_waits(self.handle, int(limit_us), _ptr(report), _stream()))
 
     def selftest_block_waits(self, limit_us: int, st: "CacheState", mask_bits: torch.Tensor) -> None:
         """Enqueue the kernel whose waits between thread blocks run out (device status becomes 1, st stays as it is)."""

@@ -286,6 +286,12 @@ dip_status dip_selftest_bounded_wait(dip_ctx *ctx, int limit_us, unsigned long l
     return dip_launch_bounded_wait_selftest(ctx, 1000ull * (unsigned long long)limit_us, waited_ns, (cudaStream_t)stream);
 }
 
+dip_status dip_selftest_group_waits(dip_ctx *ctx, int limit_us, unsigned long long *report, void *stream)
+{
+    if (!ctx_ok(ctx) || limit_us < 1 || limit_us > 1000000 || !report || !dip_aligned16(report)) return DIP_ERR_INVALID_ARG;
+    return dip_launch_group_waits_selftest(ctx, 1000ull * (unsigned long long)limit_us, report, (cudaStream_t)stream);
+}
+
 dip_status dip_selftest_block_waits(dip_ctx *ctx, int limit_us, const dip_cache_state *st, const uint32_t *mask_bits, void *stream)
 {
     if (!ctx_ok(ctx) || limit_us < 1 || limit_us > 1000000 || !mask_bits || !dip_aligned16(mask_bits)) return DIP_ERR_INVALID_ARG;

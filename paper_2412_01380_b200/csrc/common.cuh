@@ -300,3 +300,5 @@ dip_status dip_launch_combine_rows(dip_ctx *ctx, const float *rows, const dip_ex
 dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const dip_grouped_matrix *up, const void *rows,
                               const float *row_scales, int n_rows, const int32_t *offset, void *out, bool out_f32, float *out_scales,
                               cudaStream_t stream);
+// grouped.cu: kernels in which a wait of theirs runs out while copies are (as it were) under way (status word 1).
+dip_status dip_launch_group_waits_selftest(dip_ctx *ctx, unsigned long long limit_ns, unsigned long long *report, cudaStream_t stream);

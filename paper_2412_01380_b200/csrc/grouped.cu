@@ -103,7 +103,8 @@ struct __align__(1024) GroupedSmem {
     float2 w_scale[GP_SCALE_SLOTS * GP_SCALE_STEPS];     // of a tile's two blocks of weights (gate/up: one of each)
     uint32_t tmem_base;
     int last;
-    int fail;
+    int fail, peer_fail;                            // a wait of this block (PAIR: of the other one) has run out
+    int issued;                                     // steps that warp 0 has asked for
     float amax[4 * GP_ROWS];
     GroupedPlan plan;
 };
@@ -230,6 +231,49 @@ __device__ __forceinline__ void arrive_first(uint32_t bar, int lane)
 __device__ __forceinline__ void pair_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// A word of the other block's shared memory.
+__device__ __forceinline__ uint32_t peer_word(const void *p)
+{
+    uint32_t a;
+    asm("{\n .reg .b32 r;\n mov.u32 r, %%cluster_ctarank;\n xor.b32 r, r, 1;\n mapa.shared::cluster.u32 %0, %1, r;\n}" : "=r"(a) : "r"(smem_u32(p)));
+    return a;
+}
+__device__ __forceinline__ int peer_load(const int *p)
+{
+    int v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(peer_word(p)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void peer_store(int *p, int v) { asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(peer_word(p)), "r"(v) : "memory"); }
+
+// As many bytes less for the phase to wait for.
+__device__ __forceinline__ void mbar_complete_tx(uint64_t *bar, unsigned bytes)
+{
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+
+// A wait has run out, and no copy may be on its way into a block that leaves: one warp (PAIR: of the first block) waits for the
+// steps whose copies may not have landed.  A stage is asked for again only when its step has been read, so they are the last
+// STAGES.  No more copies are issued (a block barrier is behind; PAIR: one of both blocks).
+// mine, other: steps that this block and the second one have asked for.  Where one was ahead of the other, a step's barrier expects
+// copies that nobody asks for any more, or does not know yet of the second block's: second_bytes(j) says how many bytes those of step j are.
+template <int STAGES, bool PAIR, class Bytes>
+__device__ __forceinline__ void drain_copies(uint64_t *full, int mine, int other, const Bytes &second_bytes, unsigned long long limit_ns)
+{
+    const int steps = PAIR ? max(mine, other) : mine;
+    if (PAIR) {
+        for (int j = min(mine, other); j < steps; ++j) {
+            const unsigned bytes = second_bytes(j);
+            if (elect_one()) {
+                if (mine > other) mbar_complete_tx(&full[j % STAGES], bytes);
+                else mbar_expect_tx(&full[j % STAGES], bytes);
+            }
+            __syncwarp();
+        }
+    }
+    for (int j = max(0, steps - STAGES); j < steps; ++j) warp_wait(&full[j % STAGES], (j / STAGES) & 1, limit_ns);
 }
 
 // 8, 16 or 32 columns of this warp's 32 lanes: thread = lane, register = column.  The wait names the registers, so that nothing
@@ -770,6 +814,22 @@ __device__ __forceinline__ void take_tile(const GroupedParams &p, GroupedSmem<K>
     }
 }
 
+// Every warp's roles are through (PAIR: in both blocks: the first one's MMAs have read the second one's memory, all has arrived at its
+// barriers), and each block knows of the other's failure.
+template <bool PAIR, int THREADS, typename Smem>
+__device__ __forceinline__ void roles_end(Smem &s, int tid)
+{
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    asm volatile("barrier.cta.sync 3, %0;" ::"n"(THREADS) : "memory");
+    if (PAIR) {
+        if (tid == 0 && *(volatile int *)&s.fail) peer_store(&s.peer_fail, 1);
+        __syncwarp();
+        pair_barrier();
+    }
+}
+template <bool PAIR, typename Smem>
+__device__ __forceinline__ bool gave_up(Smem &s) { return (*(volatile int *)&s.fail | (PAIR ? *(volatile int *)&s.peer_fail : 0)) != 0; }
+
 template <class K>
 __global__ void __launch_bounds__(K::THREADS, 1)
 grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_constant__ CUtensorMap w_map,
@@ -810,7 +870,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
         }
         mbar_init(&s.drained[0], 1);
         mbar_init(&s.drained[1], 1);
-        s.fail = 0;
+        s.fail = s.peer_fail = s.issued = 0;
         asm volatile("prefetch.tensormap [%0];" ::"l"(&rows_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&w2_map) : "memory");
@@ -892,9 +952,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
                     __syncwarp();
                 }
             }
-            // (given up: no copy of this block's is under way when it leaves; the second block's count at the first one's barriers)
-            if (failed && rank == 0)
-                for (int j = max(0, g - STAGES); j < g; ++j) warp_wait(&s.full[j % STAGES], (j / STAGES) & 1, p.copy_wait_ns);
+            if (lane == 0) s.issued = g;
         } else if (Smem::RING && warp == 3) {
             // four rows a lane; the first lanes the weights' scales
             const int out_blocks = (p.d_out + DIP_FP8_BLOCK - 1) / DIP_FP8_BLOCK;
@@ -962,10 +1020,27 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
                     if (last) ++n;
                 }
             }
-            if (failed) {
-                if (elect_one()) grouped_commit<PAIR>(&s.drained[half]);
+        }
+        if (failed) {
+            *(volatile int *)&s.fail = 1;
+            atomicExch(p.status, 1);
+        }
+        // All roles are through.  Where any wait has run out, whoever's it was, MMAs and copies may still be under way (the last
+        // steps' copies, though the warp that issued them knows of nothing): they are waited for.
+        roles_end<PAIR, K::THREADS>(s, tid);
+        if (gave_up<PAIR>(s)) {
+            if (warp == 1 || (SPLIT && warp == 2)) {
+                if (rank == 0 && elect_one()) grouped_commit<PAIR>(&s.drained[warp - 1]);
                 __syncwarp();
-                warp_wait(&s.drained[half], 0, p.wait_limit_ns);
+                warp_wait(&s.drained[warp - 1], 0, p.wait_limit_ns);
+            }
+            if (warp == 0 && rank == 0) {
+                const auto second_bytes = [&](int j) {
+                    Run r = {};
+                    for (int i = 0, step = 0; plan.get(i, r) && step + r.k1 - r.k0 <= j; ++i) step += r.k1 - r.k0;
+                    return (unsigned)(K::B_BYTES + (r.rows > GP_ROWS ? K::A_BYTES : 0));
+                };
+                drain_copies<STAGES, PAIR>(s.full, s.issued, PAIR ? peer_load(&s.issued) : 0, second_bytes, p.wait_limit_ns);
             }
         }
     } else {
@@ -978,20 +1053,80 @@ grouped_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_consta
             if constexpr (FEW) take_few<K>(p, s, plan, r, lanes, share, place, n);
             else take_tile<K>(p, s, plan, r, r.row0 + rank * GP_ROWS, min(GP_ROWS, r.rows - rank * GP_ROWS), lanes, share, place, n, groups);
         }
+        roles_end<PAIR, K::THREADS>(s, tid);
     }
-    if (failed) {
-        *(volatile int *)&s.fail = 1;
-        atomicExch(p.status, 1);
-    }
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    if (PAIR) pair_barrier();                        // (the first block's MMAs have read this block's memory, all has arrived at its barriers)
+    if (PAIR && gave_up<PAIR>(s)) pair_barrier();       // (neither leaves before the first one has waited for all)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if (warp == 1) {
         if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(GP_TMEM_COLS) : "memory");
         else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(GP_TMEM_COLS) : "memory");
     }
     DIP_TRACE_MAX(p.tr, 2);
+}
+
+// Self-test of a wait that runs out: warp 1 of block `failing` waits for what never comes, warp 2 for what warp 1 would have done, and warp 0 of
+// the first block then waits for the copies that `mine` and `other` steps have on their way, as in grouped_kernel.  No copy is: warp 3 stands
+// for them, and counts their bytes off late.  report: how many came; how many had when the drain was through.
+template <bool PAIR>
+__global__ void __launch_bounds__(128, 1)
+group_waits_selftest_kernel(int mine, int other, int failing, int *status, unsigned long long limit_ns, unsigned long long bound_ns,
+                            unsigned long long *report)
+{
+    constexpr int STAGES = 5;
+    constexpr unsigned FIRST = 1024, SECOND = 512;   // bytes of a step, the second block's of them
+    struct Smem {
+        uint64_t full[STAGES], never, sum_full;
+        int fail, peer_fail, issued;
+    };
+    __shared__ Smem s;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = PAIR ? blockIdx.x & 1 : 0;
+    const int landed = max(0, (PAIR ? max(mine, other) : mine) - STAGES);      // steps that are through
+    if (tid == 0) {
+        for (int i = 0; i < STAGES; ++i) mbar_init(&s.full[i], 1);
+        mbar_init(&s.never, 1);
+        mbar_init(&s.sum_full, 1);
+        s.fail = s.peer_fail = 0;
+        s.issued = rank ? other : mine;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int j = 0; rank == 0 && j < mine; ++j) {
+            mbar_expect_tx(&s.full[j % STAGES], FIRST + (PAIR ? SECOND : 0));
+            if (j < landed) mbar_complete_tx(&s.full[j % STAGES], FIRST + (PAIR ? SECOND : 0));
+        }
+    }
+    __syncthreads();
+    if (PAIR) pair_barrier();
+    if (warp == 3) {
+        if (PAIR) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // (holds nobody up)
+        const unsigned long long t0 = dip_gtime();
+        for (int i = 0; i < (1 << 22) && dip_gtime() - t0 < limit_ns + min(limit_ns, 100000000ull); ++i) __nanosleep(500);
+        if (lane == 0) {
+            for (int j = landed; j < s.issued; ++j) {
+                atomicAdd(report, 1ull);
+                __threadfence();
+                if (rank == 0) mbar_complete_tx(&s.full[j % STAGES], FIRST);
+                else asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cluster.b64 [%0], %1;" ::"r"(peer_word(&s.full[j % STAGES])), "r"(SECOND)
+                                  : "memory");
+            }
+        }
+        __syncwarp();
+        if (PAIR) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else {
+        bool failed = false;
+        if (rank == failing) {
+            if (warp == 1) failed = !warp_wait(&s.never, 0, limit_ns);
+            if (warp == 2) wait_on(smem_u32(&s.sum_full), 0, s, status, bound_ns);
+        }
+        if (failed) {
+            *(volatile int *)&s.fail = 1;
+            atomicExch(status, 1);
+        }
+        roles_end<PAIR, 96>(s, tid);
+        if (gave_up<PAIR>(s) && warp == 0 && rank == 0) {
+            drain_copies<STAGES, PAIR>(s.full, s.issued, PAIR ? peer_load(&s.issued) : 0, [](int) { return SECOND; }, bound_ns);
+            if (lane == 0) report[1] = atomicAdd(report, 0ull);
+        }
+    }
+    if (PAIR && gave_up<PAIR>(s)) pair_barrier();
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -1116,5 +1251,27 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
     const int ctas = mode == GP_PAIR ? 2 * (int)min((long long)ctx->sm_count / 2, most) : (int)min((long long)ctx->sm_count, most);
     const auto start = fp8 ? (up ? launch<true, true> : launch<true, false>) : (up ? launch<false, true> : launch<false, false>);
     DIP_CUDA_TRY(ctx, start(mode, ctx, ctas, stream, maps, p));
+    return DIP_OK;
+}
+
+dip_status dip_launch_group_waits_selftest(dip_ctx *ctx, unsigned long long limit_ns, unsigned long long *report, cudaStream_t stream)
+{
+    // steps that each block has asked for, and which one's wait runs out; the first two are blocks by themselves
+    static const int cases[DIP_SELFTEST_GROUP_CASES][3] = {{3, 0, 0}, {12, 0, 0}, {4, 4, 0}, {13, 13, 1}, {9, 5, 0}, {9, 6, 1}, {5, 9, 0}, {2, 4, 1}};
+    DIP_CUDA_TRY(ctx, cudaMemsetAsync(report, 0, 2 * DIP_SELFTEST_GROUP_CASES * sizeof(*report), stream));
+    for (int i = 0; i < DIP_SELFTEST_GROUP_CASES; ++i) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(i < 2 ? 1 : 2);
+        cfg.blockDim = dim3(128);
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = cfg.gridDim.x;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        DIP_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, i < 2 ? group_waits_selftest_kernel<false> : group_waits_selftest_kernel<true>, cases[i][0],
+                                             cases[i][1], cases[i][2], ctx->status, limit_ns, ctx->block_wait_ns, report + 2 * i));
+    }
     return DIP_OK;
 }

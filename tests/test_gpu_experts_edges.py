@@ -1,4 +1,5 @@
-"""Uses of the router, the grouped products and the expert block at the edge of what a call takes: buffers that share memory."""
+"""Uses of the router, the grouped products and the expert block at the edge of what a call takes: buffers that share memory,
+waits that run out."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -77,3 +78,39 @@ def test_the_block_in_place(ctx, wtype, top_k):
     dip.dip_expert_mlp(ctx, w, x, work, y, route=route)
     dip.dip_expert_mlp(ctx, w, x, work, x, route=route)
     assert torch.equal(x, y)
+
+
+# ---- waits that run out ------------------------------------------------------------------------------------------------
+def test_a_grouped_product_that_gives_up_waits_for_its_copies_and_a_reset_mends_the_context():
+    """Warps that wait in vain end the others' waits, and no block leaves while what it has asked for is under way (alone, and in
+    pairs of which either block is ahead).  Then cut tiles, whose parts meet, on the same context."""
+    c = dip.Context(0)
+    try:
+        report = torch.full((dip.SELFTEST_GROUP_CASES, 2), -1, dtype=torch.int64, device="cuda")
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        c.selftest_group_waits(2000, report)
+        b.record()
+        assert c.device_status() == dip.DEVICE_WAIT_TIMEOUT
+        # twice the limit each, and not the second that the other waits have
+        assert 2 * 2 * dip.SELFTEST_GROUP_CASES <= a.elapsed_time(b) < 500
+        # copies under way: of the last five steps, those that each block has asked for
+        under_way = [3, 5, 4 + 4, 5 + 5, 5 + 1, 5 + 2, 1 + 5, 2 + 4]
+        assert report.tolist() == [[n, n] for n in under_way]
+        c.reset_device_status()
+        g = gen_of(3)
+        for fp8 in (False, True):
+            for counts in ([1, 0, 3], [70, 0, 90], [400, 0, 250]):
+                w, x = eu.matrix(g, fp8, 3, 352, 8192), eu.rows_of(g, fp8, sum(counts), 8192)
+                o = eu.offsets(counts)
+                y = torch.zeros((sum(counts), 352), device="cuda")
+                dip.dip_grouped_product(c, dip.GroupedMatrix(*w), dip.Rows.of(*x), y, offset=o)
+                want, bound = eu.product64(*w, eu.values64(*x), o)
+                eu.assert_within(y, want, eu.rounded(want, bound, torch.float32), "y")
+        assert c.device_status() == dip.DEVICE_OK
+        for limit, bad in ((0, report), (2_000_000, report), (1000, report[:3]), (1000, report.int()), (1000, report.cpu())):
+            with pytest.raises(dip.DipError):
+                c.selftest_group_waits(limit, bad)
+    finally:
+        torch.cuda.synchronize()
+        c.close()
