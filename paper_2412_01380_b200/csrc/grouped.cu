@@ -490,17 +490,18 @@ __device__ __forceinline__ void take_few(const GroupedParams &p, GroupedSmem<K> 
 #pragma unroll
             for (int j = 0; j < N; ++j) u[j] = 0.f;
         }
-        // a lane keeps the scales of row t0 + lane and of the one 32 behind it, and asks for the next step's in good time
+        // a lane keeps the scales of row t0 + lane and of the one 32 behind it, and asks for the next step's in good time (plain loads: when
+        // this kernel starts, the one in front may still be writing them)
         const float *xs = p.row_scales + (size_t)min(r.row0 + t0 + lane, r.row0 + r.rows - 1) * in_blocks;
         const float *ys = p.row_scales + (size_t)min(r.row0 + t0 + 32 + lane, r.row0 + r.rows - 1) * in_blocks;
         const size_t at = ((size_t)r.expert * out_blocks + min((r.out0 + side) / DIP_FP8_BLOCK, out_blocks - 1)) * in_blocks;
         const float *ws = p.w_scales + at, *us = GATED ? p.up_scales + at : ws;
-        float next_x = __ldg(xs + r.k0), next_w = __ldg(ws + r.k0), next_u = __ldg(us + r.k0), next_y = __ldg(ys + r.k0);
+        float next_x = xs[r.k0], next_w = __ldg(ws + r.k0), next_u = __ldg(us + r.k0), next_y = ys[r.k0];
         for (int k = r.k0; k < r.k1; ++k, ++n) {
             const float sx = next_x, sy = next_y, w = next_w, v = next_u;
             if (k + 1 < r.k1) {
-                next_x = __ldg(xs + k + 1);
-                if (N > 32) next_y = __ldg(ys + k + 1);
+                next_x = xs[k + 1];
+                if (N > 32) next_y = ys[k + 1];
                 next_w = __ldg(ws + k + 1);
                 if (GATED) next_u = __ldg(us + k + 1);
             }

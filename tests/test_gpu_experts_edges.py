@@ -80,6 +80,30 @@ def test_the_block_in_place(ctx, wtype, top_k):
     assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("rows", [1, 7, 40])
+def test_rows_and_scales_that_the_launch_in_front_writes(ctx, rows):
+    """A product starts before the launch that stages its rows is through: new rows and scales in the same buffers, launch after
+    launch, give what they give one at a time."""
+    g = gen_of(4)
+    m = dip.GroupedMatrix(*eu.matrix(g, True, 1, 608, 1280))
+    x = [(torch.randn((rows, 1280), generator=g, device="cuda") * 4.0 ** (i % 7 - 3)).bfloat16() for i in range(40)]
+    staged, want = dip.Rows(rows, 1280, dip.W_FP8_B128, "cuda"), []
+    for v in x:
+        y = torch.zeros((rows, 608), device="cuda")
+        dip.dip_stage_rows(ctx, v, staged)
+        torch.cuda.synchronize()
+        dip.dip_grouped_product(ctx, m, staged, y)
+        torch.cuda.synchronize()
+        want.append(y)
+    got = [torch.zeros_like(y) for y in want]
+    torch.cuda.synchronize()
+    for v, y in zip(x, got):
+        dip.dip_stage_rows(ctx, v, staged)
+        dip.dip_grouped_product(ctx, m, staged, y)
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
 # ---- waits that run out ------------------------------------------------------------------------------------------------
 def test_a_grouped_product_that_gives_up_waits_for_its_copies_and_a_reset_mends_the_context():
     """Warps that wait in vain end the others' waits, and no block leaves while what it has asked for is under way (alone, and in
