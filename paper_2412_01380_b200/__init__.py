@@ -686,8 +686,11 @@ def dip_route_experts(ctx: Context, logits: torch.Tensor, route: ExpertRoute, re
         _refuse("the route holds 1 .. %d tokens", route.max_tokens)
     if route.device != ctx.device:
         _refuse("the route is not on the context's device")
-    route.struct.n_tokens = n
-    ctx.check(_lib.dip_route_experts(ctx.handle, logits.data_ptr(), bf16, bool(renormalize), route.ref, _stream()))
+    before, route.struct.n_tokens = route.struct.n_tokens, n
+    status = _lib.dip_route_experts(ctx.handle, logits.data_ptr(), bf16, bool(renormalize), route.ref, _stream())
+    if status != OK:
+        route.struct.n_tokens = before                       # (nothing was launched)
+        ctx.check(status)
 
 
 def _check_route(ctx: Context, route: Optional[ExpertRoute], n_tokens: int) -> None:
