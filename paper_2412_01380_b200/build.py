@@ -4,6 +4,7 @@ Each .cu file is compiled to an object of its own (in parallel, and only when it
 is newer than the object), then the objects are linked into the shared library.
 """
 import os
+import re
 import subprocess
 import sys
 from concurrent.futures import ThreadPoolExecutor
@@ -21,6 +22,18 @@ NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
+
+# Registers per thread that a launch of the grouped products must have (8-bit: "1"), because their warps deal them out again: with fewer the
+# warps that take more would wait for ever, and every launch is refused.
+GROUPED_REGISTERS = {"1": 168, "0": 96}
+
+
+def check_registers(log: str) -> None:
+    """log: what ptxas -v says of grouped.cu.  Kind<8 bits, gate/up, kind>; kind 0 (few rows) deals none out."""
+    found = re.findall(r"Compiling entry function '[^']*grouped_kernel[^']*KindILb([01])ELb([01])ELi([0-2])E.*?Used (\d+) registers", log, re.S)
+    short = ["%s of %d" % (f, GROUPED_REGISTERS[f[0]]) for f in found if f[2] != "0" and int(f[3]) < GROUPED_REGISTERS[f[0]]]
+    if len(found) != 12 or short:
+        raise RuntimeError("grouped.cu: %d of 12 kernels, too few registers in (8 bits, gate/up, kind, registers): %s" % (len(found), short))
 
 
 def _nvcc() -> str:
@@ -44,8 +57,14 @@ def _compile(src: str, force: bool, verbose: bool) -> str:
     obj = os.path.join(OBJ, src[:-3] + ".o")
     if force or _stale(obj, [path] + HEADERS):
         tmp = obj + ".tmp.%d" % os.getpid()
-        cmd = [_nvcc(), *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []), "-c", path, "-o", tmp]
-        subprocess.run(cmd, check=True)
+        grouped = src == "grouped.cu"
+        cmd = [_nvcc(), *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose or grouped else []), "-c", path, "-o", tmp]
+        done = subprocess.run(cmd, stderr=subprocess.PIPE if grouped else None, text=True)
+        if grouped and (verbose or done.returncode):
+            sys.stderr.write(done.stderr)
+        done.check_returncode()
+        if grouped:
+            check_registers(done.stderr)
         os.replace(tmp, obj)
     return obj
 
