@@ -301,10 +301,10 @@ gemv_kernel(const GemvParams p)
     __syncthreads();
     if (s.abort) {
         // a wait ran out: let the copies already issued into this CTA's shared memory land
-        // (bounded again) before the ring is reused or the CTA leaves
+        // (bounded again, but not by the limit that was too short for one of them) before the ring is reused or the CTA leaves
         if (tid == 0) {
             for (int it = max(0, s.issued - GV_STAGES); it < s.issued; ++it)
-                (void)mbar_wait(&s.full[it % GV_STAGES], (it / GV_STAGES) & 1, p.wait_limit_ns);
+                (void)mbar_wait(&s.full[it % GV_STAGES], (it / GV_STAGES) & 1, p.drain_ns);
         }
         __syncthreads();
     }
@@ -864,6 +864,7 @@ dip_status dip_launch_gemv(dip_ctx *ctx, const dip_mlp_weights *w, int which,
     p.tickets = ctx->tickets;
     p.status = ctx->status;
     p.wait_limit_ns = ctx->wait_limit_ns;
+    p.drain_ns = ctx->block_wait_ns;
     p.key_coarse = nullptr;
     p.key_stamp = nullptr;
     p.key_gamma = 1.0f;
