@@ -58,6 +58,7 @@ struct __align__(1024) TcSmem {
     uint32_t tmem_base;
     int n_total;
     int fail;
+    int rounds;                                  // whose MMAs have been issued
     int wsum[TC_WARPS];
     uint32_t words[DIP_MAX_D / 32];
     int pre[DIP_MAX_D / 32];
@@ -163,7 +164,7 @@ gemv_tc_kernel(const GemvParams p, const TcParams q)
             mbar_init(&s.full[i], TC_LOAD_WARPS);
             mbar_init(&s.done[i], 1);
         }
-        s.fail = 0;
+        s.fail = s.rounds = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -309,6 +310,7 @@ gemv_tc_kernel(const GemvParams p, const TcParams q)
                     tc_mma(tmem, x_d0 + (uint64_t)(kb * (TC_B_KB_BYTES >> 4)), w_d0 + (uint64_t)(kb * (TC_A_KB_BYTES >> 4)),
                            (gg > 0 || kb > 0) ? 1u : 0u);
                 tc_commit(&s.done[buf]);
+                s.rounds = gg + 1;
             }
         }
         g += n_rounds;
@@ -317,9 +319,11 @@ gemv_tc_kernel(const GemvParams p, const TcParams q)
     if (failed) s.fail = 1;
     __syncthreads();
     failed = s.fail != 0;
-    // ---- the last round's commit covers every MMA of the kernel ----
-    if (g > 0 && !failed) {
-        if (!mbar_wait(&s.done[(g - 1) % TC_BUFS], ((g - 1) / TC_BUFS) & 1, p.wait_limit_ns)) failed = true;
+    // ---- the last round's commit covers every MMA of the kernel: also where a wait ran out, because the ring is used again and the tensor
+    //      memory is freed ----
+    const int rounds = s.rounds;
+    if (rounds > 0) {
+        if (!mbar_wait(&s.done[(rounds - 1) % TC_BUFS], ((rounds - 1) / TC_BUFS) & 1, q.block_wait_ns)) failed = true;
     }
     if (failed && lane == 0) atomicExch(p.status, 1);
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
