@@ -138,3 +138,112 @@ def test_a_grouped_product_that_gives_up_waits_for_its_copies_and_a_reset_mends_
     finally:
         torch.cuda.synchronize()
         c.close()
+
+
+# ---- sizes at the ends of what a call takes ----------------------------------------------------------------------------
+@pytest.mark.parametrize("wtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("d_in,d_out", [(32768, 32), (32, 32768)])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_widest_and_narrowest(ctx, wtype, d_in, d_out, rows):
+    g, fp8 = gen_of(d_in + rows), wtype == "fp8"
+    w, x = eu.matrix(g, fp8, 1, d_out, d_in), eu.rows_of(g, fp8, rows, d_in)
+    y = torch.zeros((rows, d_out), device="cuda")
+    dip.dip_grouped_product(ctx, dip.GroupedMatrix(*w), dip.Rows.of(*x), y)
+    want, bound = eu.product64(*w, eu.values64(*x))
+    eu.assert_within(y, want, eu.rounded(want, bound, torch.float32), "y")
+
+
+@pytest.mark.parametrize("wtype", ["bf16", "fp8"])
+def test_most_experts(ctx, wtype):
+    """512 experts, 16 for each token; a group of many rows, and most of few or none."""
+    g, fp8 = gen_of(6), wtype == "fp8"
+    w = block(g, fp8, 512, 64, 96)
+    z = torch.randn((50, 512), generator=g, device="cuda")
+    z[:, 511] = 9
+    x = torch.randn((50, 64), generator=g, device="cuda").bfloat16()
+    route, work, y = dip.ExpertRoute(50, 512, 16, "cuda"), dip.ExpertWork(50, 16, w, "cuda"), torch.zeros_like(x)
+    dip.dip_route_experts(ctx, z, route)
+    dip.dip_expert_mlp(ctx, w, x, work, y, route=route)
+    assert int(route.offset[-1] - route.offset[-2]) == 50
+    want, bound = eu.product64(w.down.values, w.down.scales, eu.values64(work.h.values, work.h.scales), route.offset)
+    eu.assert_within(work.out, want, bound, "out")
+    at, share = route.token_row.long(), route.weight.double()[:, :, None]
+    total, off = (want[at] * share).sum(1), ((bound[at] + want[at].abs() * 2.0 ** -23 * 17) * share).sum(1)
+    eu.assert_within(y, total, eu.rounded(total, off, torch.bfloat16), "y")
+
+
+@pytest.mark.parametrize("wtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("top_k", [1, 3])
+def test_a_batch_of_nothing_but_padding(ctx, wtype, top_k):
+    g = gen_of(7)
+    w = block(g, wtype == "fp8", 4, 160, 288)
+    x = torch.full((33, 160), float("nan"), device="cuda", dtype=torch.bfloat16)
+    route, work, y = dip.ExpertRoute(33, 4, top_k, "cuda"), dip.ExpertWork(33, top_k, w, "cuda"), torch.full_like(x, 5.0)
+    for t in (work.rows.values, work.h.values):
+        t.view(torch.uint8).fill_(0x7f)                            # (NaN codes; finite bfloat16)
+    work.out.fill_(float("nan"))
+    dip.dip_route_experts(ctx, torch.full((33, 4), -float("inf"), device="cuda"), route)
+    dip.dip_expert_mlp(ctx, w, x, work, y, route=route)
+    assert (y == 0).all() and torch.isnan(work.out).all()
+
+
+@pytest.mark.parametrize("wtype", ["bf16", "fp8"])
+def test_positions_beyond_32_bits(ctx, wtype):
+    """Rows and outputs of more than 2^31 values (and 2^32 bytes): the last rows' values, and the rows in front of them."""
+    tokens, top_k, d_in, d_out = 65536, 16, 2080, 4128
+    rows_there = tokens * top_k
+    g, fp8 = gen_of(8), wtype == "fp8"
+    z = torch.zeros((tokens, 16), device="cuda")                   # every token, every expert: rows of a group are the tokens
+    x = torch.randn((tokens, d_in), generator=g, device="cuda").bfloat16()
+    w = eu.matrix(g, fp8, 16, d_out, d_in)
+    route, staged = dip.ExpertRoute(tokens, 16, top_k, "cuda"), dip.Rows(rows_there, d_in, WTYPES[wtype], "cuda")
+    dip.dip_route_experts(ctx, z, route)
+    dip.dip_stage_rows(ctx, x, staged, route=route)
+    y = torch.empty((rows_there, d_out), device="cuda", dtype=torch.bfloat16)
+    dip.dip_grouped_product(ctx, dip.GroupedMatrix(*w), staged, y, offset=route.offset)
+    for e in (0, 7, 8, 15):
+        some = torch.tensor([0, 1, 127, 128, 40000, tokens - 1], device="cuda")
+        r = some + e * tokens
+        want_rows = x[some]
+        if fp8:
+            want_rows, s = eu.quantise(want_rows)
+            assert torch.equal(staged.scales[r], s)
+        assert torch.equal(staged.values[r].view(torch.uint8), want_rows.view(torch.uint8))
+        want, bound = eu.product64(w[0][e:e + 1], None if w[1] is None else w[1][e:e + 1], eu.values64(want_rows, s if fp8 else None))
+        eu.assert_within(y[r], want, eu.rounded(want, bound, torch.bfloat16), "y of expert %d" % e)
+    del staged
+    out = torch.zeros((rows_there, d_in), device="cuda")           # 8.7 GB
+    out[-tokens:] = x.float()
+    got = torch.empty_like(x)
+    dip.dip_combine_rows(ctx, out, route, got)
+    # only the last expert's rows are not zero; its share of 16 equal logits
+    want = x.double() * route.weight[:, -1:].double()
+    eu.assert_within(got, want, eu.rounded(want, want.abs() * 2.0 ** -24, torch.bfloat16), "weighted sum")
+
+
+# ---- graphs ------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("wtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("tokens", [1, 300, 4500])
+def test_the_first_call_of_a_context_may_be_a_captured_one(wtype, tokens):
+    """Nothing has to have run before (kernels of few, some and many rows for each expert)."""
+    g = gen_of(9)
+    c = dip.Context(0)
+    try:
+        w = block(g, wtype == "fp8", 4, 160, 288)
+        x, z = torch.randn((tokens, 160), generator=g, device="cuda").bfloat16(), torch.randn((tokens, 4), generator=g, device="cuda")
+        route, work, y = dip.ExpertRoute(tokens, 4, 2, "cuda"), dip.ExpertWork(tokens, 2, w, "cuda"), torch.zeros_like(x)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            dip.dip_route_experts(c, z, route)
+            dip.dip_expert_mlp(c, w, x, work, y, route=route)
+        graph.replay()
+        got = y.clone()
+        dip.dip_route_experts(c, z, route)
+        dip.dip_expert_mlp(c, w, x, work, y, route=route)
+        assert torch.equal(got, y) and y.float().abs().max() > 0
+        assert c.device_status() == dip.DEVICE_OK
+        del graph
+    finally:
+        torch.cuda.synchronize()
+        c.close()
