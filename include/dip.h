@@ -595,7 +595,7 @@ dip_status dip_sparse_gemv_down_noalloc(const dip_mlp_weights *w, const float *h
  * grouped by expert: rows offset[e] .. offset[e + 1] - 1 belong to expert e
  * (offset [n_experts + 1], device int32, not decreasing, offset[0] = 0; an offset below
  * one in front of it counts as that one, what lies outside [0, n_rows] is cut off).  Rows behind offset[n_experts] are not
- * read and not written.  offset == NULL: one expert, and all rows are its own.
+ * written, and no result depends on them (a tile that ends among them may be loaded whole, within n_rows).  offset == NULL: one expert, and all rows are its own.
  * What a call writes must not overlap what it reads (rows, scales, weights, offsets, routes) or what else it writes
  * (DIP_ERR_INVALID_ARG); dip_expert_mlp may write over a buffer that is used up by then, so y may be x.
  *

@@ -40,7 +40,8 @@ constexpr int GP_A_BYTES = GP_ROWS * GP_STEP_BYTES, GP_B_BYTES = GP_COLS * GP_ST
 constexpr int GP_TMEM_COLS = 512;
 constexpr int GP_MIN_STEPS = 4;                     // a part of a tile has at least so many
 // Steps' worth of time that a cut tile's parts take to meet: written, counted, read and added (7 us for a tile of 128 rows; 3.5 us for one row,
-// and as many steps more as there are rows.  8 rows each for 16 experts, 4096 to 2048: 50.7 us with whole tiles, 56.5 cut).
+// and as many steps more as there are rows.  8 rows each for 16 experts, 4096 to 2048, bfloat16: 50.7 us with whole tiles, 56.5 cut).
+// One constant for both types, though their steps do not take the same time.
 constexpr int GP_JOIN_FEW = 8, GP_JOIN = 20;
 constexpr int GP_TWO_RUNS = 6;                      // steps' worth of time that a block loses between two runs
 constexpr int GP_SCALE_STEPS = 8, GP_SCALE_SLOTS = 4;   // steps of scales that come together, and how many such groups there is room for
@@ -669,7 +670,7 @@ __device__ __forceinline__ void take_tile(const GroupedParams &p, GroupedSmem<K>
         // (which of the tile's two blocks of weights a group of columns belongs to)
         const bool block0 = !GATED && !SPLIT && share == 1, block1 = GATED || SPLIT || share == 1;
         // (registers: with 32 columns gate/up keeps some of its own in memory and a prompt's product of 5120 to 17920 takes 476 us instead
-        // of 441; plain products have the room, and take 675 instead of 701)
+        // of 441; plain products keep 20 bytes a thread there (pairs; whole tiles 60), and take 675 instead of 701)
         constexpr int L = GATED ? 16 : 32;
         const uint32_t full = smem_u32(&s.sum_full[0][SPLIT ? share : 0]), empty = smem_u32(&s.sum_empty[0][SPLIT ? share : 0]);
         constexpr uint32_t NEXT = sizeof(s.sum_full[0]);             // from one accumulator's barrier to the other's
@@ -1205,7 +1206,8 @@ cudaError_t launch(int mode, dip_ctx *ctx, int ctas, cudaStream_t stream, const 
 // 8 rows for each of 32 experts, 1024 to 1024, 18.8 / 19.3 (8-bit 10.2 / 11.5), 32 rows 20.3 / 19.8 (12.9 / 11.7); one expert, 4096 to 5120, 8 rows
 // 18.3 / 26.9 (16.2 / 22.0), 24 rows 29.0 / 25.6 (24.8 / 22.8).  Whole tiles / pairs: 100 rows for each of 64 experts, gate/up of 2048 to 1408, 139 / 164;
 // 16 experts, 4096 to 4096, 150 rows 116 / 123, 200 rows 149 / 145; 1024 rows for each of 8, gate/up of 4096 to 14336, 1648 / 1430 (8-bit
-// 1304 / 1255).
+// 1304 / 1255).  What this leaves out: 8-bit pairs were compared at 1024 rows only, and groups of unequal size not at all (an expert of 257 to
+// 384 rows fills half of its second pair tile, or less).
 constexpr int GP_FEW_UP_TO = 12, GP_PAIR_ROWS = 192;
 
 dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const dip_grouped_matrix *up, const void *rows,
