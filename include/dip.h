@@ -69,7 +69,8 @@ enum {
     DIP_FP8_BLOCK = 128,       /* input indices (and outputs) that share a scale in DIP_W_FP8_B128   */
     DIP_MAX_EXPERTS = 512,
     DIP_MAX_TOP_K = 16,        /* experts per token                                                  */
-    DIP_MAX_TOKENS = 65536     /* tokens per call of the router and the expert block                 */
+    DIP_MAX_TOKENS = 65536,    /* tokens per call of the router and the expert block                 */
+    DIP_MAX_OUT = 262144       /* outputs of a 4-bit matrix in dip_grouped_product (a head)          */
 };
 
 typedef struct dip_ctx dip_ctx;   /* opaque; owns scratch workspace on one device */
@@ -601,21 +602,26 @@ dip_status dip_sparse_gemv_down_noalloc(const dip_mlp_weights *w, const float *h
  *
  * Weights are the matrices as checkpoints have them, row-major
  * [n_experts][d_out][d_in]; d_out and d_in are multiples of 32, at least 32 and at
- * most DIP_MAX_D.
+ * most DIP_MAX_D (d_out of INT4 in dip_grouped_product: DIP_MAX_OUT, a head's).
  *   DIP_W_BF16      rows are bfloat16.
  *   DIP_W_FP8_B128  values are e4m3 codes, scales [n_experts][ceil(d_out/128)]
  *                   [ceil(d_in/128)] binary32; rows are e4m3 codes too, with scales
  *                   [n_rows][ceil(d_in/128)] (dip_stage_rows).  A product is
  *                   the sum over the blocks b of 128 input indices of
  *                   (sum of code * code in b) * (row scale * weight scale of b).
+ *   DIP_W_INT4_G128 the arrays that dip_pack_weights takes, per expert: codes
+ *                   [n_experts][d_out][d_in / 2] bytes, the even input index in the
+ *                   low nibble, value = (code - 8) * scale, scales [n_experts][ceil(d_in/128)]
+ *                   [d_out] binary16; rows are bfloat16.  A product is the sum over the groups
+ *                   g of 128 input indices of (sum of (code - 8) * x in g) * scale of g.
  * ======================================================================== */
 typedef struct {
-    int32_t wtype;           /* DIP_W_BF16 or DIP_W_FP8_B128 */
+    int32_t wtype;           /* DIP_W_BF16, DIP_W_FP8_B128 or DIP_W_INT4_G128 */
     int32_t n_experts;
     int32_t d_out;
     int32_t d_in;
     const void *values;
-    const float *scales;     /* NULL unless FP8 */
+    const void *scales;      /* NULL for BF16; binary32 for FP8, binary16 for INT4 */
 } dip_grouped_matrix;
 
 /* What a router decides, and the grouping of the rows that follows from it (caller's buffers):
@@ -671,7 +677,7 @@ dip_status dip_stage_rows(dip_ctx *ctx, const void *x, int n_tokens, int d, cons
  *   binary32 (y_f32 != 0).  1 <= n_rows <= DIP_MAX_TOKENS * DIP_MAX_TOP_K.
  * dip_grouped_gate_up — h[r] = silu(Wg[e(r)] rows[r]) * (Wu[e(r)] rows[r]) in
  * one pass over rows and weights: the first half of Eq. 2 for every group.  h [n_rows][d_out]
- * is bfloat16, or (FP8) e4m3 codes with h_scales, as dip_stage_rows makes them of the binary32 h.
+ * is bfloat16 (BF16, INT4), or (FP8) e4m3 codes with h_scales, as dip_stage_rows makes them of the binary32 h.
  * ------------------------------------------------------------------------ */
 dip_status dip_grouped_product(dip_ctx *ctx, const dip_grouped_matrix *w, const void *rows, const float *row_scales,
                                int n_rows, const int32_t *offset, void *y, int y_f32, void *stream);
@@ -688,7 +694,7 @@ dip_status dip_combine_rows(dip_ctx *ctx, const float *rows, const dip_expert_ro
 
 /* Buffers of dip_expert_mlp for n = n_tokens * top_k rows (n_tokens without a route); the caller's. */
 typedef struct {
-    void *rows;          /* [n][d_model]: bfloat16, or e4m3.  NULL for BF16 without a route    */
+    void *rows;          /* [n][d_model]: bfloat16, or e4m3.  NULL for BF16 / INT4 without a route */
     float *row_scales;   /* [n][ceil(d_model/128)], FP8 only                                   */
     void *h;             /* [n][d_ff]: bfloat16, or e4m3                                       */
     float *h_scales;     /* [n][ceil(d_ff/128)], FP8 only                                      */

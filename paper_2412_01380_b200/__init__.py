@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libdip.so")
 
 W_F32, W_BF16, W_INT4_G128, W_FP8_B128 = 0, 1, 2, 3
 MAX_D, MAX_BATCH, INT4_GROUP, CACHE_META_INTS = 32768, 16, 128, 8
-FP8_BLOCK, MAX_EXPERTS, MAX_TOP_K, MAX_TOKENS = 128, 512, 16, 65536
+FP8_BLOCK, MAX_EXPERTS, MAX_TOP_K, MAX_TOKENS, MAX_OUT = 128, 512, 16, 65536, 262144
 SELFTEST_GROUP_CASES = 8
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CUDA, ERR_WORKSPACE = 0, 1, 2, 3, 4
 DEVICE_OK, DEVICE_WAIT_TIMEOUT, DEVICE_TIER_INCONSISTENT = 0, 1, 2
@@ -559,27 +559,34 @@ def _blocks(d: int) -> int:
 
 
 _ROW_DTYPES = {W_BF16: torch.bfloat16, W_FP8_B128: torch.float8_e4m3fn}
+_ROWS_OF = {W_BF16: W_BF16, W_FP8_B128: W_FP8_B128, W_INT4_G128: W_BF16}       # the rows that a type of weights multiplies
+_MATRIX_TYPES = {torch.bfloat16: W_BF16, torch.float8_e4m3fn: W_FP8_B128, torch.uint8: W_INT4_G128}
 
 
 class GroupedMatrix:
     """Matrices [n_experts, d_out, d_in] (or one [d_out, d_in]), bfloat16, or float8_e4m3fn with binary32 scales
-    [n_experts, ceil(d_out / 128), ceil(d_in / 128)].  Nothing is copied: the tensors stay the caller's layout."""
+    [n_experts, ceil(d_out / 128), ceil(d_in / 128)], or 4-bit codes as uint8 [n_experts, d_out, d_in / 2] (the even input index in the
+    low nibble) with binary16 scales [n_experts, ceil(d_in / 128), d_out].  Nothing is copied: the tensors stay the caller's layout."""
 
     def __init__(self, values: torch.Tensor, scales: Optional[torch.Tensor] = None):
         if values.dim() == 2:
             values, scales = values[None], None if scales is None else scales[None]
-        if values.dim() != 3 or values.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
-            _refuse("values must be [n_experts, d_out, d_in], bfloat16 or float8_e4m3fn")
-        self.wtype = W_BF16 if values.dtype == torch.bfloat16 else W_FP8_B128
+        if values.dim() != 3 or values.dtype not in _MATRIX_TYPES:
+            _refuse("values must be [n_experts, d_out, d_in], bfloat16 or float8_e4m3fn, or uint8 [n_experts, d_out, d_in / 2]")
+        self.wtype = _MATRIX_TYPES[values.dtype]
         self.n_experts, self.d_out, self.d_in = values.shape
-        if (scales is not None) != (self.wtype == W_FP8_B128):
-            _refuse("scales belong to float8_e4m3fn values, and only to them")
+        if self.wtype == W_INT4_G128:
+            self.d_in *= 2
+        if (scales is None) != (self.wtype == W_BF16):
+            _refuse("scales belong to float8_e4m3fn and uint8 values, and only to them")
         if not values.is_cuda or not values.is_contiguous():
             _refuse("values must be a contiguous device tensor")
         if scales is not None:
-            if (scales.dtype != torch.float32 or scales.device != values.device or not scales.is_contiguous() or
-                    tuple(scales.shape) != (self.n_experts, _blocks(self.d_out), _blocks(self.d_in))):
-                _refuse("scales must be contiguous float32 [n_experts, ceil(d_out / 128), ceil(d_in / 128)] beside the values")
+            dtype, shape = (torch.float32, (_blocks(self.d_out), _blocks(self.d_in))) if self.wtype == W_FP8_B128 else \
+                (torch.float16, (_blocks(self.d_in), self.d_out))
+            if (scales.dtype != dtype or scales.device != values.device or not scales.is_contiguous() or
+                    tuple(scales.shape) != (self.n_experts, *shape)):
+                _refuse("scales must be contiguous %s %s beside the values", dtype, (self.n_experts, *shape))
         self.values, self.scales, self.device = values, scales, values.get_device()
         self.struct = GroupedMatrixStruct(self.wtype, self.n_experts, self.d_out, self.d_in, _ptr(values), _ptr(scales))
         self.ref = C.byref(self.struct)
@@ -667,9 +674,9 @@ class ExpertWork:
             _refuse("1 .. %d tokens, top_k 0 .. %d", MAX_TOKENS, MAX_TOP_K)
         self.max_rows, self.routed = int(max_tokens) * max(1, int(top_k)), top_k > 0
         self.wtype, self.d_model, self.d_ff = w.wtype, w.d_model, w.d_ff
-        fp8 = w.wtype == W_FP8_B128
-        self.rows = Rows(self.max_rows, w.d_model, w.wtype, device) if fp8 or self.routed else None
-        self.h = Rows(self.max_rows, w.d_ff, w.wtype, device)
+        fp8, rtype = w.wtype == W_FP8_B128, _ROWS_OF[w.wtype]
+        self.rows = Rows(self.max_rows, w.d_model, rtype, device) if fp8 or self.routed else None
+        self.h = Rows(self.max_rows, w.d_ff, rtype, device)
         self.out = torch.empty((self.max_rows, w.d_model), device=device) if self.routed else None
         self.device = self.h.device
         self.struct = ExpertWorkStruct(self.rows.ptr if self.rows else None, self.rows.scales_ptr if self.rows else None,
@@ -723,7 +730,7 @@ def dip_stage_rows(ctx: Context, x: torch.Tensor, rows: Rows, route: Optional[Ex
 
 def dip_grouped_product(ctx: Context, w: GroupedMatrix, rows: Rows, y: torch.Tensor, offset: Optional[torch.Tensor] = None) -> None:
     """y [>= rows.n_rows, d_out], bfloat16 or float32; offset int32 [n_experts + 1], None: one expert."""
-    if rows.device != ctx.device or w.device != ctx.device or rows.wtype != w.wtype or rows.d != w.d_in:
+    if rows.device != ctx.device or w.device != ctx.device or rows.wtype != _ROWS_OF[w.wtype] or rows.d != w.d_in:
         _refuse("rows and weights must be on the context's device and agree in type and width")
     f32 = isinstance(y, torch.Tensor) and y.dtype is torch.float32
     _matrix(y, torch.float32 if f32 else torch.bfloat16, None, w.d_out, "y", ctx.device)
@@ -738,7 +745,7 @@ def dip_grouped_gate_up(ctx: Context, gate: GroupedMatrix, up: GroupedMatrix, ro
                         offset: Optional[torch.Tensor] = None) -> None:
     """h = silu(gate rows) * (up rows), rounded (and for e4m3 quantised) as the next product takes it."""
     for m in (gate, up):
-        if (not rows.device == h.device == m.device == ctx.device or not rows.wtype == h.wtype == m.wtype or rows.d != m.d_in or
+        if (not rows.device == h.device == m.device == ctx.device or not rows.wtype == h.wtype == _ROWS_OF[m.wtype] or m.wtype != gate.wtype or rows.d != m.d_in or
                 h.d != m.d_out or m.n_experts != gate.n_experts):
             _refuse("rows, h and weights must be on the context's device and agree in type, width and number of experts")
     if not 1 <= rows.n_rows <= h.max_rows:

@@ -10,11 +10,13 @@ bool width_ok(int d) { return d >= 32 && d <= DIP_MAX_D && d % 32 == 0; }
 // NULL or misaligned
 bool bad(const void *p) { return !p || !dip_aligned16(p); }
 
-bool matrix_ok(const dip_grouped_matrix *w)
+// head: one of the widths that only a plain 4-bit product takes
+bool matrix_ok(const dip_grouped_matrix *w, bool head = false)
 {
-    if (!w || (w->wtype != DIP_W_BF16 && w->wtype != DIP_W_FP8_B128)) return false;
-    if (w->n_experts < 1 || w->n_experts > DIP_MAX_EXPERTS || !width_ok(w->d_out) || !width_ok(w->d_in) || bad(w->values)) return false;
-    return w->wtype == DIP_W_FP8_B128 ? !bad(w->scales) : !w->scales;
+    if (!w || (w->wtype != DIP_W_BF16 && w->wtype != DIP_W_FP8_B128 && w->wtype != DIP_W_INT4_G128)) return false;
+    const bool out_ok = head && w->wtype == DIP_W_INT4_G128 ? w->d_out >= 32 && w->d_out <= DIP_MAX_OUT && w->d_out % 32 == 0 : width_ok(w->d_out);
+    if (w->n_experts < 1 || w->n_experts > DIP_MAX_EXPERTS || !out_ok || !width_ok(w->d_in) || bad(w->values)) return false;
+    return w->wtype == DIP_W_BF16 ? !w->scales : !bad(w->scales);
 }
 
 bool route_ok(const dip_expert_route *r)
@@ -24,7 +26,7 @@ bool route_ok(const dip_expert_route *r)
     return !(bad(r->expert) || bad(r->weight) || bad(r->offset) || bad(r->row_token) || bad(r->token_row));
 }
 
-// A float type's rows, and the scales that go with it.
+// The rows that go with a type of weights (4-bit ones take bfloat16), and their scales.
 bool rows_ok(int wtype, const void *rows, const float *scales)
 {
     return !bad(rows) && (wtype == DIP_W_FP8_B128 ? !bad(scales) : !scales);
@@ -66,11 +68,13 @@ Range row_scales_of(const float *scales, int n, int d) { return {scales, (size_t
 
 Range values_of(const dip_grouped_matrix *w)
 {
-    return {w ? w->values : nullptr, w ? (size_t)w->n_experts * row_bytes(w->wtype, w->d_out, w->d_in) : 0};
+    if (!w) return {};
+    return {w->values, (size_t)w->n_experts * (w->wtype == DIP_W_INT4_G128 ? (size_t)w->d_out * w->d_in / 2 : row_bytes(w->wtype, w->d_out, w->d_in))};
 }
 Range scales_of(const dip_grouped_matrix *w)
 {
-    return {w ? w->scales : nullptr, w ? (size_t)w->n_experts * blocks(w->d_out) * blocks(w->d_in) * sizeof(float) : 0};
+    if (!w) return {};
+    return {w->scales, (size_t)w->n_experts * blocks(w->d_in) * (w->wtype == DIP_W_INT4_G128 ? (size_t)w->d_out * 2 : blocks(w->d_out) * sizeof(float))};
 }
 
 size_t choice_bytes(const dip_expert_route *r) { return r ? (size_t)r->n_tokens * r->top_k * 4 : 0; }
@@ -137,7 +141,7 @@ dip_status dip_stage_rows(dip_ctx *ctx, const void *x, int n_tokens, int d, cons
 dip_status dip_grouped_product(dip_ctx *ctx, const dip_grouped_matrix *w, const void *rows, const float *row_scales, int n_rows,
                                const int32_t *offset, void *y, int y_f32, void *stream)
 {
-    if (!dip_ctx_current(ctx) || !matrix_ok(w) || !rows_ok(w->wtype, rows, row_scales) || !n_rows_ok(n_rows) || bad(y))
+    if (!dip_ctx_current(ctx) || !matrix_ok(w, true) || !rows_ok(w->wtype, rows, row_scales) || !n_rows_ok(n_rows) || bad(y))
         return DIP_ERR_INVALID_ARG;
     if (offset ? !dip_aligned16(offset) : w->n_experts != 1) return DIP_ERR_INVALID_ARG;
     if (product_clash(w, nullptr, rows, row_scales, n_rows, offset, y, (size_t)n_rows * w->d_out * (y_f32 ? 4 : 2), nullptr))

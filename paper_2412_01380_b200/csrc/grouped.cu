@@ -1214,6 +1214,7 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
                               const float *row_scales, int n_rows, const int32_t *offset, void *out, bool out_f32, float *out_scales,
                               cudaStream_t stream)
 {
+    if (w.wtype == DIP_W_INT4_G128) return dip_launch_int4_few(ctx, w, up, rows, n_rows, offset, out, out_f32, stream);
     const bool fp8 = w.wtype == DIP_W_FP8_B128;
     const int met = min(w.n_experts, n_rows);
     const int mode = n_rows <= GP_FEW_UP_TO * met ? GP_FEW_ROWS : n_rows >= GP_PAIR_ROWS * met && ctx->sm_count % 2 == 0 ? GP_PAIR : GP_WHOLE;
@@ -1228,8 +1229,8 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
     }
     const int width = up ? GP_COLS / 2 : GP_COLS, tile_rows = mode == GP_PAIR ? 2 * GP_ROWS : mode == GP_WHOLE ? GP_ROWS : GP_FEW;
     GroupedParams p = {};
-    p.w_scales = w.scales;
-    p.up_scales = up ? up->scales : nullptr;
+    p.w_scales = static_cast<const float *>(w.scales);
+    p.up_scales = up ? static_cast<const float *>(up->scales) : nullptr;
     p.row_scales = row_scales;
     p.n_experts = w.n_experts;
     p.d_out = w.d_out;
