@@ -6,10 +6,11 @@
 // Bound by the stream of codes, so what matters is that every SM has enough of it under way and that the ALUs, which turn codes into
 // bfloat16, keep up:
 //   * A unit is 64 outputs (gate/up: 32 of each) by one group: 4 KB of codes, 64 bytes of a row at a time.  Each warp has a ring of
-//     units that it fills with asynchronous copies of its own and waits for by itself; a lane reads back what it copied.
+//     units that it fills with asynchronous copies of its own and waits for by itself; a lane reads back what it copied.  (Twelve warps: with
+//     eight the ALUs waited, with sixteen shared memory has no room for a second unit ahead.)
 //   * A lane's 16 bytes of a row are 32 consecutive codes, and the sums of a group do not depend on the order of its inputs, so the four lanes
-//     of a quad simply take a quarter of the group each, and MMA j takes the codes that one AND brings out of a word: nibbles s and s + 4,
-//     left at the bottom of two bfloat16 of 128 (128 + code is exact there, 136 is subtracted).  x is paired alike.
+//     of a quad simply take a quarter of the group each, and an MMA takes the codes that one AND brings out of a word, nibbles s and s + 4
+//     (int4_codes.cuh).  x is paired alike.
 //   * All units, tile after tile, are dealt out to the blocks in equal runs, and a block's to its warps: whatever the sizes, nobody has
 //     more than a unit too many.  Where whole tiles are hardly worse for the blocks, they stay whole: parts of a tile that meet in
 //     the workspace cost a write, a count and a read (the block that comes last adds them up in order; nobody waits).
@@ -23,10 +24,10 @@
 
 namespace {
 
-constexpr int IF_WARPS = 8, IF_THREADS = IF_WARPS * 32;
+constexpr int IF_WARPS = 12, IF_THREADS = IF_WARPS * 32;
 constexpr int IF_OUTS = 64;                 // outputs of a tile (gate/up: as many sums, of half as many outputs)
 constexpr int IF_PITCH = IF_OUTS + 4;       // floats of a row of partial sums in shared memory (conflict-free)
-constexpr int IF_TILES = 4;                 // tiles that a block has in hand at a time
+constexpr int IF_STAGES = 3;                // units of a warp that are under way or in hand
 constexpr int IF_JOIN = 24;                 // units' worth of time that parts of a tile take to meet
 
 struct FewParams {
@@ -42,51 +43,49 @@ struct FewParams {
     unsigned long long *tr;
 };
 
-template <int NT> struct __align__(16) FewStage {
+struct __align__(16) FewStage {
     uint4 codes[8][32];                     // tile of 16 outputs, half of it; lane
-    uint4 x[NT][4][32];
     __half scales[IF_OUTS];
-    static constexpr int COUNT = NT == 1 ? 4 : 2;   // of a warp (what shared memory has room for)
+};
+
+// A tile: 8 * NT rows of one expert, 64 sums of each.
+struct FewTile {
+    int expert, row0, rows, out0;
+    int w0, w1;                             // the warps that have units of it
+    int b0, b1;                             // and the blocks (b0 == b1: this one alone)
 };
 
 template <int NT> struct __align__(16) FewSmem {
-    FewStage<NT> ring[IF_WARPS][FewStage<NT>::COUNT];
-    float part[IF_WARPS + IF_TILES][8 * NT][IF_PITCH];
+    static constexpr int TILES = NT == 1 ? 20 : 4;      // that a block has in hand at a time (what there is room for)
+    FewStage ring[IF_WARPS][IF_STAGES];
+    float part[IF_WARPS + TILES][8 * NT][IF_PITCH];
+    FewTile tile[TILES];
     int start[DIP_MAX_EXPERTS + 1];         // first row of each expert
     int tiles[DIP_MAX_EXPERTS + 1];         // tiles in front of it
     int last;
 };
 
-// 16 bytes to shared memory, asynchronously; zeros instead where there is nothing to read.
-__device__ __forceinline__ void copy16(void *dst, const void *src, bool there)
+// 16 bytes to shared memory, asynchronously; or zeros.
+__device__ __forceinline__ void copy16(void *dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16_or_0(void *dst, const void *src, bool there)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-
-// A tile: 8 * NT rows of one expert, 64 sums of each.
-struct FewTile {
-    int expert, row0, rows, out0;
-};
-
-template <bool GATED, int NT>
-__device__ __forceinline__ FewTile few_tile(const FewParams &p, const FewSmem<NT> &s, int tile)
+__device__ __forceinline__ void mma_bf16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    int lo = 0, hi = p.n_experts;           // the expert with tiles[e] <= tile < tiles[e + 1]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (s.tiles[mid] <= tile) lo = mid;
-        else hi = mid;
-    }
-    const int n = s.start[lo + 1] - s.start[lo], chunks = (n + 8 * NT - 1) / (8 * NT), in = tile - s.tiles[lo], col = in / chunks;
-    const int first = (in - col * chunks) * 8 * NT;
-    return {lo, s.start[lo] + first, min(8 * NT, n - first), col * (GATED ? IF_OUTS / 2 : IF_OUTS)};
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // First rows and tiles of the experts, by one warp.
@@ -124,17 +123,27 @@ __device__ __forceinline__ void few_plan(const FewParams &p, FewSmem<NT> &s)
     for (int i = i0; i < i1; ++i) s.tiles[i] += incl - n;
 }
 
-// Of n units dealt out to `parts` in equal runs: where run i starts, and whose a unit is (no run is empty: parts <= n).
-__device__ __forceinline__ long long run_start(long long n, int parts, int i) { return n * i / parts; }
-__device__ __forceinline__ int run_of(long long n, int parts, long long unit) { return (int)(((unit + 1) * parts - 1) / n); }
+// Of n units dealt out to `parts` in runs that differ by one at most: where run i starts, and whose a unit is (no run is empty: parts <= n).
+__device__ __forceinline__ int run_start(int n, int parts, int i)
+{
+    const int each = n / parts;
+    return each * i + min(i, n - each * parts);
+}
+__device__ __forceinline__ int run_of(int n, int parts, int unit)
+{
+    const int each = n / parts, longer = n - each * parts, of_these = longer * (each + 1);
+    return unit < of_these ? unit / (each + 1) : longer + (unit - of_these) / each;
+}
 
+// (32 bits hold all numbers of units: launches have at most 16 rows per expert that can have any, so 2^13 in all)
 template <bool GATED, int NT>
 __global__ void __launch_bounds__(IF_THREADS, 1)
 int4_few_kernel(const FewParams p)
 {
     extern __shared__ unsigned char if_smem_raw[];
-    FewSmem<NT> &s = *reinterpret_cast<FewSmem<NT> *>(if_smem_raw);
-    constexpr int STAGES = FewStage<NT>::COUNT;
+    using Smem = FewSmem<NT>;
+    Smem &s = *reinterpret_cast<Smem *>(if_smem_raw);
+    constexpr int STAGES = IF_STAGES, FULL = GATED ? IF_OUTS / 16 : IF_OUTS / 8;      // eights of outputs of a whole tile
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane >> 2, in_quad = lane & 3;
     DIP_TRACE_MIN(p.tr, 0);
     dip_grid_dependency_wait();
@@ -143,69 +152,114 @@ int4_few_kernel(const FewParams p)
     __syncthreads();
     dip_launch_dependents();
 
-    const int tiles = s.tiles[p.n_experts], G = p.groups, blocks = gridDim.x;
-    const long long units = (long long)tiles * G;
-    const int whole_each = (tiles + blocks - 1) / blocks;
-    const bool whole = (long long)whole_each * G <= units / blocks + IF_JOIN;
-    const int parts = (int)min((long long)blocks, units);
-    long long u0 = 0, u1 = 0;               // this block's units
-    if (whole) {
-        u0 = min(units, (long long)run_start(tiles, blocks, blockIdx.x) * G);
-        u1 = min(units, (long long)run_start(tiles, blocks, blockIdx.x + 1) * G);
-    } else if ((int)blockIdx.x < parts) {
-        u0 = run_start(units, parts, blockIdx.x);
-        u1 = run_start(units, parts, blockIdx.x + 1);
+    const int tiles = s.tiles[p.n_experts], G = p.groups, blocks = gridDim.x, units = tiles * G;
+    const bool whole = (tiles + blocks - 1) / blocks * G <= units / blocks + IF_JOIN;
+    const int parts = min(blocks, whole ? tiles : units);
+    int u0 = 0, u1 = 0;                     // this block's units
+    if ((int)blockIdx.x < parts) {
+        u0 = whole ? run_start(tiles, parts, blockIdx.x) * G : run_start(units, parts, blockIdx.x);
+        u1 = whole ? run_start(tiles, parts, blockIdx.x + 1) * G : run_start(units, parts, blockIdx.x + 1);
     }
 
     while (u0 < u1) {
         // the next tiles
-        const int t0 = (int)(u0 / G), t1 = min(t0 + IF_TILES, (int)((u1 + G - 1) / G));
-        const long long end = min(u1, (long long)t1 * G);
-        const int n = (int)(end - u0), warps = min(IF_WARPS, n);
+        const int t0 = u0 / G, t1 = min(t0 + Smem::TILES, (u1 + G - 1) / G), end = min(u1, t1 * G), n = end - u0, warps = min(IF_WARPS, n);
+        if (tid < t1 - t0) {
+            const int tile = t0 + tid;
+            int lo = 0, hi = p.n_experts;   // the expert with tiles[e] <= tile < tiles[e + 1]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (s.tiles[mid] <= tile) lo = mid;
+                else hi = mid;
+            }
+            const int rows = s.start[lo + 1] - s.start[lo], chunks = (rows + 8 * NT - 1) / (8 * NT), in = tile - s.tiles[lo], col = in / chunks;
+            const int first = (in - col * chunks) * 8 * NT, a = max(tile * G, u0), z = min((tile + 1) * G, end);
+            FewTile t = {lo, s.start[lo] + first, min(8 * NT, rows - first), col * (GATED ? IF_OUTS / 2 : IF_OUTS)};
+            t.w0 = run_of(n, warps, a - u0);
+            t.w1 = run_of(n, warps, z - 1 - u0);
+            t.b0 = t.b1 = blockIdx.x;
+            if (z - a < G) {
+                t.b0 = run_of(units, parts, tile * G);
+                t.b1 = run_of(units, parts, (tile + 1) * G - 1);
+            }
+            s.tile[tid] = t;
+        }
+        __syncthreads();
         if (warp < warps) {
-            int load = (int)run_start(n, warps, warp), done = load;
-            const int stop = (int)run_start(n, warps, warp + 1);
-            // where the copies are
-            int lt = (int)((u0 + load) / G), lg = (int)((u0 + load) - (long long)lt * G);
-            FewTile t = few_tile<GATED, NT>(p, s, lt);
-            const auto copy = [&](FewStage<NT> &st) {
-                const int left = p.d_in - lg * DIP_INT4_GROUP;               // inputs from this group on
-                const bool mine = in_quad * 32 < left;
-                const size_t half = (size_t)p.d_in / 2, at = (size_t)lg * (DIP_INT4_GROUP / 2) + in_quad * 16;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const bool up = GATED && i >= 4;
-                    const int o = t.out0 + (GATED ? i & 3 : i) * 8 + quad;
-                    const uint8_t *from = up ? p.up_codes : p.codes;
-                    copy16(&st.codes[i][lane], mine ? from + ((size_t)t.expert * p.d_out + min(o, p.d_out - 1)) * half + at : from, mine);
-                }
-#pragma unroll
-                for (int m = 0; m < NT; ++m) {
-                    const bool there = mine && 8 * m + quad < t.rows;
-                    const __nv_bfloat16 *from = p.rows + (there ? (size_t)(t.row0 + 8 * m + quad) * p.d_in + lg * DIP_INT4_GROUP + in_quad * 32 : 0);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) copy16(&st.x[m][i][lane], there ? from + 8 * i : from, there);
-                }
-                if (lane < 8) {
-                    const bool up = GATED && lane >= 4;
-                    const int o = t.out0 + (GATED ? lane & 3 : lane) * 8;
-                    const __half *from = up ? p.up_scales : p.scales;
-                    copy16(st.scales + 8 * lane, o < p.d_out ? from + ((size_t)t.expert * G + lg) * p.d_out + o : from, o < p.d_out);
-                }
+            const int first = run_start(n, warps, warp), stop = run_start(n, warps, warp + 1);
+            // what is copied next: unit, its tile (among those in hand) and group
+            int load = first, lt = (u0 + first) / G - t0, lg = u0 + first - (lt + t0) * G;
+            const size_t half = (size_t)p.d_in / 2;
+            const uint8_t *from_codes, *from_up = nullptr;                  // of this lane's row of the first 8 outputs
+            const __half *from_scales;
+            int eights;                                                     // eights of the tile's outputs that there are
+            const auto locate = [&] {
+                const FewTile &t = s.tile[lt];
+                const size_t o = (size_t)t.expert * p.d_out + t.out0;
+                from_codes = p.codes + (o + quad) * half + in_quad * 16;
+                if (GATED) from_up = p.up_codes + (o + quad) * half + in_quad * 16;
+                from_scales = (GATED && (lane & 4) ? p.up_scales : p.scales) + (size_t)t.expert * p.groups * p.d_out + t.out0 + lane % FULL * 8;
+                eights = min(FULL, (p.d_out - t.out0) / 8);
             };
-            const auto next = [&](int slot) {
+            locate();
+            const auto next = [&](FewStage &st) {
                 if (load < stop) {
-                    copy(s.ring[warp][slot]);
+                    const int at = lg * (DIP_INT4_GROUP / 2);
+                    const uint8_t *from = from_codes + at, *up = GATED ? from_up + at : nullptr;
+                    const size_t step = 8 * half;
+                    if (eights == FULL && (lg + 1) * DIP_INT4_GROUP <= p.d_in) {
+#pragma unroll
+                        for (int i = 0; i < FULL; ++i, from += step) copy16(&st.codes[i][lane], from);
+                        if (GATED) {
+#pragma unroll
+                            for (int i = FULL; i < 8; ++i, up += step) copy16(&st.codes[i][lane], up);
+                        }
+                        if (lane < 8) copy16(st.scales + 8 * lane, from_scales + (size_t)lg * p.d_out);
+                    } else {
+                        // (zeros for the inputs that are not there: x is zero there too)
+                        const bool mine = lg * DIP_INT4_GROUP + in_quad * 32 < p.d_in;
+#pragma unroll 1
+                        for (int i = 0; i < eights; ++i, from += step, up += step) {
+                            copy16_or_0(&st.codes[i][lane], from, mine);
+                            if (GATED) copy16_or_0(&st.codes[FULL + i][lane], up, mine);
+                        }
+                        if (lane < 8 && lane % FULL < eights) copy16(st.scales + 8 * lane, from_scales + (size_t)lg * p.d_out);
+                    }
                     ++load;
                     if (++lg == G && load < stop) {
                         lg = 0;
-                        t = few_tile<GATED, NT>(p, s, ++lt);
+                        ++lt;
+                        locate();
                     }
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
             };
+            int xt = lt, xg = lg;                                           // whose x is loaded next
 #pragma unroll
-            for (int i = 0; i < STAGES - 1; ++i) next(i);
+            for (int i = 0; i < STAGES - 1; ++i) next(s.ring[warp][i]);
+            uint4 x[NT][4] = {};                                            // (comes straight into registers, a group ahead)
+            const __nv_bfloat16 *from_x;
+            int tile_rows;
+            const auto locate_x = [&] {
+                from_x = p.rows + (size_t)(s.tile[xt].row0 + quad) * p.d_in + in_quad * 32;
+                tile_rows = s.tile[xt].rows;
+            };
+            // (the sums of rows that are not there are nobody's, so whatever was here in front may stand for them)
+            const auto load_x = [&] {
+                const int at = xg * DIP_INT4_GROUP;
+                const bool in = at + in_quad * 32 < p.d_in;
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    const uint4 *from = reinterpret_cast<const uint4 *>(from_x + (size_t)8 * m * p.d_in + at);
+                    if (in && 8 * m + quad < tile_rows) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[m][i] = from[i];
+                    }
+                    if (!in) x[m][0] = x[m][1] = x[m][2] = x[m][3] = make_uint4(0u, 0u, 0u, 0u);
+                }
+            };
+            locate_x();
+            load_x();
             float acc[4][NT][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -213,130 +267,150 @@ int4_few_kernel(const FewParams p)
                 for (int m = 0; m < NT; ++m)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) acc[i][m][j] = 0.f;
-            int tile = (int)((u0 + done) / G), g = (int)((u0 + done) - (long long)tile * G), slot = 0;
-            while (done < stop) {
+            int slot = 0;
+            for (int done = first; done < stop; ++done) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
                 __syncwarp();                           // (also: the unit in front has been read by all lanes)
-                next((slot + STAGES - 1) % STAGES);
-                const FewStage<NT> &st = s.ring[warp][slot];
+                const FewStage &st = s.ring[warp][slot];
+                next(s.ring[warp][slot == 0 ? STAGES - 1 : slot - 1]);
+                const int tile = xt;
+                const bool tile_ends = xg + 1 == G || done + 1 == stop;
                 uint32_t b[NT][16];
 #pragma unroll
                 for (int m = 0; m < NT; ++m)
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const uint4 v = st.x[m][w][lane];
+                        const uint4 v = x[m][w];
                         b[m][4 * w] = __byte_perm(v.x, v.z, 0x5410);        // inputs 0 and 4 of the word's eight, then 1 and 5, ...
-                        b[m][4 * w + 1] = __byte_perm(v.x, v.z, 0x7632);
+                        b[m][4 * w + 1] = int4_sixteenth(__byte_perm(v.x, v.z, 0x7632));
                         b[m][4 * w + 2] = __byte_perm(v.y, v.w, 0x5410);
-                        b[m][4 * w + 3] = __byte_perm(v.y, v.w, 0x7632);
+                        b[m][4 * w + 3] = int4_sixteenth(__byte_perm(v.y, v.w, 0x7632));
                     }
+                if (done + 1 < stop) {
+                    if (++xg == G) {
+                        xg = 0;
+                        ++xt;
+                        locate_x();
+                    }
+                    load_x();
+                }
+                // (IL sums of 16 outputs side by side: MMAs that wait for one another take 20 cycles each)
+                constexpr int IL = 2;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint4 lo = st.codes[2 * i][lane], hi = st.codes[2 * i + 1][lane];
-                    float d[NT][4];
+                for (int i0 = 0; i0 < 4; i0 += IL) {
+                    uint4 q[2 * IL];
 #pragma unroll
-                    for (int m = 0; m < NT; ++m) d[m][0] = d[m][1] = d[m][2] = d[m][3] = 0.f;
+                    for (int i = 0; i < 2 * IL; ++i) q[i] = st.codes[2 * i0 + i][lane];
+                    float d[IL][NT][4];
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        uint32_t a[4], c[4];
-                        int4_pairs(w == 0 ? lo.x : w == 1 ? lo.y : w == 2 ? lo.z : lo.w, a);
-                        int4_pairs(w == 0 ? hi.x : w == 1 ? hi.y : w == 2 ? hi.z : hi.w, c);
+                    for (int w = 0; w < 4; ++w)
+#pragma unroll
+                        for (int i = 0; i < IL; ++i) {
+                            const uint4 lo = q[2 * i], hi = q[2 * i + 1];
+                            uint32_t a[4], c[4];
+                            int4_pairs(w == 0 ? lo.x : w == 1 ? lo.y : w == 2 ? lo.z : lo.w, a);
+                            int4_pairs(w == 0 ? hi.x : w == 1 ? hi.y : w == 2 ? hi.z : hi.w, c);
+#pragma unroll
+                            for (int m = 0; m < NT; ++m) {
+                                if (w == 0) mma_bf16_first(d[i][m], a[0], c[0], a[1], c[1], b[m][0], b[m][1]);
+                                else mma_bf16(d[i][m], a[0], c[0], a[1], c[1], b[m][4 * w], b[m][4 * w + 1]);
+                                mma_bf16(d[i][m], a[2], c[2], a[3], c[3], b[m][4 * w + 2], b[m][4 * w + 3]);
+                            }
+                        }
+#pragma unroll
+                    for (int i = 0; i < IL; ++i) {
+                        const __half *sc = st.scales + 16 * (i0 + i) + quad;
+                        const float s0 = __half2float(sc[0]), s1 = __half2float(sc[8]);
 #pragma unroll
                         for (int m = 0; m < NT; ++m) {
-                            mma_bf16(d[m], a[0], c[0], a[1], c[1], b[m][4 * w], b[m][4 * w + 1]);
-                            mma_bf16(d[m], a[2], c[2], a[3], c[3], b[m][4 * w + 2], b[m][4 * w + 3]);
+                            acc[i0 + i][m][0] = fmaf(d[i][m][0], s0, acc[i0 + i][m][0]);
+                            acc[i0 + i][m][1] = fmaf(d[i][m][1], s0, acc[i0 + i][m][1]);
+                            acc[i0 + i][m][2] = fmaf(d[i][m][2], s1, acc[i0 + i][m][2]);
+                            acc[i0 + i][m][3] = fmaf(d[i][m][3], s1, acc[i0 + i][m][3]);
                         }
                     }
-                    const float s0 = __half2float(st.scales[16 * i + quad]), s1 = __half2float(st.scales[16 * i + 8 + quad]);
-#pragma unroll
-                    for (int m = 0; m < NT; ++m) {
-                        acc[i][m][0] = fmaf(d[m][0], s0, acc[i][m][0]);
-                        acc[i][m][1] = fmaf(d[m][1], s0, acc[i][m][1]);
-                        acc[i][m][2] = fmaf(d[m][2], s1, acc[i][m][2]);
-                        acc[i][m][3] = fmaf(d[m][3], s1, acc[i][m][3]);
-                    }
                 }
-                slot = (slot + 1) % STAGES;
-                ++done;
-                if (++g == G || done == stop) {
+                slot = slot == STAGES - 1 ? 0 : slot + 1;
+                if (tile_ends) {
                     // this warp's part of the tile
-                    float(*to)[IF_PITCH] = s.part[warp + tile - t0];
+                    float(*to)[IF_PITCH] = s.part[warp + tile];
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int m = 0; m < NT; ++m)
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                to[8 * m + 2 * in_quad + (j & 1)][16 * i + quad + 8 * (j >> 1)] = acc[i][m][j];
+                                to[8 * m + 2 * in_quad + (j & 1)][16 * i + quad + 8 * (j >> 1)] = acc[i][m][j] * INT4_PRODUCT;
                                 acc[i][m][j] = 0.f;
                             }
-                    g = 0;
-                    ++tile;
                 }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
         }
         __syncthreads();
-        for (int tile = t0; tile < t1; ++tile) {
-            const FewTile t = few_tile<GATED, NT>(p, s, tile);
-            const long long a = max((long long)tile * G, u0) - u0, z = min((long long)(tile + 1) * G, end) - u0;
-            const int w0 = run_of(n, warps, a), w1 = run_of(n, warps, z - 1);
-            const bool cut = z - a < G;
-            // sums of 4 neighbouring outputs of one row; gate/up: 4 of each
-            constexpr int QUADS = IF_OUTS / 4;
-            const int r = tid / QUADS, c = (GATED ? tid % QUADS / 2 * 4 + tid % 2 * (IF_OUTS / 2) : tid % QUADS * 4);
-            const int b0 = cut ? run_of(units, parts, (long long)tile * G) : 0, b1 = cut ? run_of(units, parts, (long long)(tile + 1) * G - 1) : 0;
-            float4 v = {};
-            if (r < t.rows) {
-                for (int w = w0; w <= w1; ++w) {
-                    const float4 q = *reinterpret_cast<const float4 *>(&s.part[w + tile - t0][r][c]);
-                    v.x += q.x;
-                    v.y += q.y;
-                    v.z += q.z;
-                    v.w += q.w;
-                }
-            }
-            if (cut) {
-                constexpr size_t PART = (size_t)8 * NT * IF_OUTS;
-                // a block's first tile may have begun in front of it, its last one may go on behind it
-                const auto part_at = [&](int b) {
-                    return reinterpret_cast<float4 *>(p.partials + (2 * (size_t)b + (b == b0 ? 1 : 0)) * PART) + r * QUADS + c / 4;
-                };
-                if (r < t.rows) *part_at(blockIdx.x) = v;
-                __threadfence();
-                __syncthreads();
-                if (tid == 0) {
-                    s.last = atomicAdd(p.tickets + b0, 1u) == (unsigned)(b1 - b0);
-                    if (s.last) p.tickets[b0] = 0u;
-                    __threadfence();
-                }
-                __syncthreads();
-                if (!s.last) continue;
-                v = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (r < t.rows) {
-                    for (int b = b0; b <= b1; ++b) {
-                        const float4 q = __ldcg(part_at(b));
-                        v.x += q.x;
-                        v.y += q.y;
-                        v.z += q.z;
-                        v.w += q.w;
-                    }
-                }
-            }
+        // Sums of 4 neighbouring outputs of a row per thread; gate/up: of gate or up, the neighbouring thread has the other one.
+        constexpr int QUADS = IF_OUTS / 4, PER_TILE = 8 * NT * QUADS;
+        constexpr size_t PART = (size_t)8 * NT * IF_OUTS;
+        const auto leave = [&](const FewTile &t, int r, int c, const float4 &v) {
             const size_t row = (size_t)(t.row0 + r) * p.d_out;
+            const int o = t.out0 + c;
             if (GATED) {
-                // (the neighbouring thread has the other one of gate and up)
                 float4 u;
                 u.x = __shfl_down_sync(0xffffffffu, v.x, 1);
                 u.y = __shfl_down_sync(0xffffffffu, v.y, 1);
                 u.z = __shfl_down_sync(0xffffffffu, v.z, 1);
                 u.w = __shfl_down_sync(0xffffffffu, v.w, 1);
-                if (r < t.rows && tid % 2 == 0 && t.out0 + c < p.d_out)
-                    *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.out) + row + t.out0 + c) =
+                if (r < t.rows && tid % 2 == 0 && o < p.d_out)
+                    *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.out) + row + o) =
                         bf16x4(silu_f32(v.x) * u.x, silu_f32(v.y) * u.y, silu_f32(v.z) * u.z, silu_f32(v.w) * u.w);
-            } else if (r < t.rows && t.out0 + c < p.d_out) {
-                if (p.out_f32) *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + row + t.out0 + c) = v;
-                else *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.out) + row + t.out0 + c) = bf16x4(v.x, v.y, v.z, v.w);
+            } else if (r < t.rows && o < p.d_out) {
+                if (p.out_f32) *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + row + o) = v;
+                else *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.out) + row + o) = bf16x4(v.x, v.y, v.z, v.w);
+            }
+        };
+        // (whole warps: PER_TILE and the number of threads are multiples of 32)
+        for (int i = tid; i < (t1 - t0) * PER_TILE; i += IF_THREADS) {
+            const int k = i / PER_TILE, q = i % QUADS, r = i / QUADS % (8 * NT), c = GATED ? q / 2 * 4 + q % 2 * (IF_OUTS / 2) : q * 4;
+            const FewTile t = s.tile[k];
+            float4 v = {};
+            if (r < t.rows) {
+                for (int w = t.w0; w <= t.w1; ++w) {
+                    const float4 a = *reinterpret_cast<const float4 *>(&s.part[w + k][r][c]);
+                    v.x += a.x;
+                    v.y += a.y;
+                    v.z += a.z;
+                    v.w += a.w;
+                }
+            }
+            // A tile that is cut: a block's first one may have begun in front of it, its last one may go on behind it.
+            if (t.b0 == t.b1) leave(t, r, c, v);
+            else if (r < t.rows) reinterpret_cast<float4 *>(p.partials + (2 * (size_t)blockIdx.x + ((int)blockIdx.x == t.b0)) * PART)[r * QUADS + q] = v;
+        }
+        for (int k = 0; k < t1 - t0; k = k == t1 - t0 - 1 ? k + 1 : t1 - t0 - 1) {           // (the first one and the last one)
+            const FewTile t = s.tile[k];
+            if (t.b0 == t.b1) continue;
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                s.last = atomicAdd(p.tickets + t.b0, 1u) == (unsigned)(t.b1 - t.b0);
+                if (s.last) p.tickets[t.b0] = 0u;
+                __threadfence();
+            }
+            __syncthreads();
+            if (!s.last) continue;
+            for (int i = tid; i < PER_TILE; i += IF_THREADS) {
+                const int q = i % QUADS, r = i / QUADS, c = GATED ? q / 2 * 4 + q % 2 * (IF_OUTS / 2) : q * 4;
+                float4 v = {};
+                if (r < t.rows) {
+                    for (int b = t.b0; b <= t.b1; ++b) {
+                        const float4 a = __ldcg(reinterpret_cast<const float4 *>(p.partials + (2 * (size_t)b + (b == t.b0)) * PART) + r * QUADS + q);
+                        v.x += a.x;
+                        v.y += a.y;
+                        v.z += a.z;
+                        v.w += a.w;
+                    }
+                }
+                leave(t, r, c, v);
             }
         }
         u0 = end;
@@ -351,7 +425,6 @@ cudaError_t launch(dip_ctx *ctx, int ctas, cudaStream_t stream, const FewParams 
     static dip_per_device_once once;
     constexpr size_t smem = sizeof(FewSmem<NT>);
     static_assert(smem <= 227 * 1024, "fits a CTA's shared memory");
-    static_assert(8 * NT * (IF_OUTS / 4) <= IF_THREADS, "a thread for each four sums");
     const cudaError_t e = dip_raise_smem_limit(once, ctx->device, int4_few_kernel<GATED, NT>, smem);
     if (e != cudaSuccess) return e;
     return dip_launch_pdl(int4_few_kernel<GATED, NT>, dim3(ctas), dim3(IF_THREADS), smem, stream, p);
