@@ -25,6 +25,15 @@ __device__ __forceinline__ uint32_t int4_sixteenth(uint32_t x)
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(x), "r"(0x3d803d80u));
     return v;
 }
+// The same word as four pairs of neighbours (codes 0 and 1, 2 and 3, ...), all of them (code - 8) / 64, for operands that are in order.
+__device__ __forceinline__ void int4_in_order(uint32_t w, uint32_t *v)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t byte = __byte_perm(w, 0u, 0x4040 + 0x0101 * j) & 0x00f0000fu;       // a byte's codes stay where they are in it
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[j]) : "r"(byte), "r"(0x7d007f00u), "r"(0xbe00be00u));      // * (2^127, 2^123) - 1/8
+    }
+}
 constexpr float INT4_PRODUCT = 64.f;            // a product by these operands times this is the product
 
 // Four values, each rounded once to bfloat16.
