@@ -70,7 +70,7 @@ enum {
     DIP_MAX_EXPERTS = 512,
     DIP_MAX_TOP_K = 16,        /* experts per token                                                  */
     DIP_MAX_TOKENS = 65536,    /* tokens per call of the router and the expert block                 */
-    DIP_MAX_OUT = 262144       /* outputs of a 4-bit matrix in dip_grouped_product (a head)          */
+    DIP_MAX_OUT = 262144       /* outputs of a 4-bit matrix in dip_grouped_product (a head), logits  */
 };
 
 typedef struct dip_ctx dip_ctx;   /* opaque; owns scratch workspace on one device */
@@ -179,7 +179,7 @@ dip_status dip_selftest_group_waits(dip_ctx *ctx, int limit_us, unsigned long lo
  *   kind: 1 select (DIP), 2 select (cache-aware), 3 cache update, 4 gate/up GEMV,
  *         5 down GEMV, 6 cache update and slot assignment, 7 reads of the slow tier (two-tier step; parts
  *         of a GEMV's launch, or of one that does both), 9 neuron-major product (Gate / Up pruning),
- *         10 grouped gate/up product, 11 grouped product.
+ *         10 grouped gate/up product, 11 grouped product, 12 choice of tokens.
  * ------------------------------------------------------------------------ */
 typedef struct {
     int32_t kind;
@@ -711,6 +711,35 @@ typedef struct {
 dip_status dip_expert_mlp(dip_ctx *ctx, const dip_grouped_matrix *gate, const dip_grouped_matrix *up,
                           const dip_grouped_matrix *down, const void *x, int n_tokens,
                           const dip_expert_route *route, const dip_expert_work *work, void *y, void *stream);
+
+/* ========================================================================
+ * dip_sample_tokens — each row's token from its logits and one given number.
+ *   logits  [n_rows][pitch], binary32 or (logits_bf16 != 0) bfloat16; the first vocab of a row are read.  pitch >= vocab
+ *           is the distance of rows in items.  (Here pointers need only be aligned to their items.)
+ *   how     device arrays [n_rows], each may be NULL; NULL itself: all are.
+ *   uniform [n_rows] binary32, taken to lie in [0, 1) (below 0 or NaN counts as 0, from 1 on as the end).
+ *   token   [n_rows] out;  prob [n_rows] out, may be NULL: its probability among the tokens that were left.
+ * Definition, for a row z and e_i = exp((z_i - max z) / temperature).  A logit of -infinity or NaN is closed: its e is 0.
+ *   order    logit descending, index ascending
+ *   top_k    keeps the first top_k of the order                     (<= 0 or >= vocab, or NULL: all)
+ *   top_p    then keeps those in front of which the sum of e is below top_p times the sum of all that top_k kept; the
+ *            first one always                                       (>= 1 or NaN, or NULL: all)
+ *   min_p    then keeps those with e >= min(min_p, 1)               (<= 0 or NaN, or NULL: all)
+ *   token    the smallest index at which the sum of the kept e in order of index exceeds uniform times their sum
+ *   temperature <= 0 or NaN: the first of the order, prob 1         (NULL: 1).  Infinite: all open logits alike.
+ * Where logits of +infinity stand, they share alike and the others get 0.  A row without an open logit (padding): token
+ * -1, prob 0.  Sums are exact, of weights held as whole multiples of 2^-45 of the largest: results do not depend on the device.
+ * 1 <= n_rows <= DIP_MAX_TOKENS, 1 <= vocab <= DIP_MAX_OUT.  What is written must not overlap what is read or what else is
+ * written.  Uses none of the context's workspace.
+ * ======================================================================== */
+typedef struct {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p;
+    const float *min_p;
+} dip_sampling;
+dip_status dip_sample_tokens(dip_ctx *ctx, const void *logits, int logits_bf16, int n_rows, int vocab, int64_t pitch,
+                             const dip_sampling *how, const float *uniform, int32_t *token, float *prob, void *stream);
 
 #ifdef __cplusplus
 }

@@ -167,6 +167,15 @@ _lib.dip_expert_mlp.argtypes = [_vp, C.POINTER(GroupedMatrixStruct), C.POINTER(G
                                 C.POINTER(GroupedMatrixStruct), _vp, _i32, C.POINTER(ExpertRouteStruct),
                                 C.POINTER(ExpertWorkStruct), _vp, _vp]
 
+
+
+class SamplingStruct(C.Structure):
+    _fields_ = [("temperature", _vp), ("top_k", _vp), ("top_p", _vp), ("min_p", _vp)]
+
+
+_lib.dip_sample_tokens.restype = _i32
+_lib.dip_sample_tokens.argtypes = [_vp, _vp, _i32, _i32, _i32, C.c_int64, C.POINTER(SamplingStruct), _vp, _vp, _vp, _vp]
+
 EXPORTED = ["dip_create", "dip_create_ex", "dip_destroy", "dip_status_string", "dip_last_error", "dip_sm_count",
             "dip_device_status", "dip_reset_device_status", "dip_selftest_bounded_wait", "dip_selftest_block_waits", "dip_selftest_group_waits", "dip_stack_step_probed",
             "dip_trace_begin", "dip_trace_reset", "dip_trace_read", "dip_trace_end",
@@ -176,7 +185,7 @@ EXPORTED = ["dip_create", "dip_create_ex", "dip_destroy", "dip_status_string", "
             "dip_residual_rmsnorm", "dip_stack_step", "dip_mlp_step_tiered", "dip_mlp_step_neuron_pruned",
             "dip_sparse_gemv_down_noalloc",
             "dip_route_experts", "dip_stage_rows", "dip_grouped_product", "dip_grouped_gate_up", "dip_combine_rows",
-            "dip_expert_mlp"]
+            "dip_expert_mlp", "dip_sample_tokens"]
 
 
 class TraceRecord(C.Structure):
@@ -185,7 +194,7 @@ class TraceRecord(C.Structure):
 
 
 TRACE_KINDS = {1: "select", 2: "select_ca", 3: "cache_update", 4: "gemv_gate_up", 5: "gemv_down",
-               6: "tier_books", 7: "tier_fetch", 9: "rowdot", 10: "grouped_gate_up", 11: "grouped_product"}
+               6: "tier_books", 7: "tier_fetch", 9: "rowdot", 10: "grouped_gate_up", 11: "grouped_product", 12: "sample"}
 for _name in ("dip_trace_begin", "dip_trace_reset", "dip_trace_end"):
     getattr(_lib, _name).restype = _i32
     getattr(_lib, _name).argtypes = [_vp]
@@ -788,3 +797,35 @@ def dip_expert_mlp(ctx: Context, w: ExpertWeights, x: torch.Tensor, work: Expert
         _refuse("buffers for %d rows %s a route, %d are needed", work.max_rows, "with" if work.routed else "without", n)
     ctx.check(_lib.dip_expert_mlp(ctx.handle, w.gate.ref, w.up.ref, w.down.ref, x.data_ptr(), n_tokens,
                                   route.ref if route is not None else None, work.ref, y.data_ptr(), _stream()))
+
+
+# ---- the choice of tokens --------------------------------------------------------------------------------------------------
+def _per_row(t, dtype, n: int, name: str, device: int):
+    """The address of a contiguous [n] tensor of that type on that device, None for None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != device or t.shape != (n,) or not t.is_contiguous():
+        _refuse("%s must be a contiguous tensor [%d] of %s on device %d", name, n, dtype, device)
+    return t.data_ptr()
+
+
+def dip_sample_tokens(ctx: Context, logits: torch.Tensor, uniform: torch.Tensor, token: torch.Tensor,
+                      prob: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
+                      top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                      min_p: Optional[torch.Tensor] = None) -> None:
+    """logits [n, vocab], binary32 or bfloat16, rows any distance apart; uniform float32 [n] in [0, 1) -> token int32 [n] and its
+    probability prob float32 [n].  temperature, top_p, min_p float32 [n], top_k int32 [n], or None."""
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in (torch.float32, torch.bfloat16) or logits.get_device() != ctx.device:
+        _refuse("logits must be a float32 or bfloat16 tensor on device %d", ctx.device)
+    if logits.dim() != 2 or logits.shape[0] < 1 or logits.shape[1] < 1 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        _refuse("logits must be [n, vocab] with neighbouring logits of a row side by side")
+    if token is None or uniform is None:
+        _refuse("token and uniform are needed")
+    (n, vocab), device = logits.shape, ctx.device
+    how = SamplingStruct(_per_row(temperature, torch.float32, n, "temperature", device), _per_row(top_k, torch.int32, n, "top_k", device),
+                         _per_row(top_p, torch.float32, n, "top_p", device), _per_row(min_p, torch.float32, n, "min_p", device))
+    u, t, p = (_per_row(uniform, torch.float32, n, "uniform", device), _per_row(token, torch.int32, n, "token", device),
+               _per_row(prob, torch.float32, n, "prob", device))
+    pitch = logits.stride(0) if n > 1 else vocab
+    ctx.check(_lib.dip_sample_tokens(ctx.handle, logits.data_ptr(), logits.dtype is torch.bfloat16, n, vocab, pitch, C.byref(how), u, t, p,
+                                     _stream()))
