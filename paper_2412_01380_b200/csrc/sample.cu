@@ -5,9 +5,13 @@
 // so results depend neither on how a row is shared out nor on the order of atomics, and a row's 2^18 weights fit 64 bits.
 //
 // Top-k and top-p both keep the front of the row's order (logit descending, index ascending), which ends at some element: its key and
-// its index.  Finding it is a histogram (of counts, or of weights) over bins of equal width below the largest logit, whose bins
-// each block adds up a part of; then, in the bin where the front ends, either all pairs of its elements compared (up to
-// SP_LIST), or histograms of the keys' next bits until one key is left, and a count in order of index among its ties.
+// its index.  A histogram of counts says in which bin that is (bins of bfloat16 are its values, so their weights are known exactly; bins of
+// binary32 are of equal width, with the sum of what is left in each, and their weights are known to some 10^-5, which is checked).
+//   few   what is left up to that bin is at most SP_LIST elements: they go to the row's first block, which does the rest by itself
+//   many  the elements of the bin (binary32: of the bins where the border can be) go there, which finds the border; or, ties of one
+//         bfloat16 value, they are counted in order of index; then all blocks draw
+//   else  (a crowd in one bin, borders that the check refuses, a long top-k with a top-p behind it) histograms of weights over ever fewer keys
+// Several thousand elements in shared memory are searched by histograms of their own (`reach`).
 // The draw adds up the kept weights per warp (whose elements are consecutive), then looks closer where the sum crosses the number.
 #include <initializer_list>
 
@@ -18,8 +22,10 @@ namespace {
 
 constexpr int SP_THREADS = 512, SP_WARPS = SP_THREADS / 32;
 constexpr int SP_CLUSTER = 8;                   // most blocks per row
-constexpr int SP_BINS = 2048;
-constexpr int SP_LIST = 512;                    // elements that are compared pair by pair
+constexpr int SP_BINS = 2048;                   // of a histogram of weights
+constexpr int SP_PAIRS = 512;                   // elements that are compared pair by pair
+constexpr int SP_LIST = 2048;                   // elements that one block looks after
+constexpr int SP_REACH = SP_THREADS;            // bins by which it does
 constexpr int SP_TABLE = 512;                   // 2^(j / 512)
 constexpr int SP_ONE_BITS = 45;                 // the largest weight is 2^45
 constexpr float SP_SPREAD = 64.f;               // logits further below the largest one share the last bin of the first histogram
@@ -42,18 +48,36 @@ struct SampleBorder {
     int index;
 };
 
-struct __align__(16) SampleSmem {
-    double table[SP_TABLE];
+struct SampleList {
+    u64 mass[SP_LIST];
+    unsigned key[SP_LIST];
+    int index[SP_LIST];
+};
+struct SampleWeights {                          // the last resort's
     u64 mass[SP_BINS];
     unsigned count[SP_BINS];
-    u64 list_mass[SP_LIST];
-    unsigned list_key[SP_LIST];
-    int list_index[SP_LIST];
-    int listed;
-    u64 scan[SP_WARPS + 1];
+    u64 list_mass[SP_PAIRS];
+    unsigned list_key[SP_PAIRS];
+    int list_index[SP_PAIRS];
+};
+
+struct __align__(16) SampleSmem {
+    double table[SP_TABLE];
+    union {
+        unsigned bins[8192];                    // counts; binary32: 4096 of them and what is left in each (1/1024 of a bin's width)
+        SampleList list;
+        SampleWeights weights;
+    };
+    u64 reach[SP_REACH];
+    unsigned reach_count[SP_REACH];
+    int final_slot[32];
+    int finals, reached, listed;
+    u64 reach_before;
+    u64 tiny[2];
+    u64 scan[SP_WARPS + 1], scan_max[SP_WARPS];
     // what the blocks of a cluster tell one another
-    u64 total[SP_CLUSTER];
-    float top[SP_CLUSTER], low[SP_CLUSTER];
+    u64 total[SP_CLUSTER], sums[3][SP_CLUSTER];
+    float top, low;
     int first[SP_CLUSTER];
     unsigned key_lo[SP_CLUSTER], key_hi[SP_CLUSTER];
     struct {
@@ -61,6 +85,13 @@ struct __align__(16) SampleSmem {
         unsigned count;
         u64 before;
     } found;
+    struct {
+        int bin;
+        unsigned count;                         // of its elements, and of those in front of it
+        unsigned in_front;
+        u64 before;                             // and the weight of those
+    } cut[2];
+    u64 all_count, all_weight;                  // (bfloat16: exact)
     SampleBorder border;
     float block_top[SP_WARPS], block_low[SP_WARPS];
     int block_first[SP_WARPS];
@@ -78,9 +109,10 @@ __device__ __forceinline__ unsigned cluster_size()
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
     return n;
 }
-__device__ __forceinline__ void cluster_sync()
+__device__ __forceinline__ void cluster_sync(unsigned blocks)
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (blocks == 1) __syncthreads();
+    else asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Where block `rank` has what is at p here.
 __device__ __forceinline__ uint32_t at_rank(const void *p, unsigned rank)
@@ -128,16 +160,14 @@ struct Row {
     // exp((z - top) / temperature): 2^(k / 512) from the table times the third-order sum for what is left (within 10^-14)
     __device__ __forceinline__ double weight(float z) const
     {
-        if (z == top) return 1.0;
-        if (top == INFINITY) return 0.0;
-        const double y = ((double)z - (double)top) * steps;
-        if (!(y > -60.0 * SP_TABLE)) return 0.0;
+        const double y = fmax(((double)z - (double)top) * steps, -64.0 * SP_TABLE);          // (of infinities: not a number, which fmax drops)
         const double magic = 6755399441055744.0, k = y + magic;
         const int i = __double2loint(k);
         const double f = (y - (k - magic)) * (0.69314718055994530942 / SP_TABLE);
         const double t = s.table[i & (SP_TABLE - 1)];
         const double e = fma(t, f * fma(f, fma(f, 1.0 / 6.0, 0.5), 1.0), t);
-        return __hiloint2double(__double2hiint(e) + ((i >> 9) << 20), __double2loint(e));
+        const double w = __hiloint2double(__double2hiint(e) + ((i >> 9) << 20), __double2loint(e));
+        return z == top ? 1.0 : y > -60.0 * SP_TABLE ? w : 0.0;
     }
     __device__ __forceinline__ u64 mass(float z) const
     {
@@ -149,6 +179,300 @@ struct Row {
     {
         const unsigned k = key_of(z);
         return z > -INFINITY && (k > b.key || (k == b.key && begin + i <= b.index));
+    }
+
+    // Bins in order of falling logits.  bfloat16: one per value from 2^-12 to 2^20 either way, the first, the last and the two in the middle
+    // for all beyond.  (Places are such that a thread's consecutive bins and its neighbours' fall on different banks.)
+    static constexpr bool HALF = sizeof(T) == 2;
+    static constexpr int BINS = HALF ? 8192 : 4096, HALF_FIRST = 115 << 7;
+    static constexpr float REST = 1024.f;
+    __device__ __forceinline__ int place(int bin) const { return bin ^ (bin >> 4 & 15); }
+    __device__ __forceinline__ int bin_of(float z) const
+    {
+        if (HALF) {
+            const int m = min(max((int)(__float_as_uint(z) >> 16 & 0x7fffu) - HALF_FIRST, 0), 4095);
+            return __float_as_int(z) < 0 ? 4096 + m : 4095 - m;
+        }
+        return min(BINS - 1, (int)((top - z) * scale * 2.f));
+    }
+    __device__ __forceinline__ bool middle(int bin) const { return bin == 4095 || bin == 4096; }           // (HALF)
+    __device__ __forceinline__ bool mixed(int bin) const { return HALF ? middle(bin) || bin == 0 || bin == 8191 : true; }
+    __device__ __forceinline__ float value_of(int bin) const
+    {
+        return __uint_as_float(bin < 4096 ? (unsigned)(HALF_FIRST + 4095 - bin) << 16 : ((unsigned)(HALF_FIRST + bin - 4096) << 16) | 0x80000000u);
+    }
+    // The weight of a bin's elements.  HALF: exact (the last bin's are 0: see `plain` below); else as if each had the middle one's.
+    __device__ __forceinline__ u64 bin_mass(int bin, unsigned count, unsigned rest) const
+    {
+        if (count == 0) return 0;
+        if (HALF) {
+            if (middle(bin)) {
+                u64 q = 0;
+                for (unsigned r = 0; r < blocks; ++r) q += get64(at_rank(&s.tiny[bin - 4095], r));
+                return q;
+            }
+            return bin == 8191 ? 0 : count * mass(value_of(bin));
+        }
+        const float below = ((float)bin + ((float)rest + 0.5f * count) / (REST * count)) / (2.f * scale);
+        return (u64)__double2ull_rn((double)(exp2f(below * (float)(steps * (-1.0 / SP_TABLE))) * (float)count) * (double)(1ull << 40));
+    }
+    __device__ __forceinline__ void histogram() const
+    {
+        for (int i = threadIdx.x; i < 8192 / 4; i += SP_THREADS) reinterpret_cast<uint4 *>(s.bins)[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (threadIdx.x < 2) s.tiny[threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll 4
+        for (int i = threadIdx.x; i < n; i += SP_THREADS) {
+            const float z = value(i);
+            if (!(z > -INFINITY)) continue;
+            const int bin = bin_of(z);
+            atomicAdd(&s.bins[place(bin)], 1u);
+            if (HALF) {
+                if (middle(bin)) atomicAdd(&s.tiny[bin - 4095], mass(z));
+            } else {
+                const float at = (top - z) * scale * 2.f;
+                atomicAdd(&s.bins[BINS + place(bin)], (unsigned)(fminf(at - (float)bin, 1.f) * REST));
+            }
+        }
+        cluster_sync(blocks);
+    }
+    // The bins where a count (top_k > 0), or a weight, is reached: the latter (HALF) exactly, or between cut[0] and cut[1] if all is well.
+    __device__ __forceinline__ void cuts(int top_k, float top_p) const
+    {
+        const int mine = BINS / blocks, each = (mine + SP_THREADS - 1) / SP_THREADS, b0 = rank * mine + threadIdx.x * each;
+        const int in = max(0, min(each, (int)((rank + 1) * mine) - b0));
+        u64 weights = 0, counts = 0;
+#pragma unroll 4
+        for (int j = 0; j < in; ++j) {
+            unsigned count = 0, rest = 0;
+            const int at = place(b0 + j);
+            for (unsigned r = 0; r < blocks; ++r) {
+                count += get32(at_rank(&s.bins[at], r));
+                if (!HALF) rest += get32(at_rank(&s.bins[BINS + at], r));
+            }
+            s.bins[at] = count;                 // (nobody else reads these of this block)
+            if (!HALF) s.bins[BINS + at] = rest;
+            counts += count;
+            if (top_k == 0) weights += bin_mass(b0 + j, count, rest);
+        }
+        u64 block_counts, block_weights = 0;
+        u64 before_c = scan(counts, block_counts), before_w = top_k == 0 ? scan(weights, block_weights) : 0;
+        if (threadIdx.x < blocks) {
+            put64(at_rank(&s.sums[0][rank], threadIdx.x), block_counts);
+            put64(at_rank(&s.sums[1][rank], threadIdx.x), block_weights);
+        }
+        cluster_sync(blocks);
+        u64 all_c = 0, all_w = 0;
+        for (unsigned r = 0; r < blocks; ++r) {
+            before_c += r < rank ? s.sums[0][r] : 0;
+            before_w += r < rank ? s.sums[1][r] : 0;
+            all_c += s.sums[0][r];
+            all_w += s.sums[1][r];
+        }
+        if (threadIdx.x == 0) {
+            s.all_count = all_c;
+            s.all_weight = all_w;
+        }
+        const double goal = fmax((double)top_p, 0.0) * (double)all_w;
+#pragma unroll
+        for (int c = 0; c < (HALF ? 1 : 2); ++c) {
+            const u64 want = top_k ? min((u64)top_k, all_c)
+                             : HALF ? max(1ull, (u64)ceil(goal)) : min(all_w, max(1ull, (u64)(c ? goal * (1 + 1.0 / 2048) + 2 : goal * (1 - 1.0 / 2048))));
+            const u64 before = top_k ? before_c : before_w, here = top_k ? counts : weights;
+            if (before < want && want <= before + here) {
+                u64 bc = before_c, bw = before_w;
+                for (int j = 0; j < in; ++j) {
+                    const int at = place(b0 + j);
+                    const unsigned count = s.bins[at];
+                    const u64 w = top_k ? 0 : bin_mass(b0 + j, count, HALF ? 0 : s.bins[BINS + at]), b = top_k ? bc : bw, u = top_k ? count : w;
+                    if (b < want && want <= b + u) {
+                        for (unsigned r = 0; r < blocks; ++r) {
+                            put32(at_rank(&s.cut[c].bin, r), b0 + j);
+                            put32(at_rank(&s.cut[c].count, r), count);
+                            put32(at_rank(&s.cut[c].in_front, r), (unsigned)bc);
+                            put64(at_rank(&s.cut[c].before, r), bw);
+                            if (HALF) put64(at_rank(&s.found.before, r), want);
+                        }
+                    }
+                    bc += count;
+                    bw += w;
+                }
+            }
+        }
+        cluster_sync(blocks);
+    }
+
+    // Sends the elements of the bins first .. last to the first block's list (if there are at most SP_LIST; s.listed of the first
+    // block counts all).  sums: [0] the weight of all elements in front of them, [1] their own, [2] of all behind them, if `weigh`.
+    // Ends with a cluster barrier, after which every block has all blocks' sums.
+    __device__ __forceinline__ void collect(int first, int last, bool weigh, u64 (&sums)[3]) const
+    {
+        u64 mine[3] = {0, 0, 0};
+        const uint32_t listed = at_rank(&s.listed, 0);
+#pragma unroll 4
+        for (int i = threadIdx.x; i < n; i += SP_THREADS) {
+            const float z = value(i);
+            const bool open = z > -INFINITY;
+            const int bin = open ? bin_of(z) : BINS;
+            const bool in = bin >= first && bin <= last;
+            u64 q = 0;
+            if (weigh || in) q = mass(z);
+            if (weigh) mine[bin < first ? 0 : bin <= last ? 1 : 2] += q;
+            if (in) {
+                unsigned slot;
+                asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(slot) : "r"(listed) : "memory");
+                if (slot < SP_LIST) {
+                    put32(at_rank(&s.list.key[slot], 0), key_of(z));
+                    put32(at_rank(&s.list.index[slot], 0), begin + i);
+                    put64(at_rank(&s.list.mass[slot], 0), q);
+                }
+            }
+        }
+        if (weigh) {
+#pragma unroll
+            for (int j = 0; j < 3; ++j) {
+                u64 sum;
+                scan(mine[j], sum);
+                if (threadIdx.x < blocks) put64(at_rank(&s.sums[j][rank], threadIdx.x), sum);
+            }
+        }
+        cluster_sync(blocks);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            sums[j] = 0;
+            if (weigh)
+                for (unsigned r = 0; r < blocks; ++r) sums[j] += s.sums[j][r];
+        }
+    }
+
+    // Of m elements, each with a number of its own and a share (0: none), the one at which the sum of shares in order of the numbers
+    // reaches `want` (1 up to the sum of all).  By one block.
+    template <class Number, class Share>
+    __device__ int reach(int m, const Number &number, const Share &share, u64 want) const
+    {
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+        u64 lo = ~0ull, hi = 0, before = 0;
+        for (int i = tid; i < m; i += SP_THREADS)
+            if (share(i)) {
+                lo = min(lo, number(i));
+                hi = max(hi, number(i));
+            }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+            hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        }
+        __syncthreads();
+        if (lane == 0) {
+            s.scan[warp] = lo;
+            s.scan_max[warp] = hi;
+        }
+        __syncthreads();
+        for (int w = 0; w < SP_WARPS; ++w) {
+            lo = min(lo, s.scan[w]);
+            hi = max(hi, s.scan_max[w]);
+        }
+        for (;;) {
+            const int bits = lo == hi ? 0 : 64 - __clzll(hi - lo), shift = max(0, bits - 9);
+            s.reach[tid] = 0;
+            s.reach_count[tid] = 0;
+            if (tid == 0) s.finals = s.reached = 0;
+            __syncthreads();
+            for (int i = tid; i < m; i += SP_THREADS) {
+                const u64 q = share(i), a = number(i);
+                if (!q || a < lo || a > hi) continue;
+                const int bin = (int)((a - lo) >> shift);
+                atomicAdd(&s.reach_count[bin], 1u);
+                atomicAdd(&s.reach[bin], q);
+            }
+            __syncthreads();
+            u64 ignored;
+            const u64 here = s.reach[tid], b = before + scan(here, ignored);
+            if (b < want && want <= b + here) {
+                s.reached = tid;
+                s.reach_before = b;
+            }
+            __syncthreads();
+            before = s.reach_before;            // (there is one: 1 <= want <= the sum)
+            const int few = s.reach_count[s.reached];
+            lo += (u64)s.reached << shift;
+            hi = min(hi, lo + ((1ull << shift) - 1));
+            if (few <= 32) break;
+            __syncthreads();
+        }
+        for (int i = tid; i < m; i += SP_THREADS)
+            if (share(i) && number(i) >= lo && number(i) <= hi) s.final_slot[atomicAdd(&s.finals, 1)] = i;
+        __syncthreads();
+        if (tid < s.finals) {
+            const int i = s.final_slot[tid];
+            const u64 a = number(i);
+            u64 b = before;
+            for (int j = 0; j < s.finals; ++j)
+                if (number(s.final_slot[j]) < a) b += share(s.final_slot[j]);
+            if (b < want && want <= b + share(i)) s.reached = i;
+        }
+        __syncthreads();
+        return s.reached;
+    }
+    __device__ __forceinline__ u64 number_in_order(int i) const { return ((u64)~s.list.key[i] << 20) | (unsigned)s.list.index[i]; }
+
+    // The first block has all that can be left in its list: everything else.  all: the weight that top_p is a share of (top_k > 0: of what
+    // that leaves).
+    __device__ void finish(int top_k, float top_p, float min_p, float u, u64 all, int32_t *token, float *prob) const
+    {
+        const int m = s.listed;
+        u64 last = ~0ull;                       // the border's number
+        const auto number = [&](int i) { return number_in_order(i); };
+        const auto weight_in = [&](int i) -> u64 { return number_in_order(i) <= last ? s.list.mass[i] : 0; };
+        const auto sum_of = [&](const auto &share) {
+            u64 mine = 0, sum;
+            for (int i = threadIdx.x; i < m; i += SP_THREADS) mine += share(i);
+            scan(mine, sum);
+            return sum;
+        };
+        if (top_k) {
+            last = number(reach(m, number, [](int) { return 1ull; }, min(top_k, m)));
+            if (top_p < 1.f) all = sum_of(weight_in);
+        }
+        if (top_p < 1.f) last = number(reach(m, number, weight_in, max(1ull, (u64)ceil(fmax((double)top_p, 0.0) * (double)all))));
+        const double least = fmin((double)min_p, 1.0);
+        const auto drawn = [&](int i) -> u64 {
+            if (min_p > 0.f) {
+                const unsigned k = s.list.key[i];
+                if (weight(__uint_as_float(k ^ (~(unsigned)((int)k >> 31) | 0x80000000u))) < least) return 0;
+            }
+            return weight_in(i);
+        };
+        const u64 sum = sum_of(drawn), mark = min(sum - 1, (u64)(fmax((double)u, 0.0) * (double)sum));
+        const int i = reach(m, [&](int j) { return (u64)s.list.index[j]; }, drawn, mark + 1);
+        if (threadIdx.x == 0) {
+            const unsigned k = s.list.key[i];
+            *token = s.list.index[i];
+            if (prob) *prob = (float)(weight(__uint_as_float(k ^ (~(unsigned)((int)k >> 31) | 0x80000000u))) * (double)(1ull << SP_ONE_BITS) / (double)sum);
+        }
+    }
+
+    // The border is the nth (from 1) in order of index among the elements with that key.
+    __device__ __forceinline__ void among_ties(unsigned key, u64 nth) const
+    {
+        const int each = (n + SP_THREADS - 1) / SP_THREADS, i0 = min(n, threadIdx.x * each), i1 = min(n, i0 + each);
+        int here = 0;
+        for (int i = i0; i < i1; ++i) here += key_of(value(i)) == key;
+        u64 block_sum, all;
+        u64 in_front = scan(here, block_sum);
+        in_front += gather(block_sum, all);
+        if (in_front < nth && nth <= in_front + here) {
+            for (int i = i0; i < i1; ++i)
+                if (key_of(value(i)) == key && ++in_front == nth) tell(key, begin + i);
+        }
+        cluster_sync(blocks);
+    }
+    __device__ __forceinline__ void tell(unsigned key, int index) const
+    {
+        for (unsigned r = 0; r < blocks; ++r) {
+            put32(at_rank(&s.border.key, r), key);
+            put32(at_rank(&s.border.index, r), index);
+        }
     }
 
     // Exclusive sums over the block's threads; `sum`: of all.
@@ -177,7 +501,7 @@ struct Row {
     __device__ __forceinline__ u64 gather(u64 mine, u64 &all) const
     {
         if (threadIdx.x < blocks) put64(at_rank(&s.total[rank], threadIdx.x), mine);
-        cluster_sync();
+        cluster_sync(blocks);
         u64 before = 0;
         all = 0;
         for (unsigned r = 0; r < blocks; ++r) {
@@ -190,8 +514,8 @@ struct Row {
     __device__ __forceinline__ void clear() const
     {
         for (int i = threadIdx.x; i < SP_BINS; i += SP_THREADS) {
-            s.mass[i] = 0;
-            s.count[i] = 0;
+            s.weights.mass[i] = 0;
+            s.weights.count[i] = 0;
         }
         if (threadIdx.x == 0) s.listed = 0;
         __syncthreads();
@@ -199,10 +523,10 @@ struct Row {
     template <bool MASS>
     __device__ __forceinline__ void add(int bin, float z) const
     {
-        atomicAdd(&s.count[bin], 1u);
+        atomicAdd(&s.weights.count[bin], 1u);
         if (MASS) {
             const u64 q = mass(z);
-            unsigned *w = reinterpret_cast<unsigned *>(&s.mass[bin]);
+            unsigned *w = reinterpret_cast<unsigned *>(&s.weights.mass[bin]);
             const unsigned lo = (unsigned)q, was = atomicAdd(w, lo), hi = (unsigned)(q >> 32) + (was + lo < lo);
             if (hi) atomicAdd(w + 1, hi);
         }
@@ -213,7 +537,7 @@ struct Row {
     template <bool MASS, class Goal>
     __device__ __forceinline__ u64 locate(u64 want, const Goal &goal) const
     {
-        cluster_sync();                         // (all blocks have counted)
+        cluster_sync(blocks);                         // (all blocks have counted)
         const int mine = SP_BINS / blocks, each = (mine + SP_THREADS - 1) / SP_THREADS, b0 = rank * mine + threadIdx.x * each;
         const int in = max(0, min(each, (int)((rank + 1) * mine) - b0));
         u64 unit[SP_BINS / SP_THREADS], sum = 0;
@@ -224,8 +548,8 @@ struct Row {
             count[j] = 0;
             if (j < in) {
                 for (unsigned r = 0; r < blocks; ++r) {
-                    count[j] += get32(at_rank(&s.count[b0 + j], r));
-                    if (MASS) unit[j] += get64(at_rank(&s.mass[b0 + j], r));
+                    count[j] += get32(at_rank(&s.weights.count[b0 + j], r));
+                    if (MASS) unit[j] += get64(at_rank(&s.weights.mass[b0 + j], r));
                 }
                 if (!MASS) unit[j] = count[j];
                 sum += unit[j];
@@ -250,7 +574,7 @@ struct Row {
             }
             want = ~0ull;
         }
-        cluster_sync();
+        cluster_sync(blocks);
         return want;
     }
 
@@ -271,7 +595,7 @@ struct Row {
         u64 before = s.found.before;
         unsigned lo = 0, hi = 0xffffffffu;      // keys among which the border's is
         bool by_bin = true;
-        while (s.found.count > SP_LIST) {
+        while (s.found.count > SP_PAIRS) {
             if (by_bin) {
                 // the keys of that bin
                 unsigned a = 0xffffffffu, z = 0u;
@@ -293,14 +617,14 @@ struct Row {
                     atomicMin(&s.key_lo[0], a);
                     atomicMax(&s.key_hi[0], z);
                 }
-                cluster_sync();
+                cluster_sync(blocks);
                 lo = 0xffffffffu;
                 hi = 0u;
                 for (unsigned r = 0; r < blocks; ++r) {
                     lo = min(lo, get32(at_rank(&s.key_lo[0], r)));
                     hi = max(hi, get32(at_rank(&s.key_hi[0], r)));
                 }
-                cluster_sync();
+                cluster_sync(blocks);
                 by_bin = false;
             }
             if (lo == hi) break;
@@ -320,7 +644,7 @@ struct Row {
             const unsigned k = key_of(z);
             return kept(z, i, border) && (by_bin ? first_bin(z) == bin : k >= lo && k <= hi);
         };
-        if (s.found.count > SP_LIST) {
+        if (s.found.count > SP_PAIRS) {
             // ties: the one of them in order of index at which it is reached
             u64 nth = want - before;
             if (MASS) {
@@ -352,21 +676,21 @@ struct Row {
                 if (!there(z, i)) continue;
                 unsigned slot;
                 asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(slot) : "r"(listed) : "memory");
-                put32(at_rank(&s.list_key[slot], 0), key_of(z));
-                put32(at_rank(&s.list_index[slot], 0), begin + i);
-                if (MASS) put64(at_rank(&s.list_mass[slot], 0), mass(z));
+                put32(at_rank(&s.weights.list_key[slot], 0), key_of(z));
+                put32(at_rank(&s.weights.list_index[slot], 0), begin + i);
+                if (MASS) put64(at_rank(&s.weights.list_mass[slot], 0), mass(z));
             }
-            cluster_sync();
+            cluster_sync(blocks);
             if (rank == 0) {
                 const int m = s.listed;
                 if (threadIdx.x < m) {
-                    const unsigned key = s.list_key[threadIdx.x];
-                    const int index = s.list_index[threadIdx.x];
-                    const u64 own = MASS ? s.list_mass[threadIdx.x] : 1;
+                    const unsigned key = s.weights.list_key[threadIdx.x];
+                    const int index = s.weights.list_index[threadIdx.x];
+                    const u64 own = MASS ? s.weights.list_mass[threadIdx.x] : 1;
                     u64 b = before;
                     for (int j = 0; j < m; ++j) {
-                        const unsigned k = s.list_key[j];
-                        if (k > key || (k == key && s.list_index[j] < index)) b += MASS ? s.list_mass[j] : 1;
+                        const unsigned k = s.weights.list_key[j];
+                        if (k > key || (k == key && s.weights.list_index[j] < index)) b += MASS ? s.weights.list_mass[j] : 1;
                     }
                     if (b < want && want <= b + own) {
                         for (unsigned r = 0; r < blocks; ++r) {
@@ -377,7 +701,7 @@ struct Row {
                 }
             }
         }
-        cluster_sync();
+        cluster_sync(blocks);
         border = s.border;
     }
 };
@@ -401,6 +725,12 @@ sample_kernel(const SampleParams p)
     const int skew = (int)(((uintptr_t)from & 15) / sizeof(T));
     T *items = reinterpret_cast<T *>(sp_smem_raw + sizeof(SampleSmem)) + skew;
     const int head = min(n, (PER - skew) % PER), vectors = (n - head) / PER;
+    // (on the way: the largest logit, and the lowest one that is open)
+    float top = -INFINITY, low = INFINITY;
+    const auto look = [&](float z) {
+        top = fmaxf(top, z);                    // (NaN is not taken)
+        low = fminf(low, z > -INFINITY ? z : INFINITY);
+    };
     {
         const uint4 *v = reinterpret_cast<const uint4 *>(from + head);
         uint4 *to = reinterpret_cast<uint4 *>(items + head);
@@ -412,25 +742,28 @@ sample_kernel(const SampleParams p)
                 if (i + u * SP_THREADS < vectors) a[u] = __ldcs(v + i + u * SP_THREADS);
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (i + u * SP_THREADS < vectors) to[i + u * SP_THREADS] = a[u];
+                if (i + u * SP_THREADS < vectors) {
+                    to[i + u * SP_THREADS] = a[u];
+                    const unsigned w[4] = {a[u].x, a[u].y, a[u].z, a[u].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (sizeof(T) == 2) look(__uint_as_float(w[j] << 16) + 0.f);
+                        look(__uint_as_float(sizeof(T) == 2 ? w[j] & 0xffff0000u : w[j]) + 0.f);
+                    }
+                }
         }
-        if (tid < head) items[tid] = from[tid];
         const int done = head + vectors * PER;
-        if (tid < n - done) items[done + tid] = from[done + tid];
+        for (int i = tid; i < head + n - done; i += SP_THREADS) {
+            const int at = i < head ? i : done + i - head;
+            const T one = from[at];
+            items[at] = one;
+            look(item_value(&one, 0));
+        }
     }
     dip_launch_dependents();
     const float temperature = p.temperature ? p.temperature[row] : 1.f;
     const int top_k = p.top_k ? p.top_k[row] : 0;
     const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f, u = p.uniform[row];
-    __syncthreads();
-
-    // the largest logit, the first one of them, and how far below it the others are
-    float top = -INFINITY, low = INFINITY;
-    for (int i = tid; i < n; i += SP_THREADS) {
-        const float z = item_value(items, i);
-        top = fmaxf(top, z);                    // (NaN is not taken)
-        if (z > -INFINITY) low = fminf(low, z);
-    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -440,26 +773,32 @@ sample_kernel(const SampleParams p)
         s.block_top[warp] = top;
         s.block_low[warp] = low;
     }
+    if (tid == 0) {
+        s.listed = 0;
+        s.cut[0].bin = s.cut[1].bin = -1;
+    }
     __syncthreads();
     for (int w = 0; w < SP_WARPS; ++w) {
         top = fmaxf(top, s.block_top[w]);
         low = fminf(low, s.block_low[w]);
     }
-    cluster_sync();                             // (all blocks are there)
-    if (tid < (int)blocks) {
-        put32(at_rank(&s.top[rank], tid), __float_as_uint(top));
-        put32(at_rank(&s.low[rank], tid), __float_as_uint(low));
-    }
-    cluster_sync();
-    for (unsigned r = 0; r < blocks; ++r) {
-        top = fmaxf(top, s.top[r]);
-        low = fminf(low, s.low[r]);
+    if (blocks > 1) {
+        if (tid == 0) {
+            s.top = top;
+            s.low = low;
+        }
+        cluster_sync(blocks);
+        for (unsigned r = 0; r < blocks; ++r) {
+            top = fmaxf(top, __uint_as_float(get32(at_rank(&s.top, r))));
+            low = fminf(low, __uint_as_float(get32(at_rank(&s.low, r))));
+        }
     }
     if (top == -INFINITY) {
         if (rank == 0 && tid == 0) {
             p.token[row] = -1;
             if (p.prob) p.prob[row] = 0.f;
         }
+        cluster_sync(blocks);                   // (the others have read this block's)
         DIP_TRACE_MAX(p.tr, 2);
         return;
     }
@@ -472,7 +811,7 @@ sample_kernel(const SampleParams p)
         __syncthreads();
         for (int w = 0; w < SP_WARPS; ++w) first = min(first, s.block_first[w]);
         if (tid == 0) put32(at_rank(&s.first[rank], 0), (unsigned)first);
-        cluster_sync();
+        cluster_sync(blocks);
         if (rank == 0 && tid == 0) {
             for (unsigned r = 0; r < blocks; ++r) first = min(first, s.first[r]);
             p.token[row] = first;
@@ -486,10 +825,70 @@ sample_kernel(const SampleParams p)
     const Row<T> r = {s, items, n, begin, rank, blocks, top, SP_TABLE * 1.4426950408889634074 / (double)temperature,
                       spread > 1e-30f ? (SP_BINS - 1) / spread : 0.f};
     SampleBorder border = {0u, 0x7fffffff};
-    if (top_k > 0 && top_k < p.vocab)
-        r.template shorten<false>(border, [&](u64 all) { return min((u64)top_k, all); });
-    if (top_p < 1.f)
-        r.template shorten<true>(border, [&](u64 all) { return max(1ull, (u64)ceil(fmax((double)top_p, 0.0) * (double)all)); });
+    const bool by_count = top_k > 0 && top_k < p.vocab, by_weight = top_p < 1.f;
+    const auto share_of = [&](u64 all) { return max(1ull, (u64)ceil(fmax((double)top_p, 0.0) * (double)all)); };
+    const auto count_of = [&](u64 all) { return min((u64)top_k, all); };
+    // (bfloat16, weights by bins: the last bin's elements, from -2^20 down, weigh nothing)
+    const bool counted = (by_count || by_weight) && r.scale > 0.f && (by_count || !Row<T>::HALF || (temperature <= 1000.f && fabsf(top) < 524288.f));
+    bool count_done = !by_count, weight_done = !by_weight, alone = false;
+    u64 all_weight = 0;
+    if (counted) {
+        r.histogram();
+        r.cuts(by_count ? top_k : 0, top_p);
+        const auto first = s.cut[0], last = s.cut[Row<T>::HALF || by_count ? 0 : 1];
+        const unsigned up_to = last.in_front + last.count;
+        if (first.bin >= 0 && last.bin >= 0) {
+            u64 sums[3];
+            if (up_to <= SP_LIST) {
+                // (binary32 by weight: the sum of all is not known yet, nor that the border is among these)
+                const bool weigh = !by_count && !Row<T>::HALF;
+                all_weight = s.all_weight;
+                r.collect(0, last.bin, weigh, sums);
+                if (weigh) all_weight = sums[1] + sums[2];
+                alone = !weigh || share_of(all_weight) <= sums[1];
+            } else if (Row<T>::HALF) {
+                if (!r.mixed(last.bin)) {
+                    const float z = r.value_of(last.bin);
+                    u64 nth = count_of(s.all_count) - last.in_front;
+                    if (!by_count) {
+                        const u64 q = r.mass(z);
+                        nth = (s.found.before - last.before + q - 1) / q;
+                    }
+                    r.among_ties(key_of(z), nth);
+                    border = s.border;
+                    (by_count ? count_done : weight_done) = true;
+                }
+            } else if (up_to - first.in_front <= SP_LIST) {
+                const bool weigh = !by_count;
+                r.collect(first.bin, last.bin, weigh, sums);
+                const u64 want = weigh ? share_of(sums[0] + sums[1] + sums[2]) : count_of(s.all_count) - last.in_front;
+                if (!weigh || (sums[0] < want && want <= sums[0] + sums[1])) {
+                    if (rank == 0) {
+                        const int i = r.reach(s.listed, [&](int j) { return r.number_in_order(j); }, [&](int j) { return weigh ? s.list.mass[j] : 1ull; },
+                                              want - (weigh ? sums[0] : 0));
+                        if (tid == 0) r.tell(s.list.key[i], s.list.index[i]);
+                    }
+                    cluster_sync(blocks);
+                    border = s.border;
+                    (by_count ? count_done : weight_done) = true;
+                }
+            }
+        }
+    } else if (min_p > 0.f && !by_count && !by_weight) {
+        // (a little lower than need be: what is left out weighs less than min_p for certain)
+        const float far = -temperature * logf(fminf(min_p, 1.f));
+        u64 ignored[3];
+        r.collect(0, r.bin_of(top - far * 1.0001f - 1e-5f * fabsf(top)), false, ignored);
+        alone = get32(at_rank(&s.listed, 0)) <= SP_LIST;
+        cluster_sync(blocks);                   // (before the first block goes on or leaves)
+    }
+    if (alone) {
+        if (rank == 0) r.finish(by_count ? top_k : 0, top_p, min_p, u, all_weight, p.token + row, p.prob ? p.prob + row : nullptr);
+        DIP_TRACE_MAX(p.tr, 2);
+        return;
+    }
+    if (!count_done) r.template shorten<false>(border, count_of);
+    if (!weight_done) r.template shorten<true>(border, share_of);
 
     // the draw: a warp's elements are consecutive
     const double least = fmin((double)min_p, 1.0);
@@ -499,6 +898,7 @@ sample_kernel(const SampleParams p)
     };
     const int each = ((n + SP_WARPS - 1) / SP_WARPS + 31) & ~31, i0 = min(n, warp * each), i1 = min(n, i0 + each);
     u64 sum = 0;
+#pragma unroll 4
     for (int i = i0 + lane; i < i1; i += 32) sum += drawn(i);
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
