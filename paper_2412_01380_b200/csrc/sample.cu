@@ -65,6 +65,7 @@ struct __align__(16) SampleSmem {
     double table[SP_TABLE];
     union {
         unsigned bins[8192];                    // counts; binary32: 4096 of them and what is left in each (1/1024 of a bin's width)
+        u64 bin_mass[4096];                     // bfloat16, for the draw: of the bins from the largest logit's on
         SampleList list;
         SampleWeights weights;
     };
@@ -74,7 +75,7 @@ struct __align__(16) SampleSmem {
     int finals, reached, listed;
     u64 reach_before;
     u64 tiny[2];
-    u64 scan[SP_WARPS + 1], scan_max[SP_WARPS];
+    u64 scan[SP_WARPS + 1];
     // what the blocks of a cluster tell one another
     u64 total[SP_CLUSTER], sums[3][SP_CLUSTER];
     float top, low;
@@ -123,17 +124,13 @@ __device__ __forceinline__ uint32_t at_rank(const void *p, unsigned rank)
 }
 __device__ __forceinline__ void put32(uint32_t a, unsigned v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
 __device__ __forceinline__ void put64(uint32_t a, u64 v) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory"); }
-__device__ __forceinline__ unsigned get32(uint32_t a)
+// The same as an ordinary address (reads through it may go out together).
+template <typename V>
+__device__ __forceinline__ const V *of_rank(const V *p, unsigned rank)
 {
-    unsigned v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ u64 get64(uint32_t a)
-{
-    u64 v;
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
-    return v;
+    const V *q;
+    asm("mapa.u64 %0, %1, %2;" : "=l"(q) : "l"(p), "r"(rank));
+    return q;
 }
 
 __device__ __forceinline__ unsigned key_of(float z)
@@ -145,6 +142,14 @@ __device__ __forceinline__ unsigned key_of(float z)
 __device__ __forceinline__ float item_value(const float *p, int i) { return p[i] + 0.f; }          // (-0 is 0)
 __device__ __forceinline__ float item_value(const uint16_t *p, int i) { return __uint_as_float((unsigned)p[i] << 16) + 0.f; }
 
+// To a sum in shared memory, by its halves (the lower one says whether it ran over).
+__device__ __forceinline__ void add64(u64 *sum, u64 q)
+{
+    unsigned *w = reinterpret_cast<unsigned *>(sum);
+    const unsigned lo = (unsigned)q, was = atomicAdd(w, lo), hi = (unsigned)(q >> 32) + (was + lo < lo);
+    if (hi) atomicAdd(w + 1, hi);
+}
+
 template <typename T>
 struct Row {
     SampleSmem &s;
@@ -153,26 +158,27 @@ struct Row {
     unsigned rank, blocks;
     float top;                                  // the largest logit
     double steps;                               // 512 log2(e) / temperature
+    float steps_f;
     float scale;                                // bins per unit
 
     __device__ __forceinline__ float value(int i) const { return item_value(items, i); }
 
-    // exp((z - top) / temperature): 2^(k / 512) from the table times the third-order sum for what is left (within 10^-14)
+    // exp((z - top) / temperature) times 2^45: 2^(k / 512) from the table times the third-order sum for what is left (within 10^-14).
+    // Nine binary64 operations, which go at a quarter of binary32's rate (B200: half of its lanes, two cycles each), and a conversion.
     __device__ __forceinline__ double weight(float z) const
     {
-        const double y = fmax(((double)z - (double)top) * steps, -64.0 * SP_TABLE);          // (of infinities: not a number, which fmax drops)
-        const double magic = 6755399441055744.0, k = y + magic;
+        constexpr double STEP = 0.69314718055994530942 / SP_TABLE, magic = 6755399441055744.0;
+        const double d = (double)z - (double)top, k = fma(d, steps, magic), f = fma(d, steps, magic - k);
         const int i = __double2loint(k);
-        const double f = (y - (k - magic)) * (0.69314718055994530942 / SP_TABLE);
         const double t = s.table[i & (SP_TABLE - 1)];
-        const double e = fma(t, f * fma(f, fma(f, 1.0 / 6.0, 0.5), 1.0), t);
+        const double e = fma(t, f * fma(f, fma(f, STEP * STEP * STEP / 6, STEP * STEP / 2), STEP), t);
         const double w = __hiloint2double(__double2hiint(e) + ((i >> 9) << 20), __double2loint(e));
-        return z == top ? 1.0 : y > -60.0 * SP_TABLE ? w : 0.0;
+        // (closed logits are far below, or not a number)
+        return z == top ? (double)(1ull << SP_ONE_BITS) : (z - top) * steps_f > -60.f * SP_TABLE ? w : 0.0;
     }
     __device__ __forceinline__ u64 mass(float z) const
     {
-        const double q = weight(z) * (double)(1ull << SP_ONE_BITS) + 4503599627370496.0;
-        return (u64)__double_as_longlong(q) & 0xfffffffffffffull;
+        return (u64)__double_as_longlong(weight(z) + 4503599627370496.0) & 0xfffffffffffffull;
     }
     // whether the element is open and in front of the border (or it)
     __device__ __forceinline__ bool kept(float z, int i, const SampleBorder &b) const
@@ -208,7 +214,7 @@ struct Row {
         if (HALF) {
             if (middle(bin)) {
                 u64 q = 0;
-                for (unsigned r = 0; r < blocks; ++r) q += get64(at_rank(&s.tiny[bin - 4095], r));
+                for (unsigned r = 0; r < blocks; ++r) q += *of_rank(&s.tiny[bin - 4095], r);
                 return q;
             }
             return bin == 8191 ? 0 : count * mass(value_of(bin));
@@ -221,17 +227,22 @@ struct Row {
         for (int i = threadIdx.x; i < 8192 / 4; i += SP_THREADS) reinterpret_cast<uint4 *>(s.bins)[i] = make_uint4(0u, 0u, 0u, 0u);
         if (threadIdx.x < 2) s.tiny[threadIdx.x] = 0;
         __syncthreads();
-#pragma unroll 4
-        for (int i = threadIdx.x; i < n; i += SP_THREADS) {
-            const float z = value(i);
-            if (!(z > -INFINITY)) continue;
-            const int bin = bin_of(z);
-            atomicAdd(&s.bins[place(bin)], 1u);
-            if (HALF) {
-                if (middle(bin)) atomicAdd(&s.tiny[bin - 4095], mass(z));
-            } else {
-                const float at = (top - z) * scale * 2.f;
-                atomicAdd(&s.bins[BINS + place(bin)], (unsigned)(fminf(at - (float)bin, 1.f) * REST));
+        constexpr int U = 4;
+        for (int i0 = threadIdx.x; i0 < n; i0 += U * SP_THREADS) {
+            float z[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) z[j] = i0 + j * SP_THREADS < n ? value(i0 + j * SP_THREADS) : -INFINITY;
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                if (!(z[j] > -INFINITY)) continue;
+                const int bin = bin_of(z[j]);
+                atomicAdd(&s.bins[place(bin)], 1u);
+                if (HALF) {
+                    if (middle(bin)) add64(&s.tiny[bin - 4095], mass(z[j]));
+                } else {
+                    const float at = (top - z[j]) * scale * 2.f;
+                    atomicAdd(&s.bins[BINS + place(bin)], (unsigned)(fminf(at - (float)bin, 1.f) * REST));
+                }
             }
         }
         cluster_sync(blocks);
@@ -246,9 +257,16 @@ struct Row {
         for (int j = 0; j < in; ++j) {
             unsigned count = 0, rest = 0;
             const int at = place(b0 + j);
-            for (unsigned r = 0; r < blocks; ++r) {
-                count += get32(at_rank(&s.bins[at], r));
-                if (!HALF) rest += get32(at_rank(&s.bins[BINS + at], r));
+            unsigned counts_of[SP_CLUSTER], rests_of[SP_CLUSTER];
+#pragma unroll
+            for (unsigned r = 0; r < SP_CLUSTER; ++r) {
+                counts_of[r] = r < blocks ? *of_rank(&s.bins[at], r) : 0;
+                rests_of[r] = !HALF && r < blocks ? *of_rank(&s.bins[BINS + at], r) : 0;
+            }
+#pragma unroll
+            for (unsigned r = 0; r < SP_CLUSTER; ++r) {
+                count += counts_of[r];
+                rest += rests_of[r];
             }
             s.bins[at] = count;                 // (nobody else reads these of this block)
             if (!HALF) s.bins[BINS + at] = rest;
@@ -303,30 +321,44 @@ struct Row {
     }
 
     // Sends the elements of the bins first .. last to the first block's list (if there are at most SP_LIST; s.listed of the first
-    // block counts all).  sums: [0] the weight of all elements in front of them, [1] their own, [2] of all behind them, if `weigh`.
+    // block counts all).  sums: [0] the weight of all elements in front of them, [1] their own, [2] of all, if `weigh`.
     // Ends with a cluster barrier, after which every block has all blocks' sums.
     __device__ __forceinline__ void collect(int first, int last, bool weigh, u64 (&sums)[3]) const
     {
         u64 mine[3] = {0, 0, 0};
         const uint32_t listed = at_rank(&s.listed, 0);
-#pragma unroll 4
-        for (int i = threadIdx.x; i < n; i += SP_THREADS) {
-            const float z = value(i);
-            const bool open = z > -INFINITY;
-            const int bin = open ? bin_of(z) : BINS;
-            const bool in = bin >= first && bin <= last;
-            u64 q = 0;
-            if (weigh || in) q = mass(z);
-            if (weigh) mine[bin < first ? 0 : bin <= last ? 1 : 2] += q;
-            if (in) {
-                unsigned slot;
-                asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(slot) : "r"(listed) : "memory");
-                if (slot < SP_LIST) {
-                    put32(at_rank(&s.list.key[slot], 0), key_of(z));
-                    put32(at_rank(&s.list.index[slot], 0), begin + i);
-                    put64(at_rank(&s.list.mass[slot], 0), q);
+        constexpr int U = 4;                    // (side by side, for the latency of binary64)
+        for (int i0 = threadIdx.x; i0 < n; i0 += U * SP_THREADS) {
+            float z[U];
+            int bin[U];
+            u64 q[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                z[j] = i0 + j * SP_THREADS < n ? value(i0 + j * SP_THREADS) : -INFINITY;
+                bin[j] = z[j] > -INFINITY ? bin_of(z[j]) : BINS;
+                q[j] = 0;
+            }
+            if (weigh) {
+#pragma unroll
+                for (int j = 0; j < U; ++j) q[j] = mass(z[j]);
+#pragma unroll
+                for (int j = 0; j < U; ++j) {
+                    mine[0] += bin[j] < first ? q[j] : 0;
+                    mine[1] += bin[j] >= first && bin[j] <= last ? q[j] : 0;
+                    mine[2] += q[j];
                 }
             }
+#pragma unroll
+            for (int j = 0; j < U; ++j)
+                if (bin[j] >= first && bin[j] <= last) {
+                    unsigned slot;
+                    asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(slot) : "r"(listed) : "memory");
+                    if (slot < SP_LIST) {
+                        put32(at_rank(&s.list.key[slot], 0), key_of(z[j]));
+                        put32(at_rank(&s.list.index[slot], 0), begin + i0 + j * SP_THREADS);
+                        put64(at_rank(&s.list.mass[slot], 0), weigh ? q[j] : mass(z[j]));
+                    }
+                }
         }
         if (weigh) {
 #pragma unroll
@@ -345,33 +377,13 @@ struct Row {
         }
     }
 
-    // Of m elements, each with a number of its own and a share (0: none), the one at which the sum of shares in order of the numbers
-    // reaches `want` (1 up to the sum of all).  By one block.
+    // Of m elements, each with a number of its own (lo to hi) and a share (0: none), the one at which the sum of shares in order of the
+    // numbers reaches `want` (1 up to the sum of all).  By one block.
     template <class Number, class Share>
-    __device__ int reach(int m, const Number &number, const Share &share, u64 want) const
+    __device__ int reach(int m, const Number &number, const Share &share, u64 want, u64 lo, u64 hi) const
     {
-        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-        u64 lo = ~0ull, hi = 0, before = 0;
-        for (int i = tid; i < m; i += SP_THREADS)
-            if (share(i)) {
-                lo = min(lo, number(i));
-                hi = max(hi, number(i));
-            }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-            hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-        }
-        __syncthreads();
-        if (lane == 0) {
-            s.scan[warp] = lo;
-            s.scan_max[warp] = hi;
-        }
-        __syncthreads();
-        for (int w = 0; w < SP_WARPS; ++w) {
-            lo = min(lo, s.scan[w]);
-            hi = max(hi, s.scan_max[w]);
-        }
+        const int tid = threadIdx.x;
+        u64 before = 0;
         for (;;) {
             const int bits = lo == hi ? 0 : 64 - __clzll(hi - lo), shift = max(0, bits - 9);
             s.reach[tid] = 0;
@@ -383,7 +395,7 @@ struct Row {
                 if (!q || a < lo || a > hi) continue;
                 const int bin = (int)((a - lo) >> shift);
                 atomicAdd(&s.reach_count[bin], 1u);
-                atomicAdd(&s.reach[bin], q);
+                add64(&s.reach[bin], q);
             }
             __syncthreads();
             u64 ignored;
@@ -414,14 +426,16 @@ struct Row {
         __syncthreads();
         return s.reached;
     }
-    __device__ __forceinline__ u64 number_in_order(int i) const { return ((u64)~s.list.key[i] << 20) | (unsigned)s.list.index[i]; }
+    __device__ __forceinline__ u64 number_in_order(int i) const { return ((u64)(key_of(top) - s.list.key[i]) << 18) | (unsigned)s.list.index[i]; }
+    // (no number of an element down to logit z is above)
+    __device__ __forceinline__ u64 last_number(float z) const { return ((u64)(key_of(top) - key_of(z)) << 18) | 0x3ffffu; }
 
     // The first block has all that can be left in its list: everything else.  all: the weight that top_p is a share of (top_k > 0: of what
     // that leaves).
-    __device__ void finish(int top_k, float top_p, float min_p, float u, u64 all, int32_t *token, float *prob) const
+    __device__ void finish(int top_k, float top_p, float min_p, float u, u64 all, float lowest, int vocab, int32_t *token, float *prob) const
     {
-        const int m = s.listed;
-        u64 last = ~0ull;                       // the border's number
+        const int m = min(s.listed, SP_LIST);
+        u64 last = last_number(lowest);         // the border's number
         const auto number = [&](int i) { return number_in_order(i); };
         const auto weight_in = [&](int i) -> u64 { return number_in_order(i) <= last ? s.list.mass[i] : 0; };
         const auto sum_of = [&](const auto &share) {
@@ -431,11 +445,11 @@ struct Row {
             return sum;
         };
         if (top_k) {
-            last = number(reach(m, number, [](int) { return 1ull; }, min(top_k, m)));
+            last = number(reach(m, number, [](int) { return 1ull; }, min(top_k, m), 0, last));
             if (top_p < 1.f) all = sum_of(weight_in);
         }
-        if (top_p < 1.f) last = number(reach(m, number, weight_in, max(1ull, (u64)ceil(fmax((double)top_p, 0.0) * (double)all))));
-        const double least = fmin((double)min_p, 1.0);
+        if (top_p < 1.f) last = number(reach(m, number, weight_in, max(1ull, (u64)ceil(fmax((double)top_p, 0.0) * (double)all)), 0, last));
+        const double least = fmin((double)min_p, 1.0) * (double)(1ull << SP_ONE_BITS);
         const auto drawn = [&](int i) -> u64 {
             if (min_p > 0.f) {
                 const unsigned k = s.list.key[i];
@@ -444,11 +458,11 @@ struct Row {
             return weight_in(i);
         };
         const u64 sum = sum_of(drawn), mark = min(sum - 1, (u64)(fmax((double)u, 0.0) * (double)sum));
-        const int i = reach(m, [&](int j) { return (u64)s.list.index[j]; }, drawn, mark + 1);
+        const int i = reach(m, [&](int j) { return (u64)s.list.index[j]; }, drawn, mark + 1, 0, vocab - 1);
         if (threadIdx.x == 0) {
             const unsigned k = s.list.key[i];
             *token = s.list.index[i];
-            if (prob) *prob = (float)(weight(__uint_as_float(k ^ (~(unsigned)((int)k >> 31) | 0x80000000u))) * (double)(1ull << SP_ONE_BITS) / (double)sum);
+            if (prob) *prob = (float)(weight(__uint_as_float(k ^ (~(unsigned)((int)k >> 31) | 0x80000000u))) / (double)sum);
         }
     }
 
@@ -488,13 +502,15 @@ struct Row {
         __syncthreads();                        // (the sums in front have been read)
         if (lane == 31) s.scan[warp] = incl;
         __syncthreads();
-        u64 before = 0;
-        sum = 0;
-        for (int w = 0; w < SP_WARPS; ++w) {
-            const u64 a = s.scan[w];
-            before += w < warp ? a : 0;
-            sum += a;
+        u64 sums = s.scan[lane & (SP_WARPS - 1)];
+        const u64 own = sums;
+#pragma unroll
+        for (int o = 1; o < SP_WARPS; o <<= 1) {
+            const u64 a = __shfl_up_sync(0xffffffffu, sums, o, SP_WARPS);
+            if ((lane & (SP_WARPS - 1)) >= o) sums += a;
         }
+        sum = __shfl_sync(0xffffffffu, sums, SP_WARPS - 1);
+        const u64 before = __shfl_sync(0xffffffffu, sums - own, warp);
         return before + incl - v;
     }
     // The same over the cluster, given this block's sum: what is in front of this block, and all.  Ends with a cluster barrier.
@@ -525,10 +541,7 @@ struct Row {
     {
         atomicAdd(&s.weights.count[bin], 1u);
         if (MASS) {
-            const u64 q = mass(z);
-            unsigned *w = reinterpret_cast<unsigned *>(&s.weights.mass[bin]);
-            const unsigned lo = (unsigned)q, was = atomicAdd(w, lo), hi = (unsigned)(q >> 32) + (was + lo < lo);
-            if (hi) atomicAdd(w + 1, hi);
+            add64(&s.weights.mass[bin], mass(z));
         }
     }
 
@@ -548,8 +561,8 @@ struct Row {
             count[j] = 0;
             if (j < in) {
                 for (unsigned r = 0; r < blocks; ++r) {
-                    count[j] += get32(at_rank(&s.weights.count[b0 + j], r));
-                    if (MASS) unit[j] += get64(at_rank(&s.weights.mass[b0 + j], r));
+                    count[j] += *of_rank(&s.weights.count[b0 + j], r);
+                    if (MASS) unit[j] += *of_rank(&s.weights.mass[b0 + j], r);
                 }
                 if (!MASS) unit[j] = count[j];
                 sum += unit[j];
@@ -621,8 +634,8 @@ struct Row {
                 lo = 0xffffffffu;
                 hi = 0u;
                 for (unsigned r = 0; r < blocks; ++r) {
-                    lo = min(lo, get32(at_rank(&s.key_lo[0], r)));
-                    hi = max(hi, get32(at_rank(&s.key_hi[0], r)));
+                    lo = min(lo, *of_rank(&s.key_lo[0], r));
+                    hi = max(hi, *of_rank(&s.key_hi[0], r));
                 }
                 cluster_sync(blocks);
                 by_bin = false;
@@ -715,7 +728,7 @@ sample_kernel(const SampleParams p)
     constexpr int PER = 16 / sizeof(T);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     DIP_TRACE_MIN(p.tr, 0);
-    s.table[tid] = exp2((double)tid / SP_TABLE);
+    s.table[tid] = exp2((double)tid / SP_TABLE) * (double)(1ull << SP_ONE_BITS);
     dip_grid_dependency_wait();
     DIP_TRACE_MIN(p.tr, 1);
     const unsigned blocks = cluster_size(), rank = cluster_rank();
@@ -788,9 +801,15 @@ sample_kernel(const SampleParams p)
             s.low = low;
         }
         cluster_sync(blocks);
-        for (unsigned r = 0; r < blocks; ++r) {
-            top = fmaxf(top, __uint_as_float(get32(at_rank(&s.top, r))));
-            low = fminf(low, __uint_as_float(get32(at_rank(&s.low, r))));
+        const unsigned r = lane & (SP_CLUSTER - 1);
+        if (r < blocks) {
+            top = *of_rank(&s.top, r);
+            low = *of_rank(&s.low, r);
+        }
+#pragma unroll
+        for (int o = SP_CLUSTER / 2; o; o >>= 1) {
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
         }
     }
     if (top == -INFINITY) {
@@ -823,6 +842,7 @@ sample_kernel(const SampleParams p)
 
     const float spread = fminf(top - low, SP_SPREAD);
     const Row<T> r = {s, items, n, begin, rank, blocks, top, SP_TABLE * 1.4426950408889634074 / (double)temperature,
+                      (float)(SP_TABLE * 1.4426950408889634074 / (double)temperature),
                       spread > 1e-30f ? (SP_BINS - 1) / spread : 0.f};
     SampleBorder border = {0u, 0x7fffffff};
     const bool by_count = top_k > 0 && top_k < p.vocab, by_weight = top_p < 1.f;
@@ -844,7 +864,7 @@ sample_kernel(const SampleParams p)
                 const bool weigh = !by_count && !Row<T>::HALF;
                 all_weight = s.all_weight;
                 r.collect(0, last.bin, weigh, sums);
-                if (weigh) all_weight = sums[1] + sums[2];
+                if (weigh) all_weight = sums[2];
                 alone = !weigh || share_of(all_weight) <= sums[1];
             } else if (Row<T>::HALF) {
                 if (!r.mixed(last.bin)) {
@@ -861,11 +881,11 @@ sample_kernel(const SampleParams p)
             } else if (up_to - first.in_front <= SP_LIST) {
                 const bool weigh = !by_count;
                 r.collect(first.bin, last.bin, weigh, sums);
-                const u64 want = weigh ? share_of(sums[0] + sums[1] + sums[2]) : count_of(s.all_count) - last.in_front;
+                const u64 want = weigh ? share_of(sums[2]) : count_of(s.all_count) - last.in_front;
                 if (!weigh || (sums[0] < want && want <= sums[0] + sums[1])) {
                     if (rank == 0) {
                         const int i = r.reach(s.listed, [&](int j) { return r.number_in_order(j); }, [&](int j) { return weigh ? s.list.mass[j] : 1ull; },
-                                              want - (weigh ? sums[0] : 0));
+                                              want - (weigh ? sums[0] : 0), 0, r.last_number(low));
                         if (tid == 0) r.tell(s.list.key[i], s.list.index[i]);
                     }
                     cluster_sync(blocks);
@@ -879,27 +899,61 @@ sample_kernel(const SampleParams p)
         const float far = -temperature * logf(fminf(min_p, 1.f));
         u64 ignored[3];
         r.collect(0, r.bin_of(top - far * 1.0001f - 1e-5f * fabsf(top)), false, ignored);
-        alone = get32(at_rank(&s.listed, 0)) <= SP_LIST;
+        alone = *of_rank(&s.listed, 0) <= SP_LIST;
         cluster_sync(blocks);                   // (before the first block goes on or leaves)
     }
     if (alone) {
-        if (rank == 0) r.finish(by_count ? top_k : 0, top_p, min_p, u, all_weight, p.token + row, p.prob ? p.prob + row : nullptr);
+        if (rank == 0) r.finish(by_count ? top_k : 0, top_p, min_p, u, all_weight, low, p.vocab, p.token + row, p.prob ? p.prob + row : nullptr);
         DIP_TRACE_MAX(p.tr, 2);
         return;
     }
     if (!count_done) r.template shorten<false>(border, count_of);
     if (!weight_done) r.template shorten<true>(border, share_of);
 
-    // the draw: a warp's elements are consecutive
-    const double least = fmin((double)min_p, 1.0);
+    // The draw: a warp's elements are consecutive.  Where a block has more bfloat16 logits than there are values of them that count, their weights
+    // are worked out once.
+    const int top_bin = r.bin_of(top);
+    int known = 0;                              // bins whose weights are in s.bin_mass
+    if (Row<T>::HALF && n > 4096 && fabsf(top) < INFINITY) {
+        known = min(4096, 8191 - top_bin);
+        if (border.key) known = min(known, r.bin_of(__uint_as_float(border.key ^ (~(unsigned)((int)border.key >> 31) | 0x80000000u))) - top_bin + 1);
+        __syncthreads();
+        for (int i = tid; i < known; i += SP_THREADS) s.bin_mass[i] = r.mass(r.value_of(top_bin + i));
+        __syncthreads();
+    }
+    const double least = fmin((double)min_p, 1.0) * (double)(1ull << SP_ONE_BITS);
+    const auto open = [&](float z, int i) { return border.key ? r.kept(z, i, border) : z > -INFINITY; };
+    const auto mass_of = [&](float z) -> u64 {
+        if (Row<T>::HALF) {
+            const int bin = r.bin_of(z) - top_bin;
+            if (bin < known && !r.mixed(bin + top_bin)) return s.bin_mass[bin];
+        }
+        return r.mass(z);
+    };
     const auto drawn = [&](int i) -> u64 {
         const float z = r.value(i);
-        return r.kept(z, i, border) && !(min_p > 0.f && r.weight(z) < least) ? r.mass(z) : 0;
+        return open(z, i) && !(min_p > 0.f && r.weight(z) < least) ? mass_of(z) : 0;
     };
     const int each = ((n + SP_WARPS - 1) / SP_WARPS + 31) & ~31, i0 = min(n, warp * each), i1 = min(n, i0 + each);
     u64 sum = 0;
-#pragma unroll 4
-    for (int i = i0 + lane; i < i1; i += 32) sum += drawn(i);
+    constexpr int U = 4;
+    for (int i = i0; i < i1; i += 32 * U) {
+        float z[U];
+        bool in[U], any = false;
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int at = i + 32 * j + lane;
+            z[j] = at < i1 ? r.value(at) : -INFINITY;
+            in[j] = open(z[j], at);
+            any |= in[j];
+        }
+        if (!__any_sync(0xffffffffu, any)) continue;
+        u64 q[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) q[j] = Row<T>::HALF ? (in[j] ? mass_of(z[j]) : 0) : r.mass(z[j]);
+#pragma unroll
+        for (int j = 0; j < U; ++j) sum += in[j] && !(min_p > 0.f && r.weight(z[j]) < least) ? q[j] : 0;
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) s.scan[warp] = sum;
@@ -922,7 +976,7 @@ sample_kernel(const SampleParams p)
             int i = k0;
             for (u64 q; at + (q = drawn(i)) <= mark; ++i) at += q;
             p.token[row] = begin + i;
-            if (p.prob) p.prob[row] = (float)(r.weight(r.value(i)) * (double)(1ull << SP_ONE_BITS) / (double)all);
+            if (p.prob) p.prob[row] = (float)(r.weight(r.value(i)) / (double)all);
         }
     }
     DIP_TRACE_MAX(p.tr, 2);
