@@ -44,7 +44,7 @@ struct SampleParams {
 };
 
 struct SampleBorder {
-    unsigned key;
+    float z;
     int index;
 };
 
@@ -77,7 +77,7 @@ struct __align__(16) SampleSmem {
     u64 tiny[2];
     u64 scan[SP_WARPS + 1];
     // what the blocks of a cluster tell one another
-    u64 total[SP_CLUSTER], sums[3][SP_CLUSTER];
+    u64 total[SP_CLUSTER], sums[3], part[3][SP_WARPS];
     float top, low;
     int first[SP_CLUSTER];
     unsigned key_lo[SP_CLUSTER], key_hi[SP_CLUSTER];
@@ -90,8 +90,14 @@ struct __align__(16) SampleSmem {
         int bin;
         unsigned count;                         // of its elements, and of those in front of it
         unsigned in_front;
-        u64 before;                             // and the weight of those
+        u64 before, want;                       // and the weight of those; what is reached in it
     } cut[2];
+    struct {
+        int coarse;
+        u64 before_c, before_w, want;
+    } near[2];                                  // the neighbouring bins among which a cut is
+    unsigned coarse_count[128];
+    u64 coarse_weight[128];
     u64 all_count, all_weight;                  // (bfloat16: exact)
     SampleBorder border;
     float block_top[SP_WARPS], block_low[SP_WARPS];
@@ -139,6 +145,8 @@ __device__ __forceinline__ unsigned key_of(float z)
     return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
 
+__device__ __forceinline__ float value_of_key(unsigned key) { return __uint_as_float(key ^ (~(unsigned)((int)key >> 31) | 0x80000000u)); }
+
 __device__ __forceinline__ float item_value(const float *p, int i) { return p[i] + 0.f; }          // (-0 is 0)
 __device__ __forceinline__ float item_value(const uint16_t *p, int i) { return __uint_as_float((unsigned)p[i] << 16) + 0.f; }
 
@@ -180,12 +188,8 @@ struct Row {
     {
         return (u64)__double_as_longlong(weight(z) + 4503599627370496.0) & 0xfffffffffffffull;
     }
-    // whether the element is open and in front of the border (or it)
-    __device__ __forceinline__ bool kept(float z, int i, const SampleBorder &b) const
-    {
-        const unsigned k = key_of(z);
-        return z > -INFINITY && (k > b.key || (k == b.key && begin + i <= b.index));
-    }
+    // whether the element is open and in front of the border (or it; the border of all is (-infinity, -1))
+    __device__ __forceinline__ bool kept(float z, int i, const SampleBorder &b) const { return z > b.z || (z == b.z && begin + i <= b.index); }
 
     // Bins in order of falling logits.  bfloat16: one per value from 2^-12 to 2^20 either way, the first, the last and the two in the middle
     // for all beyond.  (Places are such that a thread's consecutive bins and its neighbours' fall on different banks.)
@@ -208,21 +212,13 @@ struct Row {
         return __uint_as_float(bin < 4096 ? (unsigned)(HALF_FIRST + 4095 - bin) << 16 : ((unsigned)(HALF_FIRST + bin - 4096) << 16) | 0x80000000u);
     }
     // The weight of a bin's elements.  HALF: exact (the last bin's are 0: see `plain` below); else as if each had the middle one's.
-    __device__ __forceinline__ u64 bin_mass(int bin, unsigned count, unsigned rest) const
+    __device__ __forceinline__ u64 bin_mass(int bin, unsigned count, unsigned rest, const u64 *tiny) const
     {
-        if (count == 0) return 0;
-        if (HALF) {
-            if (middle(bin)) {
-                u64 q = 0;
-                for (unsigned r = 0; r < blocks; ++r) q += *of_rank(&s.tiny[bin - 4095], r);
-                return q;
-            }
-            return bin == 8191 ? 0 : count * mass(value_of(bin));
-        }
+        if (HALF) return middle(bin) ? tiny[bin - 4095] : bin == 8191 ? 0 : count * mass(value_of(bin));
         const float below = ((float)bin + ((float)rest + 0.5f * count) / (REST * count)) / (2.f * scale);
-        return (u64)__double2ull_rn((double)(exp2f(below * (float)(steps * (-1.0 / SP_TABLE))) * (float)count) * (double)(1ull << 40));
+        return __float2ull_rn(exp2f(below * steps_f * (-1.f / SP_TABLE)) * (float)count * 1099511627776.f);       // (times 2^40)
     }
-    __device__ __forceinline__ void histogram() const
+    __device__ __forceinline__ void histogram(bool weights) const
     {
         for (int i = threadIdx.x; i < 8192 / 4; i += SP_THREADS) reinterpret_cast<uint4 *>(s.bins)[i] = make_uint4(0u, 0u, 0u, 0u);
         if (threadIdx.x < 2) s.tiny[threadIdx.x] = 0;
@@ -239,142 +235,213 @@ struct Row {
                 atomicAdd(&s.bins[place(bin)], 1u);
                 if (HALF) {
                     if (middle(bin)) add64(&s.tiny[bin - 4095], mass(z[j]));
-                } else {
+                } else if (weights) {
                     const float at = (top - z[j]) * scale * 2.f;
                     atomicAdd(&s.bins[BINS + place(bin)], (unsigned)(fminf(at - (float)bin, 1.f) * REST));
                 }
             }
         }
-        cluster_sync(blocks);
+        __syncthreads();
     }
     // The bins where a count (top_k > 0), or a weight, is reached: the latter (HALF) exactly, or between cut[0] and cut[1] if all is well.
+    // Every block finds them for itself, from the others' sums of 64 (32) neighbouring bins and then from their bins: between SMs 128 bytes take
+    // tens of cycles, so not all bins are read.  Ends with a cluster barrier (the bins have been read).
+    static constexpr int COARSE = 128, FINE = BINS / COARSE;
     __device__ __forceinline__ void cuts(int top_k, float top_p) const
     {
-        const int mine = BINS / blocks, each = (mine + SP_THREADS - 1) / SP_THREADS, b0 = rank * mine + threadIdx.x * each;
-        const int in = max(0, min(each, (int)((rank + 1) * mine) - b0));
-        u64 weights = 0, counts = 0;
+        constexpr int EACH = BINS / SP_THREADS, SHARE = SP_THREADS / COARSE;
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+        u64 weight = 0, count = 0;
 #pragma unroll 4
-        for (int j = 0; j < in; ++j) {
-            unsigned count = 0, rest = 0;
-            const int at = place(b0 + j);
-            unsigned counts_of[SP_CLUSTER], rests_of[SP_CLUSTER];
-#pragma unroll
-            for (unsigned r = 0; r < SP_CLUSTER; ++r) {
-                counts_of[r] = r < blocks ? *of_rank(&s.bins[at], r) : 0;
-                rests_of[r] = !HALF && r < blocks ? *of_rank(&s.bins[BINS + at], r) : 0;
-            }
-#pragma unroll
-            for (unsigned r = 0; r < SP_CLUSTER; ++r) {
-                count += counts_of[r];
-                rest += rests_of[r];
-            }
-            s.bins[at] = count;                 // (nobody else reads these of this block)
-            if (!HALF) s.bins[BINS + at] = rest;
-            counts += count;
-            if (top_k == 0) weights += bin_mass(b0 + j, count, rest);
+        for (int j = 0; j < EACH; ++j) {
+            const int bin = tid * EACH + j;
+            const unsigned c = s.bins[place(bin)];
+            count += c;
+            if (top_k == 0 && c) weight += bin_mass(bin, c, HALF ? 0 : s.bins[BINS + place(bin)], s.tiny);
         }
-        u64 block_counts, block_weights = 0;
-        u64 before_c = scan(counts, block_counts), before_w = top_k == 0 ? scan(weights, block_weights) : 0;
-        if (threadIdx.x < blocks) {
-            put64(at_rank(&s.sums[0][rank], threadIdx.x), block_counts);
-            put64(at_rank(&s.sums[1][rank], threadIdx.x), block_weights);
+#pragma unroll
+        for (int o = 1; o < SHARE; o <<= 1) {
+            count += __shfl_xor_sync(0xffffffffu, count, o);
+            weight += __shfl_xor_sync(0xffffffffu, weight, o);
+        }
+        if (tid % SHARE == 0) {
+            s.coarse_count[tid / SHARE] = (unsigned)count;
+            s.coarse_weight[tid / SHARE] = weight;
         }
         cluster_sync(blocks);
-        u64 all_c = 0, all_w = 0;
-        for (unsigned r = 0; r < blocks; ++r) {
-            before_c += r < rank ? s.sums[0][r] : 0;
-            before_w += r < rank ? s.sums[1][r] : 0;
-            all_c += s.sums[0][r];
-            all_w += s.sums[1][r];
+        count = weight = 0;
+        if (tid < COARSE) {
+            unsigned c[SP_CLUSTER];
+            u64 w[SP_CLUSTER];
+#pragma unroll
+            for (unsigned r = 0; r < SP_CLUSTER; ++r) {
+                c[r] = r < blocks ? *of_rank(&s.coarse_count[tid], r) : 0;
+                w[r] = r < blocks && top_k == 0 ? *of_rank(&s.coarse_weight[tid], r) : 0;
+            }
+#pragma unroll
+            for (unsigned r = 0; r < SP_CLUSTER; ++r) {
+                count += c[r];
+                weight += w[r];
+            }
         }
-        if (threadIdx.x == 0) {
-            s.all_count = all_c;
-            s.all_weight = all_w;
-        }
+        u64 all_c, all_w = 0;
+        const u64 before_c = scan(count, all_c), before_w = top_k == 0 ? scan(weight, all_w) : 0;
         const double goal = fmax((double)top_p, 0.0) * (double)all_w;
 #pragma unroll
         for (int c = 0; c < (HALF ? 1 : 2); ++c) {
             const u64 want = top_k ? min((u64)top_k, all_c)
                              : HALF ? max(1ull, (u64)ceil(goal)) : min(all_w, max(1ull, (u64)(c ? goal * (1 + 1.0 / 2048) + 2 : goal * (1 - 1.0 / 2048))));
-            const u64 before = top_k ? before_c : before_w, here = top_k ? counts : weights;
-            if (before < want && want <= before + here) {
-                u64 bc = before_c, bw = before_w;
-                for (int j = 0; j < in; ++j) {
-                    const int at = place(b0 + j);
-                    const unsigned count = s.bins[at];
-                    const u64 w = top_k ? 0 : bin_mass(b0 + j, count, HALF ? 0 : s.bins[BINS + at]), b = top_k ? bc : bw, u = top_k ? count : w;
-                    if (b < want && want <= b + u) {
-                        for (unsigned r = 0; r < blocks; ++r) {
-                            put32(at_rank(&s.cut[c].bin, r), b0 + j);
-                            put32(at_rank(&s.cut[c].count, r), count);
-                            put32(at_rank(&s.cut[c].in_front, r), (unsigned)bc);
-                            put64(at_rank(&s.cut[c].before, r), bw);
-                            if (HALF) put64(at_rank(&s.found.before, r), want);
-                        }
-                    }
-                    bc += count;
-                    bw += w;
+            const u64 before = top_k ? before_c : before_w, here = top_k ? count : weight;
+            if (before < want && want <= before + here) s.near[c] = {tid, before_c, before_w, want};
+        }
+        if (tid == 0) {
+            s.all_count = all_c;
+            s.all_weight = all_w;
+        }
+        __syncthreads();
+        if (warp < (HALF ? 1 : 2) && s.near[warp].coarse >= 0) {
+            const auto near = s.near[warp];
+            constexpr int PER = FINE / 32;
+            unsigned c[PER];
+            u64 w[PER], bc = 0, bw = 0;
+            unsigned k[PER][SP_CLUSTER], rest[PER][SP_CLUSTER];
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const int at = place(near.coarse * FINE + lane * PER + j);
+#pragma unroll
+                for (unsigned r = 0; r < SP_CLUSTER; ++r) {
+                    k[j][r] = r < blocks ? *of_rank(&s.bins[at], r) : 0;
+                    rest[j][r] = !HALF && top_k == 0 && r < blocks ? *of_rank(&s.bins[BINS + at], r) : 0;
                 }
+            }
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const int bin = near.coarse * FINE + lane * PER + j;
+                c[j] = 0;
+                w[j] = 0;
+#pragma unroll
+                for (unsigned r = 0; r < SP_CLUSTER; ++r) {
+                    c[j] += k[j][r];
+                    if (top_k == 0 && !HALF && k[j][r]) w[j] += bin_mass(bin, k[j][r], rest[j][r], nullptr);
+                }
+                if (top_k == 0 && HALF && c[j]) {
+                    if (middle(bin))
+                        for (unsigned r = 0; r < blocks; ++r) w[j] += *of_rank(&s.tiny[bin - 4095], r);
+                    else w[j] = bin_mass(bin, c[j], 0, s.tiny);
+                }
+                bc += c[j];
+                bw += w[j];
+            }
+            const u64 own_c = bc, own_w = bw;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 x = __shfl_up_sync(0xffffffffu, bc, o), y = __shfl_up_sync(0xffffffffu, bw, o);
+                if (lane >= o) {
+                    bc += x;
+                    bw += y;
+                }
+            }
+            bc += near.before_c - own_c;
+            bw += near.before_w - own_w;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const u64 b = top_k ? bc : bw, u = top_k ? c[j] : w[j];
+                if (b < near.want && near.want <= b + u) s.cut[warp] = {near.coarse * FINE + lane * PER + j, c[j], (unsigned)bc, bw, near.want};
+                bc += c[j];
+                bw += w[j];
             }
         }
         cluster_sync(blocks);
     }
 
-    // Sends the elements of the bins first .. last to the first block's list (if there are at most SP_LIST; s.listed of the first
-    // block counts all).  sums: [0] the weight of all elements in front of them, [1] their own, [2] of all, if `weigh`.
-    // Ends with a cluster barrier, after which every block has all blocks' sums.
-    __device__ __forceinline__ void collect(int first, int last, bool weigh, u64 (&sums)[3]) const
+    // Brings the elements of the bins first .. last into the first block's list, if there are at most SP_LIST: the number of them comes back
+    // (each block lists its own, then the first one fetches them).  sums: [0] the weight of all elements in front of them, [1] their own, [2]
+    // of all, if `weigh`.  Ends with a cluster barrier.
+    __device__ __forceinline__ unsigned collect(int first, int last, bool weigh, u64 (&sums)[3]) const
     {
         u64 mine[3] = {0, 0, 0};
-        const uint32_t listed = at_rank(&s.listed, 0);
         constexpr int U = 4;                    // (side by side, for the latency of binary64)
         for (int i0 = threadIdx.x; i0 < n; i0 += U * SP_THREADS) {
             float z[U];
             int bin[U];
             u64 q[U];
+            bool any = weigh;
 #pragma unroll
             for (int j = 0; j < U; ++j) {
                 z[j] = i0 + j * SP_THREADS < n ? value(i0 + j * SP_THREADS) : -INFINITY;
                 bin[j] = z[j] > -INFINITY ? bin_of(z[j]) : BINS;
+                any |= bin[j] >= first && bin[j] <= last;
                 q[j] = 0;
             }
-            if (weigh) {
+            if (!any) continue;
 #pragma unroll
-                for (int j = 0; j < U; ++j) q[j] = mass(z[j]);
+            for (int j = 0; j < U; ++j) q[j] = mass(z[j]);
 #pragma unroll
-                for (int j = 0; j < U; ++j) {
-                    mine[0] += bin[j] < first ? q[j] : 0;
-                    mine[1] += bin[j] >= first && bin[j] <= last ? q[j] : 0;
-                    mine[2] += q[j];
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < U; ++j)
+            for (int j = 0; j < U; ++j) {
+                mine[2] += q[j];
+                if (first > 0) mine[0] += bin[j] < first ? q[j] : 0;
                 if (bin[j] >= first && bin[j] <= last) {
-                    unsigned slot;
-                    asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(slot) : "r"(listed) : "memory");
+                    mine[1] += q[j];
+                    const int slot = atomicAdd(&s.listed, 1);
                     if (slot < SP_LIST) {
-                        put32(at_rank(&s.list.key[slot], 0), key_of(z[j]));
-                        put32(at_rank(&s.list.index[slot], 0), begin + i0 + j * SP_THREADS);
-                        put64(at_rank(&s.list.mass[slot], 0), weigh ? q[j] : mass(z[j]));
+                        s.list.key[slot] = key_of(z[j]);
+                        s.list.index[slot] = begin + i0 + j * SP_THREADS;
+                        s.list.mass[slot] = q[j];
                     }
                 }
+            }
         }
         if (weigh) {
+            const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
             for (int j = 0; j < 3; ++j) {
-                u64 sum;
-                scan(mine[j], sum);
-                if (threadIdx.x < blocks) put64(at_rank(&s.sums[j][rank], threadIdx.x), sum);
+#pragma unroll
+                for (int o = 16; o; o >>= 1) mine[j] += __shfl_xor_sync(0xffffffffu, mine[j], o);
+                if (lane == 0) s.part[j][warp] = mine[j];
+            }
+            __syncthreads();
+            if (threadIdx.x < 3) {
+                u64 sum = 0;
+                for (int w = 0; w < SP_WARPS; ++w) sum += s.part[threadIdx.x][w];
+                s.sums[threadIdx.x] = sum;
             }
         }
         cluster_sync(blocks);
+        unsigned counts[SP_CLUSTER], all = 0;
+#pragma unroll
+        for (unsigned r = 0; r < SP_CLUSTER; ++r) counts[r] = r < blocks ? *of_rank(&s.listed, r) : 0;
+#pragma unroll
+        for (unsigned r = 0; r < SP_CLUSTER; ++r) all += counts[r];
 #pragma unroll
         for (int j = 0; j < 3; ++j) {
             sums[j] = 0;
-            if (weigh)
-                for (unsigned r = 0; r < blocks; ++r) sums[j] += s.sums[j][r];
+            if (weigh) {
+                u64 a[SP_CLUSTER];
+#pragma unroll
+                for (unsigned r = 0; r < SP_CLUSTER; ++r) a[r] = r < blocks ? *of_rank(&s.sums[j], r) : 0;
+#pragma unroll
+                for (unsigned r = 0; r < SP_CLUSTER; ++r) sums[j] += a[r];
+            }
         }
+        if (rank == 0 && all <= SP_LIST) {
+            for (unsigned i = counts[0] + threadIdx.x; i < all; i += SP_THREADS) {
+                unsigned r = 0, j = i;
+#pragma unroll
+                for (unsigned k = 0; k < SP_CLUSTER - 1; ++k)
+                    if (r == k && j >= counts[k]) {
+                        j -= counts[k];
+                        ++r;
+                    }
+                const unsigned key = *of_rank(&s.list.key[j], r);
+                const int index = *of_rank(&s.list.index[j], r);
+                const u64 q = *of_rank(&s.list.mass[j], r);
+                s.list.key[i] = key;
+                s.list.index[i] = index;
+                s.list.mass[i] = q;
+            }
+        }
+        cluster_sync(blocks);
+        return all;
     }
 
     // Of m elements, each with a number of its own (lo to hi) and a share (0: none), the one at which the sum of shares in order of the
@@ -432,9 +499,9 @@ struct Row {
 
     // The first block has all that can be left in its list: everything else.  all: the weight that top_p is a share of (top_k > 0: of what
     // that leaves).
-    __device__ void finish(int top_k, float top_p, float min_p, float u, u64 all, float lowest, int vocab, int32_t *token, float *prob) const
+    __device__ __forceinline__ void finish(int m, int top_k, float top_p, float min_p, float u, u64 all, float lowest, int vocab, int32_t *token,
+                                           float *prob) const
     {
-        const int m = min(s.listed, SP_LIST);
         u64 last = last_number(lowest);         // the border's number
         const auto number = [&](int i) { return number_in_order(i); };
         const auto weight_in = [&](int i) -> u64 { return number_in_order(i) <= last ? s.list.mass[i] : 0; };
@@ -453,7 +520,7 @@ struct Row {
         const auto drawn = [&](int i) -> u64 {
             if (min_p > 0.f) {
                 const unsigned k = s.list.key[i];
-                if (weight(__uint_as_float(k ^ (~(unsigned)((int)k >> 31) | 0x80000000u))) < least) return 0;
+                if (weight(value_of_key(k)) < least) return 0;
             }
             return weight_in(i);
         };
@@ -462,29 +529,29 @@ struct Row {
         if (threadIdx.x == 0) {
             const unsigned k = s.list.key[i];
             *token = s.list.index[i];
-            if (prob) *prob = (float)(weight(__uint_as_float(k ^ (~(unsigned)((int)k >> 31) | 0x80000000u))) / (double)sum);
+            if (prob) *prob = (float)(weight(value_of_key(k)) / (double)sum);
         }
     }
 
-    // The border is the nth (from 1) in order of index among the elements with that key.
-    __device__ __forceinline__ void among_ties(unsigned key, u64 nth) const
+    // The border is the nth (from 1) in order of index among the elements of that logit.
+    __device__ __forceinline__ void among_ties(float tie, u64 nth) const
     {
         const int each = (n + SP_THREADS - 1) / SP_THREADS, i0 = min(n, threadIdx.x * each), i1 = min(n, i0 + each);
         int here = 0;
-        for (int i = i0; i < i1; ++i) here += key_of(value(i)) == key;
+        for (int i = i0; i < i1; ++i) here += value(i) == tie;
         u64 block_sum, all;
         u64 in_front = scan(here, block_sum);
         in_front += gather(block_sum, all);
         if (in_front < nth && nth <= in_front + here) {
             for (int i = i0; i < i1; ++i)
-                if (key_of(value(i)) == key && ++in_front == nth) tell(key, begin + i);
+                if (value(i) == tie && ++in_front == nth) tell(tie, begin + i);
         }
         cluster_sync(blocks);
     }
-    __device__ __forceinline__ void tell(unsigned key, int index) const
+    __device__ __forceinline__ void tell(float z, int index) const
     {
         for (unsigned r = 0; r < blocks; ++r) {
-            put32(at_rank(&s.border.key, r), key);
+            put32(at_rank(&s.border.z, r), __float_as_uint(z));
             put32(at_rank(&s.border.index, r), index);
         }
     }
@@ -661,8 +728,7 @@ struct Row {
             // ties: the one of them in order of index at which it is reached
             u64 nth = want - before;
             if (MASS) {
-                const unsigned u = lo ^ (~(unsigned)((int)lo >> 31) | 0x80000000u);
-                const u64 q = mass(__uint_as_float(u));
+                const u64 q = mass(value_of_key(lo));
                 nth = (nth + q - 1) / q;
             }
             // (a thread's elements are consecutive)
@@ -675,10 +741,7 @@ struct Row {
             if (in_front < nth && nth <= in_front + here) {
                 for (int i = i0; i < i1; ++i)
                     if (there(value(i), i) && ++in_front == nth) {
-                        for (unsigned r = 0; r < blocks; ++r) {
-                            put32(at_rank(&s.border.key, r), lo);
-                            put32(at_rank(&s.border.index, r), begin + i);
-                        }
+                        tell(value_of_key(lo), begin + i);
                     }
             }
         } else {
@@ -706,10 +769,7 @@ struct Row {
                         if (k > key || (k == key && s.weights.list_index[j] < index)) b += MASS ? s.weights.list_mass[j] : 1;
                     }
                     if (b < want && want <= b + own) {
-                        for (unsigned r = 0; r < blocks; ++r) {
-                            put32(at_rank(&s.border.key, r), key);
-                            put32(at_rank(&s.border.index, r), index);
-                        }
+                        tell(value_of_key(key), index);
                     }
                 }
             }
@@ -789,6 +849,7 @@ sample_kernel(const SampleParams p)
     if (tid == 0) {
         s.listed = 0;
         s.cut[0].bin = s.cut[1].bin = -1;
+        s.near[0].coarse = s.near[1].coarse = -1;
     }
     __syncthreads();
     for (int w = 0; w < SP_WARPS; ++w) {
@@ -844,7 +905,7 @@ sample_kernel(const SampleParams p)
     const Row<T> r = {s, items, n, begin, rank, blocks, top, SP_TABLE * 1.4426950408889634074 / (double)temperature,
                       (float)(SP_TABLE * 1.4426950408889634074 / (double)temperature),
                       spread > 1e-30f ? (SP_BINS - 1) / spread : 0.f};
-    SampleBorder border = {0u, 0x7fffffff};
+    SampleBorder border = {-INFINITY, -1};
     const bool by_count = top_k > 0 && top_k < p.vocab, by_weight = top_p < 1.f;
     const auto share_of = [&](u64 all) { return max(1ull, (u64)ceil(fmax((double)top_p, 0.0) * (double)all)); };
     const auto count_of = [&](u64 all) { return min((u64)top_k, all); };
@@ -852,8 +913,9 @@ sample_kernel(const SampleParams p)
     const bool counted = (by_count || by_weight) && r.scale > 0.f && (by_count || !Row<T>::HALF || (temperature <= 1000.f && fabsf(top) < 524288.f));
     bool count_done = !by_count, weight_done = !by_weight, alone = false;
     u64 all_weight = 0;
+    unsigned listed = 0;
     if (counted) {
-        r.histogram();
+        r.histogram(!by_count);
         r.cuts(by_count ? top_k : 0, top_p);
         const auto first = s.cut[0], last = s.cut[Row<T>::HALF || by_count ? 0 : 1];
         const unsigned up_to = last.in_front + last.count;
@@ -863,7 +925,7 @@ sample_kernel(const SampleParams p)
                 // (binary32 by weight: the sum of all is not known yet, nor that the border is among these)
                 const bool weigh = !by_count && !Row<T>::HALF;
                 all_weight = s.all_weight;
-                r.collect(0, last.bin, weigh, sums);
+                listed = r.collect(0, last.bin, weigh, sums);
                 if (weigh) all_weight = sums[2];
                 alone = !weigh || share_of(all_weight) <= sums[1];
             } else if (Row<T>::HALF) {
@@ -872,21 +934,21 @@ sample_kernel(const SampleParams p)
                     u64 nth = count_of(s.all_count) - last.in_front;
                     if (!by_count) {
                         const u64 q = r.mass(z);
-                        nth = (s.found.before - last.before + q - 1) / q;
+                        nth = (last.want - last.before + q - 1) / q;
                     }
-                    r.among_ties(key_of(z), nth);
+                    r.among_ties(z, nth);
                     border = s.border;
                     (by_count ? count_done : weight_done) = true;
                 }
             } else if (up_to - first.in_front <= SP_LIST) {
                 const bool weigh = !by_count;
-                r.collect(first.bin, last.bin, weigh, sums);
+                listed = r.collect(first.bin, last.bin, weigh, sums);
                 const u64 want = weigh ? share_of(sums[2]) : count_of(s.all_count) - last.in_front;
                 if (!weigh || (sums[0] < want && want <= sums[0] + sums[1])) {
                     if (rank == 0) {
-                        const int i = r.reach(s.listed, [&](int j) { return r.number_in_order(j); }, [&](int j) { return weigh ? s.list.mass[j] : 1ull; },
+                        const int i = r.reach(listed, [&](int j) { return r.number_in_order(j); }, [&](int j) { return weigh ? s.list.mass[j] : 1ull; },
                                               want - (weigh ? sums[0] : 0), 0, r.last_number(low));
-                        if (tid == 0) r.tell(s.list.key[i], s.list.index[i]);
+                        if (tid == 0) r.tell(value_of_key(s.list.key[i]), s.list.index[i]);
                     }
                     cluster_sync(blocks);
                     border = s.border;
@@ -898,12 +960,11 @@ sample_kernel(const SampleParams p)
         // (a little lower than need be: what is left out weighs less than min_p for certain)
         const float far = -temperature * logf(fminf(min_p, 1.f));
         u64 ignored[3];
-        r.collect(0, r.bin_of(top - far * 1.0001f - 1e-5f * fabsf(top)), false, ignored);
-        alone = *of_rank(&s.listed, 0) <= SP_LIST;
-        cluster_sync(blocks);                   // (before the first block goes on or leaves)
+        listed = r.collect(0, r.bin_of(top - far * 1.0001f - 1e-5f * fabsf(top)), false, ignored);
+        alone = listed <= SP_LIST;
     }
     if (alone) {
-        if (rank == 0) r.finish(by_count ? top_k : 0, top_p, min_p, u, all_weight, low, p.vocab, p.token + row, p.prob ? p.prob + row : nullptr);
+        if (rank == 0) r.finish(listed, by_count ? top_k : 0, top_p, min_p, u, all_weight, low, p.vocab, p.token + row, p.prob ? p.prob + row : nullptr);
         DIP_TRACE_MAX(p.tr, 2);
         return;
     }
@@ -916,13 +977,13 @@ sample_kernel(const SampleParams p)
     int known = 0;                              // bins whose weights are in s.bin_mass
     if (Row<T>::HALF && n > 4096 && fabsf(top) < INFINITY) {
         known = min(4096, 8191 - top_bin);
-        if (border.key) known = min(known, r.bin_of(__uint_as_float(border.key ^ (~(unsigned)((int)border.key >> 31) | 0x80000000u))) - top_bin + 1);
+        if (border.z > -INFINITY) known = min(known, r.bin_of(border.z) - top_bin + 1);
         __syncthreads();
         for (int i = tid; i < known; i += SP_THREADS) s.bin_mass[i] = r.mass(r.value_of(top_bin + i));
         __syncthreads();
     }
     const double least = fmin((double)min_p, 1.0) * (double)(1ull << SP_ONE_BITS);
-    const auto open = [&](float z, int i) { return border.key ? r.kept(z, i, border) : z > -INFINITY; };
+    const auto open = [&](float z, int i) { return r.kept(z, i, border); };
     const auto mass_of = [&](float z) -> u64 {
         if (Row<T>::HALF) {
             const int bin = r.bin_of(z) - top_bin;
