@@ -168,8 +168,34 @@ struct Row {
     double steps;                               // 512 log2(e) / temperature
     float steps_f;
     float scale;                                // bins per unit
+    int head, vectors;                          // items in front of the first boundary of 16 bytes; whole pieces of 16 bytes from there on
 
     __device__ __forceinline__ float value(int i) const { return item_value(items, i); }
+
+    // Pieces of 16 bytes: those of the row, then what is in front of the first one and behind the last one; -infinity for what is not there.
+    static constexpr int PER = 16 / sizeof(T);
+    __device__ __forceinline__ int pieces() const { return vectors + 2; }
+    __device__ __forceinline__ int piece(int v, float (&z)[PER]) const
+    {
+        if (v < vectors) {
+            const uint4 a = reinterpret_cast<const uint4 *>(items + head)[v];
+            const unsigned w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (sizeof(T) == 2) {
+                    z[2 * j] = __uint_as_float(w[j] << 16) + 0.f;
+                    z[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u) + 0.f;
+                } else {
+                    z[j] = __uint_as_float(w[j]) + 0.f;
+                }
+            }
+            return head + v * PER;
+        }
+        const int first = v == vectors ? 0 : head + vectors * PER, last = v == vectors ? head : n;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) z[j] = first + j < last ? value(first + j) : -INFINITY;
+        return first;
+    }
 
     // exp((z - top) / temperature) times 2^45: 2^(k / 512) from the table times the third-order sum for what is left (within 10^-14).
     // Nine binary64 operations, which go at a quarter of binary32's rate (B200: half of its lanes, two cycles each), and a conversion.
@@ -223,13 +249,11 @@ struct Row {
         for (int i = threadIdx.x; i < 8192 / 4; i += SP_THREADS) reinterpret_cast<uint4 *>(s.bins)[i] = make_uint4(0u, 0u, 0u, 0u);
         if (threadIdx.x < 2) s.tiny[threadIdx.x] = 0;
         __syncthreads();
-        constexpr int U = 4;
-        for (int i0 = threadIdx.x; i0 < n; i0 += U * SP_THREADS) {
-            float z[U];
+        for (int v = threadIdx.x; v < pieces(); v += SP_THREADS) {
+            float z[PER];
+            piece(v, z);
 #pragma unroll
-            for (int j = 0; j < U; ++j) z[j] = i0 + j * SP_THREADS < n ? value(i0 + j * SP_THREADS) : -INFINITY;
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
+            for (int j = 0; j < PER; ++j) {
                 if (!(z[j] > -INFINITY)) continue;
                 const int bin = bin_of(z[j]);
                 atomicAdd(&s.bins[place(bin)], 1u);
@@ -360,33 +384,36 @@ struct Row {
     __device__ __forceinline__ unsigned collect(int first, int last, bool weigh, u64 (&sums)[3]) const
     {
         u64 mine[3] = {0, 0, 0};
-        constexpr int U = 4;                    // (side by side, for the latency of binary64)
-        for (int i0 = threadIdx.x; i0 < n; i0 += U * SP_THREADS) {
-            float z[U];
-            int bin[U];
-            u64 q[U];
+        for (int v = threadIdx.x; v < pieces(); v += SP_THREADS) {
+            float z[PER];
+            const int i0 = piece(v, z);
+            int bin[PER];
             bool any = weigh;
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                z[j] = i0 + j * SP_THREADS < n ? value(i0 + j * SP_THREADS) : -INFINITY;
+            for (int j = 0; j < PER; ++j) {
                 bin[j] = z[j] > -INFINITY ? bin_of(z[j]) : BINS;
                 any |= bin[j] >= first && bin[j] <= last;
-                q[j] = 0;
             }
             if (!any) continue;
+            // (four weights side by side, for the latency of binary64)
 #pragma unroll
-            for (int j = 0; j < U; ++j) q[j] = mass(z[j]);
+            for (int j0 = 0; j0 < PER; j0 += 4) {
+                u64 q[4];
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                mine[2] += q[j];
-                if (first > 0) mine[0] += bin[j] < first ? q[j] : 0;
-                if (bin[j] >= first && bin[j] <= last) {
-                    mine[1] += q[j];
-                    const int slot = atomicAdd(&s.listed, 1);
-                    if (slot < SP_LIST) {
-                        s.list.key[slot] = key_of(z[j]);
-                        s.list.index[slot] = begin + i0 + j * SP_THREADS;
-                        s.list.mass[slot] = q[j];
+                for (int j = 0; j < 4; ++j) q[j] = mass(z[j0 + j]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int at = bin[j0 + j];
+                    mine[2] += q[j];
+                    if (first > 0) mine[0] += at < first ? q[j] : 0;
+                    if (at >= first && at <= last) {
+                        mine[1] += q[j];
+                        const int slot = atomicAdd(&s.listed, 1);
+                        if (slot < SP_LIST) {
+                            s.list.key[slot] = key_of(z[j0 + j]);
+                            s.list.index[slot] = begin + i0 + j0 + j;
+                            s.list.mass[slot] = q[j];
+                        }
                     }
                 }
             }
@@ -533,19 +560,63 @@ struct Row {
         }
     }
 
+    // Of all elements in order of index, each with a share, the one at which the sum of shares exceeds mark(sum of all): found(its place in
+    // this block, its logit, the sum of all), by one thread of one block.  shares(z, i, q): those of a piece's elements, whether any has one.
+    // A warp's elements are consecutive; the warp whose they are is then looked at by the whole block.
+    template <class Shares, class Share, class Mark, class Found>
+    __device__ __forceinline__ void in_order(const Shares &shares, const Share &share, const Mark &mark, const Found &found) const
+    {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        // (the first warp also has what is in front of the first whole piece, the last one what is behind the last)
+        const int each = (vectors + SP_WARPS - 1) / SP_WARPS, v0 = min(vectors, warp * each), v1 = min(vectors, v0 + each);
+        u64 sum = 0;
+        for (int v = v0 + lane; v < v1; v += 32) {
+            float z[PER];
+            u64 q[PER];
+            const int i = piece(v, z);
+            if (shares(z, i, q)) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) sum += q[j];
+            }
+        }
+        if (lane == 0 && (warp == 0 || warp == SP_WARPS - 1)) {
+            for (int i = warp ? head + vectors * PER : 0; i < (warp ? n : head); ++i) sum += share(value(i), i);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        __syncthreads();
+        if (lane == 0) s.part[0][warp] = sum;
+        __syncthreads();
+        u64 block_sum = 0, all;
+        for (int w = 0; w < SP_WARPS; ++w) block_sum += s.part[0][w];
+        const u64 before = gather(block_sum, all), want = mark(all);
+        if (before <= want && want < before + block_sum) {
+            u64 at = before;
+            int w = 0;
+            for (; at + s.part[0][w] <= want; ++w) at += s.part[0][w];
+            const int j0 = w == 0 ? 0 : head + min(vectors, w * each) * PER;
+            const int j1 = w == SP_WARPS - 1 ? n : head + min(vectors, (w + 1) * each) * PER, part = (j1 - j0 + SP_THREADS - 1) / SP_THREADS;
+            const int k0 = min(j1, j0 + (int)threadIdx.x * part), k1 = min(j1, k0 + part);
+            u64 mine = 0, ignored;
+            for (int i = k0; i < k1; ++i) mine += share(value(i), i);
+            at += scan(mine, ignored);
+            if (at <= want && want < at + mine) {
+                int i = k0;
+                for (u64 q; at + (q = share(value(i), i)) <= want; ++i) at += q;
+                found(i, value(i), all);
+            }
+        }
+    }
     // The border is the nth (from 1) in order of index among the elements of that logit.
     __device__ __forceinline__ void among_ties(float tie, u64 nth) const
     {
-        const int each = (n + SP_THREADS - 1) / SP_THREADS, i0 = min(n, threadIdx.x * each), i1 = min(n, i0 + each);
-        int here = 0;
-        for (int i = i0; i < i1; ++i) here += value(i) == tie;
-        u64 block_sum, all;
-        u64 in_front = scan(here, block_sum);
-        in_front += gather(block_sum, all);
-        if (in_front < nth && nth <= in_front + here) {
-            for (int i = i0; i < i1; ++i)
-                if (value(i) == tie && ++in_front == nth) tell(tie, begin + i);
-        }
+        in_order(
+            [&](const float (&z)[PER], int, u64 (&q)[PER]) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) q[j] = z[j] == tie;
+                return true;
+            },
+            [&](float z, int) -> u64 { return z == tie; }, [&](u64) { return nth - 1; }, [&](int i, float z, u64) { tell(z, begin + i); });
         cluster_sync(blocks);
     }
     __device__ __forceinline__ void tell(float z, int index) const
@@ -904,7 +975,7 @@ sample_kernel(const SampleParams p)
     const float spread = fminf(top - low, SP_SPREAD);
     const Row<T> r = {s, items, n, begin, rank, blocks, top, SP_TABLE * 1.4426950408889634074 / (double)temperature,
                       (float)(SP_TABLE * 1.4426950408889634074 / (double)temperature),
-                      spread > 1e-30f ? (SP_BINS - 1) / spread : 0.f};
+                      spread > 1e-30f ? (SP_BINS - 1) / spread : 0.f, head, vectors};
     SampleBorder border = {-INFINITY, -1};
     const bool by_count = top_k > 0 && top_k < p.vocab, by_weight = top_p < 1.f;
     const auto share_of = [&](u64 all) { return max(1ull, (u64)ceil(fmax((double)top_p, 0.0) * (double)all)); };
@@ -971,7 +1042,7 @@ sample_kernel(const SampleParams p)
     if (!count_done) r.template shorten<false>(border, count_of);
     if (!weight_done) r.template shorten<true>(border, share_of);
 
-    // The draw: a warp's elements are consecutive.  Where a block has more bfloat16 logits than there are values of them that count, their weights
+    // The draw.  Where a block has more bfloat16 logits than there are values of them that count, their weights
     // are worked out once.
     const int top_bin = r.bin_of(top);
     int known = 0;                              // bins whose weights are in s.bin_mass
@@ -991,55 +1062,30 @@ sample_kernel(const SampleParams p)
         }
         return r.mass(z);
     };
-    const auto drawn = [&](int i) -> u64 {
-        const float z = r.value(i);
-        return open(z, i) && !(min_p > 0.f && r.weight(z) < least) ? mass_of(z) : 0;
-    };
-    const int each = ((n + SP_WARPS - 1) / SP_WARPS + 31) & ~31, i0 = min(n, warp * each), i1 = min(n, i0 + each);
-    u64 sum = 0;
-    constexpr int U = 4;
-    for (int i = i0; i < i1; i += 32 * U) {
-        float z[U];
-        bool in[U], any = false;
+    const auto drawn = [&](float z, int i) -> u64 { return open(z, i) && !(min_p > 0.f && r.weight(z) < least) ? mass_of(z) : 0; };
+    constexpr int PIECE = Row<T>::PER;
+    r.in_order(
+        [&](const float (&z)[PIECE], int i, u64 (&q)[PIECE]) {
+            bool any = false;
 #pragma unroll
-        for (int j = 0; j < U; ++j) {
-            const int at = i + 32 * j + lane;
-            z[j] = at < i1 ? r.value(at) : -INFINITY;
-            in[j] = open(z[j], at);
-            any |= in[j];
-        }
-        if (!__any_sync(0xffffffffu, any)) continue;
-        u64 q[U];
+            for (int j = 0; j < PIECE; ++j) any |= open(z[j], i + j);
+            if (!any) return false;
 #pragma unroll
-        for (int j = 0; j < U; ++j) q[j] = Row<T>::HALF ? (in[j] ? mass_of(z[j]) : 0) : r.mass(z[j]);
+            for (int j = 0; j < PIECE; ++j) q[j] = Row<T>::HALF ? drawn(z[j], i + j) : r.mass(z[j]);
+            if (!Row<T>::HALF) {
 #pragma unroll
-        for (int j = 0; j < U; ++j) sum += in[j] && !(min_p > 0.f && r.weight(z[j]) < least) ? q[j] : 0;
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) s.scan[warp] = sum;
-    __syncthreads();
-    u64 block_sum = 0, all;
-    for (int w = 0; w < SP_WARPS; ++w) block_sum += s.scan[w];
-    const u64 before = r.gather(block_sum, all);
-    // the smallest index at which the sum in order of index is above u of all
-    const u64 mark = min(all - 1, (u64)(fmax((double)u, 0.0) * (double)all));
-    if (before <= mark && mark < before + block_sum) {
-        u64 at = before;
-        int w = 0;
-        for (; at + s.scan[w] <= mark; ++w) at += s.scan[w];
-        const int j0 = min(n, w * each), j1 = min(n, j0 + each), part = (each + SP_THREADS - 1) / SP_THREADS;
-        const int k0 = min(j1, j0 + tid * part), k1 = min(j1, k0 + part);
-        u64 mine = 0, ignored;
-        for (int i = k0; i < k1; ++i) mine += drawn(i);
-        at += r.scan(mine, ignored);
-        if (at <= mark && mark < at + mine) {
-            int i = k0;
-            for (u64 q; at + (q = drawn(i)) <= mark; ++i) at += q;
+                for (int j = 0; j < PIECE; ++j)
+                    if (!open(z[j], i + j) || (min_p > 0.f && r.weight(z[j]) < least)) q[j] = 0;
+            }
+            return true;
+        },
+        drawn,
+        // the smallest index at which the sum in order of index is above u of all
+        [&](u64 all) { return min(all - 1, (u64)(fmax((double)u, 0.0) * (double)all)); },
+        [&](int i, float z, u64 all) {
             p.token[row] = begin + i;
-            if (p.prob) p.prob[row] = (float)(r.weight(r.value(i)) / (double)all);
-        }
-    }
+            if (p.prob) p.prob[row] = (float)(r.weight(z) / (double)all);
+        });
     DIP_TRACE_MAX(p.tr, 2);
 }
 
