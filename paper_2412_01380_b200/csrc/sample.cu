@@ -15,6 +15,8 @@
 // The draw adds up the kept weights per warp (whose elements are consecutive), then looks closer where the sum crosses the number.
 #include <initializer_list>
 
+#include <cuda_bf16.h>
+
 #include "common.cuh"
 #include "gemv_common.cuh"
 
@@ -35,7 +37,7 @@ typedef unsigned long long u64;
 struct SampleParams {
     const void *logits;
     size_t pitch;
-    int vocab, slice;
+    int vocab, slice, resident;                 // whether a block's part of the row is copied to shared memory
     const float *temperature, *top_p, *min_p, *uniform;
     const int32_t *top_k;
     int32_t *token;
@@ -147,6 +149,15 @@ __device__ __forceinline__ unsigned key_of(float z)
 
 __device__ __forceinline__ float value_of_key(unsigned key) { return __uint_as_float(key ^ (~(unsigned)((int)key >> 31) | 0x80000000u)); }
 
+// The larger ones of two pairs of bfloat16 (a number beside what is none).
+__device__ __forceinline__ unsigned max2(unsigned a, unsigned b)
+{
+    unsigned m;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return m;
+}
+__device__ __forceinline__ float larger(unsigned pair) { return fmaxf(__uint_as_float(pair << 16), __uint_as_float(pair & 0xffff0000u)); }
+
 __device__ __forceinline__ float item_value(const float *p, int i) { return p[i] + 0.f; }          // (-0 is 0)
 __device__ __forceinline__ float item_value(const uint16_t *p, int i) { return __uint_as_float((unsigned)p[i] << 16) + 0.f; }
 
@@ -161,7 +172,7 @@ __device__ __forceinline__ void add64(u64 *sum, u64 q)
 template <typename T>
 struct Row {
     SampleSmem &s;
-    const T *items;                             // this block's, in shared memory
+    const T *items;                             // this block's, in shared memory or where they came from
     int n, begin;                               // how many; the first one's index
     unsigned rank, blocks;
     float top;                                  // the largest logit
@@ -172,29 +183,52 @@ struct Row {
 
     __device__ __forceinline__ float value(int i) const { return item_value(items, i); }
 
-    // Pieces of 16 bytes: those of the row, then what is in front of the first one and behind the last one; -infinity for what is not there.
+    // Pieces of 16 bytes (-infinity for what is not there).
     static constexpr int PER = 16 / sizeof(T);
-    __device__ __forceinline__ int pieces() const { return vectors + 2; }
-    __device__ __forceinline__ int piece(int v, float (&z)[PER]) const
+    __device__ __forceinline__ void decode(const uint4 &a, float (&z)[PER]) const
     {
-        if (v < vectors) {
-            const uint4 a = reinterpret_cast<const uint4 *>(items + head)[v];
-            const unsigned w[4] = {a.x, a.y, a.z, a.w};
+        const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (sizeof(T) == 2) {
-                    z[2 * j] = __uint_as_float(w[j] << 16) + 0.f;
-                    z[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u) + 0.f;
-                } else {
-                    z[j] = __uint_as_float(w[j]) + 0.f;
-                }
+        for (int j = 0; j < 4; ++j) {
+            if (sizeof(T) == 2) {
+                z[2 * j] = __uint_as_float(w[j] << 16) + 0.f;
+                z[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u) + 0.f;
+            } else {
+                z[j] = __uint_as_float(w[j]) + 0.f;
             }
-            return head + v * PER;
         }
-        const int first = v == vectors ? 0 : head + vectors * PER, last = v == vectors ? head : n;
+    }
+    // f(logits of a piece, place of the first one) for the pieces first, first + step, ..., below last (all: of the block's threads), with the
+    // next one under way.
+    // (HALF: pieces without a logit from `least` up are passed over.)
+    template <class F>
+    __device__ __forceinline__ void walk(int first, int last, int step, const F &f, float least = -INFINITY) const
+    {
+        const uint4 *from = reinterpret_cast<const uint4 *>(items + head);
+        uint4 a = first < last ? from[first] : make_uint4(0u, 0u, 0u, 0u);
+        for (int v = first; v < last; v += step) {
+            const uint4 next = v + step < last ? from[v + step] : a;
+            if (sizeof(T) == 2 && !(larger(max2(max2(a.x, a.y), max2(a.z, a.w))) >= least)) {
+                a = next;
+                continue;
+            }
+            float z[PER];
+            decode(a, z);
+            f(z, head + v * PER);
+            a = next;
+        }
+    }
+    template <class F>
+    __device__ __forceinline__ void walk_all(const F &f) const
+    {
+        walk(threadIdx.x, vectors, SP_THREADS, f);
+        if (threadIdx.x < 2) {                  // (what is in front of the first whole piece, and behind the last one)
+            const int first = threadIdx.x ? head + vectors * PER : 0, last = threadIdx.x ? n : head;
+            float z[PER];
 #pragma unroll
-        for (int j = 0; j < PER; ++j) z[j] = first + j < last ? value(first + j) : -INFINITY;
-        return first;
+            for (int j = 0; j < PER; ++j) z[j] = first + j < last ? value(first + j) : -INFINITY;
+            f(z, first);
+        }
     }
 
     // exp((z - top) / temperature) times 2^45: 2^(k / 512) from the table times the third-order sum for what is left (within 10^-14).
@@ -249,9 +283,7 @@ struct Row {
         for (int i = threadIdx.x; i < 8192 / 4; i += SP_THREADS) reinterpret_cast<uint4 *>(s.bins)[i] = make_uint4(0u, 0u, 0u, 0u);
         if (threadIdx.x < 2) s.tiny[threadIdx.x] = 0;
         __syncthreads();
-        for (int v = threadIdx.x; v < pieces(); v += SP_THREADS) {
-            float z[PER];
-            piece(v, z);
+        walk_all([&](const float (&z)[PER], int) {
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
                 if (!(z[j] > -INFINITY)) continue;
@@ -264,7 +296,7 @@ struct Row {
                     atomicAdd(&s.bins[BINS + place(bin)], (unsigned)(fminf(at - (float)bin, 1.f) * REST));
                 }
             }
-        }
+        });
         __syncthreads();
     }
     // The bins where a count (top_k > 0), or a weight, is reached: the latter (HALF) exactly, or between cut[0] and cut[1] if all is well.
@@ -384,9 +416,7 @@ struct Row {
     __device__ __forceinline__ unsigned collect(int first, int last, bool weigh, u64 (&sums)[3]) const
     {
         u64 mine[3] = {0, 0, 0};
-        for (int v = threadIdx.x; v < pieces(); v += SP_THREADS) {
-            float z[PER];
-            const int i0 = piece(v, z);
+        walk_all([&](const float (&z)[PER], int i0) {
             int bin[PER];
             bool any = weigh;
 #pragma unroll
@@ -394,7 +424,7 @@ struct Row {
                 bin[j] = z[j] > -INFINITY ? bin_of(z[j]) : BINS;
                 any |= bin[j] >= first && bin[j] <= last;
             }
-            if (!any) continue;
+            if (!any) return;
             // (four weights side by side, for the latency of binary64)
 #pragma unroll
             for (int j0 = 0; j0 < PER; j0 += 4) {
@@ -417,7 +447,7 @@ struct Row {
                     }
                 }
             }
-        }
+        });
         if (weigh) {
             const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -561,24 +591,23 @@ struct Row {
     }
 
     // Of all elements in order of index, each with a share, the one at which the sum of shares exceeds mark(sum of all): found(its place in
-    // this block, its logit, the sum of all), by one thread of one block.  shares(z, i, q): those of a piece's elements, whether any has one.
+    // this block, its logit, the sum of all), by one thread of one block.  shares(z, i, q): those of a piece's elements, whether any has one;
+    // none below `least` has.
     // A warp's elements are consecutive; the warp whose they are is then looked at by the whole block.
     template <class Shares, class Share, class Mark, class Found>
-    __device__ __forceinline__ void in_order(const Shares &shares, const Share &share, const Mark &mark, const Found &found) const
+    __device__ __forceinline__ void in_order(float least, const Shares &shares, const Share &share, const Mark &mark, const Found &found) const
     {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         // (the first warp also has what is in front of the first whole piece, the last one what is behind the last)
         const int each = (vectors + SP_WARPS - 1) / SP_WARPS, v0 = min(vectors, warp * each), v1 = min(vectors, v0 + each);
         u64 sum = 0;
-        for (int v = v0 + lane; v < v1; v += 32) {
-            float z[PER];
+        walk(v0 + lane, v1, 32, [&](const float (&z)[PER], int i) {
             u64 q[PER];
-            const int i = piece(v, z);
             if (shares(z, i, q)) {
 #pragma unroll
                 for (int j = 0; j < PER; ++j) sum += q[j];
             }
-        }
+        }, least);
         if (lane == 0 && (warp == 0 || warp == SP_WARPS - 1)) {
             for (int i = warp ? head + vectors * PER : 0; i < (warp ? n : head); ++i) sum += share(value(i), i);
         }
@@ -611,7 +640,7 @@ struct Row {
     __device__ __forceinline__ void among_ties(float tie, u64 nth) const
     {
         in_order(
-            [&](const float (&z)[PER], int, u64 (&q)[PER]) {
+            tie, [&](const float (&z)[PER], int, u64 (&q)[PER]) {
 #pragma unroll
                 for (int j = 0; j < PER; ++j) q[j] = z[j] == tie;
                 return true;
@@ -867,32 +896,36 @@ sample_kernel(const SampleParams p)
     // the block's part of the row, at the same place within 16 bytes as in global memory
     const T *from = static_cast<const T *>(p.logits) + (size_t)row * p.pitch + begin;
     const int skew = (int)(((uintptr_t)from & 15) / sizeof(T));
-    T *items = reinterpret_cast<T *>(sp_smem_raw + sizeof(SampleSmem)) + skew;
+    T *copy = reinterpret_cast<T *>(sp_smem_raw + sizeof(SampleSmem)) + skew;
+    const T *items = p.resident ? copy : from;
     const int head = min(n, (PER - skew) % PER), vectors = (n - head) / PER;
-    // (on the way: the largest logit, and the lowest one that is open)
-    float top = -INFINITY, low = INFINITY;
+    // (on the way: the largest logit, and binary32's lowest one that is open)
+    float top = -INFINITY, low = sizeof(T) == 2 ? -3.402823466e38f : INFINITY;
+    unsigned tops = 0xff80ff80u;
     const auto look = [&](float z) {
         top = fmaxf(top, z);                    // (NaN is not taken)
         low = fminf(low, z > -INFINITY ? z : INFINITY);
     };
     {
         const uint4 *v = reinterpret_cast<const uint4 *>(from + head);
-        uint4 *to = reinterpret_cast<uint4 *>(items + head);
+        uint4 *to = reinterpret_cast<uint4 *>(copy + head);
         constexpr int U = 4;
         for (int i = tid; i < vectors; i += U * SP_THREADS) {
             uint4 a[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (i + u * SP_THREADS < vectors) a[u] = __ldcs(v + i + u * SP_THREADS);
+                if (i + u * SP_THREADS < vectors) a[u] = __ldcg(v + i + u * SP_THREADS);
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (i + u * SP_THREADS < vectors) {
-                    to[i + u * SP_THREADS] = a[u];
-                    const unsigned w[4] = {a[u].x, a[u].y, a[u].z, a[u].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (sizeof(T) == 2) look(__uint_as_float(w[j] << 16) + 0.f);
-                        look(__uint_as_float(sizeof(T) == 2 ? w[j] & 0xffff0000u : w[j]) + 0.f);
+                    if (p.resident) to[i + u * SP_THREADS] = a[u];
+                    if (sizeof(T) == 2) {
+                        tops = max2(tops, max2(max2(a[u].x, a[u].y), max2(a[u].z, a[u].w)));
+                    } else {
+                        look(__uint_as_float(a[u].x));
+                        look(__uint_as_float(a[u].y));
+                        look(__uint_as_float(a[u].z));
+                        look(__uint_as_float(a[u].w));
                     }
                 }
         }
@@ -900,10 +933,12 @@ sample_kernel(const SampleParams p)
         for (int i = tid; i < head + n - done; i += SP_THREADS) {
             const int at = i < head ? i : done + i - head;
             const T one = from[at];
-            items[at] = one;
+            if (p.resident) copy[at] = one;
             look(item_value(&one, 0));
         }
     }
+    if (sizeof(T) == 2) top = fmaxf(top, larger(tops));
+    top += 0.f;                                 // (-0 is 0)
     dip_launch_dependents();
     const float temperature = p.temperature ? p.temperature[row] : 1.f;
     const int top_k = p.top_k ? p.top_k[row] : 0;
@@ -1065,7 +1100,7 @@ sample_kernel(const SampleParams p)
     const auto drawn = [&](float z, int i) -> u64 { return open(z, i) && !(min_p > 0.f && r.weight(z) < least) ? mass_of(z) : 0; };
     constexpr int PIECE = Row<T>::PER;
     r.in_order(
-        [&](const float (&z)[PIECE], int i, u64 (&q)[PIECE]) {
+        border.z, [&](const float (&z)[PIECE], int i, u64 (&q)[PIECE]) {
             bool any = false;
 #pragma unroll
             for (int j = 0; j < PIECE; ++j) any |= open(z[j], i + j);
@@ -1093,7 +1128,7 @@ template <typename T>
 cudaError_t launch(dip_ctx *ctx, int rows, int blocks, cudaStream_t stream, const SampleParams &p)
 {
     static dip_per_device_once once;
-    const size_t smem = sizeof(SampleSmem) + ((size_t)p.slice * sizeof(T) + 31) / 16 * 16;
+    const size_t smem = sizeof(SampleSmem) + (p.resident ? ((size_t)p.slice * sizeof(T) + 31) / 16 * 16 : 0);
     cudaError_t e = dip_raise_smem_limit(once, ctx->device, sample_kernel<T>, 227 * 1024);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -1148,16 +1183,17 @@ extern "C" dip_status dip_sample_tokens(dip_ctx *ctx, const void *logits, int lo
     if (!apart({{token, each}, {prob, each}}, {{logits, ((size_t)(n_rows - 1) * pitch + vocab) * item}, {how->temperature, each}, {how->top_k, each},
                                                {how->top_p, each}, {how->min_p, each}, {uniform, each}}))
         return DIP_ERR_INVALID_ARG;
-    // As many blocks per row as its items need (two blocks share an SM), and more where SMs are idle.
-    const size_t room = 110 * 1024 - sizeof(SampleSmem) - 64;
+    // As many blocks per row as find room (two per SM).  Their parts of the rows stay in shared memory if they fit beside what else is there, and
+    // are read again, out of L2, if not.
     int blocks = 1;
-    while (blocks < SP_CLUSTER && ((size_t)vocab * item > room * blocks || ((long long)n_rows * blocks * 2 <= ctx->sm_count && vocab > 2048 * blocks)))
-        blocks *= 2;
+    while (blocks < SP_CLUSTER && n_rows * blocks * 2 <= 2 * ctx->sm_count && vocab > 2048 * blocks) blocks *= 2;
+    const int slice = ((vocab + blocks - 1) / blocks + 31) & ~31;
     SampleParams p = {};
     p.logits = logits;
     p.pitch = (size_t)pitch;
     p.vocab = vocab;
-    p.slice = ((vocab + blocks - 1) / blocks + 31) & ~31;
+    p.slice = slice;
+    p.resident = (size_t)slice * item + 64 + sizeof(SampleSmem) <= (n_rows * blocks <= ctx->sm_count ? 220 : 112) * 1024;
     p.temperature = how->temperature;
     p.top_k = how->top_k;
     p.top_p = how->top_p;
