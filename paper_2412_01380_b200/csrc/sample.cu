@@ -79,7 +79,7 @@ struct __align__(16) SampleSmem {
     u64 tiny[2];
     u64 scan[SP_WARPS + 1];
     // what the blocks of a cluster tell one another
-    u64 total[SP_CLUSTER], sums[3], part[3][SP_WARPS];
+    u64 total[SP_CLUSTER], sums[3], part[3][SP_WARPS], of_all;
     float top, low;
     int first[SP_CLUSTER];
     unsigned key_lo[SP_CLUSTER], key_hi[SP_CLUSTER];
@@ -593,48 +593,54 @@ struct Row {
     // Of all elements in order of index, each with a share, the one at which the sum of shares exceeds mark(sum of all): found(its place in
     // this block, its logit, the sum of all), by one thread of one block.  shares(z, i, q): those of a piece's elements, whether any has one;
     // none below `least` has.
-    // A warp's elements are consecutive; the warp whose they are is then looked at by the whole block.
+    // A warp's elements are consecutive; those of the warp that has it are shared out among the warps in turn, until there is one for each thread.
     template <class Shares, class Share, class Mark, class Found>
     __device__ __forceinline__ void in_order(float least, const Shares &shares, const Share &share, const Mark &mark, const Found &found) const
     {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        // (the first warp also has what is in front of the first whole piece, the last one what is behind the last)
-        const int each = (vectors + SP_WARPS - 1) / SP_WARPS, v0 = min(vectors, warp * each), v1 = min(vectors, v0 + each);
-        u64 sum = 0;
-        walk(v0 + lane, v1, 32, [&](const float (&z)[PER], int i) {
-            u64 q[PER];
-            if (shares(z, i, q)) {
+        int p0 = 0, p1 = vectors;               // pieces
+        bool front = true, back = true;         // with what is in front of the first one, behind the last one
+        u64 at = 0, want = 0;
+        for (bool first = true;; first = false) {
+            const int each = (p1 - p0 + SP_WARPS - 1) / SP_WARPS, v0 = min(p1, p0 + warp * each), v1 = min(p1, v0 + each);
+            u64 sum = 0;
+            walk(v0 + lane, v1, 32, [&](const float (&z)[PER], int i) {
+                u64 q[PER];
+                if (shares(z, i, q)) {
 #pragma unroll
-                for (int j = 0; j < PER; ++j) sum += q[j];
+                    for (int j = 0; j < PER; ++j) sum += q[j];
+                }
+            }, least);
+            if (warp == 0 && front && lane < head) sum += share(value(lane), lane);
+            const int behind = head + vectors * PER + lane;
+            if (warp == SP_WARPS - 1 && back && behind < n) sum += share(value(behind), behind);
+#pragma unroll
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            __syncthreads();
+            if (lane == 0) s.part[0][warp] = sum;
+            __syncthreads();
+            if (first) {
+                u64 block_sum = 0, all;
+                for (int w = 0; w < SP_WARPS; ++w) block_sum += s.part[0][w];
+                at = gather(block_sum, all);
+                want = mark(all);
+                if (!(at <= want && want < at + block_sum)) return;
+                s.of_all = all;
             }
-        }, least);
-        if (lane == 0 && (warp == 0 || warp == SP_WARPS - 1)) {
-            for (int i = warp ? head + vectors * PER : 0; i < (warp ? n : head); ++i) sum += share(value(i), i);
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        __syncthreads();
-        if (lane == 0) s.part[0][warp] = sum;
-        __syncthreads();
-        u64 block_sum = 0, all;
-        for (int w = 0; w < SP_WARPS; ++w) block_sum += s.part[0][w];
-        const u64 before = gather(block_sum, all), want = mark(all);
-        if (before <= want && want < before + block_sum) {
-            u64 at = before;
             int w = 0;
-            for (; at + s.part[0][w] <= want; ++w) at += s.part[0][w];
-            const int j0 = w == 0 ? 0 : head + min(vectors, w * each) * PER;
-            const int j1 = w == SP_WARPS - 1 ? n : head + min(vectors, (w + 1) * each) * PER, part = (j1 - j0 + SP_THREADS - 1) / SP_THREADS;
-            const int k0 = min(j1, j0 + (int)threadIdx.x * part), k1 = min(j1, k0 + part);
-            u64 mine = 0, ignored;
-            for (int i = k0; i < k1; ++i) mine += share(value(i), i);
-            at += scan(mine, ignored);
-            if (at <= want && want < at + mine) {
-                int i = k0;
-                for (u64 q; at + (q = share(value(i), i)) <= want; ++i) at += q;
-                found(i, value(i), all);
-            }
+            for (; w < SP_WARPS - 1 && at + s.part[0][w] <= want; ++w) at += s.part[0][w];
+            p0 = min(p1, p0 + w * each);
+            p1 = min(p1, p0 + each);
+            front &= w == 0;
+            back &= w == SP_WARPS - 1;
+            if ((p1 - p0 + 2) * PER <= SP_THREADS) break;
         }
+        const int i = (front ? 0 : head + p0 * PER) + threadIdx.x, end = back ? n : head + p1 * PER;
+        const float z = i < end ? value(i) : -INFINITY;
+        const u64 q = i < end ? share(z, i) : 0;
+        u64 ignored;
+        const u64 b = at + scan(q, ignored);
+        if (b <= want && want < b + q) found(i, z, s.of_all);
     }
     // The border is the nth (from 1) in order of index among the elements of that logit.
     __device__ __forceinline__ void among_ties(float tie, u64 nth) const
@@ -1088,29 +1094,34 @@ sample_kernel(const SampleParams p)
         for (int i = tid; i < known; i += SP_THREADS) s.bin_mass[i] = r.mass(r.value_of(top_bin + i));
         __syncthreads();
     }
+    // (what min_p leaves, too, is the front of the order; only within a hair of its end does it take the weight itself to tell)
     const double least = fmin((double)min_p, 1.0) * (double)(1ull << SP_ONE_BITS);
-    const auto open = [&](float z, int i) { return r.kept(z, i, border); };
-    const auto mass_of = [&](float z) -> u64 {
-        if (Row<T>::HALF) {
-            const int bin = r.bin_of(z) - top_bin;
-            if (bin < known && !r.mixed(bin + top_bin)) return s.bin_mass[bin];
-        }
-        return r.mass(z);
+    const float cut = min_p > 0.f ? temperature * logf(fminf(min_p, 1.f)) : -INFINITY, hair = 1e-4f * -cut + 1e-5f * fabsf(top);
+    const float sure = min_p > 0.f ? top + cut + hair : -INFINITY, doubtful = min_p > 0.f ? top + cut - hair : -INFINITY;
+    const auto left = [&](float z, int i) {
+        return r.kept(z, i, border) && (z >= sure || z == top || (z >= doubtful && !(r.weight(z) < least)));
     };
-    const auto drawn = [&](float z, int i) -> u64 { return open(z, i) && !(min_p > 0.f && r.weight(z) < least) ? mass_of(z) : 0; };
+    const auto drawn = [&](float z, int i) -> u64 { return left(z, i) ? r.mass(z) : 0; };
     constexpr int PIECE = Row<T>::PER;
     r.in_order(
         border.z, [&](const float (&z)[PIECE], int i, u64 (&q)[PIECE]) {
-            bool any = false;
+            bool in[PIECE], any = false, unknown = !Row<T>::HALF;
 #pragma unroll
-            for (int j = 0; j < PIECE; ++j) any |= open(z[j], i + j);
+            for (int j = 0; j < PIECE; ++j) any |= in[j] = left(z[j], i + j);
             if (!any) return false;
+            if (Row<T>::HALF) {
 #pragma unroll
-            for (int j = 0; j < PIECE; ++j) q[j] = Row<T>::HALF ? drawn(z[j], i + j) : r.mass(z[j]);
-            if (!Row<T>::HALF) {
+                for (int j = 0; j < PIECE; ++j) {
+                    const int bin = r.bin_of(z[j]), at = bin - top_bin;
+                    unknown |= in[j] && (at >= known || r.mixed(bin));
+                    q[j] = in[j] && at < known ? s.bin_mass[at] : 0;
+                }
+            }
+            if (unknown) {
 #pragma unroll
-                for (int j = 0; j < PIECE; ++j)
-                    if (!open(z[j], i + j) || (min_p > 0.f && r.weight(z[j]) < least)) q[j] = 0;
+                for (int j = 0; j < PIECE; ++j) q[j] = r.mass(z[j]);
+#pragma unroll
+                for (int j = 0; j < PIECE; ++j) q[j] = in[j] ? q[j] : 0;
             }
             return true;
         },
