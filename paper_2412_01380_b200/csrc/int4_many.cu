@@ -10,7 +10,8 @@
 //     rows need the room to be read twice, once per half (128 columns by 256 outputs: 32 + 16 KB in and 64 + 16 KB read per group of
 //     1024 cycles of MMAs; the other way round, 256 rows by 128 outputs, more than L2 gives an SM).
 //   warp 0       issues the copies: a ring of groups (rows, codes)
-//   warp 1       issues the MMAs: one group of one half into one of three accumulators of 128 columns
+//   warps 1, 2   issue the MMAs, a half each: a group into one of three accumulators of 128 columns.  (Waits, issue and a commit take a warp some 600
+//                cycles, more than the MMAs; one commit tells all who wait for a half, since each takes 50 to 150.)
 //   warps 4-7    codes to bfloat16, one group of one half into one of two operand areas of tensor memory (64 columns each)
 //   warps 8-15   take the accumulators out; each four warps have half of the rows
 // Tiles are dealt out, cut along K and joined as those of the other types are (grouped_common.cuh).
@@ -45,10 +46,12 @@ template <bool GATED_> struct ManyKind {
 struct __align__(1024) ManySmem {
     unsigned char x[IM_STAGES][2][IM_X_BYTES / 2];      // 64 inputs each
     unsigned char codes[IM_STAGES][2][IM_CODE_BYTES / 2];
-    uint64_t full[IM_STAGES], empty[IM_STAGES];     // a group's copies have landed; its MMAs have read them
-    uint64_t operand_full[2], operand_empty[2];
-    uint64_t sum_full[IM_SUMS], sum_empty[IM_SUMS];
-    uint64_t drained;
+    __half scales[2 * IM_STAGES][2][IM_HALF];       // (twice the stages: the sums are taken out up to three halves behind the MMAs that free a stage)
+    uint64_t full[IM_STAGES], scales_full[2 * IM_STAGES];    // a group's copies have landed
+    uint64_t operand_full[2];
+    uint64_t done[IM_STAGES][2];                    // a half's MMAs are through: its sums may be taken out, its operand and its copies replaced
+    uint64_t sum_empty[IM_SUMS];
+    uint64_t drained[2];
     uint32_t tmem_base;
     int last;
     int fail, peer_fail;
@@ -67,6 +70,13 @@ __device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[32])
                  : "memory");
 }
 
+// Neighbouring bytes (whole pieces of 16) to shared memory.
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, unsigned bytes, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+
 // D += A B with A in tensor memory.
 __device__ __forceinline__ void many_mma(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t shape, uint32_t accumulate)
 {
@@ -83,32 +93,25 @@ __device__ __forceinline__ void put(void *out, size_t at, float v, int out_f32)
 
 template <class K>
 __device__ __forceinline__ void many_take(const GroupedParams &p, ManySmem &s, const Schedule<K> &plan, const Run &r, uint32_t lanes, int share,
-                                          int place, int &buf, unsigned &phase)
+                                          int place, int &buf, int &g)
 {
     constexpr bool GATED = K::GATED;
     constexpr int N = GP_ROWS / 2, L = 16;           // rows of a thread, at most; columns that are loaded together
     const int lane = threadIdx.x & 31, per = (r.rows + 15) / 16 * 8, t0 = share * per, rows = min(per, r.rows - t0);      // (may be none)
     const int o = r.out0 + place;                    // gate/up: of both; plain: the second one's is IM_HALF further on
-    const __half *scales0 = static_cast<const __half *>(static_cast<const void *>(p.w_scales)), *scales1 = scales0;
-    if (GATED) scales1 = static_cast<const __half *>(static_cast<const void *>(p.up_scales));
-    const size_t first = ((size_t)r.expert * p.steps + r.k0) * p.d_out;
-    scales0 += first + min(o, p.d_out - 1);
-    scales1 += first + min(GATED ? o : o + IM_HALF, p.d_out - 1);
     float acc[2][N];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < N; ++j) acc[h][j] = 0.f;
-    __half next0 = *scales0, next1 = *scales1;
-    for (int k = r.k0; k < r.k1; ++k) {
-        const float s0 = __half2float(next0) * INT4_PRODUCT, s1 = __half2float(next1) * INT4_PRODUCT;
-        if (k + 1 < r.k1) {
-            next0 = *(scales0 += p.d_out);
-            next1 = *(scales1 += p.d_out);
-        }
+    for (int k = r.k0; k < r.k1; ++k, ++g) {
+        const int st = g % IM_STAGES, slot = g % (2 * IM_STAGES);
+        const unsigned through = (g / IM_STAGES) & 1;
+        wait_on(smem_u32(&s.scales_full[slot]), (g / (2 * IM_STAGES)) & 1, s, p.status, p.wait_limit_ns);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            wait_on(smem_u32(&s.sum_full[buf]), phase, s, p.status, p.wait_limit_ns);
+            const float scale = __half2float(s.scales[slot][h][place]) * INT4_PRODUCT;
+            wait_on(smem_u32(&s.done[st][h]), through, s, p.status, p.wait_limit_ns);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t from = lanes + buf * GP_ROWS + t0;
             // one load is under way while the one in front is added
@@ -120,13 +123,12 @@ __device__ __forceinline__ void many_take(const GroupedParams &p, ManySmem &s, c
                     tmem_wait(v[c & 1]);
                     if (L * (c + 1) < per) tmem_ld(from + L * (c + 1), v[(c + 1) & 1]);
 #pragma unroll
-                    for (int j = 0; j < L; j += 2) fma2(acc[h][L * c + j], acc[h][L * c + j + 1], v[c & 1][j], v[c & 1][j + 1], h ? s1 : s0);
+                    for (int j = 0; j < L; j += 2) fma2(acc[h][L * c + j], acc[h][L * c + j + 1], v[c & 1][j], v[c & 1][j + 1], scale);
                 }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             arrive_first<false>(smem_u32(&s.sum_empty[buf]), lane);
             buf = buf == IM_SUMS - 1 ? 0 : buf + 1;
-            phase ^= buf == 0;
         }
     }
 
@@ -188,17 +190,16 @@ int4_many_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_cons
     if (tid == 0) {
         for (int i = 0; i < IM_STAGES; ++i) {
             mbar_init(&s.full[i], 1);
-            mbar_init(&s.empty[i], 1);
+            mbar_init(&s.scales_full[2 * i], 1);
+            mbar_init(&s.scales_full[2 * i + 1], 1);
+            mbar_init(&s.done[i][0], 1);
+            mbar_init(&s.done[i][1], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.operand_full[i], 4);
-            mbar_init(&s.operand_empty[i], 1);
+            mbar_init(&s.drained[i], 1);
         }
-        for (int i = 0; i < IM_SUMS; ++i) {
-            mbar_init(&s.sum_full[i], 1);
-            mbar_init(&s.sum_empty[i], K::OUT_WARPS);
-        }
-        mbar_init(&s.drained, 1);
+        for (int i = 0; i < IM_SUMS; ++i) mbar_init(&s.sum_empty[i], K::OUT_WARPS);
         s.fail = s.peer_fail = s.issued = 0;
         asm volatile("prefetch.tensormap [%0];" ::"l"(&rows_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&w_map) : "memory");
@@ -230,15 +231,25 @@ int4_many_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_cons
             int g = 0;                               // groups so far
             for (int i = 0; !failed && plan.get(i, r); ++i) {
                 const int boxes = (r.rows + IM_BOX - 1) / IM_BOX, w_row = r.expert * p.d_out + r.out0;
+                // scales of the halves' outputs that there are
+                const unsigned some0 = min(IM_HALF, p.d_out - r.out0) * 2, some1 = GATED ? some0 : max(0, min(IM_HALF, p.d_out - r.out0 - IM_HALF)) * 2;
                 const unsigned bytes = IM_CODE_BYTES + boxes * IM_BOX * DIP_INT4_GROUP * 2;
-                for (int k = r.k0; k < r.k1; ++k, ++g) {
+                const __half *scales = static_cast<const __half *>(static_cast<const void *>(p.w_scales)), *scales1 = scales + IM_HALF;
+                if (GATED) scales1 = static_cast<const __half *>(static_cast<const void *>(p.up_scales));
+                size_t from = ((size_t)r.expert * p.steps + r.k0) * p.d_out + r.out0;
+                for (int k = r.k0; k < r.k1; ++k, ++g, from += p.d_out) {
                     const int st = g % IM_STAGES;
-                    if (g >= IM_STAGES && !warp_wait(&s.empty[st], (g / IM_STAGES - 1) & 1, p.wait_limit_ns)) {
+                    if (g >= IM_STAGES && (!warp_wait(&s.done[st][0], (g / IM_STAGES - 1) & 1, p.wait_limit_ns) ||
+                                           !warp_wait(&s.done[st][1], (g / IM_STAGES - 1) & 1, p.wait_limit_ns))) {
                         failed = true;
                         break;
                     }
                     if (elect_one()) {
                         mbar_expect_tx(&s.full[st], bytes);
+                        const int slot = g % (2 * IM_STAGES);
+                        mbar_expect_tx(&s.scales_full[slot], some0 + some1);
+                        bulk_load(s.scales[slot][0], scales + from, some0, &s.scales_full[slot]);
+                        if (some1) bulk_load(s.scales[slot][1], scales1 + from, some1, &s.scales_full[slot]);
                         tma_load<false>(s.codes[st][0], &w_map, k * (DIP_INT4_GROUP / 2), w_row, &s.full[st]);
                         tma_load<false>(s.codes[st][1], &w2_map, k * (DIP_INT4_GROUP / 2), GATED ? w_row : w_row + IM_HALF, &s.full[st]);
                         for (int b = 0; b < boxes; ++b) {
@@ -250,38 +261,36 @@ int4_many_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_cons
                 }
             }
             if (lane == 0) s.issued = g;
-        } else if (warp == 1) {
+        } else if (warp <= 2) {
+            const int h = warp - 1;
+            const uint32_t a = tmem + IM_OPERAND + h * IM_OPERAND_COLS;
+            const bool elected = elect_one();
             Run r;
-            int g = 0, n = 0, buf = 0;               // groups, halves of them so far; the next accumulator
-            unsigned phase = 1;                      // (of the accumulator's last release: the first three need none)
+            int g = 0, buf = h;                      // groups so far; the next accumulator: halves take them in turn
+            unsigned phase = 1;                      // of its last release (the first three need none)
             for (int i = 0; !failed && plan.get(i, r); ++i) {
                 const uint32_t shape = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)((r.rows + 15) / 16 * 2) << 17) | (8u << 24);
-                for (int k = r.k0; k < r.k1 && !failed; ++k, ++g) {
+                for (int k = r.k0; k < r.k1; ++k, ++g) {
                     const int st = g % IM_STAGES;
-                    if (!warp_wait(&s.full[st], (g / IM_STAGES) & 1, p.copy_wait_ns)) {
+                    if ((2 * g + h >= IM_SUMS && !warp_wait(&s.sum_empty[buf], phase, p.wait_limit_ns)) ||
+                        !warp_wait(&s.full[st], (g / IM_STAGES) & 1, p.copy_wait_ns) || !warp_wait(&s.operand_full[h], g & 1, p.wait_limit_ns)) {
                         failed = true;
                         break;
                     }
-                    for (int h = 0; h < 2; ++h, ++n) {
-                        if ((n >= IM_SUMS && !warp_wait(&s.sum_empty[buf], phase, p.wait_limit_ns)) ||
-                            !warp_wait(&s.operand_full[h], g & 1, p.wait_limit_ns)) {
-                            failed = true;
-                            break;
-                        }
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint64_t b0 = operand_desc(s.x[st][0]), b1 = operand_desc(s.x[st][1]);
-                        const uint32_t to = tmem + buf * GP_ROWS, a = tmem + IM_OPERAND + h * IM_OPERAND_COLS;
-                        if (elect_one()) {
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t b0 = operand_desc(s.x[st][0]), b1 = operand_desc(s.x[st][1]);
+                    const uint32_t to = tmem + buf * GP_ROWS;
+                    if (elected) {
 #pragma unroll
-                            for (int q = 0; q < 8; ++q)          // 16 inputs each
-                                many_mma(to, a + 8 * q, (q < 4 ? b0 : b1) + 2 * (q & 3), shape, q ? 1u : 0u);
-                            grouped_commit<false>(&s.operand_empty[h]);
-                            grouped_commit<false>(&s.sum_full[buf]);
-                            if (h) grouped_commit<false>(&s.empty[st]);
-                        }
-                        __syncwarp();
-                        buf = buf == IM_SUMS - 1 ? 0 : buf + 1;
-                        phase ^= buf == 0;
+                        for (int q = 0; q < 8; ++q)              // 16 inputs each
+                            many_mma(to, a + 8 * q, (q < 4 ? b0 : b1) + 2 * (q & 3), shape, q ? 1u : 0u);
+                        grouped_commit<false>(&s.done[st][h]);
+                    }
+                    __syncwarp();
+                    buf += 2;
+                    if (buf >= IM_SUMS) {
+                        buf -= IM_SUMS;
+                        phase ^= 1u;
                     }
                 }
             }
@@ -293,17 +302,27 @@ int4_many_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_cons
         // All roles are through.  Where any wait has run out, MMAs and copies may still be under way: they are waited for.
         roles_end<false, K::THREADS>(s, tid);
         if (gave_up<false>(s)) {
-            if (warp == 1) {
-                if (elect_one()) grouped_commit<false>(&s.drained);
+            if (warp == 1 || warp == 2) {
+                if (elect_one()) grouped_commit<false>(&s.drained[warp - 1]);
                 __syncwarp();
-                warp_wait(&s.drained, 0, p.wait_limit_ns);
+                warp_wait(&s.drained[warp - 1], 0, p.wait_limit_ns);
             }
-            if (warp == 0) drain_copies<IM_STAGES, false>(s.full, s.issued, 0, [](int) { return 0u; }, p.wait_limit_ns);
+            if (warp == 0) {
+                drain_copies<IM_STAGES, false>(s.full, s.issued, 0, [](int) { return 0u; }, p.wait_limit_ns);
+                drain_copies<2 * IM_STAGES, false>(s.scales_full, s.issued, 0, [](int) { return 0u; }, p.wait_limit_ns);
+            }
         }
     } else if (warp < 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(K::REGS_CODES));
         const int place = (warp & 3) * 32 + lane;    // lane of tensor memory
         const uint32_t to = tmem + ((uint32_t)((warp & 3) * 32) << 16) + IM_OPERAND;
+        // a half's stores are through: the MMAs may have it
+        const auto hand_over = [&](int h) {
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            arrive_first<false>(smem_u32(&s.operand_full[h]), lane);
+        };
         Run r;
         int g = 0;
         for (int i = 0; plan.get(i, r); ++i) {
@@ -312,8 +331,6 @@ int4_many_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_cons
                 wait_on(smem_u32(&s.full[st]), (g / IM_STAGES) & 1, s, p.status, p.wait_limit_ns);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    if (g >= 1) wait_on(smem_u32(&s.operand_empty[h]), (g - 1) & 1, s, p.status, p.wait_limit_ns);
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const unsigned char *row = s.codes[st][h] + place * (DIP_INT4_GROUP / 2);
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
@@ -327,13 +344,16 @@ int4_many_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_cons
                             int4_in_order(w.z, v + 16 * q + 8);
                             int4_in_order(w.w, v + 16 * q + 12);
                         }
+                        if (c == 0) {
+                            // (the half in front, whose stores have had the time of this one's first)
+                            if (h == 1) hand_over(0);
+                            if (g >= 1) wait_on(smem_u32(&s.done[(g - 1) % IM_STAGES][h]), ((g - 1) / IM_STAGES) & 1, s, p.status, p.wait_limit_ns);
+                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        }
                         tmem_st(to + h * IM_OPERAND_COLS + 32 * c, v);
                     }
-                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    arrive_first<false>(smem_u32(&s.operand_full[h]), lane);
                 }
+                hand_over(1);
             }
         }
         roles_end<false, K::THREADS>(s, tid);
@@ -341,10 +361,9 @@ int4_many_kernel(const __grid_constant__ CUtensorMap rows_map, const __grid_cons
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(K::REGS_MANY));
         const int share = (warp - 8) >> 2, place = (warp & 3) * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        int buf = 0;
-        unsigned phase = 0;
+        int buf = 0, g = 0;                          // accumulator, groups so far
         Run r;
-        for (int i = 0; plan.get(i, r); ++i) many_take<K>(p, s, plan, r, lanes, share, place, buf, phase);
+        for (int i = 0; plan.get(i, r); ++i) many_take<K>(p, s, plan, r, lanes, share, place, buf, g);
         roles_end<false, K::THREADS>(s, tid);
     }
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
