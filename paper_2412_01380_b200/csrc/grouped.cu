@@ -25,6 +25,7 @@
 // parts meet in the partial sums' workspace; the block that comes last adds them up in order of K, so results do not
 // depend on who that is, and nobody waits.
 #include <cuda_bf16.h>
+#include <math.h>
 
 #include "common.cuh"
 #include "float8.cuh"
@@ -808,8 +809,17 @@ cudaError_t launch(int mode, dip_ctx *ctx, int ctas, cudaStream_t stream, const 
 // 1304 / 1255).  What this leaves out: 8-bit pairs were compared at 1024 rows only, and groups of unequal size not at all (an expert of 257 to
 // 384 rows fills half of its second pair tile, or less).
 constexpr int GP_FEW_UP_TO = 12, GP_PAIR_ROWS = 192;
-// 4-bit weights: few up to
-constexpr int GP_INT4_FEW_UP_TO = 16;
+// 4-bit weights: the kernel for few rows, or the one for many, whichever should be through first, rows taken to be spread evenly.  A block of the first goes
+// through 64 outputs by 128 inputs by 16 rows in 0.2 (one matrix) to 0.3 us (many small ones), a block of the second through 256 by 128 by 128 in 1.2,
+// behind 12 us more, and 8 where tiles have to be cut.  In us, few / many: one matrix of 5120 to 17920, 16 rows 22 / 40, 24 rows 36 / 41, 48 rows 51 / 43;
+// 2080 to 1056, 200 rows 12.9 / 40; 14336 to 4096, 24 rows 25 / 53; 4096 to 102400, 32 rows 144 / 121; 16 of 1056 to 2080, 32 rows each 26 / 22,
+// 50 rows 44 / 23; 64 of 1024 to 2816, 16 rows each 54 / 72, 24 rows 93 / 73.
+static bool int4_few(const dip_ctx *ctx, const dip_grouped_matrix &w, bool gated, int n_rows, int met)
+{
+    const double each = (n_rows + met - 1) / met, outs = (gated ? 2.0 : 1.0) * w.d_out, groups = (w.d_in + DIP_INT4_GROUP - 1) / DIP_INT4_GROUP;
+    const double few = met * ceil(each / 16) * ceil(outs / 64) * groups, tiles = met * ceil(each / GP_ROWS) * ceil(outs / GP_COLS);
+    return few * 0.25 <= tiles * groups * 1.2 + (tiles < ctx->sm_count ? 20.0 : 12.0) * ctx->sm_count;
+}
 
 dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const dip_grouped_matrix *up, const void *rows,
                               const float *row_scales, int n_rows, const int32_t *offset, void *out, bool out_f32, float *out_scales,
@@ -818,7 +828,7 @@ dip_status dip_launch_grouped(dip_ctx *ctx, const dip_grouped_matrix &w, const d
     const bool fp8 = w.wtype == DIP_W_FP8_B128;
     const int met = min(w.n_experts, n_rows);
     if (w.wtype == DIP_W_INT4_G128)
-        return (n_rows <= GP_INT4_FEW_UP_TO * met ? dip_launch_int4_few : dip_launch_int4_many)(ctx, w, up, rows, n_rows, offset, out, out_f32, stream);
+        return (int4_few(ctx, w, up != nullptr, n_rows, met) ? dip_launch_int4_few : dip_launch_int4_many)(ctx, w, up, rows, n_rows, offset, out, out_f32, stream);
     const int mode = n_rows <= GP_FEW_UP_TO * met ? GP_FEW_ROWS : n_rows >= GP_PAIR_ROWS * met && ctx->sm_count % 2 == 0 ? GP_PAIR : GP_WHOLE;
     const size_t w_rows = (size_t)w.n_experts * w.d_out;
     // the rows; half of a tile's weights; the other half (gate/up), or both at once

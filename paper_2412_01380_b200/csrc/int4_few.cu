@@ -6,8 +6,8 @@
 // Bound by the stream of codes, so what matters is that every SM has enough of it under way and that the ALUs, which turn codes into
 // bfloat16, keep up:
 //   * A unit is 64 outputs (gate/up: 32 of each) by one group: 4 KB of codes, 64 bytes of a row at a time.  Each warp has a ring of
-//     units that it fills with asynchronous copies of its own and waits for by itself; a lane reads back what it copied.  (Twelve warps: with
-//     eight the ALUs waited, with sixteen shared memory has no room for a second unit ahead.)
+//     units that it fills with asynchronous copies of its own and waits for by itself; a lane reads back what it copied.  (Twelve warps, or eight of
+//     more registers for 9 rows and more: with twelve 16 rows of 4096 to 102400 took 105 us instead of 77.)
 //   * A lane's 16 bytes of a row are 32 consecutive codes, and the sums of a group do not depend on the order of its inputs, so the four lanes
 //     of a quad simply take a quarter of the group each, and an MMA takes the codes that one AND brings out of a word, nibbles s and s + 4
 //     (int4_codes.cuh).  x is paired alike.
@@ -24,7 +24,8 @@
 
 namespace {
 
-constexpr int IF_WARPS = 12, IF_THREADS = IF_WARPS * 32;
+template <int NT> constexpr int IF_WARPS = NT == 1 ? 12 : 8;
+template <int NT> constexpr int IF_THREADS = IF_WARPS<NT> * 32;
 constexpr int IF_OUTS = 64;                 // outputs of a tile (gate/up: as many sums, of half as many outputs)
 constexpr int IF_PITCH = IF_OUTS + 4;       // floats of a row of partial sums in shared memory (conflict-free)
 constexpr int IF_STAGES = 3;                // units of a warp that are under way or in hand
@@ -57,8 +58,8 @@ struct FewTile {
 
 template <int NT> struct __align__(16) FewSmem {
     static constexpr int TILES = NT == 1 ? 20 : 4;      // that a block has in hand at a time (what there is room for)
-    FewStage ring[IF_WARPS][IF_STAGES];
-    float part[IF_WARPS + TILES][8 * NT][IF_PITCH];
+    FewStage ring[IF_WARPS<NT>][IF_STAGES];
+    float part[IF_WARPS<NT> + TILES][8 * NT][IF_PITCH];
     FewTile tile[TILES];
     int start[DIP_MAX_EXPERTS + 1];         // first row of each expert
     int tiles[DIP_MAX_EXPERTS + 1];         // tiles in front of it
@@ -135,9 +136,9 @@ __device__ __forceinline__ int run_of(int n, int parts, int unit)
     return unit < of_these ? unit / (each + 1) : longer + (unit - of_these) / each;
 }
 
-// (32 bits hold all numbers of units: launches have at most 16 rows per expert that can have any, so 2^13 in all)
+// (32 bits hold all numbers of units: at most 16 rows for each expert, 2^13 in all, or more where there is little to do)
 template <bool GATED, int NT>
-__global__ void __launch_bounds__(IF_THREADS, 1)
+__global__ void __launch_bounds__(IF_THREADS<NT>, 1)
 int4_few_kernel(const FewParams p)
 {
     extern __shared__ unsigned char if_smem_raw[];
@@ -163,7 +164,7 @@ int4_few_kernel(const FewParams p)
 
     while (u0 < u1) {
         // the next tiles
-        const int t0 = u0 / G, t1 = min(t0 + Smem::TILES, (u1 + G - 1) / G), end = min(u1, t1 * G), n = end - u0, warps = min(IF_WARPS, n);
+        const int t0 = u0 / G, t1 = min(t0 + Smem::TILES, (u1 + G - 1) / G), end = min(u1, t1 * G), n = end - u0, warps = min(IF_WARPS<NT>, n);
         if (tid < t1 - t0) {
             const int tile = t0 + tid;
             int lo = 0, hi = p.n_experts;   // the expert with tiles[e] <= tile < tiles[e + 1]
@@ -295,7 +296,7 @@ int4_few_kernel(const FewParams p)
                     load_x();
                 }
                 // (IL sums of 16 outputs side by side: MMAs that wait for one another take 20 cycles each)
-                constexpr int IL = 2;
+                constexpr int IL = 4;
 #pragma unroll
                 for (int i0 = 0; i0 < 4; i0 += IL) {
                     uint4 q[2 * IL];
@@ -369,7 +370,7 @@ int4_few_kernel(const FewParams p)
             }
         };
         // (whole warps: PER_TILE and the number of threads are multiples of 32)
-        for (int i = tid; i < (t1 - t0) * PER_TILE; i += IF_THREADS) {
+        for (int i = tid; i < (t1 - t0) * PER_TILE; i += IF_THREADS<NT>) {
             const int k = i / PER_TILE, q = i % QUADS, r = i / QUADS % (8 * NT), c = GATED ? q / 2 * 4 + q % 2 * (IF_OUTS / 2) : q * 4;
             const FewTile t = s.tile[k];
             float4 v = {};
@@ -398,7 +399,7 @@ int4_few_kernel(const FewParams p)
             }
             __syncthreads();
             if (!s.last) continue;
-            for (int i = tid; i < PER_TILE; i += IF_THREADS) {
+            for (int i = tid; i < PER_TILE; i += IF_THREADS<NT>) {
                 const int q = i % QUADS, r = i / QUADS, c = GATED ? q / 2 * 4 + q % 2 * (IF_OUTS / 2) : q * 4;
                 float4 v = {};
                 if (r < t.rows) {
@@ -427,7 +428,7 @@ cudaError_t launch(dip_ctx *ctx, int ctas, cudaStream_t stream, const FewParams 
     static_assert(smem <= 227 * 1024, "fits a CTA's shared memory");
     const cudaError_t e = dip_raise_smem_limit(once, ctx->device, int4_few_kernel<GATED, NT>, smem);
     if (e != cudaSuccess) return e;
-    return dip_launch_pdl(int4_few_kernel<GATED, NT>, dim3(ctas), dim3(IF_THREADS), smem, stream, p);
+    return dip_launch_pdl(int4_few_kernel<GATED, NT>, dim3(ctas), dim3(IF_THREADS<NT>), smem, stream, p);
 }
 
 }  // namespace
@@ -457,7 +458,7 @@ dip_status dip_launch_int4_few(dip_ctx *ctx, const dip_grouped_matrix &w, const 
     p.partials = ctx->partials;
     p.tickets = ctx->group_tickets;
     p.tr = dip_trace_slot(ctx, up ? 10 : 11);
-    const bool wide = n_rows > 8 * met;
+    const bool wide = n_rows > 8 * met;         // (9 rows and more at a time take as long as 16)
     const long long most = ((long long)(n_rows + 7) / 8 + met) * p.n_cols * p.groups;
     const int ctas = (int)min((long long)ctx->sm_count, most);
     DIP_CUDA_TRY(ctx, up ? (wide ? launch<true, 2>(ctx, ctas, stream, p) : launch<true, 1>(ctx, ctas, stream, p))
