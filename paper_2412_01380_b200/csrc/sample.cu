@@ -27,6 +27,7 @@ constexpr int SP_CLUSTER = 8;                   // most blocks per row
 constexpr int SP_BINS = 2048;                   // of a histogram of weights
 constexpr int SP_PAIRS = 512;                   // elements that are compared pair by pair
 constexpr int SP_LIST = 2048;                   // elements that one block looks after
+constexpr int SP_FEW = SP_THREADS / 4;          // of them, that are compared with one another
 constexpr int SP_REACH = SP_THREADS;            // bins by which it does
 constexpr int SP_TABLE = 512;                   // 2^(j / 512)
 constexpr int SP_ONE_BITS = 45;                 // the largest weight is 2^45
@@ -554,6 +555,65 @@ struct Row {
     // (no number of an element down to logit z is above)
     __device__ __forceinline__ u64 last_number(float z) const { return ((u64)(key_of(top) - key_of(z)) << 18) | 0x3ffffu; }
 
+    // The sum over the block's threads.
+    __device__ __forceinline__ u64 block_sum(u64 v) const
+    {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) s.scan[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = s.scan[threadIdx.x & (SP_WARPS - 1)];
+#pragma unroll
+        for (int o = SP_WARPS / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    }
+    // finish() for at most SP_FEW elements: everyone compared with everyone, by several threads each (searches by histograms, three of them, took 13000
+    // cycles for some fifty elements; this takes 4000).
+    __device__ __forceinline__ void finish_few(int m, int top_k, float top_p, float min_p, float u, u64 all, int32_t *token, float *prob) const
+    {
+        const int each = m <= SP_THREADS / 32 ? 32 : m <= SP_THREADS / 8 ? 8 : 4, e = threadIdx.x / each, part = threadIdx.x % each;
+        const bool there = e < m;
+        const unsigned key = there ? s.list.key[e] : 0u;
+        const int index = there ? s.list.index[e] : 0;
+        const u64 mass = there ? s.list.mass[e] : 0;
+        const auto together = [&](u64 v) {
+            for (int o = each / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            return v;
+        };
+        // what is in front in the row's order: how many, what weight
+        unsigned rank_of = 0;
+        u64 before = 0;
+#pragma unroll 8
+        for (int j = part; j < m; j += each) {
+            const unsigned k = s.list.key[j];
+            const bool first = k > key || (k == key & s.list.index[j] < index);
+            rank_of += first;
+            before += first ? s.list.mass[j] : 0;
+        }
+        rank_of = (unsigned)together(rank_of);
+        before = together(before);
+        bool left = there && (top_k == 0 || rank_of < (unsigned)top_k);
+        if (top_p < 1.f) {
+            if (top_k) all = block_sum(left && part == 0 ? mass : 0);
+            left &= before < max(1ull, (u64)ceil(fmax((double)top_p, 0.0) * (double)all));
+        }
+        const double weight_of = weight(value_of_key(key));
+        if (min_p > 0.f) left &= !(weight_of < fmin((double)min_p, 1.0) * (double)(1ull << SP_ONE_BITS));
+        const u64 sum = block_sum(left && part == 0 ? mass : 0), mark = min(sum - 1, (u64)(fmax((double)u, 0.0) * (double)sum));
+        // in order of index, of those that are left
+        if (there && part == 0 && !left) s.list.mass[e] = 0;
+        __syncthreads();
+        before = 0;
+#pragma unroll 8
+        for (int j = part; j < m; j += each) before += s.list.index[j] < index ? s.list.mass[j] : 0;
+        before = together(before);
+        if (left && part == 0 && before <= mark && mark < before + mass) {
+            *token = index;
+            if (prob) *prob = (float)(weight_of / (double)sum);
+        }
+    }
+
     // The first block has all that can be left in its list: everything else.  all: the weight that top_p is a share of (top_k > 0: of what
     // that leaves).
     __device__ __forceinline__ void finish(int m, int top_k, float top_p, float min_p, float u, u64 all, float lowest, int vocab, int32_t *token,
@@ -593,7 +653,7 @@ struct Row {
     // Of all elements in order of index, each with a share, the one at which the sum of shares exceeds mark(sum of all): found(its place in
     // this block, its logit, the sum of all), by one thread of one block.  shares(z, i, q): those of a piece's elements, whether any has one;
     // none below `least` has.
-    // A warp's elements are consecutive; those of the warp that has it are shared out among the warps in turn, until there is one for each thread.
+    // A warp's elements are consecutive; those of the warp that has it are shared out among the warps in turn, until there are few for each thread.
     template <class Shares, class Share, class Mark, class Found>
     __device__ __forceinline__ void in_order(float least, const Shares &shares, const Share &share, const Mark &mark, const Found &found) const
     {
@@ -633,14 +693,18 @@ struct Row {
             p1 = min(p1, p0 + each);
             front &= w == 0;
             back &= w == SP_WARPS - 1;
-            if ((p1 - p0 + 2) * PER <= SP_THREADS) break;
+            if ((p1 - p0 + 2) * PER <= 8 * SP_THREADS) break;
         }
-        const int i = (front ? 0 : head + p0 * PER) + threadIdx.x, end = back ? n : head + p1 * PER;
-        const float z = i < end ? value(i) : -INFINITY;
-        const u64 q = i < end ? share(z, i) : 0;
-        u64 ignored;
-        const u64 b = at + scan(q, ignored);
-        if (b <= want && want < b + q) found(i, z, s.of_all);
+        const int begin_at = front ? 0 : head + p0 * PER, end = back ? n : head + p1 * PER, each = (end - begin_at + SP_THREADS - 1) / SP_THREADS;
+        const int i0 = min(end, begin_at + (int)threadIdx.x * each), i1 = min(end, i0 + each);
+        u64 mine = 0, ignored;
+        for (int i = i0; i < i1; ++i) mine += share(value(i), i);
+        at += scan(mine, ignored);
+        if (at <= want && want < at + mine) {
+            int i = i0;
+            for (u64 q; at + (q = share(value(i), i)) <= want; ++i) at += q;
+            found(i, value(i), s.of_all);
+        }
     }
     // The border is the nth (from 1) in order of index among the elements of that logit.
     __device__ __forceinline__ void among_ties(float tie, u64 nth) const
@@ -1076,7 +1140,10 @@ sample_kernel(const SampleParams p)
         alone = listed <= SP_LIST;
     }
     if (alone) {
-        if (rank == 0) r.finish(listed, by_count ? top_k : 0, top_p, min_p, u, all_weight, low, p.vocab, p.token + row, p.prob ? p.prob + row : nullptr);
+        if (rank == 0 && listed <= SP_FEW)
+            r.finish_few(listed, by_count ? top_k : 0, top_p, min_p, u, all_weight, p.token + row, p.prob ? p.prob + row : nullptr);
+        else if (rank == 0)
+            r.finish(listed, by_count ? top_k : 0, top_p, min_p, u, all_weight, low, p.vocab, p.token + row, p.prob ? p.prob + row : nullptr);
         DIP_TRACE_MAX(p.tr, 2);
         return;
     }
