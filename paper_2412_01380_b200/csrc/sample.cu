@@ -199,9 +199,8 @@ struct Row {
             }
         }
     }
-    // f(logits of a piece, place of the first one) for the pieces first, first + step, ..., below last (all: of the block's threads), with the
-    // next one under way.
-    // (HALF: pieces without a logit from `least` up are passed over.)
+    // f(piece, place of its first logit) for the pieces first, first + step, ..., below last (all: of the block's threads), with the next one under
+    // way.  (HALF: pieces without a logit from `least` up are passed over.)
     template <class F>
     __device__ __forceinline__ void walk(int first, int last, int step, const F &f, float least = -INFINITY) const
     {
@@ -209,26 +208,25 @@ struct Row {
         uint4 a = first < last ? from[first] : make_uint4(0u, 0u, 0u, 0u);
         for (int v = first; v < last; v += step) {
             const uint4 next = v + step < last ? from[v + step] : a;
-            if (sizeof(T) == 2 && !(larger(max2(max2(a.x, a.y), max2(a.z, a.w))) >= least)) {
-                a = next;
-                continue;
-            }
-            float z[PER];
-            decode(a, z);
-            f(z, head + v * PER);
+            if (sizeof(T) == 4 || larger(max2(max2(a.x, a.y), max2(a.z, a.w))) >= least) f(a, head + v * PER);
             a = next;
         }
     }
+    // (what is in front of the first whole piece and behind the last one comes as a piece filled up with -infinity)
     template <class F>
     __device__ __forceinline__ void walk_all(const F &f) const
     {
         walk(threadIdx.x, vectors, SP_THREADS, f);
-        if (threadIdx.x < 2) {                  // (what is in front of the first whole piece, and behind the last one)
+        if (threadIdx.x < 2) {
             const int first = threadIdx.x ? head + vectors * PER : 0, last = threadIdx.x ? n : head;
-            float z[PER];
+            unsigned w[4] = {};
 #pragma unroll
-            for (int j = 0; j < PER; ++j) z[j] = first + j < last ? value(first + j) : -INFINITY;
-            f(z, first);
+            for (int j = 0; j < PER; ++j) {
+                const unsigned bits = __float_as_uint(first + j < last ? value(first + j) : -INFINITY);
+                if (sizeof(T) == 2) w[j >> 1] |= j & 1 ? bits & 0xffff0000u : bits >> 16;
+                else w[j] = bits;
+            }
+            f(make_uint4(w[0], w[1], w[2], w[3]), first);
         }
     }
 
@@ -284,17 +282,37 @@ struct Row {
         for (int i = threadIdx.x; i < 8192 / 4; i += SP_THREADS) reinterpret_cast<uint4 *>(s.bins)[i] = make_uint4(0u, 0u, 0u, 0u);
         if (threadIdx.x < 2) s.tiny[threadIdx.x] = 0;
         __syncthreads();
-        walk_all([&](const float (&z)[PER], int) {
+        walk_all([&](const uint4 &a, int) {
+            if (HALF) {
+                const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                if (!(z[j] > -INFINITY)) continue;
-                const int bin = bin_of(z[j]);
-                atomicAdd(&s.bins[place(bin)], 1u);
-                if (HALF) {
-                    if (middle(bin)) add64(&s.tiny[bin - 4095], mass(z[j]));
-                } else if (weights) {
-                    const float at = (top - z[j]) * scale * 2.f;
-                    atomicAdd(&s.bins[BINS + place(bin)], (unsigned)(fminf(at - (float)bin, 1.f) * REST));
+                for (int j = 0; j < 8; ++j) {
+                    const unsigned raw = j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu, size = raw & 0x7fffu;
+                    if (size - (HALF_FIRST + 1) < 0x7f80u - (HALF_FIRST + 1)) {
+                        const int m = min((int)size - HALF_FIRST, 4095), bin = 4096 + (m ^ ((int)(raw >> 15) - 1));
+                        atomicAdd(&s.bins[place(bin)], 1u);
+                    } else {
+                        // next to zero, infinite, or none
+                        const float z = __uint_as_float(raw << 16) + 0.f;
+                        if (z > -INFINITY) {
+                            const int bin = bin_of(z);
+                            atomicAdd(&s.bins[place(bin)], 1u);
+                            if (middle(bin)) add64(&s.tiny[bin - 4095], mass(z));
+                        }
+                    }
+                }
+            } else {
+                float z[PER];
+                decode(a, z);
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    if (!(z[j] > -INFINITY)) continue;
+                    const int bin = bin_of(z[j]);
+                    atomicAdd(&s.bins[place(bin)], 1u);
+                    if (weights) {
+                        const float at = (top - z[j]) * scale * 2.f;
+                        atomicAdd(&s.bins[BINS + place(bin)], (unsigned)(fminf(at - (float)bin, 1.f) * REST));
+                    }
                 }
             }
         });
@@ -417,7 +435,9 @@ struct Row {
     __device__ __forceinline__ unsigned collect(int first, int last, bool weigh, u64 (&sums)[3]) const
     {
         u64 mine[3] = {0, 0, 0};
-        walk_all([&](const float (&z)[PER], int i0) {
+        walk_all([&](const uint4 &a, int i0) {
+            float z[PER];
+            decode(a, z);
             int bin[PER];
             bool any = weigh;
 #pragma unroll
@@ -651,8 +671,8 @@ struct Row {
     }
 
     // Of all elements in order of index, each with a share, the one at which the sum of shares exceeds mark(sum of all): found(its place in
-    // this block, its logit, the sum of all), by one thread of one block.  shares(z, i, q): those of a piece's elements, whether any has one;
-    // none below `least` has.
+    // this block, its logit, the sum of all), by one thread of one block.  shares(piece, place): those of a piece's elements together;
+    // none below `least` has any.
     // A warp's elements are consecutive; those of the warp that has it are shared out among the warps in turn, until there are few for each thread.
     template <class Shares, class Share, class Mark, class Found>
     __device__ __forceinline__ void in_order(float least, const Shares &shares, const Share &share, const Mark &mark, const Found &found) const
@@ -664,13 +684,7 @@ struct Row {
         for (bool first = true;; first = false) {
             const int each = (p1 - p0 + SP_WARPS - 1) / SP_WARPS, v0 = min(p1, p0 + warp * each), v1 = min(p1, v0 + each);
             u64 sum = 0;
-            walk(v0 + lane, v1, 32, [&](const float (&z)[PER], int i) {
-                u64 q[PER];
-                if (shares(z, i, q)) {
-#pragma unroll
-                    for (int j = 0; j < PER; ++j) sum += q[j];
-                }
-            }, least);
+            walk(v0 + lane, v1, 32, [&](const uint4 &a, int i) { sum += shares(a, i); }, least);
             if (warp == 0 && front && lane < head) sum += share(value(lane), lane);
             const int behind = head + vectors * PER + lane;
             if (warp == SP_WARPS - 1 && back && behind < n) sum += share(value(behind), behind);
@@ -706,14 +720,16 @@ struct Row {
             found(i, value(i), s.of_all);
         }
     }
-    // The border is the nth (from 1) in order of index among the elements of that logit.
+    // The border is the nth (from 1) in order of index among the elements of that logit (HALF; not 0, which has two forms).
     __device__ __forceinline__ void among_ties(float tie, u64 nth) const
     {
         in_order(
-            tie, [&](const float (&z)[PER], int, u64 (&q)[PER]) {
+            tie, [&](const uint4 &a, int) -> u64 {
+                const unsigned w[4] = {a.x, a.y, a.z, a.w}, both = (__float_as_uint(tie) & 0xffff0000u) | __float_as_uint(tie) >> 16;
+                unsigned here = 0;
 #pragma unroll
-                for (int j = 0; j < PER; ++j) q[j] = z[j] == tie;
-                return true;
+                for (int j = 0; j < 4; ++j) here += (((w[j] ^ both) & 0xffffu) == 0) + (((w[j] ^ both) >> 16) == 0);
+                return here;
             },
             [&](float z, int) -> u64 { return z == tie; }, [&](u64) { return nth - 1; }, [&](int i, float z, u64) { tell(z, begin + i); });
         cluster_sync(blocks);
@@ -1170,12 +1186,37 @@ sample_kernel(const SampleParams p)
     };
     const auto drawn = [&](float z, int i) -> u64 { return left(z, i) ? r.mass(z) : 0; };
     constexpr int PIECE = Row<T>::PER;
+    // (bfloat16 above zero, all of whose weights are known: the weight of the nth value below the largest is the nth, so that a logit takes a difference
+    // and a look; what is behind the border, which is a tie, is taken away again)
+    const unsigned top_raw = __float_as_uint(top) >> 16;
+    const bool by_value = Row<T>::HALF && known > 0 && known < 4096 && border.z > 0.f && r.bin_of(border.z) == top_bin + known - 1 && top_bin > 0 &&
+                          r.bin_of(border.z) < 4095 && min_p <= 0.f;
+    if (by_value) {
+        __syncthreads();
+        if (tid == 0) s.bin_mass[known] = 0;
+        __syncthreads();
+    }
     r.in_order(
-        border.z, [&](const float (&z)[PIECE], int i, u64 (&q)[PIECE]) {
+        border.z, [&](const uint4 &a, int i) -> u64 {
+            u64 sum = 0;
+            if (by_value) {
+                const unsigned w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned p0 = min(top_raw - (w[j] & 0xffffu), (unsigned)known), p1 = min(top_raw - (w[j] >> 16), (unsigned)known);
+                    sum += s.bin_mass[p0] + s.bin_mass[p1];
+                    if (p0 == known - 1 && begin + i + 2 * j > border.index) sum -= s.bin_mass[known - 1];
+                    if (p1 == known - 1 && begin + i + 2 * j + 1 > border.index) sum -= s.bin_mass[known - 1];
+                }
+                return sum;
+            }
+            float z[PIECE];
+            r.decode(a, z);
+            u64 q[PIECE];
             bool in[PIECE], any = false, unknown = !Row<T>::HALF;
 #pragma unroll
             for (int j = 0; j < PIECE; ++j) any |= in[j] = left(z[j], i + j);
-            if (!any) return false;
+            if (!any) return 0;
             if (Row<T>::HALF) {
 #pragma unroll
                 for (int j = 0; j < PIECE; ++j) {
@@ -1190,7 +1231,9 @@ sample_kernel(const SampleParams p)
 #pragma unroll
                 for (int j = 0; j < PIECE; ++j) q[j] = in[j] ? q[j] : 0;
             }
-            return true;
+#pragma unroll
+            for (int j = 0; j < PIECE; ++j) sum += q[j];
+            return sum;
         },
         drawn,
         // the smallest index at which the sum in order of index is above u of all
