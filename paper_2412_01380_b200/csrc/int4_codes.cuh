@@ -28,10 +28,13 @@ __device__ __forceinline__ uint32_t int4_sixteenth(uint32_t x)
 // The same word as four pairs of neighbours (codes 0 and 1, 2 and 3, ...), all of them (code - 8) / 64, for operands that are in order.
 __device__ __forceinline__ void int4_in_order(uint32_t w, uint32_t *v)
 {
+    const uint32_t lo = w & 0x0f0f0f0fu, hi = w & 0xf0f0f0f0u;       // (a byte's codes stay where they are in it)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t byte = __byte_perm(w, 0u, 0x4040 + 0x0101 * j) & 0x00f0000fu;       // a byte's codes stay where they are in it
-        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[j]) : "r"(byte), "r"(0x7d007f00u), "r"(0xbe00be00u));      // * (2^127, 2^123) - 1/8
+        // byte j of lo, nothing, byte j of hi, nothing: "nothing" is the upper bit of lo's byte, all over
+        uint32_t both;
+        asm("prmt.b32 %0, %1, %2, %3;" : "=r"(both) : "r"(lo), "r"(hi), "r"(0x8480 + 0x1111 * j));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[j]) : "r"(both), "r"(0x7d007f00u), "r"(0xbe00be00u));      // * (2^127, 2^123) - 1/8
     }
 }
 constexpr float INT4_PRODUCT = 64.f;            // a product by these operands times this is the product
