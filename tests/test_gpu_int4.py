@@ -90,6 +90,46 @@ def test_the_widest(ctx, rows, d_in, d_out):
     check_product(ctx, [rows], d_in, d_out, torch.float32, dense=True, seed=rows)
 
 
+@pytest.mark.parametrize("experts,rows,d_in,d_out", [(512, 600, 96, 64), (512, 9000, 64, 96), (300, 40, 4096, 32), (3, 65536, 64, 64)])
+def test_the_most_experts_and_rows(ctx, experts, rows, d_in, d_out):
+    g = gen_of(8)
+    e = torch.randint(0, experts, (rows,), generator=g, device="cuda").sort().values.int()
+    check_product(ctx, torch.bincount(e.long(), minlength=experts).tolist(), d_in, d_out, torch.float32, extra=1, seed=experts)
+
+
+def test_two_graphs_of_one_context(ctx):
+    """They share its workspace, with tiles that are cut in both, and run one after the other."""
+    g = gen_of(15)
+    m = [dip.GroupedMatrix(*iu.matrix(g, 1, 416, 8192)) for _ in range(2)]
+    x = [dip.Rows.of(rows_of(g, n, 8192)) for n in (5, 150)]
+    y = [torch.zeros((r.n_rows, 416), device="cuda") for r in x]
+    graphs = []
+    for i in range(2):
+        dip.dip_grouped_product(ctx, m[i], x[i], y[i])
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            dip.dip_grouped_product(ctx, m[i], x[i], y[i])
+    want = [v.clone() for v in y]
+    for i in (0, 1, 1, 0, 1):
+        y[i].zero_()
+        graphs[i].replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y[0], want[0]) and torch.equal(y[1], want[1])
+
+
+@pytest.mark.parametrize("rows", [2, 12, 150])
+def test_large_and_small_inputs(ctx, rows):
+    """Rows of very large and of very small values, side by side: products are exact and the sums' bound holds for each row."""
+    g = gen_of(9)
+    w = iu.matrix(g, 1, 96, 640)
+    x = (torch.randn((rows, 640), generator=g, device="cuda") * torch.exp2(torch.linspace(-95, 95, rows, device="cuda"))[:, None]).bfloat16()
+    y = torch.zeros((rows, 96), device="cuda")
+    dip.dip_grouped_product(ctx, dip.GroupedMatrix(*w), dip.Rows.of(x), y)
+    want, bound = iu.product64(*w, x)
+    eu.assert_within(y, want, eu.rounded(want, bound, torch.float32), "y")
+
+
 def test_every_code_and_scale(ctx):
     """One input at a time: y is (code - 8) * scale * x exactly, for every code, and scales that are negative, subnormal, zero or large."""
     g = gen_of(3)

@@ -91,6 +91,16 @@ def test_every_share_of_a_row(ctx, n, vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("mode", ["plain", "top_p", "all", "min_p"])
+def test_rows_that_do_not_stay_in_shared_memory(ctx, mode, dtype):
+    """More rows than blocks find room for, and longer ones than fit beside what else a block has: they are read again."""
+    g = gen_of(11)
+    z = logits(g, 310, 36011, dtype)
+    z[5], z[6, 100:] = -math.inf, -math.inf
+    check(ctx, z[:, 3:], torch.rand((310,), generator=g, device="cuda"), **MODES[mode])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_closed_logits(ctx, dtype):
     g = gen_of(1)
     z = logits(g, 24, 5003, dtype)
@@ -238,6 +248,49 @@ def test_calls_at_once(ctx):
                 dip.dip_sample_tokens(ctx, v, u, t, top_p=p)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+FIRST_CALLS_UNDER_CAPTURE = """
+import sys, torch
+sys.path[:0] = [%r, %r]
+import paper_2412_01380_b200 as dip, int4_util as iu
+g = torch.Generator(device="cuda")
+ctx = dip.Context(0)
+m = dip.GroupedMatrix(*iu.matrix(g, 1, 416, 1280))
+rows = [dip.Rows.of(torch.randn((n, 1280), generator=g, device="cuda").bfloat16()) for n in (3, 12, 2000)]
+ys = [torch.zeros((r.n_rows, 416), device="cuda") for r in rows]
+z, u = torch.randn((5, 9000), generator=g, device="cuda"), torch.rand((5,), generator=g, device="cuda")
+token = torch.full((5,), -7, device="cuda", dtype=torch.int32)
+k = torch.full((5,), 40, device="cuda", dtype=torch.int32)
+
+def calls():
+    for r, y in zip(rows, ys):
+        dip.dip_grouped_product(ctx, m, r, y)
+    dip.dip_sample_tokens(ctx, z, u, token, top_k=k)
+
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    calls()
+assert (token == -7).all() and not any(y.any() for y in ys)
+graph.replay()
+torch.cuda.synchronize()
+got = [y.clone() for y in ys] + [token.clone()]
+calls()
+assert all(torch.equal(a, b) for a, b in zip(got, ys + [token])) and all(y.any() for y in ys) and (token >= 0).all()
+assert ctx.device_status() == dip.DEVICE_OK
+print("as told")
+"""
+
+
+def test_first_calls_under_capture():
+    """A process whose very first calls are captured."""
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    out = subprocess.run([sys.executable, "-c", FIRST_CALLS_UNDER_CAPTURE % (os.path.dirname(here), here)], capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0 and "as told" in out.stdout, out.stderr[-2000:]
 
 
 @pytest.mark.parametrize("n", [1, 3, 40])
