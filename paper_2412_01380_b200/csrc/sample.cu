@@ -13,6 +13,9 @@
 //   else  (a crowd in one bin, borders that the check refuses, a long top-k with a top-p behind it) histograms of weights over ever fewer keys
 // Several thousand elements in shared memory are searched by histograms of their own (`reach`).
 // The draw adds up the kept weights per warp (whose elements are consecutive), then looks closer where the sum crosses the number.
+// Bound, for few rows, by a chain of some dozen steps of 0.3 to 2 us (block scans, barriers of a cluster, reads between SMs, which take tens of cycles per
+// 128 bytes): 12 to 20 us whatever the size.  For many rows by instructions: 512 rows of 151001 bfloat16 logits by top-p take 283 us (155 MB are 24 us), of which the
+// histogram's atomics and the draw are the largest parts; 256 rows of 50257 binary32 logits without a filter 44 us (8), a weight each.
 #include <initializer_list>
 
 #include <cuda_bf16.h>
@@ -231,7 +234,7 @@ struct Row {
     }
 
     // exp((z - top) / temperature) times 2^45: 2^(k / 512) from the table times the third-order sum for what is left (within 10^-14).
-    // Nine binary64 operations, which go at a quarter of binary32's rate (B200: half of its lanes, two cycles each), and a conversion.
+    // Nine binary64 operations, at half of binary32's rate, and a conversion.
     __device__ __forceinline__ double weight(float z) const
     {
         constexpr double STEP = 0.69314718055994530942 / SP_TABLE, magic = 6755399441055744.0;
@@ -588,8 +591,8 @@ struct Row {
         for (int o = SP_WARPS / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         return v;
     }
-    // finish() for at most SP_FEW elements: everyone compared with everyone, by several threads each (searches by histograms, three of them, took 13000
-    // cycles for some fifty elements; this takes 4000).
+    // finish() for at most SP_FEW elements: everyone compared with everyone, by several threads each.  (One row of 1000 by top-p 12.4 us, by three searches
+    // with histograms 15.0; with two threads each for up to 256 elements, a row of 102400 by top-k 26 us, by searches 22.)
     __device__ __forceinline__ void finish_few(int m, int top_k, float top_p, float min_p, float u, u64 all, int32_t *token, float *prob) const
     {
         const int each = m <= SP_THREADS / 32 ? 32 : m <= SP_THREADS / 8 ? 8 : 4, e = threadIdx.x / each, part = threadIdx.x % each;
