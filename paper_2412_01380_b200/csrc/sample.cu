@@ -234,7 +234,7 @@ struct Row {
     }
 
     // exp((z - top) / temperature) times 2^45: 2^(k / 512) from the table times the third-order sum for what is left (within 10^-14).
-    // Nine binary64 operations, at half of binary32's rate, and a conversion.
+    // Ten binary64 operations, at half of binary32's rate, and a conversion.
     __device__ __forceinline__ double weight(float z) const
     {
         constexpr double STEP = 0.69314718055994530942 / SP_TABLE, magic = 6755399441055744.0;
@@ -243,8 +243,8 @@ struct Row {
         const double t = s.table[i & (SP_TABLE - 1)];
         const double e = fma(t, f * fma(f, fma(f, STEP * STEP * STEP / 6, STEP * STEP / 2), STEP), t);
         const double w = __hiloint2double(__double2hiint(e) + ((i >> 9) << 20), __double2loint(e));
-        // (closed logits are far below, or not a number)
-        return z == top ? (double)(1ull << SP_ONE_BITS) : (z - top) * steps_f > -60.f * SP_TABLE ? w : 0.0;
+        // (closed logits are far below, or not a number; asked in binary64, where neither the difference nor the steps leave the range)
+        return z == top ? (double)(1ull << SP_ONE_BITS) : k > magic - 60.0 * SP_TABLE ? w : 0.0;
     }
     __device__ __forceinline__ u64 mass(float z) const
     {
@@ -1031,7 +1031,8 @@ sample_kernel(const SampleParams p)
     dip_launch_dependents();
     const float temperature = p.temperature ? p.temperature[row] : 1.f;
     const int top_k = p.top_k ? p.top_k[row] : 0;
-    const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f, u = p.uniform[row];
+    const float top_p = p.top_p ? p.top_p[row] : 1.f, u = p.uniform[row];
+    const float min_p = p.min_p && temperature < INFINITY ? p.min_p[row] : 0.f;        // (all alike: it leaves all)
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -1155,7 +1156,7 @@ sample_kernel(const SampleParams p)
         // (a little lower than need be: what is left out weighs less than min_p for certain)
         const float far = -temperature * logf(fminf(min_p, 1.f));
         u64 ignored[3];
-        listed = r.collect(0, r.bin_of(top - far * 1.0001f - 1e-5f * fabsf(top)), false, ignored);
+        listed = r.collect(0, r.bin_of(top - far * 1.0001f - 1e-5f * fabsf(top) - 1e-37f), false, ignored);
         alone = listed <= SP_LIST;
     }
     if (alone) {
@@ -1182,7 +1183,7 @@ sample_kernel(const SampleParams p)
     }
     // (what min_p leaves, too, is the front of the order; only within a hair of its end does it take the weight itself to tell)
     const double least = fmin((double)min_p, 1.0) * (double)(1ull << SP_ONE_BITS);
-    const float cut = min_p > 0.f ? temperature * logf(fminf(min_p, 1.f)) : -INFINITY, hair = 1e-4f * -cut + 1e-5f * fabsf(top);
+    const float cut = min_p > 0.f ? temperature * logf(fminf(min_p, 1.f)) : -INFINITY, hair = 1e-4f * -cut + 1e-5f * fabsf(top) + 1e-37f;
     const float sure = min_p > 0.f ? top + cut + hair : -INFINITY, doubtful = min_p > 0.f ? top + cut - hair : -INFINITY;
     const auto left = [&](float z, int i) {
         return r.kept(z, i, border) && (z >= sure || z == top || (z >= doubtful && !(r.weight(z) < least)));

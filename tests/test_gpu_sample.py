@@ -172,6 +172,30 @@ def test_the_ends_of_the_settings(ctx):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab", [600, 5003])
+@pytest.mark.parametrize("kind", ["alike", "huge", "tiny"])
+def test_temperatures_and_logits_at_the_ends_of_their_range(ctx, kind, vocab, dtype):
+    """An infinite temperature (all alike, with any min_p), differences of logits that pass the largest binary32 number, and temperatures and
+    differences below the smallest normal one."""
+    g = gen_of(vocab)
+    n = 12
+    z = torch.randn((n, vocab), generator=g, device="cuda")
+    temperature = [math.inf]
+    if kind == "huge":
+        z, temperature = (z * 1.5e38).clamp(-3.3e38, 3.3e38), [math.inf, 1e38, 2.5e38, 3e37]
+    if kind == "tiny":
+        step = 2.0 ** -133                      # bfloat16's smallest number
+        z, temperature = torch.randint(-40, 40, (n, vocab), generator=g, device="cuda").double() * step, [4 * step, 2.0 ** -130, 2.0 ** -126]
+    z = z.to(dtype)
+    z[:, 5] = -math.inf
+    u = torch.rand((n,), generator=g, device="cuda")
+    check(ctx, z, u, temperature=temperature)
+    check(ctx, z, u, temperature=temperature, min_p=[1.0, 0.5, 3.0, 0.03])
+    check(ctx, z, u, temperature=temperature, top_p=[0.5, 0.9])
+    check(ctx, z, u, temperature=temperature, top_k=[7, 300], min_p=[0.2, 1.0, 0.0])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_rows_anywhere(ctx, dtype):
     """Rows that are apart, and that start anywhere."""
     g = gen_of(5)
