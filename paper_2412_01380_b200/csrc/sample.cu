@@ -15,7 +15,7 @@
 // The draw adds up the kept weights per warp (whose elements are consecutive), then looks closer where the sum crosses the number.
 // Bound, for few rows, by a chain of some dozen steps of 0.3 to 2 us (block scans, barriers of a cluster, reads between SMs, which take tens of cycles per
 // 128 bytes): 12 to 20 us whatever the size.  For many rows by instructions: 512 rows of 151001 bfloat16 logits by top-p take 283 us (155 MB are 24 us), of which the
-// histogram's atomics and the draw are the largest parts; 256 rows of 50257 binary32 logits without a filter 44 us (8), a weight each.
+// histogram's atomics and the draw are the largest parts; 256 rows of 50257 binary32 logits without a filter 37 us (8), a weight each.
 #include <initializer_list>
 
 #include <cuda_bf16.h>
@@ -180,7 +180,8 @@ struct Row {
     int n, begin;                               // how many; the first one's index
     unsigned rank, blocks;
     float top;                                  // the largest logit
-    double steps;                               // 512 log2(e) / temperature
+    double steps;                               // 512 log2(e) / temperature; below a logit of +infinity, so many that nothing else weighs
+    double top_wide;
     float steps_f;
     float scale;                                // bins per unit
     int head, vectors;                          // items in front of the first boundary of 16 bytes; whole pieces of 16 bytes from there on
@@ -233,18 +234,24 @@ struct Row {
         }
     }
 
-    // exp((z - top) / temperature) times 2^45: 2^(k / 512) from the table times the third-order sum for what is left (within 10^-14).
-    // Ten binary64 operations, at half of binary32's rate, and a conversion.
+    // A number's bits in a binary64 number's places: 2^-896 times it (infinity comes as 2^128; what is no number as one, too).  A conversion takes four times as
+    // long as other instructions.
+    static __device__ __forceinline__ double wide(float z)
+    {
+        return __hiloint2double((__float_as_int(z) >> 3) & 0x8fffffff, __float_as_int(z) << 29);
+    }
+    // exp((z - top) / temperature) times 2^45, of an open logit: 2^(k / 512) from the table times the third-order sum for what is left (within 10^-14).
+    // Ten binary64 operations, at half of binary32's rate.
     __device__ __forceinline__ double weight(float z) const
     {
         constexpr double STEP = 0.69314718055994530942 / SP_TABLE, magic = 6755399441055744.0;
-        const double d = (double)z - (double)top, k = fma(d, steps, magic), f = fma(d, steps, magic - k);
+        const double d = fma(wide(z), 0x1p896, -top_wide), k = fma(d, steps, magic), f = fma(d, steps, magic - k);
         const int i = __double2loint(k);
         const double t = s.table[i & (SP_TABLE - 1)];
         const double e = fma(t, f * fma(f, fma(f, STEP * STEP * STEP / 6, STEP * STEP / 2), STEP), t);
         const double w = __hiloint2double(__double2hiint(e) + ((i >> 9) << 20), __double2loint(e));
-        // (closed logits are far below, or not a number; asked in binary64, where neither the difference nor the steps leave the range)
-        return z == top ? (double)(1ull << SP_ONE_BITS) : k > magic - 60.0 * SP_TABLE ? w : 0.0;
+        // (asked in binary64, where neither the difference nor the steps leave the range)
+        return k > magic - 60.0 * SP_TABLE ? w : 0.0;
     }
     __device__ __forceinline__ u64 mass(float z) const
     {
@@ -458,7 +465,7 @@ struct Row {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int at = bin[j0 + j];
-                    mine[2] += q[j];
+                    mine[2] += at < BINS ? q[j] : 0;
                     if (first > 0) mine[0] += at < first ? q[j] : 0;
                     if (at >= first && at <= last) {
                         mine[1] += q[j];
@@ -1098,8 +1105,8 @@ sample_kernel(const SampleParams p)
     }
 
     const float spread = fminf(top - low, SP_SPREAD);
-    const Row<T> r = {s, items, n, begin, rank, blocks, top, SP_TABLE * 1.4426950408889634074 / (double)temperature,
-                      (float)(SP_TABLE * 1.4426950408889634074 / (double)temperature),
+    const double steps = SP_TABLE * 1.4426950408889634074 / (double)temperature;
+    const Row<T> r = {s, items, n, begin, rank, blocks, top, top < INFINITY ? steps : 1e300, Row<T>::wide(top) * 0x1p896, (float)steps,
                       spread > 1e-30f ? (SP_BINS - 1) / spread : 0.f, head, vectors};
     SampleBorder border = {-INFINITY, -1};
     const bool by_count = top_k > 0 && top_k < p.vocab, by_weight = top_p < 1.f;
