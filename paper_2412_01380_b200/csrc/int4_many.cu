@@ -15,9 +15,12 @@
 //   warps 4-7    codes to bfloat16, one group of one half into one of two operand areas of tensor memory (64 columns each)
 //   warps 8-15   take the accumulators out; each four warps have half of the rows
 // Tiles are dealt out, cut along K and joined as those of the other types are (grouped_common.cuh).
-// A group takes 1.04 us at 128 rows (2000 cycles; 1060 of MMAs) and hardly less at 32: bound by the instructions of all its warps, some 5000 a group
-// of which 1300 unpack codes.  8192 rows of 5120 to 17920 take 1429 us one launch after the other (1.05 PFLOP/s; the operations' floor is 929), 1620 among passes
-// that change their inputs.  What did not help: eight warps that unpack (those that take sums out then have 168 registers instead of 184: 1750 us).
+// A group takes 1.04 us at 128 rows (2000 cycles; 1060 of MMAs) and hardly less at 32.  MMAs wait for accumulators to be taken out: the warps that do are busy 1700
+// of the 2000 cycles, though their loads and additions by themselves take 330.  8192 rows of 5120 to 17920 take 1420 us one launch after the other (1.06 PFLOP/s;
+// the operations' floor is 929), 1620 among passes that change their inputs; without the additions 1350, without unpacking 1335, with one MMA of eight 1400,
+// without all three 1044, without the loads in front of the additions too 930.  What did not help: eight warps that unpack (those that take sums out then have
+// 168 registers instead of 184: 1750 us); longer waits per poll (1520); additions that are not packed (1470); a half's sums by four warps of all rows
+// instead of eight of half of them (1413, but three accumulators then need six barriers).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
