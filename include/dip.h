@@ -103,7 +103,10 @@ typedef struct dip_ctx dip_ctx;   /* opaque; owns scratch workspace on one devic
  *                      half of a call's last block keeps its select kernel if it has a cache.
  *                      Negative: a select kernel runs in front of each product instead.  The masks
  *                      are the same bits either way; the products add the same rows in a different
- *                      order. */
+ *                      order.
+ *   int4_kernel        which kernel multiplies by 4-bit row-major weights (dip_grouped_product and what is made of it): 0 = the one that
+ *                      should be through first; 1: the one for few rows; 2: the one for many.  Both take every call (but one of 2^31
+ *                      units of 64 outputs, 128 inputs and 8 rows and more, which 1 leaves to the other); their sums differ in the order of additions. */
 typedef struct {
     int32_t max_d;
     int32_t max_batch;
@@ -112,7 +115,8 @@ typedef struct {
     int32_t coarse_min_d;
     int32_t wait_limit_us;
     int32_t select_in_product;
-    int32_t reserved[3];          /* keep zero */
+    int32_t int4_kernel;
+    int32_t reserved[2];          /* keep zero */
 } dip_options;
 
 /* Create a context on `device` (a CUDA ordinal).  Allocates the scratch

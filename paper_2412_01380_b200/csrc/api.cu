@@ -106,7 +106,7 @@ dip_status dip_create_ex(dip_ctx **out, int device, const dip_options *opt)
     if (o.gemv_segment_bytes != 0 && o.gemv_segment_bytes != 512 && o.gemv_segment_bytes != 1024 &&
         o.gemv_segment_bytes != 2048)
         return DIP_ERR_INVALID_ARG;
-    if (o.wait_limit_us < 0) return DIP_ERR_INVALID_ARG;
+    if (o.wait_limit_us < 0 || o.int4_kernel < 0 || o.int4_kernel > 2) return DIP_ERR_INVALID_ARG;
     int prev_device = -1;
     if (cudaGetDevice(&prev_device) != cudaSuccess) return DIP_ERR_CUDA;
     dip_ctx *ctx = new (std::nothrow) dip_ctx();
@@ -129,6 +129,7 @@ dip_status dip_create_ex(dip_ctx **out, int device, const dip_options *opt)
     // below ~4096 columns the whole of h and its stamps is a few KB and the plain select is as fast
     ctx->coarse_min_d = o.coarse_min_d == 0 ? 4096 : (o.coarse_min_d < 0 ? 0 : o.coarse_min_d);
     ctx->fuse_select = o.select_in_product < 0 ? 0 : 1;
+    ctx->int4_kernel = o.int4_kernel;
     ctx->wait_limit_ns = o.wait_limit_us ? 1000ull * (unsigned long long)o.wait_limit_us : 1000000000ull;
     // (blocks wait for one another whenever a product has row parts: a short limit is not for them)
     ctx->block_wait_ns = ctx->wait_limit_ns > 1000000000ull ? ctx->wait_limit_ns : 1000000000ull;

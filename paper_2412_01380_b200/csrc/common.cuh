@@ -26,6 +26,7 @@ struct dip_ctx {
     int max_batch;       // most tokens per call the workspace was sized for
     int gemv_seg;        // 0 = choose per launch; else force the GEMV segment width (dip_options)
     int gemv_direct;     // one token, F32/BF16: plain-load kernel instead of the copy ring
+    int int4_kernel;     // 4-bit grouped products: 0 = choose per launch, 1 = for few rows, 2 = for many (dip_options)
     unsigned long long wait_limit_ns;   // bound of every in-kernel wait on an asynchronous copy
     unsigned long long block_wait_ns;   // and on other blocks of the launch
     // split-row partial sums of the two GEMVs (binary32); the grouped products' parts of tiles, [sm_count][2][DIP_GROUP_ROWS][DIP_GROUP_COLS]

@@ -818,6 +818,9 @@ static bool int4_few(const dip_ctx *ctx, const dip_grouped_matrix &w, bool gated
 {
     const double each = (n_rows + met - 1) / met, outs = (gated ? 2.0 : 1.0) * w.d_out, groups = (w.d_in + DIP_INT4_GROUP - 1) / DIP_INT4_GROUP;
     const double few = met * ceil(each / 16) * ceil(outs / 64) * groups, tiles = met * ceil(each / GP_ROWS) * ceil(outs / GP_COLS);
+    // (the first one counts its units in 32 bits)
+    if ((n_rows / 8 + met) * ceil(outs / 64) * groups >= 0x1p31) return false;
+    if (ctx->int4_kernel) return ctx->int4_kernel == 1;
     return few * 0.25 <= tiles * groups * 1.2 + (tiles < ctx->sm_count ? 20.0 : 12.0) * ctx->sm_count;
 }
 

@@ -151,7 +151,7 @@ __device__ __forceinline__ int run_of(int n, int parts, int unit)
     return unit < of_these ? unit / (each + 1) : longer + (unit - of_these) / each;
 }
 
-// (32 bits hold all numbers of units: at most 16 rows for each expert, 2^13 in all, or more where there is little to do)
+// (32 bits hold all numbers of units: a call of more goes to the kernel for many rows)
 template <bool GATED, int NT>
 __global__ void __launch_bounds__(IF_THREADS<NT>, 1)
 int4_few_kernel(const FewParams p)
