@@ -26,6 +26,7 @@ NVCC_FLAGS = [
 # Registers per thread that a launch of the grouped products must have (8-bit: "1"), because their warps deal them out again: with fewer the
 # warps that take more would wait for ever, and every launch is refused.
 GROUPED_REGISTERS = {"1": 168, "0": 96}
+INT4_MANY_REGISTERS = 126                       # the same of the 4-bit products of many rows
 
 
 def check_registers(log: str) -> None:
@@ -34,6 +35,17 @@ def check_registers(log: str) -> None:
     short = ["%s of %d" % (f, GROUPED_REGISTERS[f[0]]) for f in found if f[2] != "0" and int(f[3]) < GROUPED_REGISTERS[f[0]]]
     if len(found) != 12 or short:
         raise RuntimeError("grouped.cu: %d of 12 kernels, too few registers in (8 bits, gate/up, kind, registers): %s" % (len(found), short))
+
+
+def check_int4_many_registers(log: str) -> None:
+    """log: what ptxas -v says of int4_many.cu.  ManyKind<gate/up>."""
+    found = re.findall(r"Compiling entry function '[^']*int4_many_kernel[^']*ManyKindILb([01])E.*?Used (\d+) registers", log, re.S)
+    short = [f for f in found if int(f[1]) < INT4_MANY_REGISTERS]
+    if len(found) != 2 or short:
+        raise RuntimeError("int4_many.cu: %d of 2 kernels, fewer than %d registers in (gate/up, registers): %s" % (len(found), INT4_MANY_REGISTERS, short))
+
+
+REGISTER_CHECKS = {"grouped.cu": check_registers, "int4_many.cu": check_int4_many_registers}
 
 
 def _nvcc() -> str:
@@ -57,14 +69,14 @@ def _compile(src: str, force: bool, verbose: bool) -> str:
     obj = os.path.join(OBJ, src[:-3] + ".o")
     if force or _stale(obj, [path] + HEADERS):
         tmp = obj + ".tmp.%d" % os.getpid()
-        grouped = src == "grouped.cu"
-        cmd = [_nvcc(), *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose or grouped else []), "-c", path, "-o", tmp]
-        done = subprocess.run(cmd, stderr=subprocess.PIPE if grouped else None, text=True)
-        if grouped and (verbose or done.returncode):
+        check = REGISTER_CHECKS.get(src)
+        cmd = [_nvcc(), *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose or check else []), "-c", path, "-o", tmp]
+        done = subprocess.run(cmd, stderr=subprocess.PIPE if check else None, text=True)
+        if check and (verbose or done.returncode):
             sys.stderr.write(done.stderr)
         done.check_returncode()
-        if grouped:
-            check_registers(done.stderr)
+        if check:
+            check(done.stderr)
         os.replace(tmp, obj)
     return obj
 
