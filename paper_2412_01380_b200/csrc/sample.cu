@@ -1297,6 +1297,14 @@ bool apart(std::initializer_list<Bytes> written, std::initializer_list<Bytes> re
     }
     return true;
 }
+// Whether a piece meets any of n rows of `each` bytes, whose starts are `pitch` bytes apart (what lies between them is not read).
+bool meets_rows(const Bytes &a, const void *rows, size_t n, size_t each, size_t pitch)
+{
+    const uintptr_t r = (uintptr_t)rows, at = (uintptr_t)a.p;
+    if (!a.p || at + a.n <= r) return false;
+    const size_t first = at > r ? at - r : 0, row = first / pitch;
+    return row < n && (first - row * pitch < each || (row + 1 < n && (row + 1) * pitch < at + a.n - r));
+}
 
 }  // namespace
 
@@ -1312,8 +1320,8 @@ extern "C" dip_status dip_sample_tokens(dip_ctx *ctx, const void *logits, int lo
                           (const void *)uniform, (const void *)token, (const void *)prob})
         if ((uintptr_t)q % 4) return DIP_ERR_INVALID_ARG;
     const size_t item = logits_bf16 ? 2 : 4, each = (size_t)n_rows * 4;
-    if (!apart({{token, each}, {prob, each}}, {{logits, ((size_t)(n_rows - 1) * pitch + vocab) * item}, {how->temperature, each}, {how->top_k, each},
-                                               {how->top_p, each}, {how->min_p, each}, {uniform, each}}))
+    if (!apart({{token, each}, {prob, each}}, {{how->temperature, each}, {how->top_k, each}, {how->top_p, each}, {how->min_p, each}, {uniform, each}}) ||
+        meets_rows({token, each}, logits, n_rows, vocab * item, pitch * item) || meets_rows({prob, each}, logits, n_rows, vocab * item, pitch * item))
         return DIP_ERR_INVALID_ARG;
     // As many blocks per row as find room (two per SM).  Their parts of the rows stay in shared memory if they fit beside what else is there, and
     // are read again, out of L2, if not.
