@@ -728,7 +728,7 @@ dip_status dip_expert_mlp(dip_ctx *ctx, const dip_grouped_matrix *gate, const di
  *   top_k    keeps the first top_k of the order                     (<= 0 or >= vocab, or NULL: all)
  *   top_p    then keeps those in front of which the sum of e is below top_p times the sum of all that top_k kept; the
  *            first one always                                       (>= 1 or NaN, or NULL: all)
- *   min_p    then keeps those with e >= min(min_p, 1)               (<= 0 or NaN, or NULL: all)
+ *   min_p    then keeps those with e >= min(min_p, 1)               (<= 0 or NaN, or NULL: all; from 1 on: the largest logit and its equals)
  *   token    the smallest index at which the sum of the kept e in order of index exceeds uniform times their sum
  *   temperature <= 0 or NaN: the first of the order, prob 1         (NULL: 1).  Infinite: all open logits alike.
  * Where logits of +infinity stand, they share alike and the others get 0.  A row without an open logit (padding): token

@@ -253,6 +253,12 @@ struct Row {
         // (asked in binary64, where neither the difference nor the steps leave the range)
         return k > magic - 60.0 * SP_TABLE ? w : 0.0;
     }
+    // Whether min_p (above 0) keeps a logit.  From 1 on it keeps the largest alone; that is not asked of weights, since a weight that
+    // is smaller by less than 2^-53 is rounded to the largest one's.
+    __device__ __forceinline__ bool likely(float z, float min_p) const
+    {
+        return min_p < 1.f ? !(weight(z) < (double)min_p * (double)(1ull << SP_ONE_BITS)) : z == top;
+    }
     __device__ __forceinline__ u64 mass(float z) const
     {
         return (u64)__double_as_longlong(weight(z) + 4503599627370496.0) & 0xfffffffffffffull;
@@ -629,7 +635,7 @@ struct Row {
             left &= before < max(1ull, (u64)ceil(fmax((double)top_p, 0.0) * (double)all));
         }
         const double weight_of = weight(value_of_key(key));
-        if (min_p > 0.f) left &= !(weight_of < fmin((double)min_p, 1.0) * (double)(1ull << SP_ONE_BITS));
+        if (min_p > 0.f) left &= likely(value_of_key(key), min_p);
         const u64 sum = block_sum(left && part == 0 ? mass : 0), mark = min(sum - 1, (u64)(fmax((double)u, 0.0) * (double)sum));
         // in order of index, of those that are left
         if (there && part == 0 && !left) s.list.mass[e] = 0;
@@ -663,11 +669,10 @@ struct Row {
             if (top_p < 1.f) all = sum_of(weight_in);
         }
         if (top_p < 1.f) last = number(reach(m, number, weight_in, max(1ull, (u64)ceil(fmax((double)top_p, 0.0) * (double)all)), 0, last));
-        const double least = fmin((double)min_p, 1.0) * (double)(1ull << SP_ONE_BITS);
         const auto drawn = [&](int i) -> u64 {
             if (min_p > 0.f) {
                 const unsigned k = s.list.key[i];
-                if (weight(value_of_key(k)) < least) return 0;
+                if (!likely(value_of_key(k), min_p)) return 0;
             }
             return weight_in(i);
         };
@@ -1189,11 +1194,10 @@ sample_kernel(const SampleParams p)
         __syncthreads();
     }
     // (what min_p leaves, too, is the front of the order; only within a hair of its end does it take the weight itself to tell)
-    const double least = fmin((double)min_p, 1.0) * (double)(1ull << SP_ONE_BITS);
     const float cut = min_p > 0.f ? temperature * logf(fminf(min_p, 1.f)) : -INFINITY, hair = 1e-4f * -cut + 1e-5f * fabsf(top) + 1e-37f;
     const float sure = min_p > 0.f ? top + cut + hair : -INFINITY, doubtful = min_p > 0.f ? top + cut - hair : -INFINITY;
     const auto left = [&](float z, int i) {
-        return r.kept(z, i, border) && (z >= sure || z == top || (z >= doubtful && !(r.weight(z) < least)));
+        return r.kept(z, i, border) && (z >= sure || z == top || (z >= doubtful && r.likely(z, min_p)));
     };
     const auto drawn = [&](float z, int i) -> u64 { return left(z, i) ? r.mass(z) : 0; };
     constexpr int PIECE = Row<T>::PER;
