@@ -813,7 +813,9 @@ constexpr int GP_FEW_UP_TO = 12, GP_PAIR_ROWS = 192;
 // through 64 outputs by 128 inputs by 16 rows in 0.2 (one matrix) to 0.3 us (many small ones), a block of the second through 256 by 128 by 128 in 1.2,
 // behind 12 us more, and 8 where tiles have to be cut.  In us, few / many: one matrix of 5120 to 17920, 16 rows 22 / 40, 24 rows 36 / 41, 48 rows 51 / 43;
 // 2080 to 1056, 200 rows 12.9 / 40; 14336 to 4096, 24 rows 25 / 53; 4096 to 102400, 32 rows 144 / 121; 16 of 1056 to 2080, 32 rows each 26 / 22,
-// 50 rows 44 / 23; 64 of 1024 to 2816, 16 rows each 54 / 72, 24 rows 93 / 73.
+// 50 rows 44 / 23; 64 of 1024 to 2816, 16 rows each 54 / 72, 24 rows 93 / 73.  Rows that are not spread evenly cost up to twice the other kernel's time and
+// more, since the host does not know them: 1024 rows for 128 experts of 1024 to 2816 56 / 121 when even, 75 / 126 with half of them at one expert, 79 / 116
+// falling off as 1 / rank, 48 / 22 all at one; 2048 rows 100 / 124, 136 / 135, 152 / 124 and 89 / 37.
 static bool int4_few(const dip_ctx *ctx, const dip_grouped_matrix &w, bool gated, int n_rows, int met)
 {
     const double each = (n_rows + met - 1) / met, outs = (gated ? 2.0 : 1.0) * w.d_out, groups = (w.d_in + DIP_INT4_GROUP - 1) / DIP_INT4_GROUP;

@@ -246,7 +246,8 @@ struct Run {
 };
 
 // The runs of this block, in order.  Every role walks through them for itself, and keeps nothing of this in registers meanwhile.
-// (32 bits hold it all: at most 2^21 tiles, and fewer than a block's worth of cut ones of at most 512 steps.)
+// (32 bits hold it all: fewer than 2^24 tiles, and fewer cut ones than blocks, of at most 512 steps, whose number is multiplied by that of blocks.)
+static_assert((long long)(DIP_MAX_TOKENS * DIP_MAX_TOP_K / GP_ROWS + DIP_MAX_EXPERTS) * (DIP_MAX_OUT / GP_COLS) < 1 << 24, "tiles of 128 rows by 256 outputs");
 template <class K>
 struct Schedule {
     static constexpr bool GATED = K::GATED, PAIR = K::PAIR;

@@ -14,8 +14,9 @@
 //   * All units, tile after tile, are dealt out to the blocks in equal runs, and a block's to its warps: whatever the sizes, nobody has
 //     more than a unit too many.  Where whole tiles are hardly worse for the blocks, they stay whole: parts of a tile that meet in
 //     the workspace cost a write, a count and a read (the block that comes last adds them up in order; nobody waits).
-// One row of 4096 to 102400 takes 49 us (4.4 TB/s; 218 MB at the measured rate are 33): its copies alone take 42, the rest without them 44, of which
-// codes to bfloat16 are half: 288 of some 570 instructions of a unit (ALU pipe busy 48 %, multiply-adds 44, issue slots 58, mma.sync 26).  Twelve
+// One row of 4096 to 102400 takes 50 us (4.3 TB/s; 218 MB at the measured rate are 33): its copies alone take 42, since they come as runs of 64 bytes of
+// a row (longer runs reach more: pieces of 512 bytes 6.3 TB/s), the rest without them 44.  Codes to bfloat16 are 288 of some 570 instructions of a unit; the
+// other half are copies and their addresses, reads of shared memory, MMAs, x, scales and sums (ALU pipe busy 48 %, multiply-adds 44, issue slots 58, mma.sync 26).  Twelve
 // warps or eight, four MMAs side by side or one, bare codes with the 8 taken off the sums (46 us for one row, 53 instead of 50 for eight) change little.
 // Before and behind it 5 us go into the first loads and the last sums.
 #include <cuda_bf16.h>
@@ -371,6 +372,7 @@ int4_few_kernel(const FewParams p)
             const size_t row = (size_t)(t.row0 + r) * p.d_out;
             const int o = t.out0 + c;
             if (GATED) {
+                // (h is rounded once, to bfloat16: it is an operand of the next product, whose MMAs take no more)
                 float4 u;
                 u.x = __shfl_down_sync(0xffffffffu, v.x, 1);
                 u.y = __shfl_down_sync(0xffffffffu, v.y, 1);

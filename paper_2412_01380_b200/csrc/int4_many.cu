@@ -21,6 +21,8 @@
 // without all three 1044, without the loads in front of the additions too 930.  What did not help: eight warps that unpack (those that take sums out then have
 // 168 registers instead of 184: 1750 us); longer waits per poll (1520); additions that are not packed (1470); a half's sums by four warps of all rows
 // instead of eight of half of them (1413, but three accumulators then need six barriers).
+// A tile costs the same however few its rows and outputs are: of a plain product whose outputs leave up to 128 for the last column tile, that tile's
+// second half is unpacked, multiplied and taken out for nothing.  (Compiled for 128 registers, the kernel spills 20 bytes of the loops' state.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -90,7 +92,7 @@ __device__ __forceinline__ void many_mma(uint32_t d_tmem, uint32_t a_tmem, uint6
                  ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(shape), "r"(accumulate) : "memory");
 }
 
-// A bfloat16's worth of rounding, at the row's outputs of this warp.
+// A row's output: binary32, or rounded once to bfloat16.  (h is always: it is an operand of the next product, whose MMAs take no more.)
 __device__ __forceinline__ void put(void *out, size_t at, float v, int out_f32)
 {
     if (out_f32) static_cast<float *>(out)[at] = v;

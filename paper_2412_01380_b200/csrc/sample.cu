@@ -1,6 +1,8 @@
 // The choice of a token from its logits: temperature, top-k, top-p, min-p and one given number per row (include/dip.h has the definition).
 //
-// A row is read once, into the shared memory of a cluster of up to eight blocks, and stays there.  Weights are
+// A row is shared out over a cluster of up to eight blocks.  Where the blocks' parts fit in shared memory beside what else a block has there (parts of up to
+// 67 KB with two blocks on an SM, 175 KB with one), the row is read from global memory once and stays there.  Longer parts, as in large batches of long
+// rows, are not copied: the maximum, the histogram, the list and the draw each walk through global memory, all but the first of them mostly out of L2.  Weights are
 // exp((z - max) / temperature) as whole multiples of 2^-45 of the largest one, computed in binary64: sums of them are exact whatever their order,
 // so results depend neither on how a row is shared out nor on the order of atomics, and a row's 2^18 weights fit 64 bits.
 //
@@ -14,8 +16,11 @@
 // Several thousand elements in shared memory are searched by histograms of their own (`reach`).
 // The draw adds up the kept weights per warp (whose elements are consecutive), then looks closer where the sum crosses the number.
 // Bound, for few rows, by a chain of some dozen steps of 0.3 to 2 us (block scans, barriers of a cluster, reads between SMs, which take tens of cycles per
-// 128 bytes): 12 to 20 us whatever the size.  For many rows by instructions: 512 rows of 151001 bfloat16 logits by top-p take 283 us (155 MB are 24 us), of which the
-// histogram's atomics and the draw are the largest parts; 256 rows of 50257 binary32 logits without a filter 37 us (8), a weight each.
+// 128 bytes): 12 to 27 us whatever the size.  For many rows by the work on each logit.  512 rows of 151001 bfloat16 logits by top-p take 280 us (155 MB are 24 us);
+// two blocks' rows on each of 148 SMs are 296 at a time, and a block needs, in us, 15 for the maximum, 34 for the histogram (an atomic each), 7 for the cuts, 24 for the list or
+// the ties, 35 for the draw (106 at most) or 5 for a list's end.  256 rows of 50257 binary32 logits without a filter 40 us (8): 12 until the maximum is known,
+// 26 for the draw, a weight each.  64 rows of 102400 with mixed settings 61 us: 9, 6 for the histogram, 5, 9, and 13 for the draw or 16 for a long list's end.
+// (The kernels have 64 registers a thread, for two blocks on an SM, and spill 8 bytes; bfloat16's 52.)
 #include <initializer_list>
 
 #include <cuda_bf16.h>
@@ -1327,7 +1332,9 @@ extern "C" dip_status dip_sample_tokens(dip_ctx *ctx, const void *logits, int lo
     if (!apart({{token, each}, {prob, each}}, {{how->temperature, each}, {how->top_k, each}, {how->top_p, each}, {how->min_p, each}, {uniform, each}}) ||
         meets_rows({token, each}, logits, n_rows, vocab * item, pitch * item) || meets_rows({prob, each}, logits, n_rows, vocab * item, pitch * item))
         return DIP_ERR_INVALID_ARG;
-    // As many blocks per row as find room (two per SM).  Their parts of the rows stay in shared memory if they fit beside what else is there, and
+    // As many blocks per row as find room (two per SM), if each has 1024 logits and more.  (1, 2, 4, 8 blocks, us: a row of 1000 bfloat16 logits 12.1, 13.8,
+    // 13.9, 14.8, of 9000 16.3, 16.4, 14.7, 15.0, of 32064 22.5, 19.0, 16.4, 15.2; a row of 102400 binary32 ones 40.0, 28.0, 20.3, 17.0, 64 rows 120, 75, 60.5, 61.7.)
+    // Their parts of the rows stay in shared memory if they fit beside what else is there, and
     // are read again, out of L2, if not.
     int blocks = 1;
     while (blocks < SP_CLUSTER && n_rows * blocks * 2 <= 2 * ctx->sm_count && vocab > 2048 * blocks) blocks *= 2;
