@@ -665,7 +665,7 @@ dip_status dip_route_experts(dip_ctx *ctx, const void *logits, int logits_bf16, 
 /* ------------------------------------------------------------------------
  * dip_stage_rows — the rows of a grouped product out of the tokens'
  * activations x [n_tokens][d] (bfloat16): row r is x[route->row_token[r]], or, with
- * route == NULL, x[r].  wtype DIP_W_BF16: rows [n][d] bfloat16, a copy.
+ * route == NULL, x[r].  wtype DIP_W_BF16: rows [n][d] bfloat16, a copy (what 4-bit weights take, too).
  * DIP_W_FP8_B128: rows [n][d] e4m3 codes with scales [n][ceil(d/128)]:
  * per row and block of 128 columns scale = max(max|x| / 448, 2^-126) and
  * code = round-to-nearest-even(x / scale), quotients in binary32.  A row with
