@@ -22,7 +22,7 @@
 // 168 registers instead of 184: 1750 us); longer waits per poll (1520); additions that are not packed (1470); a half's sums by four warps of all rows
 // instead of eight of half of them (1413, but three accumulators then need six barriers).
 // A tile costs the same however few its rows and outputs are: of a plain product whose outputs leave up to 128 for the last column tile, that tile's
-// second half is unpacked, multiplied and taken out for nothing.  (Compiled for 128 registers, the kernel spills 20 bytes of the loops' state.)
+// second half is unpacked, multiplied and taken out for nothing.  (Compiled for 128 registers, the kernel spills 20 bytes a thread.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
